@@ -317,6 +317,57 @@ tm_status tm_audio_cross_attn_fwd_f32out(const tm_audio_desc* desc, const void* 
                                          const void* av, const int32_t* face, float* o,
                                          hipStream_t stream);
 
+/* Rotary positions with three axes (paper Sec. 4.1: the student keeps the
+ * attention of its WAN2.1 teacher, whose queries and keys are rotated by the
+ * latent frame, row and column of their token before the attention equation of
+ * Sec. 4.2). A token at position p of the video lies in latent frame
+ * p / (grid_h * grid_w), and in row y and column x of that frame, row-major.
+ * The head_dim / 2 pairs of a (token, head) row are shared out over the axes:
+ * the first pairs_t turn with the frame, the next pairs_h with the row, the next
+ * pairs_w with the column, the rest stay. Pair i of the n pairs of an axis turns
+ * by angle = position * theta^(-i / n):
+ *     (x0, x1) -> (x0 cos - x1 sin, x0 sin + x1 cos),
+ * computed in fp32 and rounded once to the dtype (nearest even for bf16). */
+typedef struct tm_rope_desc {
+    int32_t head_dim;   /* D: 64 or 128 */
+    int32_t frames;     /* >= 1: latent frames the table covers */
+    int32_t grid_h;     /* >= 1: tokens per column of a latent frame */
+    int32_t grid_w;     /* >= 1: tokens per row; at most 2^30 positions in all */
+    int32_t pairs_t;    /* >= 0: pairs turned by the frame, */
+    int32_t pairs_h;    /* by the row */
+    int32_t pairs_w;    /* and by the column; together at most D / 2 */
+    int32_t split_half; /* 0: pair i is elements (2i, 2i + 1); else (i, i + D / 2) */
+    int32_t dtype;      /* tm_dtype of the rows */
+    float theta;        /* > 0 (10000 in the teacher) */
+} tm_rope_desc;
+
+/* Bytes of the table of a descriptor, or 0 if it is invalid or turns no pair:
+ * (cos, sin) in fp32 of every position and pair, [frames][pairs_t], then
+ * [grid_h][pairs_h], then [grid_w][pairs_w]. */
+size_t tm_rope3d_table_bytes(const tm_rope_desc* desc);
+
+/* Fill the table: device fp32 of tm_rope3d_table_bytes() bytes, 16-byte aligned;
+ * angles, cosines and sines formed in fp64. The caller keeps it as long as calls
+ * read it (a table the caller fills itself to that layout does as well). */
+tm_status tm_rope3d_table(const tm_rope_desc* desc, float* table, hipStream_t stream);
+
+/* Rotate the queries q: device [batch, n_tok, heads, D] into q_out and the keys
+ * k: device [batch, n_tok, kv_heads, D] into k_out, in one launch (k = k_out =
+ * NULL and kv_heads = 0: queries only). Row i is the token at position
+ * first_token + i, which must lie inside the table's frames (else TM_E_SHAPE).
+ * q_out may be q and k_out may be k; no output may overlap anything else.
+ * n_tok = 0 launches nothing. */
+tm_status tm_rope3d_fwd(const tm_rope_desc* desc, const float* table, int32_t batch, int32_t n_tok,
+                        int64_t first_token, const void* q, int32_t heads, const void* k,
+                        int32_t kv_heads, void* q_out, void* k_out, hipStream_t stream);
+
+/* Backward pass of tm_rope3d_fwd: given the gradients of its outputs, those of
+ * its inputs, dq = R^T dq_out and dk = R^T dk_out (the rotation by the opposite
+ * angles). Arguments as in the forward. */
+tm_status tm_rope3d_bwd(const tm_rope_desc* desc, const float* table, int32_t batch, int32_t n_tok,
+                        int64_t first_token, const void* dq_out, int32_t heads, const void* dk_out,
+                        int32_t kv_heads, void* dq, void* dk, hipStream_t stream);
+
 /* Message of the last failing call on this thread ("" if none). */
 const char* tm_last_error(void);
 

@@ -949,6 +949,149 @@ tm_status tm_audio_cross_attn_fwd_f32out(const tm_audio_desc* d, const void* q,
     return audio_fwd(d, q, first_frame, n_tok, ak, av, face, o, true, stream);
 }
 
-const char* tm_last_error(void) { return g_err; }
+}  // extern "C"
+
+namespace {
+
+// A rotary descriptor's sizes, checked.
+struct RopeGeo {
+    int64_t rows[3];  // positions of each axis: frames, grid rows, grid columns
+    int pairs[3];
+    size_t elem;
+    size_t table_bytes;
+};
+
+tm_status check_rope_desc(const tm_rope_desc* d, RopeGeo* g) {
+    if (d == nullptr) return fail(TM_E_ARG, "rope descriptor is NULL");
+    if (d->dtype != TM_F32 && d->dtype != TM_BF16)
+        return fail(TM_E_DTYPE, "dtype %d is neither TM_F32 nor TM_BF16", d->dtype);
+    if (d->head_dim != 64 && d->head_dim != 128)
+        return fail(TM_E_SHAPE, "head_dim %d unsupported (64 or 128)", d->head_dim);
+    if (d->frames < 1 || d->grid_h < 1 || d->grid_w < 1)
+        return fail(TM_E_SHAPE, "frames, grid_h and grid_w must be >= 1");
+    // each factor < 2^31, and the first product is bounded before the second
+    const int64_t grid = int64_t(d->grid_h) * d->grid_w;
+    if (grid > kMaxTokens || grid * d->frames > kMaxTokens)
+        return fail(TM_E_SHAPE, "more than 2^30 positions");
+    if (d->pairs_t < 0 || d->pairs_h < 0 || d->pairs_w < 0 ||
+        int64_t(d->pairs_t) + d->pairs_h + d->pairs_w > d->head_dim / 2)
+        return fail(TM_E_SHAPE, "the axes' pairs (%d, %d, %d) must be >= 0 and at most head_dim / 2 together",
+                    d->pairs_t, d->pairs_h, d->pairs_w);
+    if (!std::isfinite(d->theta) || !(d->theta > 0.f)) return fail(TM_E_ARG, "theta must be finite and > 0");
+    const int64_t rows[3] = {d->frames, d->grid_h, d->grid_w};
+    const int pairs[3] = {d->pairs_t, d->pairs_h, d->pairs_w};
+    int64_t n = 0;
+    for (int x = 0; x < 3; ++x) {
+        g->rows[x] = rows[x];
+        g->pairs[x] = pairs[x];
+        n += rows[x] * pairs[x];
+    }
+    g->elem = d->dtype == TM_BF16 ? 2 : 4;
+    g->table_bytes = size_t(n) * 2 * sizeof(float);
+    return TM_OK;
+}
+
+// The kernels' view of a caller's table, once its pointer and the tokens
+// [first_token, first_token + n_tok) are checked. Without any pair there is no
+// table to read.
+tm_status rope_table(const tm_rope_desc* d, const RopeGeo& g, const float* table, int64_t first_token,
+                     int64_t n_tok, tmk::RopeTable* t) {
+    const int64_t frame = g.rows[1] * g.rows[2], all = frame * g.rows[0];
+    if (first_token < 0 || first_token > all || n_tok > all - first_token)
+        return fail(TM_E_SHAPE, "tokens from %lld on lie past the table's %d frames",
+                    static_cast<long long>(first_token), d->frames);
+    if (g.table_bytes > 0) {
+        const tm_status st = check_ptr(table, g.table_bytes, "table");
+        if (st != TM_OK) return st;
+    }
+    t->table = reinterpret_cast<const float2*>(table);
+    t->table_h = t->table + g.rows[0] * g.pairs[0];
+    t->table_w = t->table_h + g.rows[1] * g.pairs[1];
+    t->pairs_t = g.pairs[0];
+    t->pairs_h = g.pairs[1];
+    t->pairs_w = g.pairs[2];
+    t->grid_w = d->grid_w;
+    t->frame_tokens = int32_t(frame);
+    return TM_OK;
+}
+
+tm_status rope(const tm_rope_desc* d, const float* table, int32_t batch, int32_t n_tok, int64_t first_token,
+               const void* q, int32_t heads, const void* k, int32_t kv_heads, void* q_out, void* k_out,
+               float sign, hipStream_t stream) {
+    RopeGeo g;
+    tm_status st = check_rope_desc(d, &g);
+    if (st != TM_OK) return st;
+    if (batch < 1 || heads < 1) return fail(TM_E_SHAPE, "batch and heads must be >= 1");
+    if (n_tok < 0) return fail(TM_E_SHAPE, "n_tok must be >= 0");
+    if (kv_heads < 0 || (k == nullptr) != (kv_heads == 0))
+        return fail(TM_E_ARG, "k and kv_heads: both or neither");
+    if (batch > 65535 || int64_t(batch) * (int64_t(heads) + kv_heads) > (int64_t(1) << 20))
+        return fail(TM_E_SHAPE, "batch * heads too large");
+    if (n_tok == 0) return TM_OK;
+    tmk::RopeArgs a{};
+    if ((st = rope_table(d, g, table, first_token, n_tok, &a.table)) != TM_OK) return st;
+    const size_t row = size_t(batch) * size_t(n_tok) * size_t(d->head_dim) * g.elem;
+    const size_t q_bytes = row * size_t(heads), k_bytes = row * size_t(kv_heads);
+    if ((st = check_ptr(q, q_bytes, "q")) != TM_OK) return st;
+    if ((st = check_ptr(q_out, q_bytes, "q_out")) != TM_OK) return st;
+    if (k != nullptr) {
+        if ((st = check_ptr(k, k_bytes, "k")) != TM_OK) return st;
+        if ((st = check_ptr(k_out, k_bytes, "k_out")) != TM_OK) return st;
+        if ((k_out != k && overlaps(k_out, k_bytes, k, k_bytes)) || overlaps(k_out, k_bytes, q, q_bytes) ||
+            overlaps(q_out, q_bytes, k, k_bytes) || overlaps(q_out, q_bytes, k_out, k_bytes))
+            return fail(TM_E_ARG, "k_out or q_out overlaps another tensor (only an output that is its input is allowed)");
+    }
+    if (q_out != q && overlaps(q_out, q_bytes, q, q_bytes)) return fail(TM_E_ARG, "q_out overlaps q without being q");
+    if (overlaps(q_out, q_bytes, table, g.table_bytes) ||
+        (k != nullptr && overlaps(k_out, k_bytes, table, g.table_bytes)))
+        return fail(TM_E_ARG, "q_out or k_out overlaps the table");
+    a.q = static_cast<const unsigned char*>(q);
+    a.k = static_cast<const unsigned char*>(k);
+    a.q_out = static_cast<unsigned char*>(q_out);
+    a.k_out = static_cast<unsigned char*>(k_out);
+    a.first_token = first_token;
+    a.n = n_tok;
+    a.B = batch;
+    a.H = heads;
+    a.Hk = kv_heads;
+    a.sign = sign;
+    const hipError_t e = tmk::launch_rope(a, d->head_dim, int(g.elem), d->split_half != 0, stream);
+    if (e != hipSuccess) return fail(TM_E_DEVICE, "rope launch: %s", hipGetErrorString(e));
+    return TM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t tm_rope3d_table_bytes(const tm_rope_desc* desc) {
+    RopeGeo g;
+    return check_rope_desc(desc, &g) == TM_OK ? g.table_bytes : 0;
+}
+
+tm_status tm_rope3d_table(const tm_rope_desc* desc, float* table, hipStream_t stream) {
+    RopeGeo g;
+    tm_status st = check_rope_desc(desc, &g);
+    if (st != TM_OK) return st;
+    if (g.table_bytes == 0) return TM_OK;  // no pair turns
+    if ((st = check_ptr(table, g.table_bytes, "table")) != TM_OK) return st;
+    const hipError_t e = tmk::launch_rope_table(g.rows, g.pairs, double(desc->theta), table, stream);
+    if (e != hipSuccess) return fail(TM_E_DEVICE, "rope table launch: %s", hipGetErrorString(e));
+    return TM_OK;
+}
+
+tm_status tm_rope3d_fwd(const tm_rope_desc* desc, const float* table, int32_t batch, int32_t n_tok,
+                        int64_t first_token, const void* q, int32_t heads, const void* k, int32_t kv_heads,
+                        void* q_out, void* k_out, hipStream_t stream) {
+    return rope(desc, table, batch, n_tok, first_token, q, heads, k, kv_heads, q_out, k_out, 1.f, stream);
+}
+
+tm_status tm_rope3d_bwd(const tm_rope_desc* desc, const float* table, int32_t batch, int32_t n_tok,
+                        int64_t first_token, const void* dq_out, int32_t heads, const void* dk_out,
+                        int32_t kv_heads, void* dq, void* dk, hipStream_t stream) {
+    return rope(desc, table, batch, n_tok, first_token, dq_out, heads, dk_out, kv_heads, dq, dk, -1.f, stream);
+}
 
 }  // extern "C"
+
+extern "C" const char* tm_last_error(void) { return g_err; }

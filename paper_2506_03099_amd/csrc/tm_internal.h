@@ -1,6 +1,5 @@
 // Internal interface between the host-side API (tm_api.cpp) and the HIP
-// kernels (attn_fwd.hip, kv_append.hip, audio_attn.hip). Not part of the
-// public ABI.
+// kernels. Not part of the public ABI.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -193,5 +192,32 @@ hipError_t launch_attn_bwd_bf16(const BwdArgs& a, int head_dim, hipStream_t s);
 // device); kernels get that address, never the symbol.
 constexpr int64_t kBwdScratchFloats = int64_t(1) << 21;
 hipError_t bwd_scratch_address(float** out);
+
+// Rotary positions: (cos, sin) of every position and pair of the three axes, the
+// frames' rows first, then the grid's rows, then its columns.
+struct RopeTable {
+    const float2* table;    // [frames][pairs_t]
+    const float2* table_h;  // [grid_h][pairs_h]
+    const float2* table_w;  // [grid_w][pairs_w]
+    int32_t pairs_t, pairs_h, pairs_w;
+    int32_t grid_w, frame_tokens;
+};
+
+// Rotation of q [B, n, H, D] and k [B, n, Hk, D] (Hk = 0: none) into q_out and
+// k_out; row i is the token at position first_token + i.
+struct RopeArgs {
+    const unsigned char* q;
+    const unsigned char* k;
+    unsigned char* q_out;
+    unsigned char* k_out;
+    RopeTable table;
+    int64_t first_token, n;
+    int64_t tok0, tok_end;  // tokens of one launch; set by the launcher
+    int32_t B, H, Hk;
+    int32_t slices;  // threads that share a token's heads; set by the launcher
+    float sign;      // of the angles: 1, or -1 for the backward pass
+};
+hipError_t launch_rope(const RopeArgs& a, int head_dim, int elem_bytes, bool halves, hipStream_t s);
+hipError_t launch_rope_table(const int64_t (&rows)[3], const int (&pairs)[3], double theta, float* out, hipStream_t s);
 
 }  // namespace tmk

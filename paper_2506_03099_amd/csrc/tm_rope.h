@@ -1,0 +1,107 @@
+// Device-side helpers of the rotary positions (rope.hip) and of the producer of
+// the 8-bit cache, which rotates keys and queries on their way (kv8_cache.hip):
+// (cos, sin) of a token's pairs, and the rotation and normalisation of a row
+// held by a few lanes. Not part of the public ABI.
+//
+// A row of D elements is held by D / 16 consecutive lanes, 8 pairs each: lane g
+// has elements 16 g .. 16 g + 15 where a pair is two neighbours, or 8 g .. 8 g +
+// 7 and D/2 + 8 g .. D/2 + 8 g + 7 where the pairs are the row's halves. Either
+// way that is two 16-byte loads in bf16, and element e of the lane's 16 pairs
+// with e ^ 1, or with e ^ 8.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "tm_device.h"
+#include "tm_internal.h"
+
+namespace tmk {
+
+constexpr int kRowElems = 16;  // elements of a row per lane
+
+// First of the run of 8 elements number `half` (0 or 1) of lane g.
+template <int D, bool HALVES>
+__device__ __forceinline__ int run_of(int g, int half) {
+    return HALVES ? half * (D / 2) + 8 * g : kRowElems * g + 8 * half;
+}
+
+// A lane's 16 elements of the row at `row`, in fp32. EB: bytes per element.
+template <int EB>
+struct RowBits {
+    u32x4_t v[EB];  // EB * 16 bytes
+};
+template <int EB, int D, bool HALVES>
+__device__ __forceinline__ RowBits<EB> load_row(const unsigned char* row, int g) {
+    RowBits<EB> r;
+#pragma unroll
+    for (int i = 0; i < EB; ++i)
+        r.v[i] = *reinterpret_cast<const u32x4_t*>(row + run_of<D, HALVES>(g, i * 2 / EB) * EB + (i % (EB / 2)) * 16);
+    return r;
+}
+template <int EB>
+__device__ __forceinline__ void unpack_row(const RowBits<EB>& r, float (&x)[kRowElems]) {
+#pragma unroll
+    for (int i = 0; i < EB; ++i)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            if constexpr (EB == 4) {
+                x[4 * i + w] = __uint_as_float(r.v[i][w]);
+            } else {
+                x[8 * i + 2 * w] = __uint_as_float(r.v[i][w] << 16);
+                x[8 * i + 2 * w + 1] = __uint_as_float(r.v[i][w] & 0xFFFF0000u);
+            }
+        }
+}
+// x rounded (nearest even) to the element type, through the L2.
+template <int EB, int D, bool HALVES>
+__device__ __forceinline__ void store_row(unsigned char* row, int g, const float (&x)[kRowElems]) {
+#pragma unroll
+    for (int i = 0; i < EB; ++i) {
+        u32x4_t v;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            if constexpr (EB == 4) {
+                v[w] = __float_as_uint(x[4 * i + w]);
+            } else {
+                const bf16x2_t p{static_cast<__bf16>(x[8 * i + 2 * w]), static_cast<__bf16>(x[8 * i + 2 * w + 1])};
+                v[w] = __builtin_bit_cast(uint32_t, p);
+            }
+        }
+        store16_through(row + run_of<D, HALVES>(g, i * 2 / EB) * EB + (i % (EB / 2)) * 16, v);
+    }
+}
+
+// (cos, sin) of pairs 8 g .. 8 g + 7 of the token at position `pos`; (1, 0) of
+// the pairs that no axis turns.
+__device__ __forceinline__ void load_turns(const RopeTable& t, int64_t pos, int g, float2 (&cs)[8]) {
+    const int p = static_cast<int>(pos);  // below frames * frame_tokens <= 2^30
+    const int f = p / t.frame_tokens, j = p - f * t.frame_tokens;
+    const int y = j / t.grid_w, x = j - y * t.grid_w;
+    // pair i of the row is entry i of these, in its axis' span
+    const float2* const at = t.table + static_cast<int64_t>(f) * t.pairs_t;
+    const float2* const ay = t.table_h + y * t.pairs_h - t.pairs_t;
+    const float2* const ax = t.table_w + x * t.pairs_w - (t.pairs_t + t.pairs_h);
+    const int end_t = t.pairs_t, end_h = end_t + t.pairs_h, end_w = end_h + t.pairs_w;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int i = 8 * g + e;
+        const float2* const from = i < end_t ? at : i < end_h ? ay : ax;
+        cs[e] = make_float2(1.f, 0.f);
+        if (i < end_w) cs[e] = from[i];
+    }
+}
+
+// (x0, x1) -> (x0 c - x1 s, x0 s + x1 c) for the lane's 8 pairs.
+template <bool HALVES>
+__device__ __forceinline__ void turn_row(float (&x)[kRowElems], const float2 (&cs)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int i = HALVES ? e : 2 * e, j = HALVES ? e + 8 : 2 * e + 1;
+        const float a = x[i], b = x[j];
+        x[i] = fmaf(a, cs[e].x, -(b * cs[e].y));
+        x[j] = fmaf(a, cs[e].y, b * cs[e].x);
+    }
+}
+
+}  // namespace tmk

@@ -67,6 +67,21 @@ class tm_audio_desc(ctypes.Structure):
     ]
 
 
+class tm_rope_desc(ctypes.Structure):
+    _fields_ = [
+        ("head_dim", ctypes.c_int32),
+        ("frames", ctypes.c_int32),
+        ("grid_h", ctypes.c_int32),
+        ("grid_w", ctypes.c_int32),
+        ("pairs_t", ctypes.c_int32),
+        ("pairs_h", ctypes.c_int32),
+        ("pairs_w", ctypes.c_int32),
+        ("split_half", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("theta", ctypes.c_float),
+    ]
+
+
 class TMError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"{STATUS_NAMES.get(status, status)}: {message}")
@@ -87,6 +102,9 @@ def lib() -> ctypes.CDLL:
         P = ctypes.c_void_p
         D = ctypes.POINTER(tm_attn_desc)
         AD = ctypes.POINTER(tm_audio_desc)
+        RD = ctypes.POINTER(tm_rope_desc)
+        rope = [RD, P, ctypes.c_int32, ctypes.c_int32, ctypes.c_int64, P, ctypes.c_int32, P,
+                ctypes.c_int32, P, P, P]
         sig = {
             "tm_kv_cache_tokens": (ctypes.c_int64, [D]),
             "tm_kv_cache_bytes": (ctypes.c_size_t, [D]),
@@ -121,6 +139,10 @@ def lib() -> ctypes.CDLL:
                                                             P, P, P, P, ctypes.c_size_t, P]),
             "tm_sparse_causal_attn_bwd_noalloc": (ctypes.c_int, [D, ctypes.c_int32, P, P, P, P, P,
                                                                  P, P, P, P, P]),
+            "tm_rope3d_table_bytes": (ctypes.c_size_t, [RD]),
+            "tm_rope3d_table": (ctypes.c_int, [RD, P, P]),
+            "tm_rope3d_fwd": (ctypes.c_int, rope),
+            "tm_rope3d_bwd": (ctypes.c_int, rope),
             "tm_last_error": (ctypes.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -140,12 +162,17 @@ def _check(status: int):
         raise TMError(status, tm_last_error())
 
 
+def _dtype(dtype):
+    if isinstance(dtype, torch.dtype):
+        return {torch.float32: TM_F32, torch.bfloat16: TM_BF16}[dtype]
+    if isinstance(dtype, str):
+        return {"f32": TM_F32, "bf16": TM_BF16}[dtype]
+    return dtype
+
+
 def make_desc(batch, heads, head_dim, tokens_per_frame, chunk_frames, ref_frames, window,
               dtype, softmax_scale=0.0) -> tm_attn_desc:
-    if isinstance(dtype, torch.dtype):
-        dtype = {torch.float32: TM_F32, torch.bfloat16: TM_BF16}[dtype]
-    elif isinstance(dtype, str):
-        dtype = {"f32": TM_F32, "bf16": TM_BF16}[dtype]
+    dtype = _dtype(dtype)
     return tm_attn_desc(batch, heads, head_dim, tokens_per_frame, chunk_frames, ref_frames,
                         window, dtype, softmax_scale)
 
@@ -310,10 +337,7 @@ def tm_sparse_causal_attn_fwd_f32out(desc: tm_attn_desc, q, q_chunk: int,
 
 def make_audio_desc(batch, heads, head_dim, tokens_per_frame, audio_per_frame, audio_frames,
                     streams=1, half_window=2, dtype="bf16", softmax_scale=0.0) -> tm_audio_desc:
-    if isinstance(dtype, torch.dtype):
-        dtype = {torch.float32: TM_F32, torch.bfloat16: TM_BF16}[dtype]
-    elif isinstance(dtype, str):
-        dtype = {"f32": TM_F32, "bf16": TM_BF16}[dtype]
+    dtype = _dtype(dtype)
     return tm_audio_desc(batch, heads, head_dim, tokens_per_frame, audio_per_frame, audio_frames,
                          streams, half_window, dtype, softmax_scale)
 
@@ -376,3 +400,70 @@ def tm_sparse_causal_attn_bwd_noalloc(desc: tm_attn_desc, n_frames: int, q, k, v
                                                    _ptr(v), _ptr(o), _ptr(lse), _ptr(dout),
                                                    _ptr(dq), _ptr(dk), _ptr(dv), _stream(stream)))
     return dq, dk, dv
+
+
+def _expect(name, t, shape, dtype):
+    """A tensor argument of the rotary and 8-bit-cache calls: the library sees
+    addresses only, and torch's allocator puts many tensors into one allocation."""
+    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype):
+        raise TMError(TM_E_SHAPE, f"{name} is not {dtype} {list(shape)}")
+
+
+def _rope_table_shape(desc):
+    return (lib().tm_rope3d_table_bytes(ctypes.byref(desc)) // 8, 2)
+
+
+def make_rope_desc(head_dim, frames, grid_h, grid_w, pairs=None, theta=10000.0, split_half=False,
+                   dtype="bf16") -> tm_rope_desc:
+    """``pairs``: pairs turned by (frame, row, column); by default a third of
+    them each for rows and columns and what is left for frames."""
+    if pairs is None:
+        third = head_dim // 2 // 3
+        pairs = (head_dim // 2 - 2 * third, third, third)
+    return tm_rope_desc(head_dim, frames, grid_h, grid_w, *pairs, int(bool(split_half)), _dtype(dtype), theta)
+
+
+def tm_rope3d_table(desc: tm_rope_desc, table=None, device="cuda", stream=None):
+    """(cos, sin) of every position and pair of the descriptor's axes, a flat
+    fp32 tensor of pairs (allocated if not given)."""
+    shape = _rope_table_shape(desc)
+    if table is None:
+        table = torch.empty(shape, dtype=torch.float32, device=device)
+    _expect("table", table, shape, torch.float32)
+    _check(lib().tm_rope3d_table(ctypes.byref(desc), _ptr(table), _stream(stream)))
+    return table
+
+
+def _rope(fn, desc, table, q, k, first_token, q_out, k_out, stream):
+    for name, t in (("q", q), ("k", k)):
+        if t is not None and (t.dim() != 4 or t.shape[3] != desc.head_dim or t.dtype != _TORCH_DTYPE[desc.dtype]):
+            raise TMError(TM_E_SHAPE, f"{name} is not [batch, n_tok, heads, {desc.head_dim}] of the descriptor's dtype")
+    if k is not None and k.shape[:2] != q.shape[:2]:
+        raise TMError(TM_E_SHAPE, "q and k differ in batch or tokens")
+    _expect("table", table, _rope_table_shape(desc), torch.float32)
+    _expect("q_out", q_out, q.shape, q.dtype)
+    if k is not None:
+        _expect("k_out", k_out, k.shape, k.dtype)
+    if q_out is None:
+        q_out = torch.empty_like(q)
+    if k_out is None and k is not None:
+        k_out = torch.empty_like(k)
+    B, n, H = q.shape[:3]
+    _check(fn(ctypes.byref(desc), _ptr(table), B, n, first_token, _ptr(q), H, _ptr(k),
+              0 if k is None else k.shape[2], _ptr(q_out), _ptr(k_out), _stream(stream)))
+    return q_out, k_out
+
+
+def tm_rope3d_fwd(desc: tm_rope_desc, table, q, k=None, first_token: int = 0, q_out=None, k_out=None,
+                  stream=None):
+    """Rotate the rows of ``q`` ([B, n_tok, H, D]) and, if given, ``k`` ([B,
+    n_tok, H_k, D]) by the latent frame, row and column of their token (row i is
+    at position ``first_token`` + i); returns (q_out, k_out), allocated if not
+    given."""
+    return _rope(lib().tm_rope3d_fwd, desc, table, q, k, first_token, q_out, k_out, stream)
+
+
+def tm_rope3d_bwd(desc: tm_rope_desc, table, dq_out, dk_out=None, first_token: int = 0, dq=None, dk=None,
+                  stream=None):
+    """Gradients (dq, dk) of ``tm_rope3d_fwd``'s inputs from those of its outputs."""
+    return _rope(lib().tm_rope3d_bwd, desc, table, dq_out, dk_out, first_token, dq, dk, stream)
