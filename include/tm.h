@@ -368,6 +368,87 @@ tm_status tm_rope3d_bwd(const tm_rope_desc* desc, const float* table, int32_t ba
                         int64_t first_token, const void* dq_out, int32_t heads, const void* dk_out,
                         int32_t kv_heads, void* dq, void* dk, hipStream_t stream);
 
+/* The KV cache in 8 bits (paper Sec. 4.3, "KV & Embedding Cachings": the caches
+ * of every step and layer stay resident; this one takes half the memory of the
+ * 16-bit one and half its traffic). Keys and values are held as 8-bit codes
+ * with an fp32 scale for each block of 64 tokens of a chunk and key head, of K
+ * and of V apart:
+ *     scale = max(m, 2^-60) * fl(1/127),   code = round(x * (1 / scale)),
+ * m the largest magnitude in the block, every operation in fp32, rounding to
+ * even at ties, so that |code| <= 127 and a value is off by at most about half
+ * a scale. It stands for code * scale. A block that holds an infinity or a NaN
+ * gets the scale NaN and reads back as NaN throughout.
+ * The chunk rules, eviction and key sets are those of tm_kv_cache. Queries, keys
+ * and values are bf16 (else TM_E_DTYPE); kv_heads key heads divide the
+ * descriptor's heads, query head h reads key head h / (heads / kv_heads). */
+typedef struct tm_kv8_cache tm_kv8_cache;
+
+/* Token rows per (batch, key head), or 0 if the descriptor is invalid: c_0 takes
+ * R*T rounded up to 64, each of the W+1 ring slots C*T rounded up to 64. */
+int64_t tm_kv8_cache_tokens(const tm_attn_desc* desc);
+
+/* Bytes of the pool of one cache, or 0 if invalid: the codes of K, then of V,
+ * B * kv_heads * tokens * D bytes each, then the scales of K and of V, one per
+ * (batch, key head, block), each rounded up to 16 bytes. Inside a block the codes
+ * (as code + 128) are in the order of the attention kernel's operands; use
+ * tm_kv8_read for the values. */
+size_t tm_kv8_cache_bytes(const tm_attn_desc* desc, int32_t kv_heads);
+
+/* As tm_kv_cache_create, _destroy, _reset, _latest and _locate, over one
+ * caller-allocated device pool of tm_kv8_cache_bytes() bytes, 16-byte aligned. */
+tm_status tm_kv8_cache_create(const tm_attn_desc* desc, int32_t kv_heads, void* pool,
+                              tm_kv8_cache** out);
+void tm_kv8_cache_destroy(tm_kv8_cache* cache);
+tm_status tm_kv8_cache_reset(tm_kv8_cache* cache);
+int32_t tm_kv8_cache_latest(const tm_kv8_cache* cache);
+tm_status tm_kv8_cache_locate(const tm_kv8_cache* cache, int32_t chunk, int32_t* token_offset,
+                              int32_t* n_tok);
+
+/* Quantise a chunk's k and v, device bf16 [B, n_tok, kv_heads, D], into the
+ * cache: order, capacities, eviction and errors as in tm_kv_append. */
+tm_status tm_kv8_append(tm_kv8_cache* cache, int32_t chunk, const void* k, const void* v,
+                        int32_t n_tok, hipStream_t stream);
+
+/* The producer of tm_qkv_produce for this cache, with the rotary positions of
+ * tm_rope3d_fwd in between: queries and keys are RMS-normalised (eps, gains
+ * q_gain [heads, D] and k_gain [kv_heads, D] or NULL, as there), rotated (rope
+ * NULL: not; table and first_token as in tm_rope3d_fwd, the descriptor's
+ * head_dim and dtype those of the cache), and the queries rounded once, to bf16,
+ * into q_out: device bf16 [B, n_tok, heads, D] (it may be q). The keys are
+ * quantised from their fp32 values, and the values v as tm_kv8_append does. */
+tm_status tm_qkv8_produce(tm_kv8_cache* cache, int32_t chunk, const void* q, const void* k,
+                          const void* v, const float* q_gain, const float* k_gain, float eps,
+                          const tm_rope_desc* rope, const float* table, int64_t first_token,
+                          void* q_out, int32_t n_tok, hipStream_t stream);
+
+/* The keys and values that a cached chunk's codes stand for: code * scale in
+ * fp32, into k_out and v_out, device [B, n_tok, kv_heads, D] with n_tok the
+ * chunk's appended length, 16-byte aligned; bf16 (nearest even), or fp32 with
+ * out_f32 set. TM_E_ORDER if the chunk was never appended or is evicted. */
+tm_status tm_kv8_read(const tm_kv8_cache* cache, int32_t chunk, void* k_out, void* v_out,
+                      int32_t out_f32, hipStream_t stream);
+
+/* Attention over the 8-bit cache (paper Sec. 4.2, attention equation, over the
+ * key set {c_0, c_{a-W}, ..., c_a} of the latest appended chunk a, which q_chunk
+ * must name, else TM_E_ORDER): q is device bf16 [B, n_q, heads, D], any number of
+ * query rows of that chunk (a whole chunk's, or one token's; 0 launches nothing).
+ * o: device, same shape, bf16 or with o_f32 set fp32; written for every row; bf16
+ * o may be q itself but must not otherwise overlap anything. lse: optional fp32
+ * [B, heads, n_q], 4-byte aligned, natural-log softmax normaliser.
+ * Arithmetic: codes and (scaled by a power of two per row) q as fp16 operands,
+ * exact but for elements of q below 2^-28 of their row's largest; fp32 sums; P
+ * rounded to fp16; the row sums add the fp32 P. o_f32 leaves out the final
+ * rounding to bf16 only. A query row with an infinity or NaN gets NaN.
+ * workspace: device memory, 16-byte aligned, not overlapping any other tensor, or
+ * NULL. Rows that do not fill the GPU share their keys out over several
+ * workgroups through it; with fewer than tm_kv8_attn_workspace() bytes (0: the call
+ * needs none; also on invalid arguments) it is not used, and the fp32 sums are
+ * ordered otherwise. Either way the result is deterministic (no atomics). */
+size_t tm_kv8_attn_workspace(const tm_kv8_cache* cache, int32_t q_chunk, int32_t n_q);
+tm_status tm_kv8_attn_fwd(const tm_kv8_cache* cache, const void* q, int32_t q_chunk, int32_t n_q,
+                          void* o, int32_t o_f32, float* lse, void* workspace,
+                          size_t workspace_bytes, hipStream_t stream);
+
 /* Message of the last failing call on this thread ("" if none). */
 const char* tm_last_error(void);
 

@@ -17,7 +17,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libtm.so")
 
 SOURCES = ["tm_api.cpp", "attn_fwd.hip", "kv_append.hip", "audio_attn.hip", "attn_bwd.hip",
-           "rope.hip"]
+           "rope.hip", "kv8_cache.hip", "attn_kv8.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

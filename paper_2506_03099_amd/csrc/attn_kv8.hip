@@ -1,0 +1,800 @@
+// Attention over the 8-bit KV cache for gfx950.
+//
+// O_i = softmax_j(scale * q_i . k_j) v_j over the keys of c_0 and of the window's
+// chunks (TalkingMachines, Sec. 4.2), with k = ks * code and v = vs * code, a
+// scale ks and vs for each block of 64 tokens and head. Blocks belong to one
+// chunk each, so a tile of 64 keys has one scale of K and one of V.
+//
+// Codes become fp16 operands, exactly: the byte code + 128 under the exponent of
+// 1024 is the fp16 number 1152 + code, less 1152 (one byte permutation and one
+// packed addition for two codes; the way over fp32 to bf16 takes twice that). So
+// q is fp16 as well: its rows are scaled by a power of two that puts their largest
+// element in [2^14, 2^15), which keeps every bf16 digit of elements down to 2^-28
+// of it. The products q . code are summed in fp32; the scales follow on the sums:
+//     x = (q . code) * (scale log2(e) ks / row's power) + log2(vs) - m,
+// one fma per score, P = 2^x in fp16 (11 digits, bf16 has 8), O += P . code, and
+// the row sum takes P / vs. Folding vs into the exponent scales P, not the 8-bit
+// operand, so nothing is rounded for it. m is the running maximum of x + m less
+// 8: P reaches 2^8 and a tile may exceed that by 2^7 before m is raised; what
+// fp16 then loses at its lower end is below 2^-33 of the largest.
+//
+// Tile kernel: as the bf16 forward (attn_fwd.hip), 8 waves of 32 query rows share
+// every 64-key tile in LDS, each wave's softmax in between its own MFMAs. The
+// tiles come as codes into registers, half the bytes, one tile ahead, and are
+// turned into fp16 operands once per workgroup on the way into LDS; the cache's
+// order makes every LDS access a contiguous KB.
+//
+// Few rows: a workgroup's waves share the keys of one block of 32 rows out; a
+// wave loads its blocks' operands straight from the cache. Bound by the cache's
+// bytes.
+
+#include <float.h>
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "tm_device.h"
+#include "tm_internal.h"
+#include "tm_kv8.h"
+
+namespace tmk {
+namespace {
+
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) f16x8_t lds_f16x8_t;
+typedef __attribute__((address_space(3))) f32x4_t lds_f32x4_t;
+typedef __attribute__((address_space(3))) u32x4_t lds_u32x4_t;
+typedef __attribute__((address_space(3))) unsigned char lds_u8;
+
+constexpr int kTileThreads = 512;
+constexpr int kTileWaves = kTileThreads / 64;
+constexpr int kTileRows = 32 * kTileWaves;
+constexpr float kHeadroom = 8.f;      // log2 of the largest P after m is set
+constexpr float kRaise = 0x1p15f;     // a lane's sum of P over half a tile that raises m
+static_assert(kTileRows == kTileRowsBf16, "the host counts tiles of this many rows");
+
+__device__ __forceinline__ f32x16_t mfma(f16x8_t a, f16x8_t b, f32x16_t c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+// 2 codes of a word as fp16: bytes 0 and 1 (HI: 2 and 3).
+template <bool HI>
+__device__ __forceinline__ f16x2_t decode2(uint32_t w) {
+    const f16x2_t x = __builtin_bit_cast(f16x2_t, pick_bytes(0x64646464u, w, HI ? 0x04030402u : 0x04010400u));
+    return x - f16x2_t{static_cast<_Float16>(1152.f), static_cast<_Float16>(1152.f)};
+}
+// 8 codes as an operand's 8 elements.
+__device__ __forceinline__ f16x8_t decode8(uint32_t a, uint32_t b) {
+    const f16x2_t p = decode2<false>(a), q = decode2<true>(a), r = decode2<false>(b), s = decode2<true>(b);
+    return f16x8_t{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
+}
+
+__device__ __forceinline__ float pin(float x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+// Zero that the compiler takes to differ between lanes: an address formed with it
+// is loaded through the vector unit, in order with the other vector loads (scalar
+// loads share the counter of the LDS reads and come back in any order).
+__device__ __forceinline__ int lane_zero() {
+    int z = 0;
+    asm volatile("" : "+v"(z));
+    return z;
+}
+
+// T at byte `off` of the lane from a base that is the same in every lane (global
+// memory by its type: a pointer put together from scalar registers would be loaded
+// from as one that may point into LDS, and counted with the LDS reads).
+template <typename T>
+__device__ __forceinline__ T load_from(const void* base, uint32_t off) {
+    typedef const __attribute__((address_space(1))) char* global_t;
+    return *(const __attribute__((address_space(1))) T*)((global_t)(uniform_ptr(base)) + off);
+}
+
+// A value that is the same in every lane, in a scalar register.
+__device__ __forceinline__ float uniform_f(float x) {
+    return __uint_as_float(__builtin_amdgcn_readfirstlane(static_cast<int>(__float_as_uint(x))));
+}
+
+// Larger of the two half-waves' values, in both.
+__device__ __forceinline__ float both_max(float x) {
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+
+// Row r (of the n_q * group of a key head) of q and o: its offset in rows of D.
+__device__ __forceinline__ int64_t row_at(const Kv8AttnArgs& a, int bat, int kvh, int r) {
+    const int i = r / a.group, g = r - i * a.group;
+    return (static_cast<int64_t>(bat) * a.n_q + i) * a.H + kvh * a.group + g;
+}
+__device__ __forceinline__ int64_t lse_at(const Kv8AttnArgs& a, int bat, int kvh, int r) {
+    const int i = r / a.group, g = r - i * a.group;
+    return (static_cast<int64_t>(bat) * a.H + kvh * a.group + g) * a.n_q + i;
+}
+
+// A query row as the B operand of the score MFMAs (lane: dimensions 16 kk + 8 hw ..
+// + 7), scaled by a power of two; returns scale_log2 over that power. A row with an
+// infinity or a NaN gets NaN, and so does its output.
+template <int D>
+__device__ __forceinline__ float load_q(const Kv8AttnArgs& a, int64_t row, bool ok, int hw, f16x8_t (&qf)[D / 16]) {
+    constexpr int KK = D / 16;
+    const __bf16* const p = static_cast<const __bf16*>(a.q) + row * D + 8 * hw;
+    bf16x8_t raw[KK];
+    uint32_t top = 0;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+        raw[kk] = ok ? *reinterpret_cast<const bf16x8_t*>(p + 16 * kk) : bf16x8_t{};
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            top = max(top, static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<__bf16>(raw[kk][e])) & 0x7FFF));
+    }
+    top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 32)));
+    const uint32_t e = top >> 7;  // the exponent field
+    const uint32_t up = min(127u + 14 + 127 - min(e, 254u), 253u);
+    const float mult = __uint_as_float(up << 23);
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+        for (int x = 0; x < 8; ++x) qf[kk][x] = static_cast<_Float16>(static_cast<float>(raw[kk][x]) * mult);
+    return e == 255 ? __uint_as_float(0x7FC00000u) : a.scale_log2 * __uint_as_float((254 - up) << 23);
+}
+
+// Waits for scalar loads, which share a counter with the LDS reads and come back in
+// any order: after this no wait for one has to wait for every LDS read in flight.
+__device__ __forceinline__ void wait_scalars() { __builtin_amdgcn_s_waitcnt(kWaitLgkmcnt0); }
+
+// The key blocks of the call, one after the other.
+struct Blocks {
+    int r = 0;     // range
+    int blk = 0;   // block of the cache
+    int keys = 0;  // keys from this block to the range's end
+    __device__ __forceinline__ void start(const Kv8AttnArgs& a, int skip) {
+        r = 0;
+        int n = (a.range_keys[0] + kCacheBlock - 1) / kCacheBlock;
+        while (skip >= n && r + 1 < a.n_ranges) {
+            skip -= n;
+            ++r;
+            n = (a.range_keys[r] + kCacheBlock - 1) / kCacheBlock;
+        }
+        blk = a.range_begin[r] + skip;
+        keys = a.range_keys[r] - skip * kCacheBlock;
+    }
+    // On by one block; stays on the last one at the end. No else branch, and the kernel arguments
+    // only on the rare path: its scalar loads are waited for there (see wait_scalars).
+    __device__ __forceinline__ void step(const Kv8AttnArgs& a) {
+        ++blk;
+        keys -= kCacheBlock;
+        if (__builtin_expect(keys <= 0, 0)) {
+            if (r + 1 < a.n_ranges) {
+                ++r;
+                blk = a.range_begin[r];
+                keys = a.range_keys[r];
+            } else {
+                --blk;
+                keys += kCacheBlock;
+            }
+            wait_scalars();
+        }
+    }
+    // On by `by` blocks; stays on the last one at the end.
+    __device__ __forceinline__ void next(const Kv8AttnArgs& a, int by) {
+        while (by > 0) {
+            const int left = (keys - 1) / kCacheBlock;  // blocks behind this one in the range
+            if (by <= left) {
+                blk += by;
+                keys -= by * kCacheBlock;
+                return;
+            }
+            if (r + 1 >= a.n_ranges) {
+                blk += left;
+                keys -= left * kCacheBlock;
+                return;
+            }
+            by -= left + 1;
+            ++r;
+            blk = a.range_begin[r];
+            keys = a.range_keys[r];
+        }
+    }
+};
+
+// Rows [q0, q1) of tile `idx` of the `nt` that cover `rows`, in blocks of 32 shared
+// out as evenly as they go.
+__device__ __forceinline__ void split_rows(int rows, int nt, int idx, int& q0, int& q1) {
+    const int blocks = (rows + 31) / 32;
+    const int each = blocks / nt, more = blocks - each * nt;
+    q0 = 32 * (idx * each + min(idx, more));
+    q1 = min(32 * ((idx + 1) * each + min(idx + 1, more)), rows);
+}
+
+// A workgroup's tile and share of its keys (whole tiles come first, then the split
+// ones' parts, a tile's next to each other).
+struct Share {
+    int tile, bat, kvh, part;
+    int64_t split;  // number of the split tile, -1: whole
+    int b0, n;      // first key block of the walk and how many
+};
+__device__ __forceinline__ Share share_of(const Kv8AttnArgs& a) {
+    Share s;
+    const int total = a.n_tiles * a.B * a.Hk;
+    int id;
+    s.part = 0;
+    s.split = -1;
+    s.b0 = 0;
+    s.n = a.n_kblocks;
+    if (static_cast<int>(blockIdx.x) < a.n_whole) {
+        id = xcd_logical_id(blockIdx.x, a.n_whole);
+    } else {
+        const int sid = xcd_logical_id(blockIdx.x - a.n_whole, (total - a.n_whole) * a.parts);
+        s.split = sid / a.parts;
+        s.part = sid - static_cast<int>(s.split) * a.parts;
+        id = a.n_whole + static_cast<int>(s.split);
+        s.b0 = static_cast<int>(static_cast<int64_t>(a.n_kblocks) * s.part / a.parts);
+        s.n = static_cast<int>(static_cast<int64_t>(a.n_kblocks) * (s.part + 1) / a.parts) - s.b0;
+    }
+    s.tile = id % a.n_tiles;
+    const int bh = id / a.n_tiles;
+    s.kvh = bh % a.Hk;
+    s.bat = bh / a.Hk;
+    return s;
+}
+// A split tile's partial rows: O not yet divided by the row sum, [rows][D], then each
+// row's maximum and sum.
+template <int D, int ROWS>
+__device__ __forceinline__ float* part_at(const Kv8AttnArgs& a, int64_t split, int part) {
+    return a.part + (split * a.parts + part) * (ROWS * (D + 2));
+}
+
+// ----------------------------------------------------------------------------
+// Few rows
+// ----------------------------------------------------------------------------
+template <int D, bool OF32>
+__global__ __launch_bounds__(64 * kKv8FewWaves, 2) void attn_kv8_few_kernel(const Kv8AttnArgs a) {
+    constexpr int KK = D / 16, DB = D / 32, NP = 2 * DB;  // pieces of K, and of V, of a block
+    constexpr int PITCH = D + 4;                           // floats per row in LDS
+    __shared__ float rows_o[kKv8FewWaves][kKv8FewRows * PITCH];
+    __shared__ float rows_m[kKv8FewWaves][kKv8FewRows], rows_l[kKv8FewWaves][kKv8FewRows];
+    const int lane = threadIdx.x & 63, hw = lane >> 5, l32 = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+    const Share s = share_of(a);
+    const int q0 = s.tile * kKv8FewRows, n_rows = min(kKv8FewRows, a.rows - q0);
+    f16x8_t qf[KK];
+    const float cq = load_q<D>(a, row_at(a, s.bat, s.kvh, min(q0 + l32, a.rows - 1)), l32 < n_rows, hw, qf);
+    const int64_t head = (static_cast<int64_t>(s.bat) * a.Hk + s.kvh) * a.n_blocks;
+
+    f32x16_t acc[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d) acc[d] = f32x16_t{};
+    float m = kNegInf, l = 0.f;
+    u32x4_t kc[NP], vc[NP];
+    float ks = 0.f, vs = 0.f;
+    auto load_k = [&](int blk) __attribute__((always_inline)) {
+        const u32x4_t* const p = reinterpret_cast<const u32x4_t*>(a.k_codes + (head + blk) * (kCacheBlock * D)) + lane;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) kc[i] = p[64 * i];
+    };
+    auto load_v = [&](int blk) __attribute__((always_inline)) {
+        const u32x4_t* const p = reinterpret_cast<const u32x4_t*>(a.v_codes + (head + blk) * (kCacheBlock * D)) + lane;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) vc[i] = p[64 * i];
+    };
+    // this wave's blocks: every kKv8FewWaves-th of the share
+    Blocks at;
+    if (wave < s.n) {
+        at.start(a, s.b0 + wave);
+        load_k(at.blk);
+        ks = a.k_scale[head + at.blk];
+        load_v(at.blk);
+        vs = a.v_scale[head + at.blk];
+    }
+    for (int j = wave; j < s.n; j += kKv8FewWaves) {
+        const int keys = at.keys;
+        f32x16_t x[2] = {f32x16_t{}, f32x16_t{}};
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int kb = i / DB, st = i % DB;
+            x[kb] = mfma(decode8(kc[i][0], kc[i][1]), qf[2 * st], x[kb]);
+            x[kb] = mfma(decode8(kc[i][2], kc[i][3]), qf[2 * st + 1], x[kb]);
+        }
+        const float c = cq * ks, add = __builtin_amdgcn_logf(vs), iv = 1.f / vs;
+        at.next(a, kKv8FewWaves);  // (past the share's end: a block that exists)
+        load_k(at.blk);
+        ks = a.k_scale[head + at.blk];
+        vs = a.v_scale[head + at.blk];
+        // x + m of the header's formula, and its maximum
+        float mx = kNegInf;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                x[kb][i] = fmaf(x[kb][i], c, add);
+                if (keys < kCacheBlock && 32 * kb + 16 * (i / 8) + 8 * hw + i % 8 >= keys) x[kb][i] = kNegInf;
+                mx = fmaxf(mx, x[kb][i]);
+            }
+        mx = both_max(mx) - kHeadroom;
+        if (__ballot(mx > m) != 0) {
+            const float nm = fmaxf(m, mx);
+            const float alpha = __builtin_amdgcn_exp2f(m == kNegInf ? kNegInf : m - nm);
+            m = nm;
+            l *= alpha;
+#pragma unroll
+            for (int d = 0; d < DB; ++d) acc[d] *= alpha;
+        }
+        // (a row with only scores of -inf so far: P = 0)
+        const float base = m == kNegInf ? 0.f : m;
+        float lt = 0.f;
+        f16x8_t pf[4];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+            const float p = __builtin_amdgcn_exp2f(x[e / 16][e % 16] - base);
+            lt += p;
+            pf[e / 8][e % 8] = static_cast<_Float16>(p);
+        }
+        l = fmaf(lt, iv, l);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int kb = i / DB, d = i % DB;
+            acc[d] = mfma(decode8(vc[i][0], vc[i][1]), pf[2 * kb], acc[d]);
+            acc[d] = mfma(decode8(vc[i][2], vc[i][3]), pf[2 * kb + 1], acc[d]);
+        }
+        load_v(at.blk);
+    }
+    // the waves' results, merged in order
+    l += __shfl_xor(l, 32);
+    if (l32 < n_rows) {
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<f32x4_t*>(&rows_o[wave][l32 * PITCH + 32 * d + 8 * g + 4 * hw]) =
+                    f32x4_t{acc[d][4 * g], acc[d][4 * g + 1], acc[d][4 * g + 2], acc[d][4 * g + 3]};
+        if (hw == 0) {
+            rows_m[wave][l32] = m;
+            rows_l[wave][l32] = l;
+        }
+    }
+    __syncthreads();
+    float* const part = s.split >= 0 ? part_at<D, kKv8FewRows>(a, s.split, s.part) : nullptr;
+    for (int n = threadIdx.x; n < n_rows * (D / 4); n += 64 * kKv8FewWaves) {
+        const int r = n / (D / 4), d = 4 * (n % (D / 4));
+        float top = kNegInf;
+#pragma unroll
+        for (int w = 0; w < kKv8FewWaves; ++w) top = fmaxf(top, rows_m[w][r]);
+        const float base = top == kNegInf ? 0.f : top;
+        float sum = 0.f;
+        f32x4_t o{};
+#pragma unroll
+        for (int w = 0; w < kKv8FewWaves; ++w) {
+            const float f = __builtin_amdgcn_exp2f(rows_m[w][r] - base);
+            sum = fmaf(f, rows_l[w][r], sum);
+            const f32x4_t ow = *reinterpret_cast<const f32x4_t*>(&rows_o[w][r * PITCH + d]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = fmaf(f, ow[e], o[e]);
+        }
+        if (part != nullptr) {
+            *reinterpret_cast<f32x4_t*>(part + r * D + d) = o;
+            if (d == 0) {
+                part[kKv8FewRows * D + 2 * r] = top;
+                part[kKv8FewRows * D + 2 * r + 1] = sum;
+            }
+            continue;
+        }
+        o *= 1.f / sum;
+        const int64_t at_o = row_at(a, s.bat, s.kvh, q0 + r) * D + d;
+        if constexpr (OF32) {
+            *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.o) + at_o) = o;
+        } else {
+            bf16x4_t h;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[e] = static_cast<__bf16>(o[e]);
+            *reinterpret_cast<bf16x4_t*>(static_cast<__bf16*>(a.o) + at_o) = h;
+        }
+        if (a.lse != nullptr && d == 0)
+            a.lse[lse_at(a, s.bat, s.kvh, q0 + r)] = (top + __log2f(sum)) * 0.69314718055994530942f;
+    }
+}
+
+// ----------------------------------------------------------------------------
+// Tiles of 256 rows
+// ----------------------------------------------------------------------------
+template <int D, bool OF32>
+__global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv8AttnArgs a) {
+    constexpr int KK = D / 16, DB = D / 32;
+    constexpr int NK = 2 * KK, NV = 4 * DB, NF = NK + NV;  // operand fragments (1 KB) and MFMAs of a tile
+    constexpr int TILEB = NK * 1024;                       // bytes of a K (or V) tile in LDS
+    constexpr int NBUF = 4;
+    constexpr int RING = 4;       // fragments read ahead of their MFMA
+    constexpr int EPG = 32 / NK;  // P elements formed per score MFMA
+    constexpr int FPG = 32 / NV;  // scores scaled per P V MFMA
+    constexpr int NP = 2 * kCacheBlock * D / 16 / kTileThreads;  // pieces of codes per thread: K and V, or one
+    static_assert(NF % RING == 0 && EPG % 2 == 0 && (NP == 1 || NP == 2), "layout");
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * NBUF * TILEB];
+    lds_u8* const L = (lds_u8*)(smem);
+
+    const int tid = threadIdx.x, lane = tid & 63, hw = lane >> 5, l32 = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Share s = share_of(a);
+    const int n = s.n;
+    int q0, q1;
+    split_rows(a.rows, a.n_tiles, s.tile, q0, q1);
+    const int64_t head = (static_cast<int64_t>(s.bat) * a.Hk + s.kvh) * a.n_blocks;
+
+    // ---- codes: thread's pieces of a block, and where they go in a tile. NP = 2: piece
+    // tid of K and of V; NP = 1: waves 0..3 take K's, the others V's. A piece is two fragments'
+    // 16 bytes of the lane, next to each other in LDS.
+    const bool v_first = NP == 1 && wave >= 4;
+    const int pw = NP == 2 ? wave : wave & 3;  // piece's kb * DB + (s or d)
+    const uint32_t lane16 = 16 * lane;
+    const uint32_t to = 2 * pw * 1024 + lane16;
+    u32x4_t codes[NP];
+    float ks, vs;   // scales of the tile whose scores come next (the same in every lane)
+    int blk[NBUF];  // block j of the walk in [j % 4]
+    int cnt[NBUF];  // keys from it to its range's end
+    const int z = lane_zero();
+    Blocks at;
+    at.start(a, s.b0);
+    // The codes of the block that the walk stands on, block u of the tiles; the walk moves on by step().
+    auto load = [&](int u) __attribute__((always_inline)) {
+        const int64_t o = (head + at.blk) * (kCacheBlock * D) + 1024 * pw;
+        if constexpr (NP == 2) {
+            codes[0] = load_from<u32x4_t>(a.k_codes + o, lane16);
+            codes[1] = load_from<u32x4_t>(a.v_codes + o, lane16);
+        } else {
+            codes[0] = load_from<u32x4_t>((v_first ? a.v_codes : a.k_codes) + o, lane16);
+        }
+        blk[u & 3] = at.blk;
+        cnt[u & 3] = at.keys;
+    };
+    auto load_scales = [&](int u) __attribute__((always_inline)) {
+        ks = load_from<float>(a.k_scale + head + blk[u & 3], z);
+        vs = load_from<float>(a.v_scale + head + blk[u & 3], z);
+    };
+    // Half h of piece p into the buffers of block u.
+    auto put = [&](int p, int h, int u) __attribute__((always_inline)) {
+        const f16x8_t f = decode8(codes[p][2 * h], codes[p][2 * h + 1]);
+        const uint32_t base = NP == 2 ? p * NBUF * TILEB : v_first ? NBUF * TILEB : 0;
+        *(lds_f16x8_t*)(L + to + base + ((u & (NBUF - 1)) * TILEB + h * 1024)) = f;
+    };
+    // Fragment f of a tile's stream: K fragments (kk = f / 2, kb = f % 2) of buffer ku, then V
+    // fragments (j = (f - NK) / DB, d) of buffer vu. In LDS: (kb, kk) and (j / 2, d, j % 2).
+    auto read_frag = [&](int f, int ku, int vu) __attribute__((always_inline)) {
+        const int j = (f - NK) / DB, d = (f - NK) % DB;
+        const uint32_t o = f < NK ? (ku & (NBUF - 1)) * TILEB + ((f & 1) * KK + (f >> 1)) * 1024
+                                  : (NBUF + (vu & (NBUF - 1))) * TILEB + (((j >> 1) * DB + d) * 2 + (j & 1)) * 1024;
+        return *(const lds_f16x8_t*)(L + (lane16 + o));
+    };
+
+    f32x16_t acc[DB];
+#pragma unroll
+    for (int i = 0; i < DB; ++i) acc[i] = f32x16_t{};
+    float m = 0.f, l = 0.f, iv = 0.f;  // iv: 1 / scale of V of the tile whose P is formed
+    uint64_t fresh = 0;  // lanes whose row has had no finite score yet (m is 0 until the first)
+    auto mask_tile = [&](f32x16_t (&x)[2], int keys) __attribute__((always_inline)) {
+        // register i of block kb is key 32 kb + 16 (i / 8) + 8 hw + i % 8 (the lane's bound formed
+        // here, so that 32 keys per lane are not kept, spilled, across the loop)
+        const int bound = keys - ((fresh_thread_index() >> 2) & 8);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (32 * kb + 16 * (i / 8) + i % 8 >= bound) x[kb][i] = kNegInf;
+    };
+    auto row_max = [&](const f32x16_t (&x)[2]) __attribute__((always_inline)) {
+        float mx = fmaxf(x[0][0], x[1][0]);
+#pragma unroll
+        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, fmaxf(x[0][i], x[1][i]));
+        return both_max(mx);
+    };
+    // P of elements e and e + 1 into their operand's word, summed into *lt. The word is pinned: else
+    // the compiler rounds behind the check's branch and keeps 32 more registers until there.
+    auto form_p2 = [&](const f32x16_t (&x)[2], u32x4_t (&pf)[4], int e, float& lt) __attribute__((always_inline)) {
+        const float p0 = __builtin_amdgcn_exp2f(x[e >> 4][e & 15]);
+        const float p1 = __builtin_amdgcn_exp2f(x[(e + 1) >> 4][(e + 1) & 15]);
+        uint32_t w = __builtin_bit_cast(uint32_t, f16x2_t{static_cast<_Float16>(p0), static_cast<_Float16>(p1)});
+        asm volatile("" : "+v"(w));
+        pf[e >> 3][(e & 7) >> 1] = w;
+        lt = e < 4 ? p0 + p1 : lt + (p0 + p1);
+    };
+
+    // ---- prologue: blocks 0..2 into LDS, block 3 in registers
+#pragma unroll
+    for (int u = 0; u < 3; ++u) {
+        load(u);
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            put(p, 0, u);
+            put(p, 1, u);
+        }
+        at.step(a);
+    }
+    load(3);
+    load_scales(0);
+    const int qrow = q0 + wave * 32 + l32;
+    f16x8_t qf[KK];
+    const float cq = load_q<D>(a, row_at(a, s.bat, s.kvh, min(qrow, a.rows - 1)), qrow < q1, hw, qf);
+    __syncthreads();
+
+    // A wave without rows takes part in the loads and barriers only.
+    const bool busy = q0 + wave * 32 < q1;
+    f32x16_t xa[2], xb[2];
+    if (busy) {
+        xa[0] = xa[1] = f32x16_t{};
+#pragma unroll
+        for (int f = 0; f < NK; ++f) xa[f & 1] = mfma(read_frag(f, 0, 0), qf[f >> 1], xa[f & 1]);
+        const float c = cq * ks, add = __builtin_amdgcn_logf(vs);
+        iv = uniform_f(1.f / vs);
+        load_scales(1);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) xa[kb][i] = fmaf(xa[kb][i], c, add);
+        if (cnt[0] < kCacheBlock) mask_tile(xa, cnt[0]);
+        const float mx = row_max(xa);
+        m = mx == kNegInf ? 0.f : mx - kHeadroom;
+        fresh = __ballot(mx == kNegInf);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) xa[kb][i] -= m;
+    }
+    f16x8_t fr[RING];
+#pragma unroll
+    for (int f = 0; f < RING; ++f) fr[f] = read_frag(f, 1, 1);
+
+    // ---- iteration t, with x = x(t) and nx receiving S(t+1); u = t % 4. Stage 1: the score
+    // MFMAs of tile t+1, each with its share of P(t). Check: a lane's sum of P beyond the bound
+    // (or not a number) raises m to the tile's maximum less the headroom, rescales O and the row
+    // sum and forms P(t) again. Stage 2: the P V MFMAs of tile t, each with its share of x(t+1),
+    // of turning block t+3's codes into operands in LDS, and of loading block t+4's. Block t+3
+    // goes where block t-1 was, whose last reads lie before the barrier that ended tile t-1. The
+    // barrier that ends tile t publishes block t+3; K(t+2), read ahead here, was published by the
+    // one before.
+    auto end_tile = [&](bool reads) __attribute__((always_inline)) {
+        // this wave's LDS writes are done when at most the reads ahead behind them are not
+        if (reads) __builtin_amdgcn_s_waitcnt(0xC07F | (RING << 8));
+        else __builtin_amdgcn_s_waitcnt(kWaitLgkmcnt0);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    auto iteration = [&](int u, f32x16_t (&x)[2], f32x16_t (&nx)[2]) __attribute__((always_inline)) {
+        at.step(a);
+        u32x4_t pf[4];
+        float lt0, lt1;
+        nx[0] = nx[1] = f32x16_t{};
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int g = 0; g < NK; ++g) {
+            nx[g & 1] = mfma(fr[g % RING], qf[g >> 1], nx[g & 1]);
+            fr[g % RING] = read_frag(g + RING, u + 1, u);
+#pragma unroll
+            for (int e = EPG * g; e < EPG * (g + 1); e += 2) form_p2(x, pf, e, (e & 2) ? lt1 : lt0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        uint64_t raise = __ballot(!(lt0 + lt1 <= kRaise));
+        if (__builtin_expect((raise | fresh) != 0, 0)) {
+            raise |= raise << 32 | raise >> 32;  // both lanes of a row; other rows keep their bits
+            const float mx = row_max(x);
+            const bool first = __builtin_amdgcn_inverse_ballot_w64(fresh) && mx != kNegInf;
+            const float up = __builtin_amdgcn_inverse_ballot_w64(raise) ? fmaxf(mx - kHeadroom, 0.f) : 0.f;
+            const float dm = first ? mx - kHeadroom : up;
+            const float alpha = first ? 1.f : __builtin_amdgcn_exp2f(-dm);  // (sum and O are still 0)
+            fresh &= __ballot(mx == kNegInf);
+            m += dm;
+            l *= alpha;
+#pragma unroll
+            for (int d = 0; d < DB; ++d) acc[d] *= alpha;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[kb][i] -= dm;
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) form_p2(x, pf, e, (e & 2) ? lt1 : lt0);
+        }
+        // (as one fma the compiler kept two copies of O: 200 registers spilled)
+        l += pin(pin(lt0 + lt1) * iv);
+        float c = cq * ks;
+        // (not zero, as a tiny row's factor may be: a masked score of -inf is still to be scaled)
+        c = c < FLT_MIN ? FLT_MIN : c;
+        const float add = __builtin_amdgcn_logf(vs) - m;
+        iv = uniform_f(__builtin_amdgcn_rcpf(vs));
+        if (__builtin_expect(cnt[(u + 1) & 3] < kCacheBlock, 0)) mask_tile(nx, cnt[(u + 1) & 3]);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            acc[k % DB] = mfma(fr[(NK + k) % RING], __builtin_bit_cast(f16x8_t, pf[k / DB]), acc[k % DB]);
+            fr[(NK + k) % RING] = read_frag((NK + k + RING) % NF, NK + k + RING < NF ? u + 1 : u + 2, u);
+#pragma unroll
+            for (int e = FPG * k; e < FPG * (k + 1); ++e) nx[e >> 4][e & 15] = pin(fmaf(nx[e >> 4][e & 15], c, add));
+            // (every write lies before the last RING reads ahead)
+            if (k % 2 == 1 && k / 2 < 2 * NP) put(k / 4, k / 2 % 2, u + 3);
+            if (k == 4 * NP) load(u + 4);
+            if (k == 4 * NP + 1) load_scales(u + 2);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        end_tile(true);
+    };
+    static_assert(4 * NP < NV && 4 * NP + RING <= NV, "writes and loads inside stage 2");
+    if (busy) {
+        for (int t = 0; t < n; t += 4) {
+            iteration(0, xa, xb);
+            if (t + 1 >= n) break;
+            iteration(1, xb, xa);
+            if (t + 2 >= n) break;
+            iteration(2, xa, xb);
+            if (t + 3 >= n) break;
+            iteration(3, xb, xa);
+        }
+    } else {
+        auto idle = [&](int u) __attribute__((always_inline)) {
+#pragma unroll
+            for (int p = 0; p < NP; ++p) {
+                put(p, 0, u + 3);
+                put(p, 1, u + 3);
+            }
+            at.step(a);
+            load(u + 4);
+            end_tile(false);
+        };
+        for (int t = 0; t < n; t += 4) {
+            idle(0);
+            if (t + 1 >= n) break;
+            idle(1);
+            if (t + 2 >= n) break;
+            idle(2);
+            if (t + 3 >= n) break;
+            idle(3);
+        }
+    }
+    __syncthreads();
+
+    // ---- the rows, through the wave's share of the LDS so that they are stored whole: O over
+    // the row sum, or a part's O as it is (fp32)
+    l += __shfl_xor(l, 32);
+    const bool part_rows = s.split >= 0;
+    float* const part = part_rows ? part_at<D, kTileRows>(a, s.split, s.part) : nullptr;
+    const float inv = part_rows ? 1.f : 1.f / l;
+    if (busy) {
+        constexpr int CPR = D / 4;  // 16-byte chunks of an fp32 row
+        static_assert(kTileRows * D * 4 <= 2 * NBUF * TILEB, "output rows must fit the LDS");
+        lds_u8* const rows = L + wave * (32 * D * 4);
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                f32x4_t w;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = acc[d][4 * g + e] * inv;
+                *(lds_f32x4_t*)(rows + l32 * (D * 4) + (((8 * d + 2 * g + hw) ^ (l32 & 15)) << 4)) = w;
+            }
+        asm volatile("" ::: "memory");
+#pragma unroll 4
+        for (int i = 0; i < 32 * CPR / 64; ++i) {
+            const int ch = 64 * i + lane, row = ch / CPR, cc = ch % CPR;
+            const f32x4_t w = *(const lds_f32x4_t*)(rows + row * (D * 4) + ((cc ^ (row & 15)) << 4));
+            const int r = q0 + wave * 32 + row;
+            if (r >= q1) continue;
+            if (part_rows) {
+                *reinterpret_cast<f32x4_t*>(part + (wave * 32 + row) * D + 4 * cc) = w;
+            } else if constexpr (OF32) {
+                *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.o) + row_at(a, s.bat, s.kvh, r) * D + 4 * cc) = w;
+            } else {
+                bf16x4_t h;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) h[e] = static_cast<__bf16>(w[e]);
+                *reinterpret_cast<bf16x4_t*>(static_cast<__bf16*>(a.o) + row_at(a, s.bat, s.kvh, r) * D + 4 * cc) = h;
+            }
+        }
+        if (qrow < q1 && hw == 0) {
+            if (part_rows) {
+                part[kTileRows * D + 2 * (wave * 32 + l32)] = m;
+                part[kTileRows * D + 2 * (wave * 32 + l32) + 1] = l;
+            } else if (a.lse != nullptr) {
+                a.lse[lse_at(a, s.bat, s.kvh, qrow)] = (m + __log2f(l)) * 0.69314718055994530942f;
+            }
+        }
+    }
+}
+
+// ----------------------------------------------------------------------------
+// Merging the parts of split tiles
+// ----------------------------------------------------------------------------
+// PG = 1: a thread adds up all parts of 4 elements of a row, in order; PG = 8: 8
+// threads take every 8th part each, their sums are added up in order.
+constexpr int kMergeThreads = 256;
+template <int D, bool OF32, int ROWS, int PG>
+__global__ __launch_bounds__(kMergeThreads) void attn_kv8_merge_kernel(const Kv8AttnArgs a) {
+    constexpr int TPR = D / 4;                           // threads that hold a row
+    constexpr int RPW = kMergeThreads / (TPR * PG);      // rows of a workgroup
+    static_assert(RPW >= 1 && ROWS % RPW == 0, "whole workgroups per tile");
+    __shared__ f32x4_t sums[PG > 1 ? kMergeThreads : 1];
+    __shared__ float lsums[PG > 1 ? kMergeThreads : 1];
+    const int tid = threadIdx.x;
+    const int d = 4 * (tid % TPR), pg = tid / TPR % PG;
+    const int64_t split = blockIdx.x / (ROWS / RPW);
+    const int r = blockIdx.x % (ROWS / RPW) * RPW + tid / (TPR * PG);  // row of the tile
+    const int id = a.n_whole + static_cast<int>(split);
+    const int tile = id % a.n_tiles, bh = id / a.n_tiles;
+    const int kvh = bh % a.Hk, bat = bh / a.Hk;
+    int q0, q1;
+    if constexpr (ROWS == kKv8FewRows) {
+        q0 = tile * kKv8FewRows;
+        q1 = min(q0 + kKv8FewRows, a.rows);
+    } else {
+        split_rows(a.rows, a.n_tiles, tile, q0, q1);
+    }
+    const bool ok = q0 + r < q1;
+    const float* const p = part_at<D, ROWS>(a, split, 0);
+    constexpr int64_t step = ROWS * (D + 2);
+    float top = kNegInf, sum = 0.f;
+    f32x4_t o{};
+    if (ok) {
+        for (int i = 0; i < a.parts; ++i) top = fmaxf(top, p[i * step + ROWS * D + 2 * r]);
+        const float base = top == kNegInf ? 0.f : top;
+#pragma unroll 4
+        for (int i = pg; i < a.parts; i += PG) {
+            const float li = p[i * step + ROWS * D + 2 * r + 1];
+            // (a part with only scores of -inf has a sum of 0 and any maximum)
+            const float f = li == 0.f ? 0.f : __builtin_amdgcn_exp2f(p[i * step + ROWS * D + 2 * r] - base);
+            const f32x4_t oi = *reinterpret_cast<const f32x4_t*>(p + i * step + r * D + d);
+            sum = fmaf(f, li, sum);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = fmaf(f, oi[e], o[e]);
+        }
+    }
+    if constexpr (PG > 1) {
+        sums[tid] = o;
+        lsums[tid] = sum;
+        __syncthreads();
+        if (pg != 0) return;
+#pragma unroll
+        for (int i = 1; i < PG; ++i) {
+            o += sums[tid + i * TPR];
+            sum += lsums[tid + i * TPR];
+        }
+    }
+    if (!ok) return;
+    o *= 1.f / sum;
+    const int64_t at = row_at(a, bat, kvh, q0 + r) * D + d;
+    if constexpr (OF32) {
+        *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.o) + at) = o;
+    } else {
+        bf16x4_t h;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = static_cast<__bf16>(o[e]);
+        *reinterpret_cast<bf16x4_t*>(static_cast<__bf16*>(a.o) + at) = h;
+    }
+    if (a.lse != nullptr && d == 0) a.lse[lse_at(a, bat, kvh, q0 + r)] = (top + __log2f(sum)) * 0.69314718055994530942f;
+}
+
+template <int D, bool OF32>
+hipError_t launch(const Kv8AttnArgs& a, hipStream_t s) {
+    const int64_t total = static_cast<int64_t>(a.n_tiles) * a.B * a.Hk, split = total - a.n_whole;
+    const unsigned grid = static_cast<unsigned>(a.n_whole + split * a.parts);
+    if (a.few) hipLaunchKernelGGL((attn_kv8_few_kernel<D, OF32>), dim3(grid), dim3(64 * kKv8FewWaves), 0, s, a);
+    else hipLaunchKernelGGL((attn_kv8_tile_kernel<D, OF32>), dim3(grid), dim3(kTileThreads), 0, s, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || split == 0) return e;
+    constexpr int TPR = D / 4;
+    if (a.few) {
+        constexpr int RPW = kMergeThreads / (TPR * 8);
+        hipLaunchKernelGGL((attn_kv8_merge_kernel<D, OF32, kKv8FewRows, 8>),
+                           dim3(static_cast<unsigned>(split * (kKv8FewRows / RPW))), dim3(kMergeThreads), 0, s, a);
+    } else {
+        constexpr int RPW = kMergeThreads / TPR;
+        hipLaunchKernelGGL((attn_kv8_merge_kernel<D, OF32, kTileRows, 1>),
+                           dim3(static_cast<unsigned>(split * (kTileRows / RPW))), dim3(kMergeThreads), 0, s, a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attn_kv8(const Kv8AttnArgs& a, int head_dim, hipStream_t s) {
+    if (head_dim == 128) return a.o_f32 ? launch<128, true>(a, s) : launch<128, false>(a, s);
+    if (head_dim == 64) return a.o_f32 ? launch<64, true>(a, s) : launch<64, false>(a, s);
+    return hipErrorInvalidValue;
+}
+
+}  // namespace tmk

@@ -1094,4 +1094,360 @@ tm_status tm_rope3d_bwd(const tm_rope_desc* desc, const float* table, int32_t ba
 
 }  // extern "C"
 
+// ---- the 8-bit cache
+
+struct tm_kv8_cache {
+    tm_kv_cache book;  // descriptor, chunk order and lengths (its pools: unused)
+    int32_t kv_heads;
+    void* pool;
+};
+
+namespace {
+
+// Sizes of an 8-bit cache: those of the 16-bit one, except that every region is
+// a whole number of blocks, so that a block and its scales belong to one chunk.
+struct Kv8Geo {
+    Geo g;
+    int64_t Hk, group;
+    int64_t blocks;       // per (batch, key head)
+    size_t code_bytes;    // of one tensor
+    size_t scale_bytes;
+    size_t bytes() const { return 2 * code_bytes + 2 * scale_bytes; }
+};
+
+tm_status check_kv8(const tm_attn_desc* d, int32_t kv_heads, Kv8Geo* k) {
+    Geo& g = k->g;
+    const tm_status st = check_desc(d, &g);
+    if (st != TM_OK) return st;
+    if (g.dtype != TM_BF16) return fail(TM_E_DTYPE, "the 8-bit cache takes TM_BF16 queries, keys and values");
+    if (kv_heads < 1 || g.H % kv_heads != 0)
+        return fail(TM_E_SHAPE, "kv_heads %d must be >= 1 and divide heads %lld", kv_heads, (long long)g.H);
+    g.ref_cap = round_up(g.RT, tmk::kCacheBlock);
+    g.slot_cap = round_up(g.CT, tmk::kCacheBlock);
+    g.capacity = g.ref_cap + (g.W + 1) * g.slot_cap;
+    if (g.capacity > kMaxTokens) return fail(TM_E_SHAPE, "cache too large (more than 2^30 tokens)");
+    k->Hk = kv_heads;
+    k->group = g.H / kv_heads;
+    k->blocks = g.capacity / tmk::kCacheBlock;
+    k->code_bytes = size_t(g.B) * size_t(k->Hk) * size_t(g.capacity) * size_t(g.D);
+    k->scale_bytes = size_t(round_up(g.B * k->Hk * k->blocks * int64_t(sizeof(float)), 16));
+    return TM_OK;
+}
+
+tm_status check_cache8(const tm_kv8_cache* c, Kv8Geo* k) {
+    if (c == nullptr) return fail(TM_E_ARG, "cache is NULL");
+    return check_kv8(&c->book.desc, c->kv_heads, k);
+}
+
+// The four arrays of a cache's pool.
+template <typename Args>
+void place(const Kv8Geo& k, void* pool, Args* a) {
+    unsigned char* p = static_cast<unsigned char*>(pool);
+    a->k_codes = p;
+    a->v_codes = p + k.code_bytes;
+    a->k_scale = reinterpret_cast<float*>(p + 2 * k.code_bytes);
+    a->v_scale = reinterpret_cast<float*>(p + 2 * k.code_bytes + k.scale_bytes);
+    a->n_blocks = int32_t(k.blocks);
+}
+
+// First token row of a cached chunk and its length.
+tm_status locate8(const tm_kv8_cache* c, const Kv8Geo& k, int32_t chunk, int64_t* offset, int32_t* n_tok) {
+    if (chunk < 0 || c->book.latest < 0 || chunk > c->book.latest)
+        return fail(TM_E_ORDER, "chunk %d not in the cache", chunk);
+    if (chunk == 0) {
+        *offset = 0;
+        *n_tok = c->book.ref_len;
+        return TM_OK;
+    }
+    const int slot = int((chunk - 1) % (k.g.W + 1));
+    if (c->book.slot_chunk[slot] != chunk) return fail(TM_E_ORDER, "chunk %d was evicted", chunk);
+    *offset = k.g.ref_cap + slot * k.g.slot_cap;
+    *n_tok = c->book.slot_len[slot];
+    return TM_OK;
+}
+
+// Shared by tm_kv8_append (q == nullptr) and tm_qkv8_produce.
+tm_status write_chunk8(tm_kv8_cache* cache, int32_t chunk, const void* q, const void* k, const void* v,
+                       const float* q_gain, const float* k_gain, float eps, const tm_rope_desc* rope_desc,
+                       const float* table, int64_t first_token, void* q_out, int32_t n_tok, hipStream_t stream) {
+    Kv8Geo z;
+    tm_status st = check_cache8(cache, &z);
+    if (st != TM_OK) return st;
+    const Geo& g = z.g;
+    tm_kv_cache& book = cache->book;
+    if (book.latest < 0 ? chunk != 0 : (chunk != book.latest && chunk != book.latest + 1))
+        return fail(TM_E_ORDER, "chunk %d cannot follow latest chunk %d", chunk, book.latest);
+    if (n_tok < 1) return fail(TM_E_SHAPE, "n_tok must be >= 1");
+    const int64_t cap = chunk == 0 ? g.RT : g.CT;
+    if (n_tok > cap)
+        return fail(TM_E_CAPACITY, "n_tok %d exceeds the %s of %lld tokens", n_tok,
+                    chunk == 0 ? "reference chunk" : "chunk", (long long)cap);
+    const size_t row = size_t(g.B) * size_t(n_tok) * size_t(g.D) * 2;
+    const size_t kv_bytes = row * size_t(z.Hk), q_bytes = row * size_t(g.H);
+    if ((st = check_ptr(k, kv_bytes, "k")) != TM_OK) return st;
+    if ((st = check_ptr(v, kv_bytes, "v")) != TM_OK) return st;
+    if ((st = check_ptr(cache->pool, z.bytes(), "pool")) != TM_OK) return st;
+    if (overlaps(k, kv_bytes, cache->pool, z.bytes()) || overlaps(v, kv_bytes, cache->pool, z.bytes()))
+        return fail(TM_E_ARG, "k/v overlap the cache's pool");
+    tmk::Kv8WriteArgs a{};
+    const bool produce = q != nullptr;
+    if (produce) {
+        if (!std::isfinite(eps) || eps < 0.f) return fail(TM_E_ARG, "eps must be finite and >= 0");
+        if ((st = check_ptr(q, q_bytes, "q")) != TM_OK) return st;
+        if ((st = check_ptr(q_out, q_bytes, "q_out")) != TM_OK) return st;
+        if (q_out != q && overlaps(q_out, q_bytes, q, q_bytes))
+            return fail(TM_E_ARG, "q_out overlaps q without being q");
+        if (overlaps(q_out, q_bytes, k, kv_bytes) || overlaps(q_out, q_bytes, v, kv_bytes) ||
+            overlaps(q_out, q_bytes, cache->pool, z.bytes()))
+            return fail(TM_E_ARG, "q_out overlaps k, v or the cache's pool");
+        const size_t gain = size_t(g.D) * sizeof(float);
+        if (q_gain != nullptr && (st = check_ptr(q_gain, size_t(g.H) * gain, "q_gain")) != TM_OK) return st;
+        if (k_gain != nullptr && (st = check_ptr(k_gain, size_t(z.Hk) * gain, "k_gain")) != TM_OK) return st;
+        if (rope_desc != nullptr) {
+            RopeGeo rg;
+            if ((st = check_rope_desc(rope_desc, &rg)) != TM_OK) return st;
+            if (rope_desc->head_dim != g.D || rope_desc->dtype != TM_BF16)
+                return fail(TM_E_ARG, "the rope descriptor's head_dim or dtype is not the cache's");
+            if ((st = rope_table(rope_desc, rg, table, first_token, n_tok, &a.table)) != TM_OK) return st;
+            if (overlaps(q_out, q_bytes, table, rg.table_bytes)) return fail(TM_E_ARG, "q_out overlaps the table");
+            a.turn = 1;
+            a.first_token = first_token;
+        }
+        a.H = int32_t(g.H);
+    }
+    const int slot = chunk == 0 ? -1 : int((chunk - 1) % (g.W + 1));
+    const int64_t offset = chunk == 0 ? 0 : g.ref_cap + slot * g.slot_cap;
+    a.q = static_cast<const unsigned char*>(q);
+    a.k = static_cast<const unsigned char*>(k);
+    a.v = static_cast<const unsigned char*>(v);
+    a.q_out = static_cast<unsigned char*>(q_out);
+    a.q_gain = q_gain;
+    a.k_gain = k_gain;
+    a.eps = eps;
+    place(z, cache->pool, &a);
+    a.B = int32_t(g.B);
+    a.n_tok = n_tok;
+    a.Hk = int32_t(z.Hk);
+    a.first_blk = int32_t(offset / tmk::kCacheBlock);
+    const hipError_t e = tmk::launch_kv8_write(a, int(g.D), produce, a.turn && rope_desc->split_half != 0, stream);
+    if (e != hipSuccess)
+        return fail(TM_E_DEVICE, "%s launch: %s", produce ? "qkv8_produce" : "kv8_append", hipGetErrorString(e));
+    if (chunk == 0) {
+        tm_kv_cache_reset(&book);
+        book.ref_len = n_tok;
+    } else {
+        book.slot_chunk[slot] = chunk;
+        book.slot_len[slot] = n_tok;
+    }
+    book.latest = chunk;
+    return TM_OK;
+}
+
+// Row tiles, key blocks and key split of an attention call over the cache.
+tm_status plan_attn8(const tm_kv8_cache* cache, const Kv8Geo& z, int32_t q_chunk, int32_t n_q, tmk::Kv8AttnArgs* a) {
+    if (cache->book.latest < 0) return fail(TM_E_ORDER, "the cache is empty");
+    if (q_chunk != cache->book.latest)
+        return fail(TM_E_ORDER, "q_chunk %d is not the latest appended chunk %d", q_chunk, cache->book.latest);
+    if (n_q < 0) return fail(TM_E_SHAPE, "n_q must be >= 0");
+    const int64_t rows = int64_t(n_q) * z.group;
+    if (rows > kMaxTokens) return fail(TM_E_SHAPE, "too many query rows");
+    Plan p;
+    const tm_status st = plan_stream(z.g, &cache->book, &p);
+    if (st != TM_OK) return st;
+    for (const auto& r : p.ranges) {
+        a->range_begin[a->n_ranges] = int32_t(r.first / tmk::kCacheBlock);
+        a->range_keys[a->n_ranges++] = int32_t(r.second - r.first);
+        a->n_kblocks += int32_t(ceil_div(r.second - r.first, tmk::kCacheBlock));
+    }
+    const int64_t BH = z.g.B * z.Hk;
+    a->n_q = n_q;
+    a->rows = int32_t(rows);
+    a->few = rows <= tmk::kKv8FewRows;
+    const int64_t n_tiles = ceil_div(rows, a->few ? tmk::kKv8FewRows : tmk::kTileRowsBf16);
+    const int64_t tiles = n_tiles * BH;
+    if (tiles > INT32_MAX / 64) return fail(TM_E_SHAPE, "grid too large");
+    a->n_tiles = int32_t(n_tiles);
+    a->n_whole = int32_t(tiles);
+    a->parts = 1;
+    if (a->few) {
+        // Two workgroups on every CU, each wave of them with two key blocks at least.
+        const int64_t parts = std::min<int64_t>({2 * tmk::kCUs / std::max<int64_t>(tiles, 1),
+                                                 a->n_kblocks / (2 * tmk::kKv8FewWaves), 256});
+        if (parts >= 2) {
+            a->n_whole = 0;
+            a->parts = int32_t(parts);
+        }
+        return TM_OK;
+    }
+    // As the 16-bit forward: the tiles beyond the last full round of one per CU
+    const int64_t rest = tiles % tmk::kCUs;
+    if (rest == 0) return TM_OK;
+    const int64_t parts = std::min<int64_t>({tmk::kCUs / rest, a->n_kblocks / 4, tmk::kMaxParts});
+    if (parts < 2 || a->n_kblocks - ceil_div(a->n_kblocks, parts) < 10) return TM_OK;
+    a->n_whole = int32_t(tiles - rest);
+    a->parts = int32_t(parts);
+    return TM_OK;
+}
+
+size_t parts_bytes(const Kv8Geo& z, const tmk::Kv8AttnArgs& a) {
+    const int64_t split = int64_t(a.n_tiles) * z.g.B * z.Hk - a.n_whole;
+    const int64_t rows = a.few ? tmk::kKv8FewRows : tmk::kTileRowsBf16;
+    return size_t(split) * size_t(a.parts) * size_t(rows * (z.g.D + 2)) * sizeof(float);
+}
+
+tm_status attn8(const tm_kv8_cache* cache, const void* q, int32_t q_chunk, int32_t n_q, void* o, bool o_f32,
+                float* lse, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    Kv8Geo z;
+    tm_status st = check_cache8(cache, &z);
+    if (st != TM_OK) return st;
+    const Geo& g = z.g;
+    tmk::Kv8AttnArgs a{};
+    if ((st = plan_attn8(cache, z, q_chunk, n_q, &a)) != TM_OK) return st;
+    if (n_q == 0) return TM_OK;
+    const size_t elems = size_t(g.B) * size_t(n_q) * size_t(g.H) * size_t(g.D);
+    const size_t q_bytes = elems * 2, o_bytes = elems * (o_f32 ? 4 : 2);
+    const size_t lse_bytes = size_t(g.B) * size_t(g.H) * size_t(n_q) * sizeof(float);
+    if ((st = check_ptr(q, q_bytes, "q")) != TM_OK) return st;
+    if ((st = check_ptr(cache->pool, z.bytes(), "pool")) != TM_OK) return st;
+    if ((st = check_ptr(o, o_bytes, "o")) != TM_OK) return st;
+    if (lse != nullptr && (st = check_ptr(lse, lse_bytes, "lse", 4)) != TM_OK) return st;
+    if (overlaps(o, o_bytes, cache->pool, z.bytes())) return fail(TM_E_ARG, "o overlaps the cache's pool");
+    if ((o != q || o_f32) && overlaps(o, o_bytes, q, q_bytes))
+        return fail(TM_E_ARG, "o overlaps q (only o == q with the same dtype is allowed)");
+    if (lse != nullptr && (overlaps(lse, lse_bytes, cache->pool, z.bytes()) || overlaps(lse, lse_bytes, q, q_bytes) ||
+                           overlaps(lse, lse_bytes, o, o_bytes)))
+        return fail(TM_E_ARG, "lse overlaps another tensor");
+    const size_t need = parts_bytes(z, a);
+    if (workspace != nullptr && need > 0 && need <= workspace_bytes) {
+        if ((st = check_ptr(workspace, need, "workspace")) != TM_OK) return st;
+        if (overlaps(workspace, need, q, q_bytes) || overlaps(workspace, need, o, o_bytes) ||
+            overlaps(workspace, need, cache->pool, z.bytes()) ||
+            (lse != nullptr && overlaps(workspace, need, lse, lse_bytes)))
+            return fail(TM_E_ARG, "workspace overlaps another tensor");
+        a.part = static_cast<float*>(workspace);
+    } else {
+        a.n_whole = int32_t(int64_t(a.n_tiles) * g.B * z.Hk);
+        a.parts = 1;
+    }
+    place(z, cache->pool, &a);
+    a.q = q;
+    a.o = o;
+    a.lse = lse;
+    a.o_f32 = o_f32;
+    a.B = int32_t(g.B);
+    a.H = int32_t(g.H);
+    a.Hk = int32_t(z.Hk);
+    a.group = int32_t(z.group);
+    a.scale_log2 = float(double(g.scale) * 1.4426950408889634);
+    const hipError_t e = tmk::launch_attn_kv8(a, int(g.D), stream);
+    if (e != hipSuccess) return fail(TM_E_DEVICE, "attention launch: %s", hipGetErrorString(e));
+    return TM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t tm_kv8_cache_tokens(const tm_attn_desc* desc) {
+    Kv8Geo z;
+    return check_kv8(desc, 1, &z) == TM_OK ? z.g.capacity : 0;
+}
+
+size_t tm_kv8_cache_bytes(const tm_attn_desc* desc, int32_t kv_heads) {
+    Kv8Geo z;
+    return check_kv8(desc, kv_heads, &z) == TM_OK ? z.bytes() : 0;
+}
+
+tm_status tm_kv8_cache_create(const tm_attn_desc* desc, int32_t kv_heads, void* pool, tm_kv8_cache** out) {
+    Kv8Geo z;
+    tm_status st = check_kv8(desc, kv_heads, &z);
+    if (st != TM_OK) return st;
+    if (out == nullptr) return fail(TM_E_ARG, "out is NULL");
+    if ((st = check_ptr(pool, z.bytes(), "pool")) != TM_OK) return st;
+    tm_kv8_cache* c = new (std::nothrow) tm_kv8_cache{};
+    if (c == nullptr) return fail(TM_E_ARG, "out of host memory");
+    c->book.desc = *desc;
+    c->kv_heads = kv_heads;
+    c->pool = pool;
+    tm_kv_cache_reset(&c->book);
+    *out = c;
+    return TM_OK;
+}
+
+void tm_kv8_cache_destroy(tm_kv8_cache* cache) { delete cache; }
+
+tm_status tm_kv8_cache_reset(tm_kv8_cache* cache) {
+    return tm_kv_cache_reset(cache == nullptr ? nullptr : &cache->book);
+}
+
+int32_t tm_kv8_cache_latest(const tm_kv8_cache* cache) { return cache ? cache->book.latest : -1; }
+
+tm_status tm_kv8_cache_locate(const tm_kv8_cache* cache, int32_t chunk, int32_t* token_offset, int32_t* n_tok) {
+    if (token_offset == nullptr || n_tok == nullptr) return fail(TM_E_ARG, "NULL argument");
+    Kv8Geo z;
+    int64_t at = 0;
+    tm_status st = check_cache8(cache, &z);
+    if (st == TM_OK) st = locate8(cache, z, chunk, &at, n_tok);
+    if (st == TM_OK) *token_offset = int32_t(at);
+    return st;
+}
+
+tm_status tm_kv8_append(tm_kv8_cache* cache, int32_t chunk, const void* k, const void* v, int32_t n_tok,
+                        hipStream_t stream) {
+    return write_chunk8(cache, chunk, nullptr, k, v, nullptr, nullptr, 0.f, nullptr, nullptr, 0, nullptr, n_tok,
+                        stream);
+}
+
+tm_status tm_qkv8_produce(tm_kv8_cache* cache, int32_t chunk, const void* q, const void* k, const void* v,
+                          const float* q_gain, const float* k_gain, float eps, const tm_rope_desc* rope_desc,
+                          const float* table, int64_t first_token, void* q_out, int32_t n_tok,
+                          hipStream_t stream) {
+    if (q == nullptr) return fail(TM_E_ARG, "q is NULL");
+    return write_chunk8(cache, chunk, q, k, v, q_gain, k_gain, eps, rope_desc, table, first_token, q_out, n_tok,
+                        stream);
+}
+
+tm_status tm_kv8_read(const tm_kv8_cache* cache, int32_t chunk, void* k_out, void* v_out, int32_t out_f32,
+                      hipStream_t stream) {
+    Kv8Geo z;
+    tm_status st = check_cache8(cache, &z);
+    if (st != TM_OK) return st;
+    int64_t at = 0;
+    int32_t n_tok = 0;
+    if ((st = locate8(cache, z, chunk, &at, &n_tok)) != TM_OK) return st;
+    const size_t bytes = size_t(z.g.B) * size_t(n_tok) * size_t(z.Hk) * size_t(z.g.D) * (out_f32 ? 4 : 2);
+    if ((st = check_ptr(k_out, bytes, "k_out")) != TM_OK) return st;
+    if ((st = check_ptr(v_out, bytes, "v_out")) != TM_OK) return st;
+    if ((st = check_ptr(cache->pool, z.bytes(), "pool")) != TM_OK) return st;
+    if (overlaps(k_out, bytes, v_out, bytes) || overlaps(k_out, bytes, cache->pool, z.bytes()) ||
+        overlaps(v_out, bytes, cache->pool, z.bytes()))
+        return fail(TM_E_ARG, "k_out and v_out overlap each other or the cache's pool");
+    tmk::Kv8ReadArgs a{};
+    place(z, cache->pool, &a);
+    a.k_out = static_cast<unsigned char*>(k_out);
+    a.v_out = static_cast<unsigned char*>(v_out);
+    a.B = int32_t(z.g.B);
+    a.n_tok = n_tok;
+    a.Hk = int32_t(z.Hk);
+    a.first_blk = int32_t(at / tmk::kCacheBlock);
+    const hipError_t e = tmk::launch_kv8_read(a, int(z.g.D), out_f32 != 0, stream);
+    if (e != hipSuccess) return fail(TM_E_DEVICE, "kv8_read launch: %s", hipGetErrorString(e));
+    return TM_OK;
+}
+
+size_t tm_kv8_attn_workspace(const tm_kv8_cache* cache, int32_t q_chunk, int32_t n_q) {
+    Kv8Geo z;
+    tmk::Kv8AttnArgs a{};
+    if (check_cache8(cache, &z) != TM_OK || plan_attn8(cache, z, q_chunk, n_q, &a) != TM_OK) return 0;
+    return parts_bytes(z, a);
+}
+
+tm_status tm_kv8_attn_fwd(const tm_kv8_cache* cache, const void* q, int32_t q_chunk, int32_t n_q, void* o,
+                          int32_t o_f32, float* lse, void* workspace, size_t workspace_bytes,
+                          hipStream_t stream) {
+    return attn8(cache, q, q_chunk, n_q, o, o_f32 != 0, lse, workspace, workspace_bytes, stream);
+}
+
+}  // extern "C"
+
 extern "C" const char* tm_last_error(void) { return g_err; }

@@ -220,4 +220,76 @@ struct RopeArgs {
 hipError_t launch_rope(const RopeArgs& a, int head_dim, int elem_bytes, bool halves, hipStream_t s);
 hipError_t launch_rope_table(const int64_t (&rows)[3], const int (&pairs)[3], double theta, float* out, hipStream_t s);
 
+// One chunk into the 8-bit cache (layout: tm_kv8.h): k, v [B, n_tok, Hk, D] in
+// bf16, into the blocks of every (batch, key head) from first_blk on. The
+// producer also takes q [B, n_tok, H, D] into q_out (which may be q), and
+// RMS-normalises and, with turn, rotates q and k.
+struct Kv8WriteArgs {
+    const unsigned char* q;
+    const unsigned char* k;
+    const unsigned char* v;
+    unsigned char* q_out;
+    const float* q_gain;  // [H, D] or null
+    const float* k_gain;  // [Hk, D] or null
+    float eps;
+    int32_t turn;
+    RopeTable table;
+    int64_t first_token;
+    unsigned char* k_codes;  // [B, Hk, n_blocks][64 * D]
+    unsigned char* v_codes;
+    float* k_scale;  // [B, Hk, n_blocks]
+    float* v_scale;
+    int32_t B, n_tok, H, Hk;
+    int32_t n_blocks;   // of 64 tokens per (batch, key head) of the cache
+    int32_t first_blk;  // the chunk's first one
+    int32_t n_blk;      // the chunk's; this and the next two set by the launcher
+    int32_t q_slices;   // threads that share a token's query heads
+    uint32_t kv_wgs;    // workgroups for K and V; those past them take queries
+};
+hipError_t launch_kv8_write(Kv8WriteArgs a, int head_dim, bool produce, bool halves, hipStream_t s);
+
+// A chunk of the 8-bit cache back into k_out, v_out [B, n_tok, Hk, D], bf16 or fp32.
+struct Kv8ReadArgs {
+    const unsigned char* k_codes;
+    const unsigned char* v_codes;
+    const float* k_scale;
+    const float* v_scale;
+    unsigned char* k_out;
+    unsigned char* v_out;
+    int32_t B, n_tok, Hk;
+    int32_t n_blocks, first_blk;
+    int32_t n_blk;  // set by the launcher
+};
+hipError_t launch_kv8_read(Kv8ReadArgs a, int head_dim, bool of32, hipStream_t s);
+
+// Attention over the 8-bit cache. The n_q * group query rows of a (batch, key
+// head), token by token, see the same keys: blocks [range_begin, range_begin +
+// ceil(range_keys / 64)) of each range, the last one's first keys only.
+struct Kv8AttnArgs {
+    const void* q;  // [B, n_q, H, D] bf16
+    void* o;        // the same, or fp32
+    float* lse;     // [B, H, n_q] or null
+    const unsigned char* k_codes;
+    const unsigned char* v_codes;
+    const float* k_scale;
+    const float* v_scale;
+    float* part;     // partial rows of the split tiles: [split tile][part][tile rows][D + 2], or null
+    int32_t o_f32;
+    int32_t B, H, Hk, group;  // group = H / Hk
+    int32_t n_q, rows;        // rows = n_q * group
+    int32_t n_blocks;         // per (batch, key head) of the cache
+    float scale_log2;         // softmax scale * log2(e)
+    int32_t few;              // rows are few: 32 a tile, their keys shared out over a workgroup's waves
+    int32_t n_tiles;          // row tiles per (batch, key head)
+    int32_t n_whole;          // tiles (of all heads) that are not split
+    int32_t parts;            // key shares of a split tile
+    int32_t n_kblocks;        // key blocks of all ranges
+    int32_t n_ranges;
+    int32_t range_begin[kMaxRanges];  // in blocks
+    int32_t range_keys[kMaxRanges];
+};
+constexpr int kKv8FewRows = 32;  // rows of a tile where rows are few
+constexpr int kKv8FewWaves = 4;  // waves that share its keys out
+hipError_t launch_attn_kv8(const Kv8AttnArgs& a, int head_dim, hipStream_t s);
+
 }  // namespace tmk

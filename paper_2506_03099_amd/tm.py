@@ -143,6 +143,21 @@ def lib() -> ctypes.CDLL:
             "tm_rope3d_table": (ctypes.c_int, [RD, P, P]),
             "tm_rope3d_fwd": (ctypes.c_int, rope),
             "tm_rope3d_bwd": (ctypes.c_int, rope),
+            "tm_kv8_cache_tokens": (ctypes.c_int64, [D]),
+            "tm_kv8_cache_bytes": (ctypes.c_size_t, [D, ctypes.c_int32]),
+            "tm_kv8_cache_create": (ctypes.c_int, [D, ctypes.c_int32, P, ctypes.POINTER(P)]),
+            "tm_kv8_cache_destroy": (None, [P]),
+            "tm_kv8_cache_reset": (ctypes.c_int, [P]),
+            "tm_kv8_cache_latest": (ctypes.c_int32, [P]),
+            "tm_kv8_cache_locate": (ctypes.c_int, [P, ctypes.c_int32, ctypes.POINTER(ctypes.c_int32),
+                                                   ctypes.POINTER(ctypes.c_int32)]),
+            "tm_kv8_append": (ctypes.c_int, [P, ctypes.c_int32, P, P, ctypes.c_int32, P]),
+            "tm_qkv8_produce": (ctypes.c_int, [P, ctypes.c_int32, P, P, P, P, P, ctypes.c_float, RD, P,
+                                               ctypes.c_int64, P, ctypes.c_int32, P]),
+            "tm_kv8_read": (ctypes.c_int, [P, ctypes.c_int32, P, P, ctypes.c_int32, P]),
+            "tm_kv8_attn_workspace": (ctypes.c_size_t, [P, ctypes.c_int32, ctypes.c_int32]),
+            "tm_kv8_attn_fwd": (ctypes.c_int, [P, P, ctypes.c_int32, ctypes.c_int32, P, ctypes.c_int32,
+                                               P, P, ctypes.c_size_t, P]),
             "tm_last_error": (ctypes.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -467,3 +482,130 @@ def tm_rope3d_bwd(desc: tm_rope_desc, table, dq_out, dk_out=None, first_token: i
                   stream=None):
     """Gradients (dq, dk) of ``tm_rope3d_fwd``'s inputs from those of its outputs."""
     return _rope(lib().tm_rope3d_bwd, desc, table, dq_out, dk_out, first_token, dq, dk, stream)
+
+
+def tm_kv8_cache_tokens(desc: tm_attn_desc) -> int:
+    return lib().tm_kv8_cache_tokens(ctypes.byref(desc))
+
+
+def tm_kv8_cache_bytes(desc: tm_attn_desc, kv_heads: int) -> int:
+    return lib().tm_kv8_cache_bytes(ctypes.byref(desc), kv_heads)
+
+
+class KV8Cache:
+    """A ``tm_kv8_cache`` handle together with the torch tensor that owns its
+    pool (codes and scales). ``kv_heads``: key heads, the descriptor's heads by
+    default."""
+
+    def __init__(self, desc: tm_attn_desc, kv_heads: int | None = None, device="cuda", pool=None):
+        self.desc = desc
+        self.kv_heads = desc.heads if kv_heads is None else kv_heads
+        h = ctypes.c_void_p()
+        if pool is None:
+            n = tm_kv8_cache_bytes(desc, self.kv_heads)
+            if n == 0:  # invalid: let the library say why
+                _check(lib().tm_kv8_cache_create(ctypes.byref(desc), self.kv_heads, None, ctypes.byref(h)))
+            pool = torch.empty(n, dtype=torch.uint8, device=device)
+        elif pool.numel() * pool.element_size() < tm_kv8_cache_bytes(desc, self.kv_heads):
+            raise TMError(TM_E_ARG, "pool is smaller than the cache")
+        self.pool = pool
+        _check(lib().tm_kv8_cache_create(ctypes.byref(desc), self.kv_heads, _ptr(pool), ctypes.byref(h)))
+        self.handle = h
+
+    @property
+    def capacity(self) -> int:
+        return tm_kv8_cache_tokens(self.desc)
+
+    def close(self):
+        if getattr(self, "handle", None) is not None and _lib is not None:
+            _lib.tm_kv8_cache_destroy(self.handle)
+            self.handle = None
+
+    __del__ = close
+
+    def latest(self) -> int:
+        return lib().tm_kv8_cache_latest(self.handle)
+
+    def locate(self, chunk: int):
+        off, n = ctypes.c_int32(), ctypes.c_int32()
+        _check(lib().tm_kv8_cache_locate(self.handle, chunk, ctypes.byref(off), ctypes.byref(n)))
+        return off.value, n.value
+
+    def reset(self):
+        _check(lib().tm_kv8_cache_reset(self.handle))
+
+    def check_rows(self, heads: int, **tensors):
+        """Each tensor must be bf16 [batch, n, heads, head_dim] of the cache, all of one n."""
+        n = None
+        for name, t in tensors.items():
+            if t.dim() != 4 or t.dtype != torch.bfloat16 or (t.shape[0], t.shape[2], t.shape[3]) != (
+                    self.desc.batch, heads, self.desc.head_dim) or n not in (None, t.shape[1]):
+                raise TMError(TM_E_SHAPE, f"{name} is not bf16 [{self.desc.batch}, n, {heads}, {self.desc.head_dim}]")
+            n = t.shape[1]
+        return n
+
+
+def tm_kv8_cache_create(desc: tm_attn_desc, kv_heads: int | None = None, device="cuda", pool=None) -> KV8Cache:
+    return KV8Cache(desc, kv_heads, device, pool)
+
+
+def tm_kv8_append(cache: KV8Cache, chunk: int, k, v, stream=None):
+    """Quantise chunk ``chunk``'s K/V (bf16 ``[B, n_tok, kv_heads, D]``) into the cache."""
+    n = cache.check_rows(cache.kv_heads, k=k, v=v)
+    _check(lib().tm_kv8_append(cache.handle, chunk, _ptr(k), _ptr(v), n, _stream(stream)))
+
+
+def tm_qkv8_produce(cache: KV8Cache, chunk: int, q, k, v, q_gain=None, k_gain=None, eps: float = 0.0,
+                    rope: tm_rope_desc | None = None, table=None, first_token: int = 0, q_out=None,
+                    stream=None):
+    """RMS-normalise the chunk's q and k rows, rotate them if ``rope`` (with its
+    ``table``) is given, and quantise k and v into the cache; returns ``q_out``
+    (allocated like q if not given)."""
+    n = cache.check_rows(cache.kv_heads, k=k, v=v)
+    if cache.check_rows(cache.desc.heads, q=q) != n:
+        raise TMError(TM_E_SHAPE, "q and k differ in tokens")
+    _expect("q_gain", q_gain, q.shape[2:], torch.float32)
+    _expect("k_gain", k_gain, k.shape[2:], torch.float32)
+    _expect("q_out", q_out, q.shape, q.dtype)
+    if rope is not None:
+        _expect("table", table, _rope_table_shape(rope), torch.float32)
+    if q_out is None:
+        q_out = torch.empty_like(q)
+    _check(lib().tm_qkv8_produce(cache.handle, chunk, _ptr(q), _ptr(k), _ptr(v), _ptr(q_gain), _ptr(k_gain),
+                                 eps, None if rope is None else ctypes.byref(rope), _ptr(table), first_token,
+                                 _ptr(q_out), n, _stream(stream)))
+    return q_out
+
+
+def tm_kv8_read(cache: KV8Cache, chunk: int, dtype=torch.bfloat16, k_out=None, v_out=None, stream=None):
+    """The keys and values that the cached chunk stands for, ``[B, n_tok,
+    kv_heads, D]`` in bf16 or fp32 (allocated if not given)."""
+    f32 = _dtype(dtype) == TM_F32
+    dt = torch.float32 if f32 else torch.bfloat16
+    shape = (cache.desc.batch, cache.locate(chunk)[1], cache.kv_heads, cache.desc.head_dim)
+    _expect("k_out", k_out, shape, dt)
+    _expect("v_out", v_out, shape, dt)
+    k_out = torch.empty(shape, dtype=dt, device=cache.pool.device) if k_out is None else k_out
+    v_out = torch.empty(shape, dtype=dt, device=cache.pool.device) if v_out is None else v_out
+    _check(lib().tm_kv8_read(cache.handle, chunk, _ptr(k_out), _ptr(v_out), int(f32), _stream(stream)))
+    return k_out, v_out
+
+
+def tm_kv8_attn_fwd(cache: KV8Cache, q, q_chunk: int, o=None, o_f32: bool = False, lse=None, stream=None):
+    """Attention of the query rows ``q`` (bf16 ``[B, n_q, H, D]``, any number of
+    rows of the latest chunk ``q_chunk``) over the 8-bit cache; returns ``o``
+    (allocated like q, or as fp32, if not given). Rows that leave the GPU idle
+    share their keys out through a workspace of torch's allocator; calls that
+    can have none (under capture, on another stream than the current one) order
+    the fp32 sums otherwise."""
+    n_q = cache.check_rows(cache.desc.heads, q=q)
+    _expect("o", o, q.shape, torch.float32 if o_f32 else torch.bfloat16)
+    _expect("lse", lse, (cache.desc.batch, cache.desc.heads, n_q), torch.float32)
+    if o is None:
+        o = torch.empty(q.shape, dtype=torch.float32, device=q.device) if o_f32 else torch.empty_like(q)
+    pq, po, pl = _ptr(q), _ptr(o), _ptr(lse)
+    stream = _stream(stream)
+    n = lib().tm_kv8_attn_workspace(cache.handle, q_chunk, n_q)
+    ws = _workspace(n, q, stream)
+    _check(lib().tm_kv8_attn_fwd(cache.handle, pq, q_chunk, n_q, po, int(o_f32), pl, _ptr(ws), n, stream))
+    return o
