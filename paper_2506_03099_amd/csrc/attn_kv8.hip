@@ -704,16 +704,18 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
 // threads take every 8th part each, their sums are added up in order.
 constexpr int kMergeThreads = 256;
 template <int D, bool OF32, int ROWS, int PG>
-__global__ __launch_bounds__(kMergeThreads) void attn_kv8_merge_kernel(const Kv8AttnArgs a) {
+__global__ __launch_bounds__(kMergeThreads) void attn_kv8_merge_kernel(const Kv8AttnArgs a, int rows_per_tile) {
     constexpr int TPR = D / 4;                           // threads that hold a row
     constexpr int RPW = kMergeThreads / (TPR * PG);      // rows of a workgroup
+    constexpr int U = 4;                                 // parts loaded together
     static_assert(RPW >= 1 && ROWS % RPW == 0, "whole workgroups per tile");
     __shared__ f32x4_t sums[PG > 1 ? kMergeThreads : 1];
-    __shared__ float lsums[PG > 1 ? kMergeThreads : 1];
+    __shared__ float lsums[PG > 1 ? kMergeThreads : 1], tops[PG > 1 ? kMergeThreads : 1];
     const int tid = threadIdx.x;
     const int d = 4 * (tid % TPR), pg = tid / TPR % PG;
-    const int64_t split = blockIdx.x / (ROWS / RPW);
-    const int r = blockIdx.x % (ROWS / RPW) * RPW + tid / (TPR * PG);  // row of the tile
+    const int wgs = (rows_per_tile + RPW - 1) / RPW;
+    const int64_t split = blockIdx.x / wgs;
+    const int r = blockIdx.x % wgs * RPW + tid / (TPR * PG);  // row of the tile
     const int id = a.n_whole + static_cast<int>(split);
     const int tile = id % a.n_tiles, bh = id / a.n_tiles;
     const int kvh = bh % a.Hk, bat = bh / a.Hk;
@@ -727,31 +729,52 @@ __global__ __launch_bounds__(kMergeThreads) void attn_kv8_merge_kernel(const Kv8
     const bool ok = q0 + r < q1;
     const float* const p = part_at<D, ROWS>(a, split, 0);
     constexpr int64_t step = ROWS * (D + 2);
+    // one pass: the sum so far is rescaled where a part raises the maximum
     float top = kNegInf, sum = 0.f;
     f32x4_t o{};
     if (ok) {
-        for (int i = 0; i < a.parts; ++i) top = fmaxf(top, p[i * step + ROWS * D + 2 * r]);
-        const float base = top == kNegInf ? 0.f : top;
-#pragma unroll 4
-        for (int i = pg; i < a.parts; i += PG) {
-            const float li = p[i * step + ROWS * D + 2 * r + 1];
-            // (a part with only scores of -inf has a sum of 0 and any maximum)
-            const float f = li == 0.f ? 0.f : __builtin_amdgcn_exp2f(p[i * step + ROWS * D + 2 * r] - base);
-            const f32x4_t oi = *reinterpret_cast<const f32x4_t*>(p + i * step + r * D + d);
-            sum = fmaf(f, li, sum);
+        for (int i0 = pg; i0 < a.parts; i0 += U * PG) {
+            float mi[U], li[U];
+            f32x4_t oi[U];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = fmaf(f, oi[e], o[e]);
+            for (int u = 0; u < U; ++u) {  // (past the end: the last part again, which then counts for nothing)
+                const float* const pi = p + min(i0 + u * PG, a.parts - 1) * step;
+                mi[u] = pi[ROWS * D + 2 * r];
+                li[u] = pi[ROWS * D + 2 * r + 1];
+                oi[u] = *reinterpret_cast<const f32x4_t*>(pi + r * D + d);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                // (a part with only scores of -inf has a sum of 0 and any maximum)
+                if (i0 + u * PG >= a.parts || li[u] == 0.f) continue;
+                const float nm = fmaxf(top, mi[u]);
+                const float keep = top == kNegInf ? 0.f : __builtin_amdgcn_exp2f(top - nm);
+                const float take = __builtin_amdgcn_exp2f(mi[u] - nm);
+                top = nm;
+                sum = fmaf(take, li[u], sum * keep);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = fmaf(take, oi[u][e], o[e] * keep);
+            }
         }
     }
     if constexpr (PG > 1) {
         sums[tid] = o;
         lsums[tid] = sum;
+        tops[tid] = top;
         __syncthreads();
         if (pg != 0) return;
 #pragma unroll
         for (int i = 1; i < PG; ++i) {
-            o += sums[tid + i * TPR];
-            sum += lsums[tid + i * TPR];
+            const float li = lsums[tid + i * TPR], mi = tops[tid + i * TPR];
+            if (li == 0.f) continue;
+            const float nm = fmaxf(top, mi);
+            const float keep = top == kNegInf ? 0.f : __builtin_amdgcn_exp2f(top - nm);
+            const float take = __builtin_amdgcn_exp2f(mi - nm);
+            top = nm;
+            sum = fmaf(take, li, sum * keep);
+            const f32x4_t oi = sums[tid + i * TPR];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = fmaf(take, oi[e], o[e] * keep);
         }
     }
     if (!ok) return;
@@ -776,15 +799,14 @@ hipError_t launch(const Kv8AttnArgs& a, hipStream_t s) {
     else hipLaunchKernelGGL((attn_kv8_tile_kernel<D, OF32>), dim3(grid), dim3(kTileThreads), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || split == 0) return e;
-    constexpr int TPR = D / 4;
+    const int rows = min(a.rows, a.few ? kKv8FewRows : kTileRows);
+    auto wgs = [&](int rpw) { return dim3(static_cast<unsigned>(split * ((rows + rpw - 1) / rpw))); };
     if (a.few) {
-        constexpr int RPW = kMergeThreads / (TPR * 8);
-        hipLaunchKernelGGL((attn_kv8_merge_kernel<D, OF32, kKv8FewRows, 8>),
-                           dim3(static_cast<unsigned>(split * (kKv8FewRows / RPW))), dim3(kMergeThreads), 0, s, a);
+        hipLaunchKernelGGL((attn_kv8_merge_kernel<D, OF32, kKv8FewRows, 8>), wgs(kMergeThreads / (D / 4 * 8)),
+                           dim3(kMergeThreads), 0, s, a, rows);
     } else {
-        constexpr int RPW = kMergeThreads / TPR;
-        hipLaunchKernelGGL((attn_kv8_merge_kernel<D, OF32, kTileRows, 1>),
-                           dim3(static_cast<unsigned>(split * (kTileRows / RPW))), dim3(kMergeThreads), 0, s, a);
+        hipLaunchKernelGGL((attn_kv8_merge_kernel<D, OF32, kTileRows, 1>), wgs(kMergeThreads / (D / 4)),
+                           dim3(kMergeThreads), 0, s, a, rows);
     }
     return hipGetLastError();
 }

@@ -61,14 +61,14 @@ __device__ __forceinline__ void normalise(float (&x)[kRowElems], const float* ga
     for (int e = 0; e < kRowElems; ++e) x[e] = x[e] * r * gain[e];
 }
 
-template <int D, bool HALVES>
+template <int D>
 __device__ __forceinline__ void load_gains(const float* gain, int g, float (&w)[kRowElems]) {
 #pragma unroll
     for (int e = 0; e < kRowElems; ++e) w[e] = 1.f;
     if (gain == nullptr) return;
 #pragma unroll
     for (int e = 0; e < kRowElems; e += 4) {
-        const f32x4_t v = *reinterpret_cast<const f32x4_t*>(gain + run_of<D, HALVES>(g, e / 8) + e % 8);
+        const f32x4_t v = *reinterpret_cast<const f32x4_t*>(gain + run_of<2, D>(g, e / 8) + e % 8);
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[e + i] = v[i];
     }
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_write_kernel(const Kv8WriteAr
                                                         // column fall on 64 different banks
     constexpr int PIECES = kCacheBlock * D / 16;        // of one tensor of the block
     static_assert(IT >= 1 && IT * RPI == kCacheBlock, "whole passes");
-    __shared__ uint32_t tile[2][kCacheBlock * PITCH];
+    __shared__ __attribute__((aligned(16))) uint32_t tile[2][kCacheBlock * PITCH];
     __shared__ uint32_t tops[2][kKv8Threads / 64];
 
     const int tid = threadIdx.x;
@@ -136,20 +136,20 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_write_kernel(const Kv8WriteAr
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int h = s + u * a.q_slices;
-                if (h < a.H) bits[u] = load_row<2, D, HALVES>(a.q + (row * a.H + h) * (D * 2), g);
+                if (h < a.H) bits[u] = load_row<2, D>(a.q + (row * a.H + h) * (D * 2), g);
             }
             float2 cs[8];
-            if (a.turn) load_turns(a.table, a.first_token + row % a.n_tok, g, cs);
+            if (a.turn) load_turns<2, D, HALVES>(a.table, a.first_token + row % a.n_tok, g, cs);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int h = s + u * a.q_slices;
                 if (h >= a.H) continue;
                 float x[kRowElems], w[kRowElems];
                 unpack_row<2>(bits[u], x);
-                load_gains<D, HALVES>(a.q_gain != nullptr ? a.q_gain + h * D : nullptr, g, w);
+                load_gains<D>(a.q_gain != nullptr ? a.q_gain + h * D : nullptr, g, w);
                 normalise<D>(x, w, a.eps);
                 if (a.turn) turn_row<HALVES>(x, cs);
-                store_row<2, D, HALVES>(a.q_out + (row * a.H + h) * (D * 2), g, x);
+                store_row<2, D>(a.q_out + (row * a.H + h) * (D * 2), g, x);
             }
             return;
         }
@@ -170,14 +170,14 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_write_kernel(const Kv8WriteAr
 #pragma unroll
         for (int i = 0; i < 2; ++i) kb[it].v[i] = vb[it].v[i] = u32x4_t{0, 0, 0, 0};
         if (t < a.n_tok) {
-            kb[it] = load_row<2, D, HALVES>(a.k + first + t * stride, g);
-            vb[it] = load_row<2, D, HALVES>(a.v + first + t * stride, g);
+            kb[it] = load_row<2, D>(a.k + first + t * stride, g);
+            vb[it] = load_row<2, D>(a.v + first + t * stride, g);
         }
     }
     float xk[IT][kRowElems], xv[IT][kRowElems];
     uint32_t mk = 0, mv = 0;
     float w[kRowElems];
-    if constexpr (PRODUCE) load_gains<D, HALVES>(a.k_gain != nullptr ? a.k_gain + h * D : nullptr, g, w);
+    if constexpr (PRODUCE) load_gains<D>(a.k_gain != nullptr ? a.k_gain + h * D : nullptr, g, w);
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
         unpack_row<2>(kb[it], xk[it]);
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_write_kernel(const Kv8WriteAr
         if constexpr (PRODUCE) {
             const int64_t t = t0 + r0 + it * RPI;
             float2 cs[8];
-            if (a.turn) load_turns(a.table, a.first_token + min(t, static_cast<int64_t>(a.n_tok - 1)), g, cs);
+            if (a.turn) load_turns<2, D, HALVES>(a.table, a.first_token + min(t, static_cast<int64_t>(a.n_tok - 1)), g, cs);
             normalise<D>(xk[it], w, a.eps);
             if (a.turn) turn_row<HALVES>(xk[it], cs);
             // (eps 0 makes NaN of a row of zeros, which rows past the chunk's end are not)
@@ -221,7 +221,7 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_write_kernel(const Kv8WriteAr
         const int r = r0 + it * RPI;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            const int c = r * PITCH + run_of<D, HALVES>(g, half) / 4;
+            const int c = r * PITCH + run_of<2, D>(g, half) / 4;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 tile[0][c + i] = codes4(xk[it] + 8 * half + 4 * i, ik);
@@ -237,12 +237,15 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_write_kernel(const Kv8WriteAr
         const uint32_t* const from = &tile[0][(32 * half + k_perm(lane % 32)) * PITCH + 8 * s + 2 * (lane / 32)];
         store16_through(ko + 16 * n, u32x4_t{from[0], from[1], from[4], from[5]});
     }
-    // V: 4 dimensions of 16 keys, transposed, are 4 pieces next to each other.
-    unsigned char* const vo = a.v_codes + at * (kCacheBlock * D);
-    for (int n = tid; n < PIECES / 4; n += kKv8Threads) {
-        const int quad = n % (D / 4), hw = n / (D / 4) % 2, half = n / (D / 4) / 2;
+    // V: 4 dimensions of 16 keys, transposed, are 4 pieces next to each other. They go through LDS
+    // once more, so that a wave stores a whole KB (four pieces a lane, each store a quarter of its
+    // lines: see the times above).
+    constexpr int QUADS = (PIECES / 4 + kKv8Threads - 1) / kKv8Threads;
+    static_assert(QUADS == 1, "a thread transposes at most once");
+    u32x4_t p[4];
+    const int quad = tid % (D / 4), hw = tid / (D / 4) % 2, half = tid / (D / 4) / 2;
+    if (tid < PIECES / 4) {
         const uint32_t* const from = &tile[1][(32 * half + 8 * hw) * PITCH + quad];
-        u32x4_t p[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {  // keys 4 (i % 2) .. of the run's first or second 16
             uint32_t r[4];
@@ -252,10 +255,17 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_write_kernel(const Kv8WriteAr
 #pragma unroll
             for (int e = 0; e < 4; ++e) p[e][i] = r[e];
         }
+    }
+    __syncthreads();
+    u32x4_t* const pieces = reinterpret_cast<u32x4_t*>(tile);
+    if (tid < PIECES / 4) {
         const int d = quad / 8, l = 4 * (quad % 8) + 32 * hw;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) store16_through(vo + 16 * ((half * (D / 32) + d) * 64 + l + e), p[e]);
+        for (int e = 0; e < 4; ++e) pieces[(half * (D / 32) + d) * 64 + l + e] = p[e];
     }
+    __syncthreads();
+    unsigned char* const vo = a.v_codes + at * (kCacheBlock * D);
+    for (int n = tid; n < PIECES; n += kKv8Threads) store16_through(vo + 16 * n, pieces[n]);
 }
 
 // The values a chunk's codes stand for, [B, n_tok, Hk, D], rounded to bf16 (OF32:
@@ -317,12 +327,12 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_read_kernel(const Kv8ReadArgs
             float v[kRowElems];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t w = tile[x][r * PITCH + 4 * g + i];
+                const uint32_t w = tile[x][r * PITCH + (run_of<EB, D>(g, 4 * i * EB / 16) + 4 * i % (16 / EB)) / 4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     v[4 * i + e] = (static_cast<float>((w >> (8 * e)) & 0xFFu) - 128.f) * (x == 0 ? sk : sv);
             }
-            store_row<EB, D, false>((x == 0 ? a.k_out : a.v_out) + first + t * stride, g, v);
+            store_row<EB, D>((x == 0 ? a.k_out : a.v_out) + first + t * stride, g, v);
         }
     }
 }

@@ -47,11 +47,11 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(const RopeArgs a) {
     for (int u = 0; u < U; ++u) {
         const int h = s + u * a.slices;
         if (h < heads)
-            bits[u] = h < a.H ? load_row<EB, D, HALVES>(a.q + (row * a.H + h) * (D * EB), g)
-                              : load_row<EB, D, HALVES>(a.k + (row * a.Hk + (h - a.H)) * (D * EB), g);
+            bits[u] = h < a.H ? load_row<EB, D>(a.q + (row * a.H + h) * (D * EB), g)
+                              : load_row<EB, D>(a.k + (row * a.Hk + (h - a.H)) * (D * EB), g);
     }
     float2 cs[8];
-    load_turns(a.table, a.first_token + i, g, cs);
+    load_turns<EB, D, HALVES>(a.table, a.first_token + i, g, cs);
 #pragma unroll
     for (int e = 0; e < 8; ++e) cs[e].y *= a.sign;
 #pragma unroll
@@ -61,7 +61,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(const RopeArgs a) {
         float x[kRowElems];
         unpack_row<EB>(bits[u], x);
         turn_row<HALVES>(x, cs);
-        store_row<EB, D, HALVES>(h < a.H ? a.q_out + (row * a.H + h) * (D * EB)
+        store_row<EB, D>(h < a.H ? a.q_out + (row * a.H + h) * (D * EB)
                                          : a.k_out + (row * a.Hk + (h - a.H)) * (D * EB), g, x);
     }
 }

@@ -3,11 +3,13 @@
 // (cos, sin) of a token's pairs, and the rotation and normalisation of a row
 // held by a few lanes. Not part of the public ABI.
 //
-// A row of D elements is held by D / 16 consecutive lanes, 8 pairs each: lane g
-// has elements 16 g .. 16 g + 15 where a pair is two neighbours, or 8 g .. 8 g +
-// 7 and D/2 + 8 g .. D/2 + 8 g + 7 where the pairs are the row's halves. Either
-// way that is two 16-byte loads in bf16, and element e of the lane's 16 pairs
-// with e ^ 1, or with e ^ 8.
+// A row of D elements is held by D / 16 consecutive lanes, 16 elements each, in runs
+// of 16 bytes: run i of lane g is the g-th 16 bytes of the row's i-th part of EB (2
+// in bf16, 4 in fp32), so that a wave's load or store of a run touches whole lines
+// (with a lane's 16 elements in one piece, every instruction touched 16 bytes of each
+// 32 or 64: rotating 1.34 GB took 444 us). Pairs of neighbours lie in a run; the
+// halves of a row are its first and second half of the runs. So element e of the lane
+// pairs with e ^ 1, or with e + 8.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -20,10 +22,16 @@ namespace tmk {
 
 constexpr int kRowElems = 16;  // elements of a row per lane
 
-// First of the run of 8 elements number `half` (0 or 1) of lane g.
-template <int D, bool HALVES>
-__device__ __forceinline__ int run_of(int g, int half) {
-    return HALVES ? half * (D / 2) + 8 * g : kRowElems * g + 8 * half;
+// Element (of the row) of the first of lane g's elements 16 i / EB .. of run i.
+template <int EB, int D>
+__device__ __forceinline__ int run_of(int g, int i) {
+    return i * (D / EB) + (16 / EB) * g;
+}
+// The pair (of the row's D / 2) that the lane's pair e (of 8) is.
+template <int EB, int D, bool HALVES>
+__device__ __forceinline__ int pair_of(int g, int e) {
+    constexpr int N = 16 / EB;  // elements of a run
+    return HALVES ? run_of<EB, D>(g, e / N) + e % N : (run_of<EB, D>(g, 2 * e / N) + 2 * e % N) / 2;
 }
 
 // A lane's 16 elements of the row at `row`, in fp32. EB: bytes per element.
@@ -31,12 +39,11 @@ template <int EB>
 struct RowBits {
     u32x4_t v[EB];  // EB * 16 bytes
 };
-template <int EB, int D, bool HALVES>
+template <int EB, int D>
 __device__ __forceinline__ RowBits<EB> load_row(const unsigned char* row, int g) {
     RowBits<EB> r;
 #pragma unroll
-    for (int i = 0; i < EB; ++i)
-        r.v[i] = *reinterpret_cast<const u32x4_t*>(row + run_of<D, HALVES>(g, i * 2 / EB) * EB + (i % (EB / 2)) * 16);
+    for (int i = 0; i < EB; ++i) r.v[i] = *reinterpret_cast<const u32x4_t*>(row + run_of<EB, D>(g, i) * EB);
     return r;
 }
 template <int EB>
@@ -54,7 +61,7 @@ __device__ __forceinline__ void unpack_row(const RowBits<EB>& r, float (&x)[kRow
         }
 }
 // x rounded (nearest even) to the element type, through the L2.
-template <int EB, int D, bool HALVES>
+template <int EB, int D>
 __device__ __forceinline__ void store_row(unsigned char* row, int g, const float (&x)[kRowElems]) {
 #pragma unroll
     for (int i = 0; i < EB; ++i) {
@@ -68,12 +75,13 @@ __device__ __forceinline__ void store_row(unsigned char* row, int g, const float
                 v[w] = __builtin_bit_cast(uint32_t, p);
             }
         }
-        store16_through(row + run_of<D, HALVES>(g, i * 2 / EB) * EB + (i % (EB / 2)) * 16, v);
+        store16_through(row + run_of<EB, D>(g, i) * EB, v);
     }
 }
 
-// (cos, sin) of pairs 8 g .. 8 g + 7 of the token at position `pos`; (1, 0) of
-// the pairs that no axis turns.
+// (cos, sin) of lane g's 8 pairs of the token at position `pos`; (1, 0) of the
+// pairs that no axis turns.
+template <int EB, int D, bool HALVES>
 __device__ __forceinline__ void load_turns(const RopeTable& t, int64_t pos, int g, float2 (&cs)[8]) {
     const int p = static_cast<int>(pos);  // below frames * frame_tokens <= 2^30
     const int f = p / t.frame_tokens, j = p - f * t.frame_tokens;
@@ -85,7 +93,7 @@ __device__ __forceinline__ void load_turns(const RopeTable& t, int64_t pos, int 
     const int end_t = t.pairs_t, end_h = end_t + t.pairs_h, end_w = end_h + t.pairs_w;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const int i = 8 * g + e;
+        const int i = pair_of<EB, D, HALVES>(g, e);
         const float2* const from = i < end_t ? at : i < end_h ? ay : ax;
         cs[e] = make_float2(1.f, 0.f);
         if (i < end_w) cs[e] = from[i];
