@@ -99,7 +99,8 @@ tm_status check_desc(const tm_attn_desc* d, Geo* g) {
 
 // The pointer must be a 16-byte (or `align`-byte) aligned device pointer of
 // the current device whose allocation covers `bytes` bytes from it.
-tm_status check_ptr(const void* p, size_t bytes, const char* name, size_t align = 16) {
+tm_status check_ptr(const void* p, size_t bytes, const char* name, size_t align = 16,
+                    hipDeviceptr_t* base_out = nullptr, size_t* size_out = nullptr) {
     if (p == nullptr) return fail(TM_E_ARG, "%s is NULL", name);
     if (reinterpret_cast<uintptr_t>(p) % align != 0)
         return fail(TM_E_ARG, "%s is not %zu-byte aligned", name, align);
@@ -127,8 +128,40 @@ tm_status check_ptr(const void* p, size_t bytes, const char* name, size_t align 
     if (q < b || q - b > size || bytes > size - (q - b))
         return fail(TM_E_ARG, "%s: %zu bytes from it run past the end of its allocation", name,
                     bytes);
+    if (base_out != nullptr) {
+        *base_out = base;
+        *size_out = size;
+    }
     return TM_OK;
 }
+
+// check_ptr for the pointers of one call: one that lies in the allocation of an
+// earlier one needs no further look-up (three calls of the runtime, 0.35 us; a
+// caching allocator puts the tensors of a small call into one allocation).
+class PtrChecks {
+    static constexpr int kKept = 4;
+    uintptr_t base_[kKept] = {};
+    size_t size_[kKept] = {};
+    int n_ = 0;
+
+public:
+    tm_status operator()(const void* p, size_t bytes, const char* name, size_t align = 16) {
+        const uintptr_t q = reinterpret_cast<uintptr_t>(p);
+        if (q % align == 0) {
+            for (int i = 0; i < n_; ++i)
+                if (q >= base_[i] && q - base_[i] <= size_[i] && bytes <= size_[i] - (q - base_[i]) && bytes > 0)
+                    return TM_OK;
+        }
+        hipDeviceptr_t base = nullptr;
+        size_t size = 0;
+        const tm_status st = check_ptr(p, bytes, name, align, &base, &size);
+        if (st == TM_OK && n_ < kKept) {
+            base_[n_] = reinterpret_cast<uintptr_t>(base);
+            size_[n_++] = size;
+        }
+        return st;
+    }
+};
 
 bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
@@ -995,13 +1028,13 @@ tm_status check_rope_desc(const tm_rope_desc* d, RopeGeo* g) {
 // [first_token, first_token + n_tok) are checked. Without any pair there is no
 // table to read.
 tm_status rope_table(const tm_rope_desc* d, const RopeGeo& g, const float* table, int64_t first_token,
-                     int64_t n_tok, tmk::RopeTable* t) {
+                     int64_t n_tok, PtrChecks& check, tmk::RopeTable* t) {
     const int64_t frame = g.rows[1] * g.rows[2], all = frame * g.rows[0];
     if (first_token < 0 || first_token > all || n_tok > all - first_token)
         return fail(TM_E_SHAPE, "tokens from %lld on lie past the table's %d frames",
                     static_cast<long long>(first_token), d->frames);
     if (g.table_bytes > 0) {
-        const tm_status st = check_ptr(table, g.table_bytes, "table");
+        const tm_status st = check(table, g.table_bytes, "table");
         if (st != TM_OK) return st;
     }
     t->table = reinterpret_cast<const float2*>(table);
@@ -1029,14 +1062,15 @@ tm_status rope(const tm_rope_desc* d, const float* table, int32_t batch, int32_t
         return fail(TM_E_SHAPE, "batch * heads too large");
     if (n_tok == 0) return TM_OK;
     tmk::RopeArgs a{};
-    if ((st = rope_table(d, g, table, first_token, n_tok, &a.table)) != TM_OK) return st;
+    PtrChecks check;
+    if ((st = rope_table(d, g, table, first_token, n_tok, check, &a.table)) != TM_OK) return st;
     const size_t row = size_t(batch) * size_t(n_tok) * size_t(d->head_dim) * g.elem;
     const size_t q_bytes = row * size_t(heads), k_bytes = row * size_t(kv_heads);
-    if ((st = check_ptr(q, q_bytes, "q")) != TM_OK) return st;
-    if ((st = check_ptr(q_out, q_bytes, "q_out")) != TM_OK) return st;
+    if ((st = check(q, q_bytes, "q")) != TM_OK) return st;
+    if ((st = check(q_out, q_bytes, "q_out")) != TM_OK) return st;
     if (k != nullptr) {
-        if ((st = check_ptr(k, k_bytes, "k")) != TM_OK) return st;
-        if ((st = check_ptr(k_out, k_bytes, "k_out")) != TM_OK) return st;
+        if ((st = check(k, k_bytes, "k")) != TM_OK) return st;
+        if ((st = check(k_out, k_bytes, "k_out")) != TM_OK) return st;
         if ((k_out != k && overlaps(k_out, k_bytes, k, k_bytes)) || overlaps(k_out, k_bytes, q, q_bytes) ||
             overlaps(q_out, q_bytes, k, k_bytes) || overlaps(q_out, q_bytes, k_out, k_bytes))
             return fail(TM_E_ARG, "k_out or q_out overlaps another tensor (only an output that is its input is allowed)");
@@ -1184,31 +1218,32 @@ tm_status write_chunk8(tm_kv8_cache* cache, int32_t chunk, const void* q, const 
                     chunk == 0 ? "reference chunk" : "chunk", (long long)cap);
     const size_t row = size_t(g.B) * size_t(n_tok) * size_t(g.D) * 2;
     const size_t kv_bytes = row * size_t(z.Hk), q_bytes = row * size_t(g.H);
-    if ((st = check_ptr(k, kv_bytes, "k")) != TM_OK) return st;
-    if ((st = check_ptr(v, kv_bytes, "v")) != TM_OK) return st;
-    if ((st = check_ptr(cache->pool, z.bytes(), "pool")) != TM_OK) return st;
+    PtrChecks check;
+    if ((st = check(k, kv_bytes, "k")) != TM_OK) return st;
+    if ((st = check(v, kv_bytes, "v")) != TM_OK) return st;
+    if ((st = check(cache->pool, z.bytes(), "pool")) != TM_OK) return st;
     if (overlaps(k, kv_bytes, cache->pool, z.bytes()) || overlaps(v, kv_bytes, cache->pool, z.bytes()))
         return fail(TM_E_ARG, "k/v overlap the cache's pool");
     tmk::Kv8WriteArgs a{};
     const bool produce = q != nullptr;
     if (produce) {
         if (!std::isfinite(eps) || eps < 0.f) return fail(TM_E_ARG, "eps must be finite and >= 0");
-        if ((st = check_ptr(q, q_bytes, "q")) != TM_OK) return st;
-        if ((st = check_ptr(q_out, q_bytes, "q_out")) != TM_OK) return st;
+        if ((st = check(q, q_bytes, "q")) != TM_OK) return st;
+        if ((st = check(q_out, q_bytes, "q_out")) != TM_OK) return st;
         if (q_out != q && overlaps(q_out, q_bytes, q, q_bytes))
             return fail(TM_E_ARG, "q_out overlaps q without being q");
         if (overlaps(q_out, q_bytes, k, kv_bytes) || overlaps(q_out, q_bytes, v, kv_bytes) ||
             overlaps(q_out, q_bytes, cache->pool, z.bytes()))
             return fail(TM_E_ARG, "q_out overlaps k, v or the cache's pool");
         const size_t gain = size_t(g.D) * sizeof(float);
-        if (q_gain != nullptr && (st = check_ptr(q_gain, size_t(g.H) * gain, "q_gain")) != TM_OK) return st;
-        if (k_gain != nullptr && (st = check_ptr(k_gain, size_t(z.Hk) * gain, "k_gain")) != TM_OK) return st;
+        if (q_gain != nullptr && (st = check(q_gain, size_t(g.H) * gain, "q_gain")) != TM_OK) return st;
+        if (k_gain != nullptr && (st = check(k_gain, size_t(z.Hk) * gain, "k_gain")) != TM_OK) return st;
         if (rope_desc != nullptr) {
             RopeGeo rg;
             if ((st = check_rope_desc(rope_desc, &rg)) != TM_OK) return st;
             if (rope_desc->head_dim != g.D || rope_desc->dtype != TM_BF16)
                 return fail(TM_E_ARG, "the rope descriptor's head_dim or dtype is not the cache's");
-            if ((st = rope_table(rope_desc, rg, table, first_token, n_tok, &a.table)) != TM_OK) return st;
+            if ((st = rope_table(rope_desc, rg, table, first_token, n_tok, check, &a.table)) != TM_OK) return st;
             if (overlaps(q_out, q_bytes, table, rg.table_bytes)) return fail(TM_E_ARG, "q_out overlaps the table");
             a.turn = 1;
             a.first_token = first_token;
@@ -1307,10 +1342,11 @@ tm_status attn8(const tm_kv8_cache* cache, const void* q, int32_t q_chunk, int32
     const size_t elems = size_t(g.B) * size_t(n_q) * size_t(g.H) * size_t(g.D);
     const size_t q_bytes = elems * 2, o_bytes = elems * (o_f32 ? 4 : 2);
     const size_t lse_bytes = size_t(g.B) * size_t(g.H) * size_t(n_q) * sizeof(float);
-    if ((st = check_ptr(q, q_bytes, "q")) != TM_OK) return st;
-    if ((st = check_ptr(cache->pool, z.bytes(), "pool")) != TM_OK) return st;
-    if ((st = check_ptr(o, o_bytes, "o")) != TM_OK) return st;
-    if (lse != nullptr && (st = check_ptr(lse, lse_bytes, "lse", 4)) != TM_OK) return st;
+    PtrChecks check;
+    if ((st = check(q, q_bytes, "q")) != TM_OK) return st;
+    if ((st = check(cache->pool, z.bytes(), "pool")) != TM_OK) return st;
+    if ((st = check(o, o_bytes, "o")) != TM_OK) return st;
+    if (lse != nullptr && (st = check(lse, lse_bytes, "lse", 4)) != TM_OK) return st;
     if (overlaps(o, o_bytes, cache->pool, z.bytes())) return fail(TM_E_ARG, "o overlaps the cache's pool");
     if ((o != q || o_f32) && overlaps(o, o_bytes, q, q_bytes))
         return fail(TM_E_ARG, "o overlaps q (only o == q with the same dtype is allowed)");
@@ -1319,7 +1355,7 @@ tm_status attn8(const tm_kv8_cache* cache, const void* q, int32_t q_chunk, int32
         return fail(TM_E_ARG, "lse overlaps another tensor");
     const size_t need = parts_bytes(z, a);
     if (workspace != nullptr && need > 0 && need <= workspace_bytes) {
-        if ((st = check_ptr(workspace, need, "workspace")) != TM_OK) return st;
+        if ((st = check(workspace, need, "workspace")) != TM_OK) return st;
         if (overlaps(workspace, need, q, q_bytes) || overlaps(workspace, need, o, o_bytes) ||
             overlaps(workspace, need, cache->pool, z.bytes()) ||
             (lse != nullptr && overlaps(workspace, need, lse, lse_bytes)))
@@ -1416,9 +1452,10 @@ tm_status tm_kv8_read(const tm_kv8_cache* cache, int32_t chunk, void* k_out, voi
     int32_t n_tok = 0;
     if ((st = locate8(cache, z, chunk, &at, &n_tok)) != TM_OK) return st;
     const size_t bytes = size_t(z.g.B) * size_t(n_tok) * size_t(z.Hk) * size_t(z.g.D) * (out_f32 ? 4 : 2);
-    if ((st = check_ptr(k_out, bytes, "k_out")) != TM_OK) return st;
-    if ((st = check_ptr(v_out, bytes, "v_out")) != TM_OK) return st;
-    if ((st = check_ptr(cache->pool, z.bytes(), "pool")) != TM_OK) return st;
+    PtrChecks check;
+    if ((st = check(k_out, bytes, "k_out")) != TM_OK) return st;
+    if ((st = check(v_out, bytes, "v_out")) != TM_OK) return st;
+    if ((st = check(cache->pool, z.bytes(), "pool")) != TM_OK) return st;
     if (overlaps(k_out, bytes, v_out, bytes) || overlaps(k_out, bytes, cache->pool, z.bytes()) ||
         overlaps(v_out, bytes, cache->pool, z.bytes()))
         return fail(TM_E_ARG, "k_out and v_out overlap each other or the cache's pool");

@@ -424,8 +424,8 @@ def _expect(name, t, shape, dtype):
         raise TMError(TM_E_SHAPE, f"{name} is not {dtype} {list(shape)}")
 
 
-def _rope_table_shape(desc):
-    return (lib().tm_rope3d_table_bytes(ctypes.byref(desc)) // 8, 2)
+def _rope_table_rows(desc):
+    return lib().tm_rope3d_table_bytes(ctypes.byref(desc)) // 8
 
 
 def make_rope_desc(head_dim, frames, grid_h, grid_w, pairs=None, theta=10000.0, split_half=False,
@@ -441,7 +441,7 @@ def make_rope_desc(head_dim, frames, grid_h, grid_w, pairs=None, theta=10000.0, 
 def tm_rope3d_table(desc: tm_rope_desc, table=None, device="cuda", stream=None):
     """(cos, sin) of every position and pair of the descriptor's axes, a flat
     fp32 tensor of pairs (allocated if not given)."""
-    shape = _rope_table_shape(desc)
+    shape = (_rope_table_rows(desc), 2)
     if table is None:
         table = torch.empty(shape, dtype=torch.float32, device=device)
     _expect("table", table, shape, torch.float32)
@@ -450,22 +450,32 @@ def tm_rope3d_table(desc: tm_rope_desc, table=None, device="cuda", stream=None):
 
 
 def _rope(fn, desc, table, q, k, first_token, q_out, k_out, stream):
-    for name, t in (("q", q), ("k", k)):
-        if t is not None and (t.dim() != 4 or t.shape[3] != desc.head_dim or t.dtype != _TORCH_DTYPE[desc.dtype]):
-            raise TMError(TM_E_SHAPE, f"{name} is not [batch, n_tok, heads, {desc.head_dim}] of the descriptor's dtype")
-    if k is not None and k.shape[:2] != q.shape[:2]:
-        raise TMError(TM_E_SHAPE, "q and k differ in batch or tokens")
-    _expect("table", table, _rope_table_shape(desc), torch.float32)
-    _expect("q_out", q_out, q.shape, q.dtype)
+    # (one call per layer and token of a decoder: about 2 us are Python's, so nothing
+    # is looked up twice)
+    D, dtype = desc.head_dim, _TORCH_DTYPE[desc.dtype]
+    shape = q.shape
+    if len(shape) != 4 or shape[3] != D or q.dtype != dtype:
+        raise TMError(TM_E_SHAPE, f"q is not {dtype} [batch, n_tok, heads, {D}]")
+    B, n, H, _ = shape
+    Hk, pk, pko = 0, None, None
     if k is not None:
-        _expect("k_out", k_out, k.shape, k.dtype)
+        kshape = k.shape
+        if len(kshape) != 4 or kshape[3] != D or k.dtype != dtype or kshape[0] != B or kshape[1] != n:
+            raise TMError(TM_E_SHAPE, f"k is not {dtype} [{B}, {n}, kv_heads, {D}]")
+        Hk = kshape[2]
+        if k_out is None:
+            k_out = torch.empty_like(k)
+        else:
+            _expect("k_out", k_out, kshape, dtype)
+        pk, pko = _ptr(k), _ptr(k_out)
     if q_out is None:
         q_out = torch.empty_like(q)
-    if k_out is None and k is not None:
-        k_out = torch.empty_like(k)
-    B, n, H = q.shape[:3]
-    _check(fn(ctypes.byref(desc), _ptr(table), B, n, first_token, _ptr(q), H, _ptr(k),
-              0 if k is None else k.shape[2], _ptr(q_out), _ptr(k_out), _stream(stream)))
+    else:
+        _expect("q_out", q_out, shape, dtype)
+    if table is not None and (table.numel() != 2 * _rope_table_rows(desc) or table.dtype != torch.float32):
+        raise TMError(TM_E_SHAPE, "table is not the descriptor's")
+    _check(fn(ctypes.byref(desc), _ptr(table), B, n, first_token, _ptr(q), H, pk, Hk, _ptr(q_out), pko,
+              _stream(stream)))
     return q_out, k_out
 
 
@@ -499,7 +509,9 @@ class KV8Cache:
 
     def __init__(self, desc: tm_attn_desc, kv_heads: int | None = None, device="cuda", pool=None):
         self.desc = desc
+        self.heads = desc.heads
         self.kv_heads = desc.heads if kv_heads is None else kv_heads
+        self._batch, self._head_dim = desc.batch, desc.head_dim
         h = ctypes.c_void_p()
         if pool is None:
             n = tm_kv8_cache_bytes(desc, self.kv_heads)
@@ -534,14 +546,18 @@ class KV8Cache:
     def reset(self):
         _check(lib().tm_kv8_cache_reset(self.handle))
 
-    def check_rows(self, heads: int, **tensors):
-        """Each tensor must be bf16 [batch, n, heads, head_dim] of the cache, all of one n."""
-        n = None
-        for name, t in tensors.items():
-            if t.dim() != 4 or t.dtype != torch.bfloat16 or (t.shape[0], t.shape[2], t.shape[3]) != (
-                    self.desc.batch, heads, self.desc.head_dim) or n not in (None, t.shape[1]):
-                raise TMError(TM_E_SHAPE, f"{name} is not bf16 [{self.desc.batch}, n, {heads}, {self.desc.head_dim}]")
-            n = t.shape[1]
+    def rows(self, name, t, heads: int) -> int:
+        """n of a tensor that has to be bf16 [batch, n, heads, head_dim] of the cache."""
+        shape = t.shape
+        if (len(shape) != 4 or shape[0] != self._batch or shape[2] != heads or shape[3] != self._head_dim
+                or t.dtype != torch.bfloat16):
+            raise TMError(TM_E_SHAPE, f"{name} is not bf16 [{self._batch}, n, {heads}, {self._head_dim}]")
+        return shape[1]
+
+    def kv_rows(self, k, v) -> int:
+        n = self.rows("k", k, self.kv_heads)
+        if self.rows("v", v, self.kv_heads) != n:
+            raise TMError(TM_E_SHAPE, "k and v differ in tokens")
         return n
 
 
@@ -551,7 +567,7 @@ def tm_kv8_cache_create(desc: tm_attn_desc, kv_heads: int | None = None, device=
 
 def tm_kv8_append(cache: KV8Cache, chunk: int, k, v, stream=None):
     """Quantise chunk ``chunk``'s K/V (bf16 ``[B, n_tok, kv_heads, D]``) into the cache."""
-    n = cache.check_rows(cache.kv_heads, k=k, v=v)
+    n = cache.kv_rows(k, v)
     _check(lib().tm_kv8_append(cache.handle, chunk, _ptr(k), _ptr(v), n, _stream(stream)))
 
 
@@ -561,14 +577,14 @@ def tm_qkv8_produce(cache: KV8Cache, chunk: int, q, k, v, q_gain=None, k_gain=No
     """RMS-normalise the chunk's q and k rows, rotate them if ``rope`` (with its
     ``table``) is given, and quantise k and v into the cache; returns ``q_out``
     (allocated like q if not given)."""
-    n = cache.check_rows(cache.kv_heads, k=k, v=v)
-    if cache.check_rows(cache.desc.heads, q=q) != n:
+    n = cache.kv_rows(k, v)
+    if cache.rows("q", q, cache.heads) != n:
         raise TMError(TM_E_SHAPE, "q and k differ in tokens")
     _expect("q_gain", q_gain, q.shape[2:], torch.float32)
     _expect("k_gain", k_gain, k.shape[2:], torch.float32)
     _expect("q_out", q_out, q.shape, q.dtype)
     if rope is not None:
-        _expect("table", table, _rope_table_shape(rope), torch.float32)
+        _expect("table", table, (_rope_table_rows(rope), 2), torch.float32)
     if q_out is None:
         q_out = torch.empty_like(q)
     _check(lib().tm_qkv8_produce(cache.handle, chunk, _ptr(q), _ptr(k), _ptr(v), _ptr(q_gain), _ptr(k_gain),
@@ -582,11 +598,13 @@ def tm_kv8_read(cache: KV8Cache, chunk: int, dtype=torch.bfloat16, k_out=None, v
     kv_heads, D]`` in bf16 or fp32 (allocated if not given)."""
     f32 = _dtype(dtype) == TM_F32
     dt = torch.float32 if f32 else torch.bfloat16
-    shape = (cache.desc.batch, cache.locate(chunk)[1], cache.kv_heads, cache.desc.head_dim)
+    shape = (cache._batch, cache.locate(chunk)[1], cache.kv_heads, cache._head_dim)
     _expect("k_out", k_out, shape, dt)
     _expect("v_out", v_out, shape, dt)
-    k_out = torch.empty(shape, dtype=dt, device=cache.pool.device) if k_out is None else k_out
-    v_out = torch.empty(shape, dtype=dt, device=cache.pool.device) if v_out is None else v_out
+    if k_out is None:
+        k_out = torch.empty(shape, dtype=dt, device=cache.pool.device)
+    if v_out is None:
+        v_out = torch.empty_like(k_out)
     _check(lib().tm_kv8_read(cache.handle, chunk, _ptr(k_out), _ptr(v_out), int(f32), _stream(stream)))
     return k_out, v_out
 
@@ -598,9 +616,9 @@ def tm_kv8_attn_fwd(cache: KV8Cache, q, q_chunk: int, o=None, o_f32: bool = Fals
     share their keys out through a workspace of torch's allocator; calls that
     can have none (under capture, on another stream than the current one) order
     the fp32 sums otherwise."""
-    n_q = cache.check_rows(cache.desc.heads, q=q)
+    n_q = cache.rows("q", q, cache.heads)
     _expect("o", o, q.shape, torch.float32 if o_f32 else torch.bfloat16)
-    _expect("lse", lse, (cache.desc.batch, cache.desc.heads, n_q), torch.float32)
+    _expect("lse", lse, (cache._batch, cache.heads, n_q), torch.float32)
     if o is None:
         o = torch.empty(q.shape, dtype=torch.float32, device=q.device) if o_f32 else torch.empty_like(q)
     pq, po, pl = _ptr(q), _ptr(o), _ptr(lse)
