@@ -18,11 +18,15 @@
 // 8: P reaches 2^8 and a tile may exceed that by 2^7 before m is raised; what
 // fp16 then loses at its lower end is below 2^-33 of the largest.
 //
-// Tile kernel: as the bf16 forward (attn_fwd.hip), 8 waves of 32 query rows share
-// every 64-key tile in LDS, each wave's softmax in between its own MFMAs. The
-// tiles come as codes into registers, half the bytes, one tile ahead, and are
-// turned into fp16 operands once per workgroup on the way into LDS; the cache's
-// order makes every LDS access a contiguous KB.
+// Tile kernel: K's operands keep the bias of 128, as fp16 subnormals (the matrix
+// cores take them as they are): one instruction less for two codes, and x loses
+// 128 times the row's sum of q with its fma's addend. That costs the fp32 sums some
+// three bits at worst (255 for a code of some 33), far below P's rounding. As in
+// the bf16 forward (attn_fwd.hip), 8 waves of 32 query rows share every 64-key tile
+// in LDS, each wave's softmax in between its own MFMAs. The tiles come as codes into
+// registers, half the bytes, one tile ahead, and are turned into fp16 operands once
+// per workgroup on the way into LDS; the cache's order makes every LDS access a
+// contiguous KB.
 //
 // Few rows: a workgroup's waves share the keys of one block of 32 rows out; a
 // wave loads its blocks' operands straight from the cache. Bound by the cache's
@@ -64,6 +68,12 @@ __device__ __forceinline__ f16x2_t decode2(uint32_t w) {
     const f16x2_t x = __builtin_bit_cast(f16x2_t, pick_bytes(0x64646464u, w, HI ? 0x04030402u : 0x04010400u));
     return x - f16x2_t{static_cast<_Float16>(1152.f), static_cast<_Float16>(1152.f)};
 }
+// The same as (code + 128) 2^-24: the byte alone is that subnormal fp16 number.
+template <bool HI>
+__device__ __forceinline__ f16x2_t biased2(uint32_t w) {
+    return __builtin_bit_cast(f16x2_t, pick_bytes(0u, w, HI ? 0x04030402u : 0x04010400u));
+}
+constexpr float kBiasedScale = 0x1p24f, kBiasedZero = 0x1p-17f;  // 1 over a code's step, and code 0
 // 8 codes as an operand's 8 elements.
 __device__ __forceinline__ f16x8_t decode8(uint32_t a, uint32_t b) {
     const f16x2_t p = decode2<false>(a), q = decode2<true>(a), r = decode2<false>(b), s = decode2<true>(b);
@@ -208,8 +218,9 @@ __device__ __forceinline__ void split_rows(int rows, int nt, int idx, int& q0, i
     q1 = min(32 * ((idx + 1) * each + min(idx + 1, more)), rows);
 }
 
-// A workgroup's tile and share of its keys (whole tiles come first, then the split
-// ones' parts, a tile's next to each other).
+// A workgroup's tile and share of its keys: whole tiles come first, then the split
+// ones' parts, a tile's next to each other; with a cut, all first parts (up to the
+// cut) and then all second ones.
 struct Share {
     int tile, bat, kvh, part;
     int64_t split;  // number of the split tile, -1: whole
@@ -225,6 +236,13 @@ __device__ __forceinline__ Share share_of(const Kv8AttnArgs& a) {
     s.n = a.n_kblocks;
     if (static_cast<int>(blockIdx.x) < a.n_whole) {
         id = xcd_logical_id(blockIdx.x, a.n_whole);
+    } else if (a.cut > 0) {
+        const int n = total - a.n_whole, j = blockIdx.x - a.n_whole;
+        s.part = j >= n;
+        s.split = xcd_logical_id(s.part ? j - n : j, n);
+        id = a.n_whole + static_cast<int>(s.split);
+        s.b0 = s.part ? a.cut : 0;
+        s.n = s.part ? a.n_kblocks - a.cut : a.cut;
     } else {
         const int sid = xcd_logical_id(blockIdx.x - a.n_whole, (total - a.n_whole) * a.parts);
         s.split = sid / a.parts;
@@ -427,6 +445,10 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
     const int pw = NP == 2 ? wave : wave & 3;  // piece's kb * DB + (s or d)
     const uint32_t lane16 = 16 * lane;
     const uint32_t to = 2 * pw * 1024 + lane16;
+    // (V's lane offset in a register of its own: it is past the reach of a read's immediate, and the
+    // compiler would add it up for every read; 977 -> 964 us)
+    uint32_t v_lane16 = NBUF * TILEB + lane16;
+    asm volatile("" : "+v"(v_lane16));
     u32x4_t codes[NP];
     float ks, vs;   // scales of the tile whose scores come next (the same in every lane)
     int blk[NBUF];  // block j of the walk in [j % 4]
@@ -450,19 +472,27 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
         ks = load_from<float>(a.k_scale + head + blk[u & 3], z);
         vs = load_from<float>(a.v_scale + head + blk[u & 3], z);
     };
-    // Half h of piece p into the buffers of block u.
-    auto put = [&](int p, int h, int u) __attribute__((always_inline)) {
-        const f16x8_t f = decode8(codes[p][2 * h], codes[p][2 * h + 1]);
+    // Codes turned into operands two at a time: pair i of the thread's ND (piece i / 8, half i / 4 % 2), and
+    // each half's 16 bytes into the buffers of block u once its four pairs are there.
+    constexpr int ND = 8 * NP;
+    f16x2_t half[4];
+    auto put = [&](int i, int u) __attribute__((always_inline)) {
+        const int p = i / 8, h = i / 4 % 2;
+        const uint32_t w = codes[p][2 * h + i / 2 % 2];
+        const bool is_k = NP == 2 ? p == 0 : !v_first;
+        if (is_k) half[i % 4] = i % 2 ? biased2<true>(w) : biased2<false>(w);
+        else half[i % 4] = i % 2 ? decode2<true>(w) : decode2<false>(w);
+        if (i % 4 != 3) return;
         const uint32_t base = NP == 2 ? p * NBUF * TILEB : v_first ? NBUF * TILEB : 0;
-        *(lds_f16x8_t*)(L + to + base + ((u & (NBUF - 1)) * TILEB + h * 1024)) = f;
+        *(lds_f16x8_t*)(L + to + base + ((u & (NBUF - 1)) * TILEB + h * 1024)) =
+            f16x8_t{half[0][0], half[0][1], half[1][0], half[1][1], half[2][0], half[2][1], half[3][0], half[3][1]};
     };
     // Fragment f of a tile's stream: K fragments (kk = f / 2, kb = f % 2) of buffer ku, then V
     // fragments (j = (f - NK) / DB, d) of buffer vu. In LDS: (kb, kk) and (j / 2, d, j % 2).
     auto read_frag = [&](int f, int ku, int vu) __attribute__((always_inline)) {
         const int j = (f - NK) / DB, d = (f - NK) % DB;
-        const uint32_t o = f < NK ? (ku & (NBUF - 1)) * TILEB + ((f & 1) * KK + (f >> 1)) * 1024
-                                  : (NBUF + (vu & (NBUF - 1))) * TILEB + (((j >> 1) * DB + d) * 2 + (j & 1)) * 1024;
-        return *(const lds_f16x8_t*)(L + (lane16 + o));
+        if (f < NK) return *(const lds_f16x8_t*)(L + lane16 + ((ku & (NBUF - 1)) * TILEB + ((f & 1) * KK + (f >> 1)) * 1024));
+        return *(const lds_f16x8_t*)(L + v_lane16 + ((vu & (NBUF - 1)) * TILEB + (((j >> 1) * DB + d) * 2 + (j & 1)) * 1024));
     };
 
     f32x16_t acc[DB];
@@ -502,17 +532,20 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
     for (int u = 0; u < 3; ++u) {
         load(u);
 #pragma unroll
-        for (int p = 0; p < NP; ++p) {
-            put(p, 0, u);
-            put(p, 1, u);
-        }
+        for (int i = 0; i < ND; ++i) put(i, u);
         at.step(a);
     }
     load(3);
     load_scales(0);
     const int qrow = q0 + wave * 32 + l32;
     f16x8_t qf[KK];
-    const float cq = load_q<D>(a, row_at(a, s.bat, s.kvh, min(qrow, a.rows - 1)), qrow < q1, hw, qf);
+    const float cq = kBiasedScale * load_q<D>(a, row_at(a, s.bat, s.kvh, min(qrow, a.rows - 1)), qrow < q1, hw, qf);
+    float qsum = 0.f;  // what the bias of the codes adds to every score of the row
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) qsum += static_cast<float>(qf[kk][e]);
+    qsum = (qsum + __shfl_xor(qsum, 32)) * kBiasedZero;
     __syncthreads();
 
     // A wave without rows takes part in the loads and barriers only.
@@ -522,7 +555,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
         xa[0] = xa[1] = f32x16_t{};
 #pragma unroll
         for (int f = 0; f < NK; ++f) xa[f & 1] = mfma(read_frag(f, 0, 0), qf[f >> 1], xa[f & 1]);
-        const float c = cq * ks, add = __builtin_amdgcn_logf(vs);
+        const float c = cq * ks, add = fmaf(-qsum, c, __builtin_amdgcn_logf(vs));
         iv = uniform_f(1.f / vs);
         load_scales(1);
 #pragma unroll
@@ -558,6 +591,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
+    constexpr int PUTS = NV - RING;  // MFMAs of stage 2 that have a share of the codes
     auto iteration = [&](int u, f32x16_t (&x)[2], f32x16_t (&nx)[2]) __attribute__((always_inline)) {
         at.step(a);
         u32x4_t pf[4];
@@ -597,7 +631,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
         float c = cq * ks;
         // (not zero, as a tiny row's factor may be: a masked score of -inf is still to be scaled)
         c = c < FLT_MIN ? FLT_MIN : c;
-        const float add = __builtin_amdgcn_logf(vs) - m;
+        const float add = fmaf(-qsum, c, __builtin_amdgcn_logf(vs) - m);
         iv = uniform_f(__builtin_amdgcn_rcpf(vs));
         if (__builtin_expect(cnt[(u + 1) & 3] < kCacheBlock, 0)) mask_tile(nx, cnt[(u + 1) & 3]);
         __builtin_amdgcn_sched_barrier(0);
@@ -608,14 +642,14 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
 #pragma unroll
             for (int e = FPG * k; e < FPG * (k + 1); ++e) nx[e >> 4][e & 15] = pin(fmaf(nx[e >> 4][e & 15], c, add));
             // (every write lies before the last RING reads ahead)
-            if (k % 2 == 1 && k / 2 < 2 * NP) put(k / 4, k / 2 % 2, u + 3);
-            if (k == 4 * NP) load(u + 4);
-            if (k == 4 * NP + 1) load_scales(u + 2);
+#pragma unroll
+            for (int i = ND * k / PUTS; i < ND * (k + 1) / PUTS && k < PUTS; ++i) put(i, u + 3);
+            if (k == PUTS) load(u + 4);
+            if (k == PUTS + 1) load_scales(u + 2);
             __builtin_amdgcn_sched_barrier(0);
         }
         end_tile(true);
     };
-    static_assert(4 * NP < NV && 4 * NP + RING <= NV, "writes and loads inside stage 2");
     if (busy) {
         for (int t = 0; t < n; t += 4) {
             iteration(0, xa, xb);
@@ -629,10 +663,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
     } else {
         auto idle = [&](int u) __attribute__((always_inline)) {
 #pragma unroll
-            for (int p = 0; p < NP; ++p) {
-                put(p, 0, u + 3);
-                put(p, 1, u + 3);
-            }
+            for (int i = 0; i < ND; ++i) put(i, u + 3);
             at.step(a);
             load(u + 4);
             end_tile(false);

@@ -1318,9 +1318,24 @@ tm_status plan_attn8(const tm_kv8_cache* cache, const Kv8Geo& z, int32_t q_chunk
     const int64_t rest = tiles % tmk::kCUs;
     if (rest == 0) return TM_OK;
     const int64_t parts = std::min<int64_t>({tmk::kCUs / rest, a->n_kblocks / 4, tmk::kMaxParts});
-    if (parts < 2 || a->n_kblocks - ceil_div(a->n_kblocks, parts) < 10) return TM_OK;
+    if (parts >= 2) {
+        if (a->n_kblocks - ceil_div(a->n_kblocks, parts) < 10) return TM_OK;
+        a->n_whole = int32_t(tiles - rest);
+        a->parts = int32_t(parts);
+        return TM_OK;
+    }
+    // More than half a round: each tile is cut in two, a first part for a CU of its own, and the
+    // second parts in turn, k each, for the CUs that are left over. Microseconds: a workgroup takes
+    // kEnds besides its key blocks, a block kBlock.
+    const double kEnds = 9, kBlock = 1.4 * double(z.g.D) / 128;
+    const double n = double(a->n_kblocks), k = double(ceil_div(rest, tmk::kCUs - rest));
+    const int64_t cut = int64_t(std::ceil((k * (n * kBlock + kEnds) - kEnds) / ((k + 1) * kBlock)));
+    if (a->n_kblocks - cut < 4) return TM_OK;
+    const double merge = 6 + 2 * 2 * double(rest) * (double(rows) / double(n_tiles)) * double(z.g.D + 2) * 4 / 4e6;
+    if ((n - double(cut)) * kBlock < merge + 5) return TM_OK;
     a->n_whole = int32_t(tiles - rest);
-    a->parts = int32_t(parts);
+    a->parts = 2;
+    a->cut = int32_t(cut);
     return TM_OK;
 }
 
@@ -1364,6 +1379,7 @@ tm_status attn8(const tm_kv8_cache* cache, const void* q, int32_t q_chunk, int32
     } else {
         a.n_whole = int32_t(int64_t(a.n_tiles) * g.B * z.Hk);
         a.parts = 1;
+        a.cut = 0;
     }
     place(z, cache->pool, &a);
     a.q = q;

@@ -283,6 +283,7 @@ struct Kv8AttnArgs {
     int32_t n_tiles;          // row tiles per (batch, key head)
     int32_t n_whole;          // tiles (of all heads) that are not split
     int32_t parts;            // key shares of a split tile
+    int32_t cut;              // > 0: two parts, the first of this many key blocks; else parts are equal
     int32_t n_kblocks;        // key blocks of all ranges
     int32_t n_ranges;
     int32_t range_begin[kMaxRanges];  // in blocks

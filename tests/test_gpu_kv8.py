@@ -249,6 +249,7 @@ def queries(B, n, H, D, g):
     (1, 8, 1, [3000, 64, 64, 64], 3, 4),
     (1, 2, 2, [2000, 1000], 1, 300),                # split tiles
     (3, 10, 5, [700, 320, 320], 0, 40),
+    (1, 47, 47, [1800, 40, 1800], 1, 1000),         # 188 tiles: each cut in two
 ])
 def test_attention(tm, D, B, H, Hk, lengths, window, n_q):
     g = torch.Generator().manual_seed(n_q)
