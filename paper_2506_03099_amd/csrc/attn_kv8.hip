@@ -267,12 +267,13 @@ __device__ __forceinline__ float* part_at(const Kv8AttnArgs& a, int64_t split, i
 // ----------------------------------------------------------------------------
 // Few rows
 // ----------------------------------------------------------------------------
-template <int D, bool OF32>
-__global__ __launch_bounds__(64 * kKv8FewWaves, 2) void attn_kv8_few_kernel(const Kv8AttnArgs a) {
+// NW waves share the keys of a tile out.
+template <int D, bool OF32, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void attn_kv8_few_kernel(const Kv8AttnArgs a) {
     constexpr int KK = D / 16, DB = D / 32, NP = 2 * DB;  // pieces of K, and of V, of a block
     constexpr int PITCH = D + 4;                           // floats per row in LDS
-    __shared__ float rows_o[kKv8FewWaves][kKv8FewRows * PITCH];
-    __shared__ float rows_m[kKv8FewWaves][kKv8FewRows], rows_l[kKv8FewWaves][kKv8FewRows];
+    __shared__ float rows_o[NW][kKv8FewRows * PITCH];
+    __shared__ float rows_m[NW][kKv8FewRows], rows_l[NW][kKv8FewRows];
     const int lane = threadIdx.x & 63, hw = lane >> 5, l32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
     const Share s = share_of(a);
@@ -297,7 +298,7 @@ __global__ __launch_bounds__(64 * kKv8FewWaves, 2) void attn_kv8_few_kernel(cons
 #pragma unroll
         for (int i = 0; i < NP; ++i) vc[i] = p[64 * i];
     };
-    // this wave's blocks: every kKv8FewWaves-th of the share
+    // this wave's blocks: every NW-th of the share
     Blocks at;
     if (wave < s.n) {
         at.start(a, s.b0 + wave);
@@ -306,7 +307,7 @@ __global__ __launch_bounds__(64 * kKv8FewWaves, 2) void attn_kv8_few_kernel(cons
         load_v(at.blk);
         vs = a.v_scale[head + at.blk];
     }
-    for (int j = wave; j < s.n; j += kKv8FewWaves) {
+    for (int j = wave; j < s.n; j += NW) {
         const int keys = at.keys;
         f32x16_t x[2] = {f32x16_t{}, f32x16_t{}};
 #pragma unroll
@@ -316,7 +317,7 @@ __global__ __launch_bounds__(64 * kKv8FewWaves, 2) void attn_kv8_few_kernel(cons
             x[kb] = mfma(decode8(kc[i][2], kc[i][3]), qf[2 * st + 1], x[kb]);
         }
         const float c = cq * ks, add = __builtin_amdgcn_logf(vs), iv = 1.f / vs;
-        at.next(a, kKv8FewWaves);  // (past the share's end: a block that exists)
+        at.next(a, NW);  // (past the share's end: a block that exists)
         load_k(at.blk);
         ks = a.k_scale[head + at.blk];
         vs = a.v_scale[head + at.blk];
@@ -374,16 +375,16 @@ __global__ __launch_bounds__(64 * kKv8FewWaves, 2) void attn_kv8_few_kernel(cons
     }
     __syncthreads();
     float* const part = s.split >= 0 ? part_at<D, kKv8FewRows>(a, s.split, s.part) : nullptr;
-    for (int n = threadIdx.x; n < n_rows * (D / 4); n += 64 * kKv8FewWaves) {
+    for (int n = threadIdx.x; n < n_rows * (D / 4); n += 64 * NW) {
         const int r = n / (D / 4), d = 4 * (n % (D / 4));
         float top = kNegInf;
 #pragma unroll
-        for (int w = 0; w < kKv8FewWaves; ++w) top = fmaxf(top, rows_m[w][r]);
+        for (int w = 0; w < NW; ++w) top = fmaxf(top, rows_m[w][r]);
         const float base = top == kNegInf ? 0.f : top;
         float sum = 0.f;
         f32x4_t o{};
 #pragma unroll
-        for (int w = 0; w < kKv8FewWaves; ++w) {
+        for (int w = 0; w < NW; ++w) {
             const float f = __builtin_amdgcn_exp2f(rows_m[w][r] - base);
             sum = fmaf(f, rows_l[w][r], sum);
             const f32x4_t ow = *reinterpret_cast<const f32x4_t*>(&rows_o[w][r * PITCH + d]);
@@ -826,7 +827,8 @@ template <int D, bool OF32>
 hipError_t launch(const Kv8AttnArgs& a, hipStream_t s) {
     const int64_t total = static_cast<int64_t>(a.n_tiles) * a.B * a.Hk, split = total - a.n_whole;
     const unsigned grid = static_cast<unsigned>(a.n_whole + split * a.parts);
-    if (a.few) hipLaunchKernelGGL((attn_kv8_few_kernel<D, OF32>), dim3(grid), dim3(64 * kKv8FewWaves), 0, s, a);
+    if (a.few == 4) hipLaunchKernelGGL((attn_kv8_few_kernel<D, OF32, 4>), dim3(grid), dim3(256), 0, s, a);
+    else if (a.few == 8) hipLaunchKernelGGL((attn_kv8_few_kernel<D, OF32, 8>), dim3(grid), dim3(512), 0, s, a);
     else hipLaunchKernelGGL((attn_kv8_tile_kernel<D, OF32>), dim3(grid), dim3(kTileThreads), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || split == 0) return e;
@@ -834,6 +836,9 @@ hipError_t launch(const Kv8AttnArgs& a, hipStream_t s) {
     auto wgs = [&](int rpw) { return dim3(static_cast<unsigned>(split * ((rows + rpw - 1) / rpw))); };
     if (a.few) {
         hipLaunchKernelGGL((attn_kv8_merge_kernel<D, OF32, kKv8FewRows, 8>), wgs(kMergeThreads / (D / 4 * 8)),
+                           dim3(kMergeThreads), 0, s, a, rows);
+    } else if (a.parts > 16) {
+        hipLaunchKernelGGL((attn_kv8_merge_kernel<D, OF32, kTileRows, 8>), wgs(kMergeThreads / (D / 4 * 8)),
                            dim3(kMergeThreads), 0, s, a, rows);
     } else {
         hipLaunchKernelGGL((attn_kv8_merge_kernel<D, OF32, kTileRows, 1>), wgs(kMergeThreads / (D / 4)),

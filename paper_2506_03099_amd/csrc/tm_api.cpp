@@ -1297,27 +1297,41 @@ tm_status plan_attn8(const tm_kv8_cache* cache, const Kv8Geo& z, int32_t q_chunk
     const int64_t BH = z.g.B * z.Hk;
     a->n_q = n_q;
     a->rows = int32_t(rows);
-    a->few = rows <= tmk::kKv8FewRows;
-    const int64_t n_tiles = ceil_div(rows, a->few ? tmk::kKv8FewRows : tmk::kTileRowsBf16);
+    // Tiles of 32 rows whose waves share the keys out, where rows are few, or all of the call's work
+    // (32 rows by 64 keys) is little: such a tile's waves turn codes into operands for themselves, and
+    // take 1.7 times as long for the work of full tiles of 256 rows, but those start later, and idle
+    // where they are not full. Measured, us, 256 and 32 rows a tile, D = 128: 1 head, 100000 keys,
+    // 64 rows 27 and 25, 192 rows 34 and 37; 40 heads, 1000 keys, 384 rows 31 and 19; 40 heads, 10000
+    // keys, 64 rows 38 and 37, 96 rows 40 and 43. D = 64: 8 heads, 100000 keys, 64 rows 49 and 41, 96
+    // rows 52 and 49, 128 rows 54 and 60.
+    const int64_t tiles32 = ceil_div(rows, tmk::kKv8FewRows) * BH;
+    const bool few = rows <= (z.g.D == 64 ? 64 : 32) ||
+                     tiles32 * a->n_kblocks <= (z.g.D == 64 ? 22000 : 8000);
+    const int64_t n_tiles = ceil_div(rows, few ? tmk::kKv8FewRows : tmk::kTileRowsBf16);
     const int64_t tiles = n_tiles * BH;
     if (tiles > INT32_MAX / 64) return fail(TM_E_SHAPE, "grid too large");
     a->n_tiles = int32_t(n_tiles);
     a->n_whole = int32_t(tiles);
     a->parts = 1;
-    if (a->few) {
-        // Two workgroups on every CU, each wave of them with two key blocks at least.
+    if (few) {
+        // Two workgroups of 4 waves on every CU, each wave with two key blocks at least. A wave takes
+        // about 0.9 us a block, and the merge 5, so a share has to save that; short caches have 8
+        // waves a workgroup instead.
         const int64_t parts = std::min<int64_t>({2 * tmk::kCUs / std::max<int64_t>(tiles, 1),
-                                                 a->n_kblocks / (2 * tmk::kKv8FewWaves), 256});
-        if (parts >= 2) {
+                                                 a->n_kblocks / 8, tmk::kKv8MaxParts});
+        a->few = 4;
+        if (parts >= 2 && a->n_kblocks - ceil_div(a->n_kblocks, parts) >= 24) {
             a->n_whole = 0;
             a->parts = int32_t(parts);
+        } else if (a->n_kblocks > 4 && tiles <= tmk::kCUs) {
+            a->few = 8;
         }
         return TM_OK;
     }
     // As the 16-bit forward: the tiles beyond the last full round of one per CU
     const int64_t rest = tiles % tmk::kCUs;
     if (rest == 0) return TM_OK;
-    const int64_t parts = std::min<int64_t>({tmk::kCUs / rest, a->n_kblocks / 4, tmk::kMaxParts});
+    const int64_t parts = std::min<int64_t>({tmk::kCUs / rest, a->n_kblocks / 4, tmk::kKv8MaxParts});
     if (parts >= 2) {
         if (a->n_kblocks - ceil_div(a->n_kblocks, parts) < 10) return TM_OK;
         a->n_whole = int32_t(tiles - rest);

@@ -279,7 +279,7 @@ struct Kv8AttnArgs {
     int32_t n_q, rows;        // rows = n_q * group
     int32_t n_blocks;         // per (batch, key head) of the cache
     float scale_log2;         // softmax scale * log2(e)
-    int32_t few;              // rows are few: 32 a tile, their keys shared out over a workgroup's waves
+    int32_t few;              // 4 or 8: tiles of 32 rows, their keys shared out over so many waves; 0: of 256
     int32_t n_tiles;          // row tiles per (batch, key head)
     int32_t n_whole;          // tiles (of all heads) that are not split
     int32_t parts;            // key shares of a split tile
@@ -290,7 +290,7 @@ struct Kv8AttnArgs {
     int32_t range_keys[kMaxRanges];
 };
 constexpr int kKv8FewRows = 32;  // rows of a tile where rows are few
-constexpr int kKv8FewWaves = 4;  // waves that share its keys out
+constexpr int kKv8MaxParts = 256;
 hipError_t launch_attn_kv8(const Kv8AttnArgs& a, int head_dim, hipStream_t s);
 
 }  // namespace tmk

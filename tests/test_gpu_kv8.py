@@ -28,6 +28,13 @@ pytestmark = pytest.mark.gpu
 BLOCK = 64
 
 
+def in_tiles(B, Hk, rows, lengths, D):
+    """Whether a call's rows go in tiles of 256 (and not of 32): the library's rule on the call's
+    sizes, which the cases below are there to straddle."""
+    work = -(-rows // 32) * B * Hk * sum(-(-n // BLOCK) for n in lengths)
+    return rows > (64 if D == 64 else 32) and work > (22000 if D == 64 else 8000)
+
+
 @pytest.fixture(scope="module")
 def tm():
     assert torch.cuda.is_available(), "GPU tests need a GPU"
@@ -249,10 +256,19 @@ def queries(B, n, H, D, g):
     (1, 8, 1, [3000, 64, 64, 64], 3, 4),
     (1, 2, 2, [2000, 1000], 1, 300),                # split tiles
     (3, 10, 5, [700, 320, 320], 0, 40),
+    # in tiles of 256 rows
     (1, 47, 47, [1800, 40, 1800], 1, 1000),         # 188 tiles: each cut in two
+    (3, 90, 90, [1000, 130, 65], 1, 97),            # 270 tiles of four blocks, the last 14 split
+    (4, 64, 64, [2000, 100, 1000, 290], 0, 65),     # whole rounds only; tiles of three blocks
+    (2, 100, 25, [700, 700, 321], 1, 129),          # shared heads: 516 rows, three tiles a head
+    (1, 5, 5, [6000, 3000, 3000], 1, 2500),         # 50 tiles of many parts
+    (1, 1, 1, [70000, 64], 0, 700),                 # three tiles of more than 16 parts
 ])
 def test_attention(tm, D, B, H, Hk, lengths, window, n_q):
     g = torch.Generator().manual_seed(n_q)
+    if H * n_q > 4000:
+        now = [lengths[0]] + lengths[max(1, len(lengths) - 1 - window):]
+        assert in_tiles(B, Hk, n_q * (H // Hk), now, D)
     cache = make(tm, B, H, Hk, D, lengths[0], max(lengths[1:] + [1]), window)
     fill(tm, cache, lengths, g)
     q = queries(B, n_q, H, D, g)
@@ -261,7 +277,7 @@ def test_attention(tm, D, B, H, Hk, lengths, window, n_q):
     assert torch.equal(o1, o2) and torch.equal(l1, l2)
 
 
-@pytest.mark.parametrize("n_q", [1, 40])
+@pytest.mark.parametrize("n_q", [1, 40, 3000])
 def test_without_a_workspace(tm, n_q):
     """The parts in one workgroup: other sums, within twice the bound of the first."""
     import ctypes
@@ -280,65 +296,69 @@ def test_without_a_workspace(tm, n_q):
     assert bool(((o1 - o2).abs() <= 2 * BOUND * size).all())
 
 
-@pytest.mark.parametrize("n_q", [1, 300])
+@pytest.mark.parametrize("n_q,H", [(1, 2), (300, 2), (300, 60)])
 @pytest.mark.parametrize("scale", [0.0, 0.7])
-def test_scores_that_rise_late_and_fall(tm, n_q, scale):
+def test_scores_that_rise_late_and_fall(tm, n_q, H, scale):
     """Keys that grow from block to block raise the running maximum again and again; then they
     shrink. The sizes keep |score| below 30."""
     D, n = 128, 1000
     g = torch.Generator().manual_seed(7)
-    cache = make(tm, 1, 2, 2, D, n, 1, 0, scale)
-    k = torch.randn((1, n, 2, D), generator=g)
+    cache = make(tm, 1, H, H, D, n, 1, 0, scale)
+    assert in_tiles(1, H, n_q, [n], D) == (H > 2)
+    k = torch.randn((1, n, H, D), generator=g)
     k = k / k.square().mean(-1, keepdim=True).sqrt()
     ramp = torch.cat([torch.linspace(0.01, 1, n // 2), torch.linspace(1, 0.01, n - n // 2)])
     size = 5.0 if scale == 0 else 0.6
-    q = queries(1, n_q, 2, D, g)
+    q = queries(1, n_q, H, D, g)
     # a common direction, so that scores grow with the ramp
     k = bf16((0.8 * q[:, :1].float().cpu() + 0.6 * k) * ramp[None, :, None, None] * size * 0.4)
-    tm.tm_kv8_append(cache, 0, k.cuda(), bf16(torch.randn((1, n, 2, D), generator=g)).cuda())
+    tm.tm_kv8_append(cache, 0, k.cuda(), bf16(torch.randn((1, n, H, D), generator=g)).cuda())
     check_attention(tm, cache, 0, q, "ramp", scale or None)
 
 
-@pytest.mark.parametrize("n_q", [1, 257])
-def test_blocks_whose_values_differ_by_orders(tm, n_q):
+@pytest.mark.parametrize("n_q,H", [(1, 1), (257, 1), (257, 310)])
+def test_blocks_whose_values_differ_by_orders(tm, n_q, H):
     """V blocks from 1e-9 to 1e6, one of zeros: the scale goes into P, so nothing over- or
     underflows, and the row sums count every key."""
     D, n = 64, 8 * BLOCK
     g = torch.Generator().manual_seed(8)
-    cache = make(tm, 1, 1, 1, D, n, 1, 0)
-    k = torch.randn((1, n, 1, D), generator=g)
-    v = torch.randn((1, n, 1, D), generator=g)
+    cache = make(tm, 1, H, H, D, n, 1, 0)
+    assert in_tiles(1, H, n_q, [n], D) == (H > 1)
+    k = torch.randn((1, n, H, D), generator=g)
+    v = torch.randn((1, n, H, D), generator=g)
     for i, s in enumerate((1.0, 1e6, 1e-9, 0.0, 3e-4, 1e3, 1e-2, 1.0)):
         v[:, 64 * i:64 * i + 64] *= s
     tm.tm_kv8_append(cache, 0, bf16(k).cuda(), bf16(v).cuda())
-    check_attention(tm, cache, 0, queries(1, n_q, 1, D, g), "orders")
+    check_attention(tm, cache, 0, queries(1, n_q, H, D, g), "orders")
 
 
-@pytest.mark.parametrize("n_q", [3, 300])
+@pytest.mark.parametrize("n_q,H", [(3, 1), (300, 1), (300, 170)])
 @pytest.mark.parametrize("size", [1e-35, 1e-12, 1e6])
-def test_queries_of_any_size(tm, n_q, size):
+def test_queries_of_any_size(tm, n_q, H, size):
     """Rows of q far from 1 (keys the other way round keep the scores below 30)."""
     D, n = 128, 300
     g = torch.Generator().manual_seed(11)
-    cache = make(tm, 1, 1, 1, D, n, 1, 0)
+    cache = make(tm, 1, H, H, D, n, 1, 0)
+    assert in_tiles(1, H, n_q, [n], D) == (H > 1)
     fill(tm, cache, [n], g, ks=1.0 if size < 1 else 1.0 / size)
-    q = bf16(queries(1, n_q, 1, D, g).float() * size)
+    q = bf16(queries(1, n_q, H, D, g).float() * size)
     q[:, 0] = 0  # a row of zeros sees the mean
     check_attention(tm, cache, 0, q, f"q * {size}")
 
 
-@pytest.mark.parametrize("n_q", [2, 100])
-def test_one_key_that_outweighs_a_long_cache(tm, n_q):
+@pytest.mark.parametrize("n_q,H", [(2, 1), (100, 40)])
+def test_one_key_that_outweighs_a_long_cache(tm, n_q, H):
     """10000 keys at 2^-24 of the largest weight still count for their share: the fp16 weights
     keep 8 bits below the largest."""
     D, n = 64, 10000
     g = torch.Generator().manual_seed(12)
-    cache = make(tm, 1, 1, 1, D, n, 1, 0)
-    k = torch.zeros((1, n, 1, D))
+    cache = make(tm, 1, H, H, D, n, 1, 0)
+    assert in_tiles(1, H, n_q, [n], D) == (H > 1)
+    k = torch.zeros((1, n, H, D))
     k[:, 77, :, 0] = 1.0
-    v = torch.ones((1, n, 1, D))
+    v = torch.ones((1, n, H, D))
     v[:, 77] = 0
-    q = torch.zeros((1, n_q, 1, D))
+    q = torch.zeros((1, n_q, H, D))
     q[..., 0] = 24 * math.log(2) * math.sqrt(D)  # exactly one score of 24 log 2, bf16 rounding aside
     tm.tm_kv8_append(cache, 0, bf16(k).cuda(), bf16(v).cuda())
     # every one of the small weights may lose a whole unit of the last place of fp16's subnormal
@@ -349,39 +369,42 @@ def test_one_key_that_outweighs_a_long_cache(tm, n_q):
     assert float(((o.double() - want).abs() / (2.0 ** -8 * size)).max()) <= 1.0
 
 
-@pytest.mark.parametrize("n_q", [4, 60])
-def test_rows_and_blocks_that_are_not_finite(tm, n_q):
+@pytest.mark.parametrize("n_q,H", [(4, 1), (60, 1), (260, 310)])
+def test_rows_and_blocks_that_are_not_finite(tm, n_q, H):
     D, n = 64, 200
     g = torch.Generator().manual_seed(13)
-    cache = make(tm, 2, 1, 1, D, n, 1, 0)
-    k, v = bf16(torch.randn((2, n, 1, D), generator=g)), bf16(torch.randn((2, n, 1, D), generator=g))
+    cache = make(tm, 2, H, H, D, n, 1, 0)
+    assert in_tiles(2, H, n_q, [n], D) == (H > 1)
+    k, v = bf16(torch.randn((2, n, H, D), generator=g)), bf16(torch.randn((2, n, H, D), generator=g))
     tm.tm_kv8_append(cache, 0, k.cuda(), v.cuda())
-    q = queries(2, n_q, 1, D, g)
+    q = queries(2, n_q, H, D, g)
     clean = tm.tm_kv8_attn_fwd(cache, q, 0)
     bad = q.clone()
     bad[0, 1, 0, 3] = float("nan")
     bad[1, 2, 0, 60] = float("inf")
     o = tm.tm_kv8_attn_fwd(cache, bad, 0)
-    rows = torch.zeros((2, n_q), dtype=torch.bool, device="cuda")
-    rows[0, 1] = rows[1, 2] = True
+    rows = torch.zeros((2, n_q, H), dtype=torch.bool, device="cuda")
+    rows[0, 1, 0] = rows[1, 2, 0] = True
     assert bool(torch.isnan(o[rows]).all()) and torch.equal(o[~rows], clean[~rows])
-    # a block without a scale makes its stream's rows NaN, no other's
+    # a block without a scale makes its stream's and head's rows NaN, no other's
     v[1, 150, 0, 0] = float("-inf")
     tm.tm_kv8_append(cache, 0, k.cuda(), v.cuda())
     o = tm.tm_kv8_attn_fwd(cache, q, 0)
-    assert bool(torch.isnan(o[1]).all()) and torch.equal(o[0], clean[0])
+    assert bool(torch.isnan(o[1, :, 0]).all()) and torch.equal(o[0], clean[0])
+    assert torch.equal(o[1, :, 1:], clean[1, :, 1:])
 
 
-@pytest.mark.parametrize("D", [64, 128])
-def test_a_row_does_not_depend_on_the_rows_beside_it(tm, D):
+@pytest.mark.parametrize("D,H", [(64, 1), (128, 1), (64, 280), (128, 101)])
+def test_a_row_does_not_depend_on_the_rows_beside_it(tm, D, H):
     """A row whose maximum is raised again and again, beside rows whose maximum is not: theirs keep
     their bits."""
     n, n_q = 640, 256
     g = torch.Generator().manual_seed(21)
-    cache = make(tm, 1, 1, 1, D, n, 1, 0)
-    k = torch.randn((1, n, 1, D), generator=g)
-    tm.tm_kv8_append(cache, 0, bf16(k).cuda(), bf16(torch.randn((1, n, 1, D), generator=g)).cuda())
-    q = queries(1, n_q, 1, D, g)
+    cache = make(tm, 1, H, H, D, n, 1, 0)
+    assert in_tiles(1, H, n_q, [n], D) == (H > 1)
+    k = torch.randn((1, n, H, D), generator=g)
+    tm.tm_kv8_append(cache, 0, bf16(k).cuda(), bf16(torch.randn((1, n, H, D), generator=g)).cuda())
+    q = queries(1, n_q, H, D, g)
     want = tm.tm_kv8_attn_fwd(cache, q, 0, o_f32=True)
     other = q.clone()
     other[0, 5::32] = 40 * k[0, n - 1].cuda()
@@ -394,9 +417,10 @@ def test_a_row_does_not_depend_on_the_rows_beside_it(tm, D):
 def test_in_place_other_stream_and_capture(tm):
     D = 128
     g = torch.Generator().manual_seed(14)
-    cache = make(tm, 1, 4, 2, D, 1000, 200, 1)
-    fill(tm, cache, [1000, 200], g)
-    for n_q in (1, 200):
+    cache = make(tm, 1, 4, 2, D, 9000, 200, 1)
+    fill(tm, cache, [9000, 200], g)
+    assert in_tiles(1, 2, 2 * 1000, [9000, 200], D)
+    for n_q in (1, 1000):
         q = queries(1, n_q, 4, D, g)
         want = tm.tm_kv8_attn_fwd(cache, q, 1)
         torch.cuda.synchronize()
@@ -443,6 +467,7 @@ def test_codes_past_2_to_the_32(tm):
     kr, vr = tm.tm_kv8_read(cache, 0)
     assert torch.equal(kr, k) and torch.equal(vr, v)
     rows = q.expand(1, 64, 1, D).contiguous()
+    assert in_tiles(1, 1, 64, [n], D)
     assert float((tm.tm_kv8_attn_fwd(cache, rows, 0, o_f32=True) - 2.0).abs().max()) <= 2.0 ** -10
 
 
