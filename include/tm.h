@@ -332,7 +332,7 @@ typedef struct tm_rope_desc {
     int32_t head_dim;   /* D: 64 or 128 */
     int32_t frames;     /* >= 1: latent frames the table covers */
     int32_t grid_h;     /* >= 1: tokens per column of a latent frame */
-    int32_t grid_w;     /* >= 1: tokens per row; at most 2^30 positions in all */
+    int32_t grid_w;     /* >= 1: tokens per row; at most 2^30 positions in all, and a table of 2 GiB */
     int32_t pairs_t;    /* >= 0: pairs turned by the frame, */
     int32_t pairs_h;    /* by the row */
     int32_t pairs_w;    /* and by the column; together at most D / 2 */

@@ -98,13 +98,14 @@ __device__ __forceinline__ float scale_of(uint32_t m) {
 // rounds to a whole number, to even at ties, and leaves it in the low bits.
 __device__ __forceinline__ uint32_t codes4(const float* x, float inv) {
 #pragma clang fp contract(off)
-    uint32_t w = 0;
+    uint32_t c[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const float c = x[e] * inv;
-        w |= ((__float_as_uint(c + 0x1.8p23f) + kCodeZero) & 0xFFu) << (8 * e);
+        const float p = x[e] * inv;
+        c[e] = __float_as_uint(p + 0x1.8p23f);
     }
-    return w;
+    const uint32_t lo = pick_bytes(c[1], c[0], 0x0C0C0400), hi = pick_bytes(c[3], c[2], 0x04000C0C);
+    return (lo | hi) ^ (kCodeZero * 0x01010101u);  // low bytes; + 128 in each
 }
 
 // D: head_dim. PRODUCE: workgroups past a.kv_wgs normalise and rotate queries, and
@@ -329,8 +330,11 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_read_kernel(const Kv8ReadArgs
             for (int i = 0; i < 4; ++i) {
                 const uint32_t w = tile[x][r * PITCH + (run_of<EB, D>(g, 4 * i * EB / 16) + 4 * i % (16 / EB)) / 4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    v[4 * i + e] = (static_cast<float>((w >> (8 * e)) & 0xFFu) - 128.f) * (x == 0 ? sk : sv);
+                for (int e = 0; e < 4; ++e) {
+                    // (code + 128) * s - 128 * s: the product and the difference are exact in the fma
+                    const float s = x == 0 ? sk : sv;
+                    v[4 * i + e] = fmaf(static_cast<float>((w >> (8 * e)) & 0xFFu), s, -128.f * s);
+                }
             }
             store_row<EB, D>((x == 0 ? a.k_out : a.v_out) + first + t * stride, g, v);
         }

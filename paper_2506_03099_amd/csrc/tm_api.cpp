@@ -1019,6 +1019,7 @@ tm_status check_rope_desc(const tm_rope_desc* d, RopeGeo* g) {
         g->pairs[x] = pairs[x];
         n += rows[x] * pairs[x];
     }
+    if (n > tmk::kMaxRopeEntries) return fail(TM_E_SHAPE, "the table would exceed 2 GiB");
     g->elem = d->dtype == TM_BF16 ? 2 : 4;
     g->table_bytes = size_t(n) * 2 * sizeof(float);
     return TM_OK;
@@ -1038,13 +1039,15 @@ tm_status rope_table(const tm_rope_desc* d, const RopeGeo& g, const float* table
         if (st != TM_OK) return st;
     }
     t->table = reinterpret_cast<const float2*>(table);
-    t->table_h = t->table + g.rows[0] * g.pairs[0];
-    t->table_w = t->table_h + g.rows[1] * g.pairs[1];
+    t->first_h = int32_t(g.rows[0] * g.pairs[0]);
+    t->first_w = int32_t(t->first_h + g.rows[1] * g.pairs[1]);
     t->pairs_t = g.pairs[0];
     t->pairs_h = g.pairs[1];
     t->pairs_w = g.pairs[2];
     t->grid_w = d->grid_w;
     t->frame_tokens = int32_t(frame);
+    t->by_w = tmk::FastDiv(uint32_t(d->grid_w));
+    t->by_frame = tmk::FastDiv(uint32_t(frame));
     return TM_OK;
 }
 

@@ -193,15 +193,33 @@ hipError_t launch_attn_bwd_bf16(const BwdArgs& a, int head_dim, hipStream_t s);
 constexpr int64_t kBwdScratchFloats = int64_t(1) << 21;
 hipError_t bwd_scratch_address(float** out);
 
+// Division of 0 <= n < 2^31 by d, 1 <= d < 2^31: n * mul >> shift with mul = floor(2^shift / d) + 1 and
+// shift = 31 + ceil(log2 d), exact since mul * d exceeds 2^shift by at most d <= 2^(shift - 31).
+struct FastDiv {
+    uint32_t mul = 0;
+    int32_t shift = 0;
+    FastDiv() = default;
+    explicit FastDiv(uint32_t d) {
+        int log2 = 0;
+        while ((uint64_t(1) << log2) < d) ++log2;
+        shift = 31 + log2;
+        mul = static_cast<uint32_t>((uint64_t(1) << shift) / d + 1);
+    }
+    __host__ __device__ int32_t of(int32_t n) const {
+        return static_cast<int32_t>(static_cast<uint64_t>(static_cast<uint32_t>(n)) * mul >> shift);
+    }
+};
+
 // Rotary positions: (cos, sin) of every position and pair of the three axes, the
 // frames' rows first, then the grid's rows, then its columns.
 struct RopeTable {
-    const float2* table;    // [frames][pairs_t]
-    const float2* table_h;  // [grid_h][pairs_h]
-    const float2* table_w;  // [grid_w][pairs_w]
+    const float2* table;    // [frames][pairs_t], [grid_h][pairs_h], [grid_w][pairs_w]
+    int32_t first_h, first_w;  // entries before the second and the third
     int32_t pairs_t, pairs_h, pairs_w;
     int32_t grid_w, frame_tokens;
+    FastDiv by_w, by_frame;
 };
+constexpr int64_t kMaxRopeEntries = int64_t(1) << 28;  // of the table: 2 GiB, so that offsets fit 32 bits
 
 // Rotation of q [B, n, H, D] and k [B, n, Hk, D] (Hk = 0: none) into q_out and
 // k_out; row i is the token at position first_token + i.

@@ -84,19 +84,29 @@ __device__ __forceinline__ void store_row(unsigned char* row, int g, const float
 template <int EB, int D, bool HALVES>
 __device__ __forceinline__ void load_turns(const RopeTable& t, int64_t pos, int g, float2 (&cs)[8]) {
     const int p = static_cast<int>(pos);  // below frames * frame_tokens <= 2^30
-    const int f = p / t.frame_tokens, j = p - f * t.frame_tokens;
-    const int y = j / t.grid_w, x = j - y * t.grid_w;
+    const int f = t.by_frame.of(p), j = p - f * t.frame_tokens;
+    const int y = t.by_w.of(j), x = j - y * t.grid_w;
     // pair i of the row is entry i of these, in its axis' span
-    const float2* const at = t.table + static_cast<int64_t>(f) * t.pairs_t;
-    const float2* const ay = t.table_h + y * t.pairs_h - t.pairs_t;
-    const float2* const ax = t.table_w + x * t.pairs_w - (t.pairs_t + t.pairs_h);
     const int end_t = t.pairs_t, end_h = end_t + t.pairs_h, end_w = end_h + t.pairs_w;
+    const int at = f * t.pairs_t, ay = t.first_h + y * t.pairs_h - end_t, ax = t.first_w + x * t.pairs_w - end_h;
+    const bool all = end_w == D / 2;
+    if (end_w == 0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) cs[e] = make_float2(1.f, 0.f);
+        return;
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const int i = pair_of<EB, D, HALVES>(g, e);
-        const float2* const from = i < end_t ? at : i < end_h ? ay : ax;
-        cs[e] = make_float2(1.f, 0.f);
-        if (i < end_w) cs[e] = from[i];
+        const int entry = (i < end_t ? at : i < end_h ? ay : ax) + i;
+        // (an entry that exists for a pair that no axis turns)
+        const uint32_t off = static_cast<uint32_t>(all || i < end_w ? entry : 0) * 8u;
+        cs[e] = *reinterpret_cast<const float2*>(reinterpret_cast<const char*>(t.table) + off);
+    }
+    if (!all) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (pair_of<EB, D, HALVES>(g, e) >= end_w) cs[e] = make_float2(1.f, 0.f);
     }
 }
 

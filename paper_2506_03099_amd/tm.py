@@ -523,6 +523,8 @@ class KV8Cache:
         self.pool = pool
         _check(lib().tm_kv8_cache_create(ctypes.byref(desc), self.kv_heads, _ptr(pool), ctypes.byref(h)))
         self.handle = h
+        self._at = ctypes.c_int32(), ctypes.c_int32()
+        self._at_refs = tuple(ctypes.byref(x) for x in self._at)
 
     @property
     def capacity(self) -> int:
@@ -539,9 +541,9 @@ class KV8Cache:
         return lib().tm_kv8_cache_latest(self.handle)
 
     def locate(self, chunk: int):
-        off, n = ctypes.c_int32(), ctypes.c_int32()
-        _check(lib().tm_kv8_cache_locate(self.handle, chunk, ctypes.byref(off), ctypes.byref(n)))
-        return off.value, n.value
+        # (one handle is not used by two threads at once)
+        _check(lib().tm_kv8_cache_locate(self.handle, chunk, *self._at_refs))
+        return self._at[0].value, self._at[1].value
 
     def reset(self):
         _check(lib().tm_kv8_cache_reset(self.handle))
