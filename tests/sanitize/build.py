@@ -16,6 +16,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(os.path.dirname(HERE))
 PKG = os.path.join(ROOT, "paper_2506_03099_amd")
 DRIVER = os.path.join(HERE, "host_abi_driver")
+KV8_DRIVER = os.path.join(HERE, "host_kv8_driver")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 
 SAN = ["-fsanitize=address,undefined", "-fno-sanitize-recover=undefined", "-fno-omit-frame-pointer"]
@@ -26,17 +27,18 @@ CXXFLAGS = ["-std=c++17", "-O1", "-g", "-D__HIP_PLATFORM_AMD__", "-I", os.path.j
 def build(verbose: bool = False) -> str:
     if not os.path.exists(os.path.join(PKG, "libtm.so")):
         raise RuntimeError("libtm.so must be built first")
-    obj = os.path.join(HERE, "host_abi_driver.o")
-    cmd = ["g++", *CXXFLAGS, *SAN, "-c", os.path.join(HERE, "host_abi_driver.cpp"), "-o", obj]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
-    cmd = ["g++", *SAN, obj, "-L", PKG, "-ltm", "-L", os.path.join(ROCM, "lib"), "-lamdhip64",
-           "-Wl,-rpath," + PKG, "-Wl,-rpath," + os.path.join(ROCM, "lib"), "-o", DRIVER]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
-    os.remove(obj)
+    for driver in (DRIVER, KV8_DRIVER):
+        obj = driver + ".o"
+        cmd = ["g++", *CXXFLAGS, *SAN, "-c", driver + ".cpp", "-o", obj]
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.run(cmd, check=True)
+        cmd = ["g++", *SAN, obj, "-L", PKG, "-ltm", "-L", os.path.join(ROCM, "lib"), "-lamdhip64",
+               "-Wl,-rpath," + PKG, "-Wl,-rpath," + os.path.join(ROCM, "lib"), "-o", driver]
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.run(cmd, check=True)
+        os.remove(obj)
     return DRIVER
 
 
