@@ -108,7 +108,7 @@ __device__ __forceinline__ uint32_t codes4(const float* x, float inv) {
     return (lo | hi) ^ (kCodeZero * 0x01010101u);  // low bytes; + 128 in each
 }
 
-// D: head_dim. PRODUCE: workgroups past a.kv_wgs normalise and rotate queries, and
+// D: head_dim. PRODUCE: the first a.q_wgs workgroups normalise and rotate queries, and
 // the keys are normalised and rotated before they are coded (a.turn: rotated at all).
 template <int D, bool PRODUCE, bool HALVES>
 __global__ __launch_bounds__(kKv8Threads) void kv8_write_kernel(const Kv8WriteArgs a) {
@@ -125,10 +125,10 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_write_kernel(const Kv8WriteAr
     const int tid = threadIdx.x;
     const int g = tid % G, r0 = tid / G;
     if constexpr (PRODUCE) {
-        if (blockIdx.x >= a.kv_wgs) {
+        if (blockIdx.x < a.q_wgs) {
             // a lane takes this part of the rows of heads s, s + S, ... of a token
             constexpr int U = 4;
-            const uint32_t idx = (blockIdx.x - a.kv_wgs) * static_cast<uint32_t>(kKv8Threads) + tid;
+            const uint32_t idx = blockIdx.x * static_cast<uint32_t>(kKv8Threads) + tid;
             const uint32_t r = idx / G;
             const int s = r % a.q_slices;
             const int64_t row = r / a.q_slices;  // of [B, n]
@@ -156,8 +156,9 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_write_kernel(const Kv8WriteAr
         }
     }
 
-    const int blk = blockIdx.x % a.n_blk;
-    const int bh = blockIdx.x / a.n_blk;
+    const uint32_t wg = blockIdx.x - (PRODUCE ? a.q_wgs : 0);
+    const int blk = wg % a.n_blk;
+    const int bh = wg / a.n_blk;
     const int h = bh % a.Hk;
     const int64_t b = bh / a.Hk;
     const int64_t stride = static_cast<int64_t>(a.Hk) * D * 2;  // bytes per source token
@@ -350,7 +351,7 @@ hipError_t launch_kv8_write(Kv8WriteArgs a, int head_dim, bool produce, bool hal
     const int64_t q_threads = produce ? static_cast<int64_t>(a.B) * a.n_tok * a.q_slices * (head_dim / kRowElems) : 0;
     const int64_t grid = kv + (q_threads + kKv8Threads - 1) / kKv8Threads;
     if (grid > INT32_MAX || q_threads > UINT32_MAX - kKv8Threads) return hipErrorInvalidValue;
-    a.kv_wgs = static_cast<uint32_t>(kv);
+    a.q_wgs = static_cast<uint32_t>(grid - kv);
 #define TM_KV8_WRITE(D_, P_, HV_)                                                                        \
     if (head_dim == D_ && produce == P_ && halves == HV_) {                                              \
         hipLaunchKernelGGL((kv8_write_kernel<D_, P_, HV_>), dim3(static_cast<unsigned>(grid)),           \

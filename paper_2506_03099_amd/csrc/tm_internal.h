@@ -262,7 +262,7 @@ struct Kv8WriteArgs {
     int32_t first_blk;  // the chunk's first one
     int32_t n_blk;      // the chunk's; this and the next two set by the launcher
     int32_t q_slices;   // threads that share a token's query heads
-    uint32_t kv_wgs;    // workgroups for K and V; those past them take queries
+    uint32_t q_wgs;     // workgroups for queries; those past them take K and V
 };
 hipError_t launch_kv8_write(Kv8WriteArgs a, int head_dim, bool produce, bool halves, hipStream_t s);
 
