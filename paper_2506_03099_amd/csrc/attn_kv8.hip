@@ -278,9 +278,10 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_kv8_few_kernel(const Kv8AttnA
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
     const Share s = share_of(a);
     const int q0 = s.tile * kKv8FewRows, n_rows = min(kKv8FewRows, a.rows - q0);
+    const int64_t head = (static_cast<int64_t>(s.bat) * a.Hk + s.kvh) * a.n_blocks;
+
     f16x8_t qf[KK];
     const float cq = load_q<D>(a, row_at(a, s.bat, s.kvh, min(q0 + l32, a.rows - 1)), l32 < n_rows, hw, qf);
-    const int64_t head = (static_cast<int64_t>(s.bat) * a.Hk + s.kvh) * a.n_blocks;
 
     f32x16_t acc[DB];
 #pragma unroll
@@ -288,15 +289,16 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_kv8_few_kernel(const Kv8AttnA
     float m = kNegInf, l = 0.f;
     u32x4_t kc[NP], vc[NP];
     float ks = 0.f, vs = 0.f;
+    const uint32_t lane16 = 16 * lane;
     auto load_k = [&](int blk) __attribute__((always_inline)) {
-        const u32x4_t* const p = reinterpret_cast<const u32x4_t*>(a.k_codes + (head + blk) * (kCacheBlock * D)) + lane;
 #pragma unroll
-        for (int i = 0; i < NP; ++i) kc[i] = p[64 * i];
+        for (int i = 0; i < NP; ++i)
+            kc[i] = load_from<u32x4_t>(a.k_codes + (head + blk) * (kCacheBlock * D) + 1024 * i, lane16);
     };
     auto load_v = [&](int blk) __attribute__((always_inline)) {
-        const u32x4_t* const p = reinterpret_cast<const u32x4_t*>(a.v_codes + (head + blk) * (kCacheBlock * D)) + lane;
 #pragma unroll
-        for (int i = 0; i < NP; ++i) vc[i] = p[64 * i];
+        for (int i = 0; i < NP; ++i)
+            vc[i] = load_from<u32x4_t>(a.v_codes + (head + blk) * (kCacheBlock * D) + 1024 * i, lane16);
     };
     // this wave's blocks: every NW-th of the share
     Blocks at;
@@ -445,12 +447,12 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
     const bool v_first = NP == 1 && wave >= 4;
     const int pw = NP == 2 ? wave : wave & 3;  // piece's kb * DB + (s or d)
     const uint32_t lane16 = 16 * lane;
-    const uint32_t to = 2 * pw * 1024 + lane16;
+    const uint32_t lds_to = 2 * pw * 1024 + lane16;
     // (V's lane offset in a register of its own: it is past the reach of a read's immediate, and the
     // compiler would add it up for every read; 977 -> 964 us)
     uint32_t v_lane16 = NBUF * TILEB + lane16;
     asm volatile("" : "+v"(v_lane16));
-    u32x4_t codes[NP];
+    u32x4_t codes[NP];  // of the block that is turned into operands next
     float ks, vs;   // scales of the tile whose scores come next (the same in every lane)
     int blk[NBUF];  // block j of the walk in [j % 4]
     int cnt[NBUF];  // keys from it to its range's end
@@ -458,13 +460,13 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
     Blocks at;
     at.start(a, s.b0);
     // The codes of the block that the walk stands on, block u of the tiles; the walk moves on by step().
-    auto load = [&](int u) __attribute__((always_inline)) {
+    auto load = [&](u32x4_t (&to)[NP], int u) __attribute__((always_inline)) {
         const int64_t o = (head + at.blk) * (kCacheBlock * D) + 1024 * pw;
         if constexpr (NP == 2) {
-            codes[0] = load_from<u32x4_t>(a.k_codes + o, lane16);
-            codes[1] = load_from<u32x4_t>(a.v_codes + o, lane16);
+            to[0] = load_from<u32x4_t>(a.k_codes + o, lane16);
+            to[1] = load_from<u32x4_t>(a.v_codes + o, lane16);
         } else {
-            codes[0] = load_from<u32x4_t>((v_first ? a.v_codes : a.k_codes) + o, lane16);
+            to[0] = load_from<u32x4_t>((v_first ? a.v_codes : a.k_codes) + o, lane16);
         }
         blk[u & 3] = at.blk;
         cnt[u & 3] = at.keys;
@@ -477,15 +479,15 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
     // each half's 16 bytes into the buffers of block u once its four pairs are there.
     constexpr int ND = 8 * NP;
     f16x2_t half[4];
-    auto put = [&](int i, int u) __attribute__((always_inline)) {
+    auto put = [&](const u32x4_t (&from)[NP], int i, int u) __attribute__((always_inline)) {
         const int p = i / 8, h = i / 4 % 2;
-        const uint32_t w = codes[p][2 * h + i / 2 % 2];
+        const uint32_t w = from[p][2 * h + i / 2 % 2];
         const bool is_k = NP == 2 ? p == 0 : !v_first;
         if (is_k) half[i % 4] = i % 2 ? biased2<true>(w) : biased2<false>(w);
         else half[i % 4] = i % 2 ? decode2<true>(w) : decode2<false>(w);
         if (i % 4 != 3) return;
         const uint32_t base = NP == 2 ? p * NBUF * TILEB : v_first ? NBUF * TILEB : 0;
-        *(lds_f16x8_t*)(L + to + base + ((u & (NBUF - 1)) * TILEB + h * 1024)) =
+        *(lds_f16x8_t*)(L + lds_to + base + ((u & (NBUF - 1)) * TILEB + h * 1024)) =
             f16x8_t{half[0][0], half[0][1], half[1][0], half[1][1], half[2][0], half[2][1], half[3][0], half[3][1]};
     };
     // Fragment f of a tile's stream: K fragments (kk = f / 2, kb = f % 2) of buffer ku, then V
@@ -528,15 +530,15 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
         lt = e < 4 ? p0 + p1 : lt + (p0 + p1);
     };
 
-    // ---- prologue: blocks 0..2 into LDS, block 3 in registers
+    // ---- prologue: blocks 0..2 into LDS, block 3 in registers; every load is issued before the first
+    // is waited for
+    u32x4_t early[3][NP];
 #pragma unroll
     for (int u = 0; u < 3; ++u) {
-        load(u);
-#pragma unroll
-        for (int i = 0; i < ND; ++i) put(i, u);
+        load(early[u], u);
         at.step(a);
     }
-    load(3);
+    load(codes, 3);
     load_scales(0);
     const int qrow = q0 + wave * 32 + l32;
     f16x8_t qf[KK];
@@ -547,6 +549,10 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
 #pragma unroll
         for (int e = 0; e < 8; ++e) qsum += static_cast<float>(qf[kk][e]);
     qsum = (qsum + __shfl_xor(qsum, 32)) * kBiasedZero;
+#pragma unroll
+    for (int u = 0; u < 3; ++u)
+#pragma unroll
+        for (int i = 0; i < ND; ++i) put(early[u], i, u);
     __syncthreads();
 
     // A wave without rows takes part in the loads and barriers only.
@@ -644,8 +650,8 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
             for (int e = FPG * k; e < FPG * (k + 1); ++e) nx[e >> 4][e & 15] = pin(fmaf(nx[e >> 4][e & 15], c, add));
             // (every write lies before the last RING reads ahead)
 #pragma unroll
-            for (int i = ND * k / PUTS; i < ND * (k + 1) / PUTS && k < PUTS; ++i) put(i, u + 3);
-            if (k == PUTS) load(u + 4);
+            for (int i = ND * k / PUTS; i < ND * (k + 1) / PUTS && k < PUTS; ++i) put(codes, i, u + 3);
+            if (k == PUTS) load(codes, u + 4);
             if (k == PUTS + 1) load_scales(u + 2);
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -664,9 +670,9 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
     } else {
         auto idle = [&](int u) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < ND; ++i) put(i, u + 3);
+            for (int i = 0; i < ND; ++i) put(codes, i, u + 3);
             at.step(a);
-            load(u + 4);
+            load(codes, u + 4);
             end_tile(false);
         };
         for (int t = 0; t < n; t += 4) {
