@@ -18,8 +18,11 @@
 // Writing: a workgroup per (batch, key head, block) takes the block's K and V
 // rows in registers, forms their largest magnitudes over the workgroup, and puts
 // the codes through LDS into the order of tm_kv8.h; nothing is read twice. The
-// producer's queries are rows of their own, in further workgroups of the same
-// launch. Bound by HBM: K and V in (2 bytes an element), codes out (1).
+// producer's queries are rows of their own, in workgroups of the same launch that
+// go first (the other way round 1.4% slower). Bound by HBM: K and V in (2 bytes an
+// element), codes out (1). Measured on a chunk of 4680 tokens, 40 heads of 128:
+// written 24.9 us (144 MB, 5.8 TB/s), read back 22.4 us (144 MB, 6.4), produced 53 us
+// from cold inputs (240 MB, 4.5 TB/s; 39 where they are in the last-level cache).
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -240,8 +243,8 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_write_kernel(const Kv8WriteAr
         store16_through(ko + 16 * n, u32x4_t{from[0], from[1], from[4], from[5]});
     }
     // V: 4 dimensions of 16 keys, transposed, are 4 pieces next to each other. They go through LDS
-    // once more, so that a wave stores a whole KB (four pieces a lane, each store a quarter of its
-    // lines: see the times above).
+    // once more, so that a wave stores a whole KB: with four pieces a lane every store instruction
+    // touched a quarter of 64 lines (with the rows loaded in the same manner, 38.7 us for 24.9).
     constexpr int QUADS = (PIECES / 4 + kKv8Threads - 1) / kKv8Threads;
     static_assert(QUADS == 1, "a thread transposes at most once");
     u32x4_t p[4];
