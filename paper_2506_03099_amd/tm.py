@@ -420,7 +420,7 @@ def tm_sparse_causal_attn_bwd_noalloc(desc: tm_attn_desc, n_frames: int, q, k, v
 def _expect(name, t, shape, dtype):
     """A tensor argument of the rotary and 8-bit-cache calls: the library sees
     addresses only, and torch's allocator puts many tensors into one allocation."""
-    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype):
+    if t is not None and (t.shape != shape or t.dtype != dtype):
         raise TMError(TM_E_SHAPE, f"{name} is not {dtype} {list(shape)}")
 
 
@@ -457,25 +457,28 @@ def _rope(fn, desc, table, q, k, first_token, q_out, k_out, stream):
     if len(shape) != 4 or shape[3] != D or q.dtype != dtype:
         raise TMError(TM_E_SHAPE, f"q is not {dtype} [batch, n_tok, heads, {D}]")
     B, n, H, _ = shape
+    if table is not None and (table.numel() != 2 * _rope_table_rows(desc) or table.dtype != torch.float32):
+        raise TMError(TM_E_SHAPE, "table is not the descriptor's")
+    _expect("q_out", q_out, shape, dtype)
     Hk, pk, pko = 0, None, None
     if k is not None:
         kshape = k.shape
         if len(kshape) != 4 or kshape[3] != D or k.dtype != dtype or kshape[0] != B or kshape[1] != n:
             raise TMError(TM_E_SHAPE, f"k is not {dtype} [{B}, {n}, kv_heads, {D}]")
-        Hk = kshape[2]
+        _expect("k_out", k_out, kshape, dtype)
+        Hk, pk = kshape[2], _ptr(k)
         if k_out is None:
             k_out = torch.empty_like(k)
+            pko = k_out.data_ptr()
         else:
-            _expect("k_out", k_out, kshape, dtype)
-        pk, pko = _ptr(k), _ptr(k_out)
+            pko = _ptr(k_out)
+    pq = _ptr(q)
     if q_out is None:
         q_out = torch.empty_like(q)
+        pqo = q_out.data_ptr()
     else:
-        _expect("q_out", q_out, shape, dtype)
-    if table is not None and (table.numel() != 2 * _rope_table_rows(desc) or table.dtype != torch.float32):
-        raise TMError(TM_E_SHAPE, "table is not the descriptor's")
-    _check(fn(ctypes.byref(desc), _ptr(table), B, n, first_token, _ptr(q), H, pk, Hk, _ptr(q_out), pko,
-              _stream(stream)))
+        pqo = _ptr(q_out)
+    _check(fn(ctypes.byref(desc), _ptr(table), B, n, first_token, pq, H, pk, Hk, pqo, pko, _stream(stream)))
     return q_out, k_out
 
 
@@ -619,13 +622,20 @@ def tm_kv8_attn_fwd(cache: KV8Cache, q, q_chunk: int, o=None, o_f32: bool = Fals
     can have none (under capture, on another stream than the current one) order
     the fp32 sums otherwise."""
     n_q = cache.rows("q", q, cache.heads)
-    _expect("o", o, q.shape, torch.float32 if o_f32 else torch.bfloat16)
-    _expect("lse", lse, (cache._batch, cache.heads, n_q), torch.float32)
+    pq = _ptr(q)
     if o is None:
         o = torch.empty(q.shape, dtype=torch.float32, device=q.device) if o_f32 else torch.empty_like(q)
-    pq, po, pl = _ptr(q), _ptr(o), _ptr(lse)
+        po = o.data_ptr()
+    else:
+        _expect("o", o, q.shape, torch.float32 if o_f32 else torch.bfloat16)
+        po = _ptr(o)
+    pl = None
+    if lse is not None:
+        _expect("lse", lse, (cache._batch, cache.heads, n_q), torch.float32)
+        pl = _ptr(lse)
+    L = lib()
     stream = _stream(stream)
-    n = lib().tm_kv8_attn_workspace(cache.handle, q_chunk, n_q)
-    ws = _workspace(n, q, stream)
-    _check(lib().tm_kv8_attn_fwd(cache.handle, pq, q_chunk, n_q, po, int(o_f32), pl, _ptr(ws), n, stream))
+    n = L.tm_kv8_attn_workspace(cache.handle, q_chunk, n_q)
+    ws = _workspace(n, q, stream) if n else None
+    _check(L.tm_kv8_attn_fwd(cache.handle, pq, q_chunk, n_q, po, o_f32, pl, _ptr(ws), n, stream))
     return o
