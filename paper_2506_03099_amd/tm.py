@@ -452,7 +452,7 @@ def tm_rope3d_table(desc: tm_rope_desc, table=None, device="cuda", stream=None):
 def _rope(fn, desc, table, q, k, first_token, q_out, k_out, stream):
     # (one call per layer and token of a decoder: about 2 us are Python's, so nothing
     # is looked up twice)
-    D, dtype = desc.head_dim, _TORCH_DTYPE[desc.dtype]
+    D, dtype = desc.head_dim, _TORCH_DTYPE.get(desc.dtype)
     shape = q.shape
     if len(shape) != 4 or shape[3] != D or q.dtype != dtype:
         raise TMError(TM_E_SHAPE, f"q is not {dtype} [batch, n_tok, heads, {D}]")
