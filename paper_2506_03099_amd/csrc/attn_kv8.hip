@@ -115,39 +115,47 @@ __device__ __forceinline__ float both_max(float x) {
 
 // Row r (of the n_q * group of a key head) of q and o: its offset in rows of D.
 __device__ __forceinline__ int64_t row_at(const Kv8AttnArgs& a, int bat, int kvh, int r) {
-    const int i = r / a.group, g = r - i * a.group;
+    const int i = a.by_group.of(r), g = r - i * a.group;
     return (static_cast<int64_t>(bat) * a.n_q + i) * a.H + kvh * a.group + g;
 }
 __device__ __forceinline__ int64_t lse_at(const Kv8AttnArgs& a, int bat, int kvh, int r) {
-    const int i = r / a.group, g = r - i * a.group;
+    const int i = a.by_group.of(r), g = r - i * a.group;
     return (static_cast<int64_t>(bat) * a.H + kvh * a.group + g) * a.n_q + i;
 }
 
-// A query row as the B operand of the score MFMAs (lane: dimensions 16 kk + 8 hw ..
-// + 7), scaled by a power of two; returns scale_log2 over that power. A row with an
-// infinity or a NaN gets NaN, and so does its output.
+// A query row's elements as the lane feeds them to the score MFMAs: dimensions 16 kk +
+// 8 hw .. + 7. (Every lane loads a row that exists: with a row of zeros for the others
+// the compiler made a branch and a wait of each load.)
 template <int D>
-__device__ __forceinline__ float load_q(const Kv8AttnArgs& a, int64_t row, bool ok, int hw, f16x8_t (&qf)[D / 16]) {
-    constexpr int KK = D / 16;
-    const __bf16* const p = static_cast<const __bf16*>(a.q) + row * D + 8 * hw;
-    bf16x8_t raw[KK];
-    uint32_t top = 0;
+__device__ __forceinline__ void load_q(const Kv8AttnArgs& a, int64_t row, int hw, u32x4_t (&raw)[D / 16]) {
+    const u32x4_t* const p = reinterpret_cast<const u32x4_t*>(static_cast<const __bf16*>(a.q) + row * D + 8 * hw);
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-        raw[kk] = ok ? *reinterpret_cast<const bf16x8_t*>(p + 16 * kk) : bf16x8_t{};
+    for (int kk = 0; kk < D / 16; ++kk) raw[kk] = p[2 * kk];
+}
+// The same as B operands, scaled by a power of two; returns scale_log2 over that power.
+// A row with an infinity or a NaN gets NaN, and so does its output.
+template <int D>
+__device__ __forceinline__ float scale_q(const u32x4_t (&raw)[D / 16], float scale_log2, f16x8_t (&qf)[D / 16]) {
+    typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+    u16x2_t tops{0, 0};
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            top = max(top, static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<__bf16>(raw[kk][e])) & 0x7FFF));
-    }
+    for (int kk = 0; kk < D / 16; ++kk)
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+            tops = __builtin_elementwise_max(tops, __builtin_bit_cast(u16x2_t, raw[kk][w] & 0x7FFF7FFFu));
+    uint32_t top = max(tops[0], tops[1]);
     top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 32)));
     const uint32_t e = top >> 7;  // the exponent field
     const uint32_t up = min(127u + 14 + 127 - min(e, 254u), 253u);
     const float mult = __uint_as_float(up << 23);
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk)
+    for (int kk = 0; kk < D / 16; ++kk)
 #pragma unroll
-        for (int x = 0; x < 8; ++x) qf[kk][x] = static_cast<_Float16>(static_cast<float>(raw[kk][x]) * mult);
-    return e == 255 ? __uint_as_float(0x7FC00000u) : a.scale_log2 * __uint_as_float((254 - up) << 23);
+        for (int w = 0; w < 4; ++w) {
+            qf[kk][2 * w] = static_cast<_Float16>(__uint_as_float(raw[kk][w] << 16) * mult);
+            qf[kk][2 * w + 1] = static_cast<_Float16>(__uint_as_float(raw[kk][w] & 0xFFFF0000u) * mult);
+        }
+    return e == 255 ? __uint_as_float(0x7FC00000u) : scale_log2 * __uint_as_float((254 - up) << 23);
 }
 
 // Waits for scalar loads, which share a counter with the LDS reads and come back in
@@ -209,59 +217,69 @@ struct Blocks {
     }
 };
 
-// Rows [q0, q1) of tile `idx` of the `nt` that cover `rows`, in blocks of 32 shared
-// out as evenly as they go.
-__device__ __forceinline__ void split_rows(int rows, int nt, int idx, int& q0, int& q1) {
-    const int blocks = (rows + 31) / 32;
-    const int each = blocks / nt, more = blocks - each * nt;
-    q0 = 32 * (idx * each + min(idx, more));
-    q1 = min(32 * ((idx + 1) * each + min(idx + 1, more)), rows);
+// Rows [q0, q1) of tile `idx`: blocks of 32 shared out as evenly as they go.
+__device__ __forceinline__ void split_rows(const Kv8AttnArgs& a, int idx, int& q0, int& q1) {
+    q0 = 32 * (idx * a.row_blocks + min(idx, a.more_row_blocks));
+    q1 = min(32 * ((idx + 1) * a.row_blocks + min(idx + 1, a.more_row_blocks)), a.rows);
 }
 
 // A workgroup's tile and share of its keys: whole tiles come first, then the split
 // ones' parts, a tile's next to each other; with a cut, all first parts (up to the
-// cut) and then all second ones.
+// cut) and then all second ones. XCDS: consecutive tiles on one XCD. (Divisions by
+// multiplication: with the runtime's own, of 64 bits where they split the keys, a
+// workgroup spent some 300 instructions here.)
 struct Share {
     int tile, bat, kvh, part;
-    int64_t split;  // number of the split tile, -1: whole
-    int b0, n;      // first key block of the walk and how many
+    int split;  // number of the split tile, -1: whole
+    int b0, n;  // first key block of the walk and how many
 };
+template <bool XCDS>
 __device__ __forceinline__ Share share_of(const Kv8AttnArgs& a) {
     Share s;
-    const int total = a.n_tiles * a.B * a.Hk;
+    const int bid = blockIdx.x, splits = a.n_tiles * a.B * a.Hk - a.n_whole;
     int id;
     s.part = 0;
     s.split = -1;
     s.b0 = 0;
     s.n = a.n_kblocks;
-    if (static_cast<int>(blockIdx.x) < a.n_whole) {
-        id = xcd_logical_id(blockIdx.x, a.n_whole);
+    if (bid < a.n_whole) {
+        id = XCDS ? xcd_logical_id(bid, a.n_whole) : bid;
     } else if (a.cut > 0) {
-        const int n = total - a.n_whole, j = blockIdx.x - a.n_whole;
-        s.part = j >= n;
-        s.split = xcd_logical_id(s.part ? j - n : j, n);
-        id = a.n_whole + static_cast<int>(s.split);
+        const int j = bid - a.n_whole;
+        s.part = j >= splits;
+        s.split = xcd_logical_id(s.part ? j - splits : j, splits);
+        id = a.n_whole + s.split;
         s.b0 = s.part ? a.cut : 0;
         s.n = s.part ? a.n_kblocks - a.cut : a.cut;
     } else {
-        const int sid = xcd_logical_id(blockIdx.x - a.n_whole, (total - a.n_whole) * a.parts);
-        s.split = sid / a.parts;
-        s.part = sid - static_cast<int>(s.split) * a.parts;
-        id = a.n_whole + static_cast<int>(s.split);
-        s.b0 = static_cast<int>(static_cast<int64_t>(a.n_kblocks) * s.part / a.parts);
-        s.n = static_cast<int>(static_cast<int64_t>(a.n_kblocks) * (s.part + 1) / a.parts) - s.b0;
+        const int j = XCDS ? xcd_logical_id(bid - a.n_whole, splits * a.parts) : bid - a.n_whole;
+        s.split = a.by_parts.of(j);
+        s.part = j - s.split * a.parts;
+        id = a.n_whole + s.split;
+        s.b0 = s.part * a.part_blocks + min(s.part, a.more_part_blocks);
+        s.n = a.part_blocks + (s.part < a.more_part_blocks);
     }
-    s.tile = id % a.n_tiles;
-    const int bh = id / a.n_tiles;
-    s.kvh = bh % a.Hk;
-    s.bat = bh / a.Hk;
+    const int bh = a.by_tiles.of(id);
+    s.tile = id - bh * a.n_tiles;
+    s.bat = a.by_heads.of(bh);
+    s.kvh = bh - s.bat * a.Hk;
     return s;
+}
+// Kernel arguments that the start of a kernel needs, read together: left to itself the
+// compiler reads them one after the other where they are first used, and waits each time.
+__device__ __forceinline__ void read_args(const Kv8AttnArgs& a) {
+    asm volatile("" ::"s"(a.q), "s"(a.k_codes), "s"(a.v_codes), "s"(a.k_scale), "s"(a.v_scale), "s"(a.B), "s"(a.H),
+                 "s"(a.Hk), "s"(a.group), "s"(a.n_q), "s"(a.rows), "s"(a.n_blocks), "s"(a.n_tiles), "s"(a.n_whole),
+                 "s"(a.parts), "s"(a.n_kblocks), "s"(a.range_begin[0]), "s"(a.range_keys[0]));
+    asm volatile("" ::"s"(a.part_blocks), "s"(a.more_part_blocks), "s"(a.by_parts.mul), "s"(a.by_parts.shift),
+                 "s"(a.by_tiles.mul), "s"(a.by_tiles.shift), "s"(a.by_heads.mul), "s"(a.by_heads.shift),
+                 "s"(a.by_group.mul), "s"(a.by_group.shift), "s"(a.scale_log2), "s"(a.n_ranges), "s"(a.cut));
 }
 // A split tile's partial rows: O not yet divided by the row sum, [rows][D], then each
 // row's maximum and sum.
 template <int D, int ROWS>
-__device__ __forceinline__ float* part_at(const Kv8AttnArgs& a, int64_t split, int part) {
-    return a.part + (split * a.parts + part) * (ROWS * (D + 2));
+__device__ __forceinline__ float* part_at(const Kv8AttnArgs& a, int split, int part) {
+    return a.part + (static_cast<int64_t>(split) * a.parts + part) * (ROWS * (D + 2));
 }
 
 // ----------------------------------------------------------------------------
@@ -276,12 +294,13 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_kv8_few_kernel(const Kv8AttnA
     __shared__ float rows_m[NW][kKv8FewRows], rows_l[NW][kKv8FewRows];
     const int lane = threadIdx.x & 63, hw = lane >> 5, l32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
-    const Share s = share_of(a);
+    read_args(a);
+    const Share s = share_of<false>(a);
     const int q0 = s.tile * kKv8FewRows, n_rows = min(kKv8FewRows, a.rows - q0);
+    u32x4_t raw[KK];
+    load_q<D>(a, row_at(a, s.bat, s.kvh, min(q0 + l32, a.rows - 1)), hw, raw);
     const int64_t head = (static_cast<int64_t>(s.bat) * a.Hk + s.kvh) * a.n_blocks;
 
-    f16x8_t qf[KK];
-    const float cq = load_q<D>(a, row_at(a, s.bat, s.kvh, min(q0 + l32, a.rows - 1)), l32 < n_rows, hw, qf);
 
     f32x16_t acc[DB];
 #pragma unroll
@@ -309,6 +328,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_kv8_few_kernel(const Kv8AttnA
         load_v(at.blk);
         vs = a.v_scale[head + at.blk];
     }
+    f16x8_t qf[KK];
+    const float cq = scale_q<D>(raw, a.scale_log2, qf);
     for (int j = wave; j < s.n; j += NW) {
         const int keys = at.keys;
         f32x16_t x[2] = {f32x16_t{}, f32x16_t{}};
@@ -435,10 +456,11 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
 
     const int tid = threadIdx.x, lane = tid & 63, hw = lane >> 5, l32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const Share s = share_of(a);
+    read_args(a);
+    const Share s = share_of<true>(a);
     const int n = s.n;
     int q0, q1;
-    split_rows(a.rows, a.n_tiles, s.tile, q0, q1);
+    split_rows(a, s.tile, q0, q1);
     const int64_t head = (static_cast<int64_t>(s.bat) * a.Hk + s.kvh) * a.n_blocks;
 
     // ---- codes: thread's pieces of a block, and where they go in a tile. NP = 2: piece
@@ -542,7 +564,9 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
     load_scales(0);
     const int qrow = q0 + wave * 32 + l32;
     f16x8_t qf[KK];
-    const float cq = kBiasedScale * load_q<D>(a, row_at(a, s.bat, s.kvh, min(qrow, a.rows - 1)), qrow < q1, hw, qf);
+    u32x4_t raw[KK];
+    load_q<D>(a, row_at(a, s.bat, s.kvh, min(qrow, a.rows - 1)), hw, raw);
+    const float cq = kBiasedScale * scale_q<D>(raw, a.scale_log2, qf);
     float qsum = 0.f;  // what the bias of the codes adds to every score of the row
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk)
@@ -742,7 +766,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
 // threads take every 8th part each, their sums are added up in order.
 constexpr int kMergeThreads = 256;
 template <int D, bool OF32, int ROWS, int PG>
-__global__ __launch_bounds__(kMergeThreads) void attn_kv8_merge_kernel(const Kv8AttnArgs a, int rows_per_tile) {
+__global__ __launch_bounds__(kMergeThreads) void attn_kv8_merge_kernel(const Kv8AttnArgs a) {
     constexpr int TPR = D / 4;                           // threads that hold a row
     constexpr int RPW = kMergeThreads / (TPR * PG);      // rows of a workgroup
     constexpr int U = 4;                                 // parts loaded together
@@ -751,18 +775,17 @@ __global__ __launch_bounds__(kMergeThreads) void attn_kv8_merge_kernel(const Kv8
     __shared__ float lsums[PG > 1 ? kMergeThreads : 1], tops[PG > 1 ? kMergeThreads : 1];
     const int tid = threadIdx.x;
     const int d = 4 * (tid % TPR), pg = tid / TPR % PG;
-    const int wgs = (rows_per_tile + RPW - 1) / RPW;
-    const int64_t split = blockIdx.x / wgs;
-    const int r = blockIdx.x % wgs * RPW + tid / (TPR * PG);  // row of the tile
-    const int id = a.n_whole + static_cast<int>(split);
-    const int tile = id % a.n_tiles, bh = id / a.n_tiles;
-    const int kvh = bh % a.Hk, bat = bh / a.Hk;
+    const int split = blockIdx.y;
+    const int r = blockIdx.x * RPW + tid / (TPR * PG);  // row of the tile
+    const int id = a.n_whole + split;
+    const int bh = a.by_tiles.of(id), tile = id - bh * a.n_tiles;
+    const int bat = a.by_heads.of(bh), kvh = bh - bat * a.Hk;
     int q0, q1;
     if constexpr (ROWS == kKv8FewRows) {
         q0 = tile * kKv8FewRows;
         q1 = min(q0 + kKv8FewRows, a.rows);
     } else {
-        split_rows(a.rows, a.n_tiles, tile, q0, q1);
+        split_rows(a, tile, q0, q1);
     }
     const bool ok = q0 + r < q1;
     const float* const p = part_at<D, ROWS>(a, split, 0);
@@ -838,24 +861,32 @@ hipError_t launch(const Kv8AttnArgs& a, hipStream_t s) {
     else hipLaunchKernelGGL((attn_kv8_tile_kernel<D, OF32>), dim3(grid), dim3(kTileThreads), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || split == 0) return e;
+    // (no more than one split tile a CU: the split is there for the CUs that a round leaves idle)
+    if (split > kCUs) return hipErrorInvalidValue;
     const int rows = min(a.rows, a.few ? kKv8FewRows : kTileRows);
-    auto wgs = [&](int rpw) { return dim3(static_cast<unsigned>(split * ((rows + rpw - 1) / rpw))); };
-    if (a.few) {
-        hipLaunchKernelGGL((attn_kv8_merge_kernel<D, OF32, kKv8FewRows, 8>), wgs(kMergeThreads / (D / 4 * 8)),
-                           dim3(kMergeThreads), 0, s, a, rows);
-    } else if (a.parts > 16) {
-        hipLaunchKernelGGL((attn_kv8_merge_kernel<D, OF32, kTileRows, 8>), wgs(kMergeThreads / (D / 4 * 8)),
-                           dim3(kMergeThreads), 0, s, a, rows);
-    } else {
-        hipLaunchKernelGGL((attn_kv8_merge_kernel<D, OF32, kTileRows, 1>), wgs(kMergeThreads / (D / 4)),
-                           dim3(kMergeThreads), 0, s, a, rows);
-    }
+    auto wgs = [&](int rpw) { return dim3((rows + rpw - 1) / rpw, static_cast<unsigned>(split)); };
+    constexpr int kOne = kMergeThreads / (D / 4), kEight = kOne / 8;  // rows of a workgroup
+    if (a.few)
+        hipLaunchKernelGGL((attn_kv8_merge_kernel<D, OF32, kKv8FewRows, 8>), wgs(kEight), dim3(kMergeThreads), 0, s, a);
+    else if (a.parts > 16)
+        hipLaunchKernelGGL((attn_kv8_merge_kernel<D, OF32, kTileRows, 8>), wgs(kEight), dim3(kMergeThreads), 0, s, a);
+    else
+        hipLaunchKernelGGL((attn_kv8_merge_kernel<D, OF32, kTileRows, 1>), wgs(kOne), dim3(kMergeThreads), 0, s, a);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_attn_kv8(const Kv8AttnArgs& a, int head_dim, hipStream_t s) {
+hipError_t launch_attn_kv8(Kv8AttnArgs a, int head_dim, hipStream_t s) {
+    a.by_group = FastDiv(static_cast<uint32_t>(a.group));
+    a.by_parts = FastDiv(static_cast<uint32_t>(a.parts));
+    a.by_tiles = FastDiv(static_cast<uint32_t>(a.n_tiles));
+    a.by_heads = FastDiv(static_cast<uint32_t>(a.Hk));
+    a.part_blocks = a.n_kblocks / a.parts;
+    a.more_part_blocks = a.n_kblocks % a.parts;
+    const int blocks = (a.rows + 31) / 32;
+    a.row_blocks = blocks / a.n_tiles;
+    a.more_row_blocks = blocks % a.n_tiles;
     if (head_dim == 128) return a.o_f32 ? launch<128, true>(a, s) : launch<128, false>(a, s);
     if (head_dim == 64) return a.o_f32 ? launch<64, true>(a, s) : launch<64, false>(a, s);
     return hipErrorInvalidValue;

@@ -306,9 +306,13 @@ struct Kv8AttnArgs {
     int32_t n_ranges;
     int32_t range_begin[kMaxRanges];  // in blocks
     int32_t range_keys[kMaxRanges];
+    // set by the launcher: divisions by group, parts, n_tiles and Hk; key blocks of a part (of the first
+    // more_part_blocks parts: one more), and 32-row blocks of a row tile of 256 likewise
+    FastDiv by_group, by_parts, by_tiles, by_heads;
+    int32_t part_blocks, more_part_blocks, row_blocks, more_row_blocks;
 };
 constexpr int kKv8FewRows = 32;  // rows of a tile where rows are few
 constexpr int kKv8MaxParts = 256;
-hipError_t launch_attn_kv8(const Kv8AttnArgs& a, int head_dim, hipStream_t s);
+hipError_t launch_attn_kv8(Kv8AttnArgs a, int head_dim, hipStream_t s);
 
 }  // namespace tmk
