@@ -36,7 +36,7 @@
 // Few rows: a workgroup's waves share the keys of one block of 32 rows out, each with
 // whole 64-key blocks, whose operands it loads straight from the cache; their results
 // are merged through LDS, those of several workgroups by a second kernel, in a fixed
-// order. Bound by the cache's bytes: one row, 65715 keys, 8 key heads, 4 streams (539
+// order. Bound by the cache's bytes: one row, 65745 keys, 8 key heads, 4 streams (539
 // MB) 93 us and 5 for the merge, 5.8 TB/s; 10920 keys, 40 heads (112 MB) 22 and 4; short
 // caches by one block's chain of loads and products (200 keys 5.6 us).
 
