@@ -864,23 +864,18 @@ template <int D, bool OF32>
 hipError_t launch(const Kv8AttnArgs& a, hipStream_t s) {
     const int64_t total = static_cast<int64_t>(a.n_tiles) * a.B * a.Hk, split = total - a.n_whole;
     const unsigned grid = static_cast<unsigned>(a.n_whole + split * a.parts);
-    if (a.few == 4) hipLaunchKernelGGL((attn_kv8_few_kernel<D, OF32, 4>), dim3(grid), dim3(256), 0, s, a);
-    else if (a.few == 8) hipLaunchKernelGGL((attn_kv8_few_kernel<D, OF32, 8>), dim3(grid), dim3(512), 0, s, a);
-    else hipLaunchKernelGGL((attn_kv8_tile_kernel<D, OF32>), dim3(grid), dim3(kTileThreads), 0, s, a);
-    hipError_t e = hipGetLastError();
+    const hipError_t e = a.few == 4   ? launch_with(attn_kv8_few_kernel<D, OF32, 4>, dim3(grid), 256, s, a)
+                         : a.few == 8 ? launch_with(attn_kv8_few_kernel<D, OF32, 8>, dim3(grid), 512, s, a)
+                                      : launch_with(attn_kv8_tile_kernel<D, OF32>, dim3(grid), kTileThreads, s, a);
     if (e != hipSuccess || split == 0) return e;
     // (no more than one split tile a CU: the split is there for the CUs that a round leaves idle)
     if (split > kCUs) return hipErrorInvalidValue;
     const int rows = min(a.rows, a.few ? kKv8FewRows : kTileRows);
     auto wgs = [&](int rpw) { return dim3((rows + rpw - 1) / rpw, static_cast<unsigned>(split)); };
     constexpr int kOne = kMergeThreads / (D / 4), kEight = kOne / 8;  // rows of a workgroup
-    if (a.few)
-        hipLaunchKernelGGL((attn_kv8_merge_kernel<D, OF32, kKv8FewRows, 8>), wgs(kEight), dim3(kMergeThreads), 0, s, a);
-    else if (a.parts > 16)
-        hipLaunchKernelGGL((attn_kv8_merge_kernel<D, OF32, kTileRows, 8>), wgs(kEight), dim3(kMergeThreads), 0, s, a);
-    else
-        hipLaunchKernelGGL((attn_kv8_merge_kernel<D, OF32, kTileRows, 1>), wgs(kOne), dim3(kMergeThreads), 0, s, a);
-    return hipGetLastError();
+    return a.few          ? launch_with(attn_kv8_merge_kernel<D, OF32, kKv8FewRows, 8>, wgs(kEight), kMergeThreads, s, a)
+           : a.parts > 16 ? launch_with(attn_kv8_merge_kernel<D, OF32, kTileRows, 8>, wgs(kEight), kMergeThreads, s, a)
+                          : launch_with(attn_kv8_merge_kernel<D, OF32, kTileRows, 1>, wgs(kOne), kMergeThreads, s, a);
 }
 
 }  // namespace

@@ -355,12 +355,9 @@ hipError_t launch_kv8_write(Kv8WriteArgs a, int head_dim, bool produce, bool hal
     const int64_t grid = kv + (q_threads + kKv8Threads - 1) / kKv8Threads;
     if (grid > INT32_MAX || q_threads > UINT32_MAX - kKv8Threads) return hipErrorInvalidValue;
     a.q_wgs = static_cast<uint32_t>(grid - kv);
-#define TM_KV8_WRITE(D_, P_, HV_)                                                                        \
-    if (head_dim == D_ && produce == P_ && halves == HV_) {                                              \
-        hipLaunchKernelGGL((kv8_write_kernel<D_, P_, HV_>), dim3(static_cast<unsigned>(grid)),           \
-                           dim3(kKv8Threads), 0, s, a);                                                  \
-        return hipGetLastError();                                                                        \
-    }
+#define TM_KV8_WRITE(D_, P_, HV_)                         \
+    if (head_dim == D_ && produce == P_ && halves == HV_) \
+        return launch_with(kv8_write_kernel<D_, P_, HV_>, dim3(static_cast<unsigned>(grid)), kKv8Threads, s, a);
     TM_KV8_WRITE(128, false, false)
     TM_KV8_WRITE(64, false, false)
     TM_KV8_WRITE(128, true, false)
@@ -375,12 +372,9 @@ hipError_t launch_kv8_read(Kv8ReadArgs a, int head_dim, bool of32, hipStream_t s
     a.n_blk = (a.n_tok + kCacheBlock - 1) / kCacheBlock;
     const int64_t grid = static_cast<int64_t>(a.n_blk) * a.B * a.Hk;
     if (grid > INT32_MAX) return hipErrorInvalidValue;
-#define TM_KV8_READ(D_, F_)                                                                      \
-    if (head_dim == D_ && of32 == F_) {                                                          \
-        hipLaunchKernelGGL((kv8_read_kernel<D_, F_>), dim3(static_cast<unsigned>(grid)),         \
-                           dim3(kKv8Threads), 0, s, a);                                          \
-        return hipGetLastError();                                                                \
-    }
+#define TM_KV8_READ(D_, F_)           \
+    if (head_dim == D_ && of32 == F_) \
+        return launch_with(kv8_read_kernel<D_, F_>, dim3(static_cast<unsigned>(grid)), kKv8Threads, s, a);
     TM_KV8_READ(128, false)
     TM_KV8_READ(64, false)
     TM_KV8_READ(128, true)

@@ -92,9 +92,8 @@ hipError_t launch_u(RopeArgs a, hipStream_t s) {
         a.tok0 = at;
         a.tok_end = at + most < a.n ? at + most : a.n;
         const int64_t blocks = ((a.tok_end - at) * per + kRopeThreads - 1) / kRopeThreads;
-        hipLaunchKernelGGL((rope_kernel<EB, D, HALVES, U>), dim3(static_cast<unsigned>(blocks), a.B),
-                           dim3(kRopeThreads), 0, s, a);
-        const hipError_t e = hipGetLastError();
+        const hipError_t e = launch_with(rope_kernel<EB, D, HALVES, U>, dim3(static_cast<unsigned>(blocks), a.B),
+                                         kRopeThreads, s, a);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

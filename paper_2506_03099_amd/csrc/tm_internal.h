@@ -193,6 +193,16 @@ hipError_t launch_attn_bwd_bf16(const BwdArgs& a, int head_dim, hipStream_t s);
 constexpr int64_t kBwdScratchFloats = int64_t(1) << 21;
 hipError_t bwd_scratch_address(float** out);
 
+// Launches a kernel whose one argument is `args` by one call of the runtime (the launch syntax makes
+// three, 0.15 us of a small call's 2.4).
+template <typename Args>
+hipError_t launch_with(void (*kernel)(Args), dim3 grid, unsigned threads, hipStream_t s, const Args& args) {
+    void* params[] = {const_cast<Args*>(&args)};
+    const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3(threads), params, 0, s);
+    if (e != hipSuccess) (void)hipGetLastError();
+    return e;
+}
+
 // Division of 0 <= n < 2^31 by d, 1 <= d < 2^31: n * mul >> shift with mul = floor(2^shift / d) + 1 and
 // shift = 31 + ceil(log2 d), exact since mul * d exceeds 2^shift by at most d <= 2^(shift - 31).
 struct FastDiv {
