@@ -18,15 +18,16 @@
 // 8: P reaches 2^8 and a tile may exceed that by 2^7 before m is raised; what
 // fp16 then loses at its lower end is below 2^-33 of the largest.
 //
-// Tile kernel: K's operands keep the bias of 128, as fp16 subnormals (the matrix
-// cores take them as they are): one instruction less for two codes, and x loses
-// 128 times the row's sum of q with its fma's addend. That costs the fp32 sums some
-// three bits at worst (255 for a code of some 33), far below P's rounding. As in
-// the bf16 forward (attn_fwd.hip), 8 waves of 32 query rows share every 64-key tile
-// in LDS, each wave's softmax in between its own MFMAs. The tiles come as codes into
-// registers, half the bytes, one tile ahead, and are turned into fp16 operands once
-// per workgroup on the way into LDS; the cache's order makes every LDS access a
-// contiguous KB (no bank conflicts). Bound by the MFMAs (60% of the cycles) and by
+// K's operands keep the bias of 128, as fp16 subnormals (the matrix cores take them as
+// they are): one instruction less for two codes, and x loses 128 times the row's sum of
+// q with its fma's addend. That costs the fp32 sums some three bits at worst (255 for a
+// code of some 33), far below P's rounding.
+//
+// Tile kernel: as in the bf16 forward (attn_fwd.hip), 8 waves of 32 query rows share
+// every 64-key tile in LDS, each wave's softmax in between its own MFMAs. The tiles come
+// as codes into registers, half the bytes, one tile ahead, and are turned into fp16
+// operands once per workgroup on the way into LDS; the cache's order makes every LDS
+// access a contiguous KB (no bank conflicts). Bound by the MFMAs (60% of the cycles) and by
 // what the waves wait for in between: 4680 queries over 10920 keys, 40 heads of 128,
 // 870-955 us on different nodes (1096-1203 TFLOP/s; an 8192^3 bf16 product 1118-1161
 // on them), 7-8% more than the bf16 forward over a 16-bit cache. Without the decoding,
@@ -37,8 +38,11 @@
 // whole 64-key blocks, whose operands it loads straight from the cache; their results
 // are merged through LDS, those of several workgroups by a second kernel, in a fixed
 // order. Bound by the cache's bytes: one row, 65745 keys, 8 key heads, 4 streams (539
-// MB) 93 us and 5 for the merge, 5.8 TB/s; 10920 keys, 40 heads (112 MB) 22 and 4; short
-// caches by one block's chain of loads and products (200 keys 5.6 us).
+// MB) 95 us a call, 4 of them for the merge (5.7 TB/s); 10920 keys, 40 heads (112 MB) 26.5.
+// Caches of some thousand keys are bound by a wave's chain of loads, decoding, products
+// and softmax: 324 vector instructions a block of D = 128. (564 before K's bias was kept, masks
+// moved behind a branch and a score took one fma, behind the maximum: 6517 keys, 18 rows,
+// 20 heads 16.3 us a call, now 15.5.)
 
 #include <float.h>
 #include <hip/hip_runtime.h>
@@ -82,6 +86,10 @@ __device__ __forceinline__ f16x2_t biased2(uint32_t w) {
     return __builtin_bit_cast(f16x2_t, pick_bytes(0u, w, HI ? 0x04030402u : 0x04010400u));
 }
 constexpr float kBiasedScale = 0x1p24f, kBiasedZero = 0x1p-17f;  // 1 over a code's step, and code 0
+__device__ __forceinline__ f16x8_t biased8(uint32_t a, uint32_t b) {
+    const f16x2_t p = biased2<false>(a), q = biased2<true>(a), r = biased2<false>(b), s = biased2<true>(b);
+    return f16x8_t{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
+}
 // 8 codes as an operand's 8 elements.
 __device__ __forceinline__ f16x8_t decode8(uint32_t a, uint32_t b) {
     const f16x2_t p = decode2<false>(a), q = decode2<true>(a), r = decode2<false>(b), s = decode2<true>(b);
@@ -164,6 +172,27 @@ __device__ __forceinline__ float scale_q(const u32x4_t (&raw)[D / 16], float sca
             qf[kk][2 * w + 1] = static_cast<_Float16>(__uint_as_float(raw[kk][w] & 0xFFFF0000u) * mult);
         }
     return e == 255 ? __uint_as_float(0x7FC00000u) : scale_log2 * __uint_as_float((254 - up) << 23);
+}
+
+// What the bias of K's codes adds to every score of the lane's row: the row's sum of q, two elements
+// an instruction and four sums apart (as one chain of additions it took 0.3 us of a small call).
+template <int KK>
+__device__ __forceinline__ float bias_of(const f16x8_t (&qf)[KK]) {
+    const f16x2_t ones{static_cast<_Float16>(1.f), static_cast<_Float16>(1.f)};
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+            sum[w] = __builtin_amdgcn_fdot2(f16x2_t{qf[kk][2 * w], qf[kk][2 * w + 1]}, ones, sum[w], false);
+    const float s = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    return (s + __shfl_xor(s, 32)) * kBiasedZero;
+}
+// The factor of a tile's scores. (Not zero, as a tiny row's may be: a masked score of -inf is still
+// to be scaled.)
+__device__ __forceinline__ float score_factor(float cq, float ks) {
+    const float c = cq * ks;
+    return c < FLT_MIN ? FLT_MIN : c;
 }
 
 // Waits for scalar loads, which share a counter with the LDS reads and come back in
@@ -337,33 +366,36 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_kv8_few_kernel(const Kv8AttnA
         vs = a.v_scale[head + at.blk];
     }
     f16x8_t qf[KK];
-    const float cq = scale_q<D>(raw, a.scale_log2, qf);
+    const float cq = kBiasedScale * scale_q<D>(raw, a.scale_log2, qf);
+    const float qsum = bias_of<KK>(qf);
     for (int j = wave; j < s.n; j += NW) {
         const int keys = at.keys;
         f32x16_t x[2] = {f32x16_t{}, f32x16_t{}};
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             const int kb = i / DB, st = i % DB;
-            x[kb] = mfma(decode8(kc[i][0], kc[i][1]), qf[2 * st], x[kb]);
-            x[kb] = mfma(decode8(kc[i][2], kc[i][3]), qf[2 * st + 1], x[kb]);
+            x[kb] = mfma(biased8(kc[i][0], kc[i][1]), qf[2 * st], x[kb]);
+            x[kb] = mfma(biased8(kc[i][2], kc[i][3]), qf[2 * st + 1], x[kb]);
         }
-        const float c = cq * ks, add = __builtin_amdgcn_logf(vs), iv = 1.f / vs;
+        const float c = score_factor(cq, ks), iv = __builtin_amdgcn_rcpf(vs);
+        const float add = fmaf(-qsum, c, __builtin_amdgcn_logf(vs));
         at.next(a, NW);  // (past the share's end: a block that exists)
         load_k(at.blk);
         ks = a.k_scale[head + at.blk];
         vs = a.v_scale[head + at.blk];
-        // x + m of the header's formula, and its maximum
-        float mx = kNegInf;
+        if (__builtin_expect(keys < kCacheBlock, 0)) {
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+            for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                x[kb][i] = fmaf(x[kb][i], c, add);
-                if (keys < kCacheBlock && 32 * kb + 16 * (i / 8) + 8 * hw + i % 8 >= keys) x[kb][i] = kNegInf;
-                mx = fmaxf(mx, x[kb][i]);
-            }
-        mx = both_max(mx) - kHeadroom;
-        if (__ballot(mx > m) != 0) {
+                for (int i = 0; i < 16; ++i)
+                    if (32 * kb + 16 * (i / 8) + 8 * hw + i % 8 >= keys) x[kb][i] = kNegInf;
+        }
+        // the maximum of x + m of the header's formula, from that of the sums (c is positive)
+        float mx = x[0][0];
+#pragma unroll
+        for (int e = 1; e < 32; ++e) mx = fmaxf(mx, x[e / 16][e % 16]);
+        mx = fmaf(both_max(mx), c, add) - kHeadroom;
+        if (__builtin_expect(__ballot(mx > m) != 0, 0)) {
             const float nm = fmaxf(m, mx);
             const float alpha = __builtin_amdgcn_exp2f(m == kNegInf ? kNegInf : m - nm);
             m = nm;
@@ -372,12 +404,12 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_kv8_few_kernel(const Kv8AttnA
             for (int d = 0; d < DB; ++d) acc[d] *= alpha;
         }
         // (a row with only scores of -inf so far: P = 0)
-        const float base = m == kNegInf ? 0.f : m;
+        const float less = add - (m == kNegInf ? 0.f : m);
         float lt = 0.f;
         f16x8_t pf[4];
 #pragma unroll
         for (int e = 0; e < 32; ++e) {
-            const float p = __builtin_amdgcn_exp2f(x[e / 16][e % 16] - base);
+            const float p = __builtin_amdgcn_exp2f(fmaf(x[e / 16][e % 16], c, less));
             lt += p;
             pf[e / 8][e % 8] = static_cast<_Float16>(p);
         }
@@ -575,12 +607,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
     u32x4_t raw[KK];
     load_q<D>(a, row_at(a, s.bat, s.kvh, min(qrow, a.rows - 1)), hw, raw);
     const float cq = kBiasedScale * scale_q<D>(raw, a.scale_log2, qf);
-    float qsum = 0.f;  // what the bias of the codes adds to every score of the row
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) qsum += static_cast<float>(qf[kk][e]);
-    qsum = (qsum + __shfl_xor(qsum, 32)) * kBiasedZero;
+    const float qsum = bias_of<KK>(qf);
 #pragma unroll
     for (int u = 0; u < 3; ++u)
 #pragma unroll
@@ -667,9 +694,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
         }
         // (as one fma the compiler kept two copies of O: 200 registers spilled)
         l += pin(pin(lt0 + lt1) * iv);
-        float c = cq * ks;
-        // (not zero, as a tiny row's factor may be: a masked score of -inf is still to be scaled)
-        c = c < FLT_MIN ? FLT_MIN : c;
+        const float c = score_factor(cq, ks);
         const float add = fmaf(-qsum, c, __builtin_amdgcn_logf(vs) - m);
         iv = uniform_f(__builtin_amdgcn_rcpf(vs));
         if (__builtin_expect(cnt[(u + 1) & 3] < kCacheBlock, 0)) mask_tile(nx, cnt[(u + 1) & 3]);
