@@ -1302,14 +1302,26 @@ tm_status plan_attn8(const tm_kv8_cache* cache, const Kv8Geo& z, int32_t q_chunk
     a->rows = int32_t(rows);
     // Tiles of 32 rows whose waves share the keys out, where rows are few, or all of the call's work
     // (32 rows by 64 keys) is little: such a tile's waves turn codes into operands for themselves, and
-    // take 1.7 times as long for the work of full tiles of 256 rows, but those start later, and idle
-    // where they are not full. Measured, us, 256 and 32 rows a tile, D = 128: 1 head, 100000 keys,
-    // 64 rows 27 and 25, 192 rows 34 and 37; 40 heads, 1000 keys, 384 rows 31 and 19; 40 heads, 10000
-    // keys, 64 rows 38 and 37, 96 rows 40 and 43. D = 64: 8 heads, 100000 keys, 64 rows 49 and 41, 96
-    // rows 52 and 49, 128 rows 54 and 60.
+    // take longer for the work of full tiles of 256 rows, but those start later, and idle where they
+    // are not full. More than two such tiles per CU are compared by both sides' times: a round of full
+    // tiles takes kEnds us and kBlock a key block, a tile of 32 rows (all CUs busy) kFixed and kWork.
+    // Over long caches full tiles gain earlier, as their keys are split as well. Measured, us, 256 and
+    // 32 rows a tile, D = 128: 1 head, 100000 keys, 64 rows 24.5 and 18.0, 384 rows 36.7 and 39.4; 40
+    // heads, 10000 keys, 64 rows 34.8 and 40.6; 40 heads, 1000 keys, 384 rows 27.9 and 20.7, 1216 rows
+    // 33.7 and 47.2; 40 heads, 1 key, 384 rows 11.3 and 8.6, 1632 rows 22.6 and 28.5. D = 64: 8 heads,
+    // 20000 keys, 64 rows 19.3 and 13.4, 384 rows 37.6 and 42.3; 40 heads, 1000 keys, 800 rows 25.1 and
+    // 20.3, 1216 rows 26.0 and 27.8; 8 heads, 1 key, 7412 rows 9.3 and 14.3.
+    const bool narrow = z.g.D == 64;
+    const double kEnds = narrow ? 8 : 9, kBlock = narrow ? 1.05 : 1.4;
+    const double kFixed = narrow ? 0.0045 : 0.0105, kWork = narrow ? 0.00066 : 0.0011;
+    const double n = double(a->n_kblocks);
     const int64_t tiles32 = ceil_div(rows, tmk::kKv8FewRows) * BH;
-    const bool few = rows <= (z.g.D == 64 ? 64 : 32) ||
-                     tiles32 * a->n_kblocks <= (z.g.D == 64 ? 22000 : 8000);
+    const int64_t rounds = ceil_div(ceil_div(rows, tmk::kTileRowsBf16) * BH, tmk::kCUs);
+    const int64_t little = narrow ? (a->n_kblocks > 80 ? 22000 : 50000) : (a->n_kblocks > 40 ? 8000 : 24000);
+    const bool few = rows <= (narrow ? 64 : 32) ||
+                     (tiles32 * a->n_kblocks <= little &&
+                      (tiles32 <= 2 * tmk::kCUs ||
+                       5 + double(tiles32) * (kFixed + kWork * n) < double(rounds) * (kEnds + kBlock * n)));
     const int64_t n_tiles = ceil_div(rows, few ? tmk::kKv8FewRows : tmk::kTileRowsBf16);
     const int64_t tiles = n_tiles * BH;
     if (tiles > INT32_MAX / 64) return fail(TM_E_SHAPE, "grid too large");
@@ -1343,10 +1355,8 @@ tm_status plan_attn8(const tm_kv8_cache* cache, const Kv8Geo& z, int32_t q_chunk
         return TM_OK;
     }
     // More than half a round: each tile is cut in two, a first part for a CU of its own, and the
-    // second parts in turn, k each, for the CUs that are left over. Microseconds: a workgroup takes
-    // kEnds besides its key blocks, a block kBlock.
-    const double kEnds = 9, kBlock = 1.4 * double(z.g.D) / 128;
-    const double n = double(a->n_kblocks), k = double(ceil_div(rest, tmk::kCUs - rest));
+    // second parts in turn, k each, for the CUs that are left over.
+    const double k = double(ceil_div(rest, tmk::kCUs - rest));
     const int64_t cut = int64_t(std::ceil((k * (n * kBlock + kEnds) - kEnds) / ((k + 1) * kBlock)));
     if (a->n_kblocks - cut < 4) return TM_OK;
     const double merge = 6 + 2 * 2 * double(rest) * (double(rows) / double(n_tiles)) * double(z.g.D + 2) * 4 / 4e6;
