@@ -1329,12 +1329,12 @@ tm_status plan_attn8(const tm_kv8_cache* cache, const Kv8Geo& z, int32_t q_chunk
     a->n_whole = int32_t(tiles);
     a->parts = 1;
     if (few) {
-        // One workgroup of 4 waves on every CU, each wave with two key blocks at least (two on every CU
-        // take longer: one row a head, 4 x 8 key heads with 65536 keys 97.6 and 103.9 us, 2 x 8 with
-        // 20000 21.7 and 23.9, 40 with 10920 27.9 and 28.5). A wave takes about 0.9 us a block, and the
-        // merge 5, so a share has to save that; short caches have 8 waves a workgroup instead.
-        const int64_t parts = std::min<int64_t>({tmk::kCUs / std::max<int64_t>(tiles, 1),
-                                                 a->n_kblocks / 8, tmk::kKv8MaxParts});
+        // One workgroup of 4 waves on every CU, each wave with a key block at least (two blocks at least
+        // take 2-8% longer below 6000 keys; two workgroups on every CU as well, us: one row a head, 20 key
+        // heads with 6690 keys 14.1 and 16.1, 40 with 10920 24.6 and 25.9; and more than 192 parts, whose
+        // merge grows: 1 with 100000 17.2 and 18.1). A wave takes about 0.9 us a block, and the merge 5, so
+        // a share has to save that; short caches have 8 waves a workgroup instead.
+        const int64_t parts = std::min<int64_t>({tmk::kCUs / std::max<int64_t>(tiles, 1), a->n_kblocks / 4, 192});
         a->few = 4;
         if (parts >= 2 && a->n_kblocks - ceil_div(a->n_kblocks, parts) >= 24) {
             a->n_whole = 0;
