@@ -67,6 +67,7 @@ constexpr int kTileThreads = 512;
 constexpr int kTileWaves = kTileThreads / 64;
 constexpr int kTileRows = 32 * kTileWaves;
 constexpr float kHeadroom = 8.f;      // log2 of the largest P after m is set
+constexpr float kLargeScore = 0x1p10f;  // of m: a sum of its size is off by 2^-14 at most
 constexpr float kRaise = 0x1p15f;     // a lane's sum of P over half a tile that raises m
 static_assert(kTileRows == kTileRowsBf16, "the host counts tiles of this many rows");
 
@@ -129,6 +130,13 @@ __device__ __forceinline__ float both_max(float x) {
     return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
 }
 
+// A row's maximum less the headroom. Where floats lie 16 apart that would round to 16 less, and 2^16 is
+// past fp16: the maximum itself then (a difference of 0, 8 or 16 is exact).
+__device__ __forceinline__ float below(float top) {
+    const float m = top - kHeadroom;
+    return top - m > kHeadroom ? top : m;
+}
+
 // Row r (of the n_q * group of a key head) of q and o: its offset in rows of D.
 __device__ __forceinline__ int64_t row_at(const Kv8AttnArgs& a, int bat, int kvh, int r) {
     const int i = a.by_group.of(r), g = r - i * a.group;
@@ -188,10 +196,11 @@ __device__ __forceinline__ float bias_of(const f16x8_t (&qf)[KK]) {
     const float s = (sum[0] + sum[1]) + (sum[2] + sum[3]);
     return (s + __shfl_xor(s, 32)) * kBiasedZero;
 }
-// The factor of a tile's scores. (Not zero, as a tiny row's may be: a masked score of -inf is still
-// to be scaled.)
+// The factor of a tile's scores from that of the row's q and the scale of K. (The codes' step comes
+// last: q of a row beyond 2^121 has no room for it. Not zero, as a tiny row's may be: a masked score
+// of -inf is still to be scaled.)
 __device__ __forceinline__ float score_factor(float cq, float ks) {
-    const float c = cq * ks;
+    const float c = cq * ks * kBiasedScale;
     return c < FLT_MIN ? FLT_MIN : c;
 }
 
@@ -366,7 +375,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_kv8_few_kernel(const Kv8AttnA
         vs = a.v_scale[head + at.blk];
     }
     f16x8_t qf[KK];
-    const float cq = kBiasedScale * scale_q<D>(raw, a.scale_log2, qf);
+    const float cq = scale_q<D>(raw, a.scale_log2, qf);
     const float qsum = bias_of<KK>(qf);
     for (int j = wave; j < s.n; j += NW) {
         const int keys = at.keys;
@@ -377,7 +386,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_kv8_few_kernel(const Kv8AttnA
             x[kb] = mfma(biased8(kc[i][0], kc[i][1]), qf[2 * st], x[kb]);
             x[kb] = mfma(biased8(kc[i][2], kc[i][3]), qf[2 * st + 1], x[kb]);
         }
-        const float c = score_factor(cq, ks), iv = __builtin_amdgcn_rcpf(vs);
+        float c = score_factor(cq, ks);
+        const float iv = __builtin_amdgcn_rcpf(vs);
         const float add = fmaf(-qsum, c, __builtin_amdgcn_logf(vs));
         at.next(a, NW);  // (past the share's end: a block that exists)
         load_k(at.blk);
@@ -394,7 +404,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_kv8_few_kernel(const Kv8AttnA
         float mx = x[0][0];
 #pragma unroll
         for (int e = 1; e < 32; ++e) mx = fmaxf(mx, x[e / 16][e % 16]);
-        mx = fmaf(both_max(mx), c, add) - kHeadroom;
+        mx = below(fmaf(both_max(mx), c, add));
         if (__builtin_expect(__ballot(mx > m) != 0, 0)) {
             const float nm = fmaxf(m, mx);
             const float alpha = __builtin_amdgcn_exp2f(m == kNegInf ? kNegInf : m - nm);
@@ -404,7 +414,16 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_kv8_few_kernel(const Kv8AttnA
             for (int d = 0; d < DB; ++d) acc[d] *= alpha;
         }
         // (a row with only scores of -inf so far: P = 0)
-        const float less = add - (m == kNegInf ? 0.f : m);
+        const float base = m == kNegInf ? 0.f : m;
+        float less = add - base;
+        // `less` is rounded at the size of m. Scores so large that it shows take their steps one by one,
+        // which leaves the difference from the maximum exact.
+        if (__builtin_expect(__ballot(fabsf(base) > kLargeScore) != 0, 0)) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) x[e / 16][e % 16] = fmaf(x[e / 16][e % 16], c, add) - base;
+            c = 1.f;
+            less = 0.f;
+        }
         float lt = 0.f;
         f16x8_t pf[4];
 #pragma unroll
@@ -606,7 +625,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
     f16x8_t qf[KK];
     u32x4_t raw[KK];
     load_q<D>(a, row_at(a, s.bat, s.kvh, min(qrow, a.rows - 1)), hw, raw);
-    const float cq = kBiasedScale * scale_q<D>(raw, a.scale_log2, qf);
+    const float cq = scale_q<D>(raw, a.scale_log2, qf);
     const float qsum = bias_of<KK>(qf);
 #pragma unroll
     for (int u = 0; u < 3; ++u)
@@ -621,7 +640,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
         xa[0] = xa[1] = f32x16_t{};
 #pragma unroll
         for (int f = 0; f < NK; ++f) xa[f & 1] = mfma(read_frag(f, 0, 0), qf[f >> 1], xa[f & 1]);
-        const float c = cq * ks, add = fmaf(-qsum, c, __builtin_amdgcn_logf(vs));
+        const float c = score_factor(cq, ks), add = fmaf(-qsum, c, __builtin_amdgcn_logf(vs));
         iv = uniform_f(1.f / vs);
         load_scales(1);
 #pragma unroll
@@ -630,7 +649,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
             for (int i = 0; i < 16; ++i) xa[kb][i] = fmaf(xa[kb][i], c, add);
         if (cnt[0] < kCacheBlock) mask_tile(xa, cnt[0]);
         const float mx = row_max(xa);
-        m = mx == kNegInf ? 0.f : mx - kHeadroom;
+        m = mx == kNegInf ? 0.f : below(mx);
         fresh = __ballot(mx == kNegInf);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
@@ -677,8 +696,8 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
             raise |= raise << 32 | raise >> 32;  // both lanes of a row; other rows keep their bits
             const float mx = row_max(x);
             const bool first = __builtin_amdgcn_inverse_ballot_w64(fresh) && mx != kNegInf;
-            const float up = __builtin_amdgcn_inverse_ballot_w64(raise) ? fmaxf(mx - kHeadroom, 0.f) : 0.f;
-            const float dm = first ? mx - kHeadroom : up;
+            const float up = __builtin_amdgcn_inverse_ballot_w64(raise) ? fmaxf(below(mx), 0.f) : 0.f;
+            const float dm = first ? below(mx) : up;
             const float alpha = first ? 1.f : __builtin_amdgcn_exp2f(-dm);  // (sum and O are still 0)
             fresh &= __ballot(mx == kNegInf);
             m += dm;

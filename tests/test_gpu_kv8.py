@@ -353,6 +353,26 @@ def test_queries_of_any_size(tm, n_q, H, size):
     check_attention(tm, cache, 0, q, f"q * {size}")
 
 
+@pytest.mark.parametrize("n_q,H", [(3, 1), (300, 1), (300, 250)])
+@pytest.mark.parametrize("size", [1e2, 1e5, 1e8, 1e20, 1e36])
+@pytest.mark.parametrize("at", [5, 170, 299])
+def test_scores_of_any_size(tm, n_q, H, size, at):
+    """One key's score is above the others' by 9 times `size` and more: its value is the output. (Its
+    P is a power of two and the others' are 0, so the quotient by the row sum is off by a few 2^-24.)"""
+    D, n = 128, 300
+    g = torch.Generator().manual_seed(17)
+    cache = make(tm, 1, H, H, D, n, 1, 0)
+    assert in_tiles(1, H, n_q, [n], D) == (H > 1)
+    k = torch.randn((1, n, H, D), generator=g).clamp(-2, 2)
+    k[:, at] = 4.0
+    tm.tm_kv8_append(cache, 0, bf16(k).cuda(), bf16(torch.randn((1, n, H, D), generator=g)).cuda())
+    # (rows of one sign)
+    q = bf16(torch.randn((1, n_q, H, D), generator=g).abs().clamp(0.1, 4) * size).cuda()
+    o = tm.tm_kv8_attn_fwd(cache, q, 0, o_f32=True)
+    want = tm.tm_kv8_read(cache, 0, torch.float32)[1][:, at:at + 1]
+    assert bool(((o - want).abs() <= 2.0 ** -20 * want.abs()).all())
+
+
 @pytest.mark.parametrize("n_q,H", [(2, 1), (100, 40)])
 def test_one_key_that_outweighs_a_long_cache(tm, n_q, H):
     """10000 keys at 2^-24 of the largest weight still count for their share: the fp16 weights
