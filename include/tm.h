@@ -414,8 +414,9 @@ tm_status tm_kv8_append(tm_kv8_cache* cache, int32_t chunk, const void* k, const
  * q_gain [heads, D] and k_gain [kv_heads, D] or NULL, as there), rotated (rope
  * NULL: not; table and first_token as in tm_rope3d_fwd, the descriptor's
  * head_dim and dtype those of the cache), and the queries rounded once, to bf16,
- * into q_out: device bf16 [B, n_tok, heads, D] (it may be q). The keys are
- * quantised from their fp32 values, and the values v as tm_kv8_append does. */
+ * into q_out: device bf16 [B, n_tok, heads, D] (it may be q; neither it nor the
+ * pool may overlap anything else). The keys are quantised from their fp32 values,
+ * and the values v as tm_kv8_append does. */
 tm_status tm_qkv8_produce(tm_kv8_cache* cache, int32_t chunk, const void* q, const void* k,
                           const void* v, const float* q_gain, const float* k_gain, float eps,
                           const tm_rope_desc* rope, const float* table, int64_t first_token,

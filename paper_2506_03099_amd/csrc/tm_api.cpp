@@ -1241,13 +1241,19 @@ tm_status write_chunk8(tm_kv8_cache* cache, int32_t chunk, const void* q, const 
         const size_t gain = size_t(g.D) * sizeof(float);
         if (q_gain != nullptr && (st = check(q_gain, size_t(g.H) * gain, "q_gain")) != TM_OK) return st;
         if (k_gain != nullptr && (st = check(k_gain, size_t(z.Hk) * gain, "k_gain")) != TM_OK) return st;
+        const struct { const float* p; size_t n; } gains[2] = {{q_gain, size_t(g.H) * gain}, {k_gain, size_t(z.Hk) * gain}};
+        for (const auto& w : gains)
+            if (w.p != nullptr && (overlaps(q_out, q_bytes, w.p, w.n) || overlaps(cache->pool, z.bytes(), w.p, w.n)))
+                return fail(TM_E_ARG, "q_out or the cache's pool overlaps a gain");
         if (rope_desc != nullptr) {
             RopeGeo rg;
             if ((st = check_rope_desc(rope_desc, &rg)) != TM_OK) return st;
             if (rope_desc->head_dim != g.D || rope_desc->dtype != TM_BF16)
                 return fail(TM_E_ARG, "the rope descriptor's head_dim or dtype is not the cache's");
             if ((st = rope_table(rope_desc, rg, table, first_token, n_tok, check, &a.table)) != TM_OK) return st;
-            if (overlaps(q_out, q_bytes, table, rg.table_bytes)) return fail(TM_E_ARG, "q_out overlaps the table");
+            if (rg.table_bytes > 0 && (overlaps(q_out, q_bytes, table, rg.table_bytes) ||
+                                       overlaps(cache->pool, z.bytes(), table, rg.table_bytes)))
+                return fail(TM_E_ARG, "q_out or the cache's pool overlaps the table");
             a.turn = 1;
             a.first_token = first_token;
         }

@@ -553,3 +553,25 @@ def test_refusals(tm):
     refused(tm.TM_E_ARG, lambda: tm.tm_qkv8_produce(cache, 0, q, k, k, rope=rope))
     assert cache.latest() == 0 and cache.locate(0) == (0, 10)
     assert tm.tm_kv8_attn_fwd(cache, q[:, :0], 0).shape == (1, 0, 4, D)
+
+
+def test_the_producer_refuses_outputs_over_its_inputs(tm):
+    D, n = 64, 32
+    cache = make(tm, 1, 2, 2, D, n, n, 1)
+    q = torch.zeros((1, n, 2, D), dtype=torch.bfloat16, device="cuda")
+    gain = torch.ones((2, D), device="cuda")
+    rope = tm.make_rope_desc(D, 1, 4, 8)
+    table = tm.tm_rope3d_table(rope)
+    out = torch.empty((1, n, 2, D), dtype=torch.bfloat16, device="cuda")
+    in_out = out.view(-1)[:4 * D].view(torch.float32).view(2, D)
+    in_pool = cache.pool[:8 * D].view(torch.float32).view(2, D)
+    size = table.numel() * 4
+    for more in ({"q_gain": in_out}, {"k_gain": in_out}, {"q_gain": in_pool}, {"k_gain": in_pool},
+                 {"rope": rope, "table": cache.pool[:size].view(torch.float32).view(-1, 2)},
+                 {"rope": rope, "table": out.view(-1)[:size // 2].view(torch.float32).view(-1, 2)}):
+        with pytest.raises(tm.TMError) as e:
+            tm.tm_qkv8_produce(cache, 0, q, q.clone(), q.clone(), q_out=out, **more)
+        assert e.value.status == tm.TM_E_ARG, more
+    assert cache.latest() == -1
+    tm.tm_qkv8_produce(cache, 0, q, q.clone(), q.clone(), gain, gain, 1e-6, rope, table, q_out=out)
+    assert cache.latest() == 0
