@@ -1338,11 +1338,12 @@ tm_status plan_attn8(const tm_kv8_cache* cache, const Kv8Geo& z, int32_t q_chunk
         // One workgroup of 4 waves on every CU, each wave with a key block at least (two blocks at least
         // take 2-8% longer below 6000 keys; two workgroups on every CU as well, us: one row a head, 20 key
         // heads with 6690 keys 14.1 and 16.1, 40 with 10920 24.6 and 25.9; and more than 192 parts, whose
-        // merge grows: 1 with 100000 17.2 and 18.1). A wave takes about 0.9 us a block, and the merge 5, so
-        // a share has to save that; short caches have 8 waves a workgroup instead.
+        // merge grows: 1 with 100000 17.2 and 18.1). The merge and the second launch take 5 us, so a share has
+        // to save that; short caches have 8 waves a workgroup instead. (Whole and split, D = 128, 1500 keys,
+        // 20 rows 12.6 and 11.2; D = 64, 2000 keys, one row 9.2 and 10.7, 3000 keys 11.9 and 11.3.)
         const int64_t parts = std::min<int64_t>({tmk::kCUs / std::max<int64_t>(tiles, 1), a->n_kblocks / 4, 192});
         a->few = 4;
-        if (parts >= 2 && a->n_kblocks - ceil_div(a->n_kblocks, parts) >= 24) {
+        if (parts >= 2 && a->n_kblocks - ceil_div(a->n_kblocks, parts) >= (narrow ? 36 : 20)) {
             a->n_whole = 0;
             a->parts = int32_t(parts);
         } else if (a->n_kblocks > 4 && tiles <= tmk::kCUs) {
