@@ -18,10 +18,10 @@
 // 8: P reaches 2^8 and a tile may exceed that by 2^7 before m is raised; what
 // fp16 then loses at its lower end is below 2^-33 of the largest.
 //
-// K's operands keep the bias of 128, as fp16 subnormals (the matrix cores take them as
-// they are): one instruction less for two codes, and x loses 128 times the row's sum of
-// q with its fma's addend. That costs the fp32 sums some three bits at worst (255 for a
-// code of some 33), far below P's rounding.
+// Both operands lose the bias of 128 before the products. (With K's codes as they are held
+// and 128 times the row's sum of q taken off the score afterwards, a packed addition less for
+// two codes, scores lose the digits by which 128 sum |q| exceeds sum |q code|: nearly all of
+// P's where one channel of K sets the scale and the others' codes are small.)
 //
 // Tile kernel: as in the bf16 forward (attn_fwd.hip), 8 waves of 32 query rows share
 // every 64-key tile in LDS, each wave's softmax in between its own MFMAs. The tiles come
@@ -80,16 +80,6 @@ template <bool HI>
 __device__ __forceinline__ f16x2_t decode2(uint32_t w) {
     const f16x2_t x = __builtin_bit_cast(f16x2_t, pick_bytes(0x64646464u, w, HI ? 0x04030402u : 0x04010400u));
     return x - f16x2_t{static_cast<_Float16>(1152.f), static_cast<_Float16>(1152.f)};
-}
-// The same as (code + 128) 2^-24: the byte alone is that subnormal fp16 number.
-template <bool HI>
-__device__ __forceinline__ f16x2_t biased2(uint32_t w) {
-    return __builtin_bit_cast(f16x2_t, pick_bytes(0u, w, HI ? 0x04030402u : 0x04010400u));
-}
-constexpr float kBiasedScale = 0x1p24f, kBiasedZero = 0x1p-17f;  // 1 over a code's step, and code 0
-__device__ __forceinline__ f16x8_t biased8(uint32_t a, uint32_t b) {
-    const f16x2_t p = biased2<false>(a), q = biased2<true>(a), r = biased2<false>(b), s = biased2<true>(b);
-    return f16x8_t{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
 }
 // 8 codes as an operand's 8 elements.
 __device__ __forceinline__ f16x8_t decode8(uint32_t a, uint32_t b) {
@@ -182,25 +172,10 @@ __device__ __forceinline__ float scale_q(const u32x4_t (&raw)[D / 16], float sca
     return e == 255 ? __uint_as_float(0x7FC00000u) : scale_log2 * __uint_as_float((254 - up) << 23);
 }
 
-// What the bias of K's codes adds to every score of the lane's row: the row's sum of q, two elements
-// an instruction and four sums apart (as one chain of additions it took 0.3 us of a small call).
-template <int KK>
-__device__ __forceinline__ float bias_of(const f16x8_t (&qf)[KK]) {
-    const f16x2_t ones{static_cast<_Float16>(1.f), static_cast<_Float16>(1.f)};
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk)
-#pragma unroll
-        for (int w = 0; w < 4; ++w)
-            sum[w] = __builtin_amdgcn_fdot2(f16x2_t{qf[kk][2 * w], qf[kk][2 * w + 1]}, ones, sum[w], false);
-    const float s = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-    return (s + __shfl_xor(s, 32)) * kBiasedZero;
-}
-// The factor of a tile's scores from that of the row's q and the scale of K. (The codes' step comes
-// last: q of a row beyond 2^121 has no room for it. Not zero, as a tiny row's may be: a masked score
-// of -inf is still to be scaled.)
+// The factor of a tile's scores from that of the row's q and the scale of K. (Not zero, as a tiny
+// row's may be: a masked score of -inf is still to be scaled.)
 __device__ __forceinline__ float score_factor(float cq, float ks) {
-    const float c = cq * ks * kBiasedScale;
+    const float c = cq * ks;
     return c < FLT_MIN ? FLT_MIN : c;
 }
 
@@ -376,19 +351,18 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_kv8_few_kernel(const Kv8AttnA
     }
     f16x8_t qf[KK];
     const float cq = scale_q<D>(raw, a.scale_log2, qf);
-    const float qsum = bias_of<KK>(qf);
     for (int j = wave; j < s.n; j += NW) {
         const int keys = at.keys;
         f32x16_t x[2] = {f32x16_t{}, f32x16_t{}};
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             const int kb = i / DB, st = i % DB;
-            x[kb] = mfma(biased8(kc[i][0], kc[i][1]), qf[2 * st], x[kb]);
-            x[kb] = mfma(biased8(kc[i][2], kc[i][3]), qf[2 * st + 1], x[kb]);
+            x[kb] = mfma(decode8(kc[i][0], kc[i][1]), qf[2 * st], x[kb]);
+            x[kb] = mfma(decode8(kc[i][2], kc[i][3]), qf[2 * st + 1], x[kb]);
         }
         float c = score_factor(cq, ks);
         const float iv = __builtin_amdgcn_rcpf(vs);
-        const float add = fmaf(-qsum, c, __builtin_amdgcn_logf(vs));
+        const float add = __builtin_amdgcn_logf(vs);
         at.next(a, NW);  // (past the share's end: a block that exists)
         load_k(at.blk);
         ks = a.k_scale[head + at.blk];
@@ -563,9 +537,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
     auto put = [&](const u32x4_t (&from)[NP], int i, int u) __attribute__((always_inline)) {
         const int p = i / 8, h = i / 4 % 2;
         const uint32_t w = from[p][2 * h + i / 2 % 2];
-        const bool is_k = NP == 2 ? p == 0 : !v_first;
-        if (is_k) half[i % 4] = i % 2 ? biased2<true>(w) : biased2<false>(w);
-        else half[i % 4] = i % 2 ? decode2<true>(w) : decode2<false>(w);
+        half[i % 4] = i % 2 ? decode2<true>(w) : decode2<false>(w);
         if (i % 4 != 3) return;
         const uint32_t base = NP == 2 ? p * NBUF * TILEB : v_first ? NBUF * TILEB : 0;
         *(lds_f16x8_t*)(L + lds_to + base + ((u & (NBUF - 1)) * TILEB + h * 1024)) =
@@ -626,7 +598,6 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
     u32x4_t raw[KK];
     load_q<D>(a, row_at(a, s.bat, s.kvh, min(qrow, a.rows - 1)), hw, raw);
     const float cq = scale_q<D>(raw, a.scale_log2, qf);
-    const float qsum = bias_of<KK>(qf);
 #pragma unroll
     for (int u = 0; u < 3; ++u)
 #pragma unroll
@@ -640,7 +611,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
         xa[0] = xa[1] = f32x16_t{};
 #pragma unroll
         for (int f = 0; f < NK; ++f) xa[f & 1] = mfma(read_frag(f, 0, 0), qf[f >> 1], xa[f & 1]);
-        const float c = score_factor(cq, ks), add = fmaf(-qsum, c, __builtin_amdgcn_logf(vs));
+        const float c = score_factor(cq, ks), add = __builtin_amdgcn_logf(vs);
         iv = uniform_f(1.f / vs);
         load_scales(1);
 #pragma unroll
@@ -714,7 +685,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
         // (as one fma the compiler kept two copies of O: 200 registers spilled)
         l += pin(pin(lt0 + lt1) * iv);
         const float c = score_factor(cq, ks);
-        const float add = fmaf(-qsum, c, __builtin_amdgcn_logf(vs) - m);
+        const float add = __builtin_amdgcn_logf(vs) - m;
         iv = uniform_f(__builtin_amdgcn_rcpf(vs));
         if (__builtin_expect(cnt[(u + 1) & 3] < kCacheBlock, 0)) mask_tile(nx, cnt[(u + 1) & 3]);
         __builtin_amdgcn_sched_barrier(0);

@@ -1,0 +1,60 @@
+"""Attention over the 8-bit cache where sizes differ widely: K with a channel far
+above the others, rows of q with a common part.
+
+The bounds are those of test_gpu_kv8.py's header. Scores are below 30 and the sums
+behind them are either of products whose sizes add up to less than 30 as well, or
+exact (said where).
+"""
+import pytest
+import torch
+
+from test_gpu_kv8 import BLOCK, bf16, check_attention, in_tiles, make, queries, tm  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+# query rows, heads, blocks of keys, whether in tiles of 256 rows
+FORMS = [
+    (1, 1, 8, False),        # one workgroup
+    (3, 2, 48, False),       # keys split over workgroups
+    (257, 1, 8, False),
+    (512, 120, 8, True),     # whole tiles
+    (1300, 9, 100, True),    # split ones
+    (1000, 47, 57, True),    # each cut in two
+]
+
+
+def put(tm, D, H, k, v):  # noqa: F811
+    cache = make(tm, 1, H, H, D, k.shape[1], 1, 0)
+    tm.tm_kv8_append(cache, 0, bf16(k).cuda(), bf16(v).cuda())
+    return cache
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n_q,H,blocks,tiles", FORMS)
+@pytest.mark.parametrize("outlier", [1, 30, 300, 3000])
+def test_a_channel_of_k_far_above_the_others(tm, D, n_q, H, blocks, tiles, outlier):  # noqa: F811
+    """Rows of q with a mean of their own and nothing in that channel: codes of the others are small, and
+    so are the scores (the sizes of a score's products add up to about 1.2 * 0.8 sqrt(D), below 30)."""
+    n = blocks * BLOCK
+    assert in_tiles(1, H, n_q, [n], D) == tiles
+    g = torch.Generator().manual_seed(33)
+    k, v = torch.randn((1, n, H, D), generator=g), torch.randn((1, n, H, D), generator=g)
+    k[..., 5] *= outlier
+    q = 1 + torch.randn((1, n_q, H, D), generator=g)
+    q[..., 5] = 0
+    check_attention(tm, put(tm, D, H, k, v), 0, bf16(q).cuda(), f"outlier {outlier}")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n_q,H,blocks,tiles", FORMS)
+@pytest.mark.parametrize("common", [40, 200])
+def test_rows_of_q_with_a_common_part(tm, D, n_q, H, blocks, tiles, common):  # noqa: F811
+    """q is whole numbers below 256, so its products with codes are whole and their sums below 2^24:
+    exact, whatever their sizes. K's rows have a mean near zero, for scores of a few units."""
+    n = blocks * BLOCK
+    assert in_tiles(1, H, n_q, [n], D) == tiles
+    g = torch.Generator().manual_seed(34)
+    k, v = torch.randn((1, n, H, D), generator=g), torch.randn((1, n, H, D), generator=g)
+    k = (k - k.mean(-1, keepdim=True)) * 0.3
+    q = torch.round(common + torch.randn((1, n_q, H, D), generator=g))
+    check_attention(tm, put(tm, D, H, k, v), 0, bf16(q).cuda(), f"common {common}")
