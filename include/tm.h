@@ -438,8 +438,11 @@ tm_status tm_kv8_read(const tm_kv8_cache* cache, int32_t chunk, void* k_out, voi
  * [B, heads, n_q], 4-byte aligned, natural-log softmax normaliser.
  * Arithmetic: codes and (scaled by a power of two per row) q as fp16 operands,
  * exact but for elements of q below 2^-28 of their row's largest; fp32 sums; P
- * rounded to fp16; the row sums add the fp32 P. o_f32 leaves out the final
- * rounding to bf16 only. A query row with an infinity or NaN gets NaN.
+ * rounded to fp16, of which weights below 2^-18 of the row's largest keep less than
+ * 11 bits, to 2^-29 of it; the row sums add the fp32 P. Every dimension has that accuracy
+ * whatever the other dimensions' and blocks' sizes, but for values below 2^-60 of the
+ * largest that the row sees, which may be off by 2^-60 of that. o_f32 leaves out the
+ * final rounding to bf16 only. A query row with an infinity or NaN gets NaN.
  * workspace: device memory, 16-byte aligned, not overlapping any other tensor, or
  * NULL. Rows that do not fill the GPU share their keys out over several
  * workgroups through it; with fewer than tm_kv8_attn_workspace() bytes (0: the call

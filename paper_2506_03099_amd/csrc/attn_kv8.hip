@@ -11,12 +11,14 @@
 // q is fp16 as well: its rows are scaled by a power of two that puts their largest
 // element in [2^14, 2^15), which keeps every bf16 digit of elements down to 2^-28
 // of it. The products q . code are summed in fp32; the scales follow on the sums:
-//     x = (q . code) * (scale log2(e) ks / row's power) + log2(vs) - m,
+//     x = (q . code) * (scale log2(e) ks / row's power) + log2(r) - m,
 // one fma per score, P = 2^x in fp16 (11 digits, bf16 has 8), O += P . code, and
-// the row sum takes P / vs. Folding vs into the exponent scales P, not the 8-bit
-// operand, so nothing is rounded for it. m is the running maximum of x + m less
-// 8: P reaches 2^8 and a tile may exceed that by 2^7 before m is raised; what
-// fp16 then loses at its lower end is below 2^-33 of the largest.
+// the row sum takes P / r. r = vs / unit is V's scale in the unit, a power of two, that O
+// is held in. Folding r into the exponent scales P, not the 8-bit operand, so nothing
+// is rounded for it; a unit that follows the scales (struct Unit) keeps r in [1/8, 2), so
+// that P stays where fp16 has its digits whatever the sizes of V. m is the running maximum of
+// x + m less 8: P reaches 2^8 and a tile may exceed that by 2^7 before m is raised; what
+// fp16 then loses at its lower end is below 2^-29 of the largest weight (2^-25 of 2^8 / 16).
 //
 // Both operands lose the bias of 128 before the products. (With K's codes as they are held
 // and 128 times the row's sum of q taken off the score afterwards, a packed addition less for
@@ -179,6 +181,36 @@ __device__ __forceinline__ float score_factor(float cq, float ks) {
     return c < FLT_MIN ? FLT_MIN : c;
 }
 
+// The unit of O: 2^(e - 127), moved where a block's scale of V lies outside [1/8, 2) of it, by the whole
+// wave, as a block's scale is the same in every lane. O follows by an exact factor, unless that takes it
+// past the ends of fp32: so the unit is kept within 2^-kDown of the largest so far (O is at most 2^15 *
+// 127 * 2^30 in it), and a block further down counts as one of 1/8 of that, off by less than 2^-60 of the
+// largest value. Scales are 2^-67 / 127 at least, so normal numbers, or NaN, which moves nothing.
+struct Unit {
+    static constexpr int kDown = 64;
+    int e = 0;    // (0: no block yet, and O is zero)
+    int top = 0;
+    __device__ __forceinline__ bool holds(float vs) const {
+        return static_cast<uint32_t>(exponent(vs) - e + 3) <= 3u;
+    }
+    __device__ __forceinline__ void move(float& vs) {
+        const int ev = exponent(vs);
+        if (ev == 255) return;
+        e = max(ev + 1, top - kDown);
+        top = max(top, e);
+        if (ev < e - 3) vs = __uint_as_float(static_cast<uint32_t>(e - 3) << 23);
+    }
+    __device__ __forceinline__ float inverse() const { return __uint_as_float(static_cast<uint32_t>(254 - e) << 23); }
+    __device__ __forceinline__ float value() const { return __uint_as_float(static_cast<uint32_t>(e) << 23); }
+    // What turns values held in the unit of exponent `from` into ones of this unit.
+    __device__ __forceinline__ float from(int f) const {
+        return f - e < -126 ? 0.f : __uint_as_float(static_cast<uint32_t>(f - e + 127) << 23);
+    }
+    static __device__ __forceinline__ int exponent(float vs) {
+        return static_cast<int>(__builtin_amdgcn_readfirstlane(static_cast<int>(__float_as_uint(vs))) >> 23);
+    }
+};
+
 // Waits for scalar loads, which share a counter with the LDS reads and come back in
 // any order: after this no wait for one has to wait for every LDS read in flight.
 __device__ __forceinline__ void wait_scalars() { __builtin_amdgcn_s_waitcnt(kWaitLgkmcnt0); }
@@ -296,8 +328,8 @@ __device__ __forceinline__ void read_args(const Kv8AttnArgs& a) {
                  "s"(a.by_tiles.mul), "s"(a.by_tiles.shift), "s"(a.by_heads.mul), "s"(a.by_heads.shift),
                  "s"(a.by_group.mul), "s"(a.by_group.shift), "s"(a.scale_log2), "s"(a.n_ranges), "s"(a.cut));
 }
-// A split tile's partial rows: O not yet divided by the row sum, [rows][D], then each
-// row's maximum and sum.
+// A split tile's partial rows: O over the part's own row sum, [rows][D] (parts have units of their
+// own), then each row's maximum and sum.
 template <int D, int ROWS>
 __device__ __forceinline__ float* part_at(const Kv8AttnArgs& a, int split, int part) {
     return a.part + (static_cast<int64_t>(split) * a.parts + part) * (ROWS * (D + 2));
@@ -312,7 +344,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_kv8_few_kernel(const Kv8AttnA
     constexpr int KK = D / 16, DB = D / 32, NP = 2 * DB;  // pieces of K, and of V, of a block
     constexpr int PITCH = D + 4;                           // floats per row in LDS
     __shared__ float rows_o[NW][kKv8FewRows * PITCH];
-    __shared__ float rows_m[NW][kKv8FewRows], rows_l[NW][kKv8FewRows];
+    __shared__ float rows_m[NW][kKv8FewRows], rows_l[NW][kKv8FewRows], units[NW];
     const int lane = threadIdx.x & 63, hw = lane >> 5, l32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
     read_args(a);
@@ -322,11 +354,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_kv8_few_kernel(const Kv8AttnA
     load_q<D>(a, row_at(a, s.bat, s.kvh, min(q0 + l32, a.rows - 1)), hw, raw);
     const int64_t head = (static_cast<int64_t>(s.bat) * a.Hk + s.kvh) * a.n_blocks;
 
-
     f32x16_t acc[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d) acc[d] = f32x16_t{};
     float m = kNegInf, l = 0.f;
+    Unit unit;
     u32x4_t kc[NP], vc[NP];
     float ks = 0.f, vs = 0.f;
     const uint32_t lane16 = 16 * lane;
@@ -361,8 +393,14 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_kv8_few_kernel(const Kv8AttnA
             x[kb] = mfma(decode8(kc[i][2], kc[i][3]), qf[2 * st + 1], x[kb]);
         }
         float c = score_factor(cq, ks);
-        const float iv = __builtin_amdgcn_rcpf(vs);
-        const float add = __builtin_amdgcn_logf(vs);
+        if (__builtin_expect(!unit.holds(vs), 0)) {
+            const int was = unit.e;
+            unit.move(vs);
+#pragma unroll
+            for (int d = 0; d < DB; ++d) acc[d] *= unit.from(was);
+        }
+        const float share = vs * unit.inverse();
+        const float iv = __builtin_amdgcn_rcpf(share), add = __builtin_amdgcn_logf(share);
         at.next(a, NW);  // (past the share's end: a block that exists)
         load_k(at.blk);
         ks = a.k_scale[head + at.blk];
@@ -429,6 +467,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_kv8_few_kernel(const Kv8AttnA
             rows_l[wave][l32] = l;
         }
     }
+    if (lane == 0) units[wave] = unit.value();
     __syncthreads();
     float* const part = s.split >= 0 ? part_at<D, kKv8FewRows>(a, s.split, s.part) : nullptr;
     for (int n = threadIdx.x; n < n_rows * (D / 4); n += 64 * NW) {
@@ -437,15 +476,20 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_kv8_few_kernel(const Kv8AttnA
 #pragma unroll
         for (int w = 0; w < NW; ++w) top = fmaxf(top, rows_m[w][r]);
         const float base = top == kNegInf ? 0.f : top;
-        float sum = 0.f;
+        float sum = 0.f, f[NW];
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            f[w] = __builtin_amdgcn_exp2f(rows_m[w][r] - base);
+            sum = fmaf(f[w], rows_l[w][r], sum);
+        }
+        const float inv = 1.f / sum;
         f32x4_t o{};
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            const float f = __builtin_amdgcn_exp2f(rows_m[w][r] - base);
-            sum = fmaf(f, rows_l[w][r], sum);
+            const float to = f[w] * inv * units[w];
             const f32x4_t ow = *reinterpret_cast<const f32x4_t*>(&rows_o[w][r * PITCH + d]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = fmaf(f, ow[e], o[e]);
+            for (int e = 0; e < 4; ++e) o[e] = fmaf(to, ow[e], o[e]);
         }
         if (part != nullptr) {
             *reinterpret_cast<f32x4_t*>(part + r * D + d) = o;
@@ -455,7 +499,6 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_kv8_few_kernel(const Kv8AttnA
             }
             continue;
         }
-        o *= 1.f / sum;
         const int64_t at_o = row_at(a, s.bat, s.kvh, q0 + r) * D + d;
         if constexpr (OF32) {
             *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.o) + at_o) = o;
@@ -554,7 +597,9 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
     f32x16_t acc[DB];
 #pragma unroll
     for (int i = 0; i < DB; ++i) acc[i] = f32x16_t{};
-    float m = 0.f, l = 0.f, iv = 0.f;  // iv: 1 / scale of V of the tile whose P is formed
+    float m = 0.f, l = 0.f, iv = 0.f;  // iv: 1 / (scale of V in the unit) of the tile whose P is formed
+    Unit unit;        // of that tile's P
+    int acc_unit = 0;  // exponent of O's, which follows before the tile's P V
     uint64_t fresh = 0;  // lanes whose row has had no finite score yet (m is 0 until the first)
     auto mask_tile = [&](f32x16_t (&x)[2], int keys) __attribute__((always_inline)) {
         // register i of block kb is key 32 kb + 16 (i / 8) + 8 hw + i % 8 (the lane's bound formed
@@ -611,8 +656,11 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
         xa[0] = xa[1] = f32x16_t{};
 #pragma unroll
         for (int f = 0; f < NK; ++f) xa[f & 1] = mfma(read_frag(f, 0, 0), qf[f >> 1], xa[f & 1]);
-        const float c = score_factor(cq, ks), add = __builtin_amdgcn_logf(vs);
-        iv = uniform_f(1.f / vs);
+        const float c = score_factor(cq, ks);
+        unit.move(vs);
+        acc_unit = unit.e;
+        const float share = vs * unit.inverse(), add = __builtin_amdgcn_logf(share);
+        iv = uniform_f(__builtin_amdgcn_rcpf(share));
         load_scales(1);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
@@ -634,7 +682,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
     // ---- iteration t, with x = x(t) and nx receiving S(t+1); u = t % 4. Stage 1: the score
     // MFMAs of tile t+1, each with its share of P(t). Check: a lane's sum of P beyond the bound
     // (or not a number) raises m to the tile's maximum less the headroom, rescales O and the row
-    // sum and forms P(t) again. Stage 2: the P V MFMAs of tile t, each with its share of x(t+1),
+    // sum and forms P(t) again; O also follows there where P(t) is in another unit. Stage 2: the P V MFMAs of tile t, each with its share of x(t+1),
     // of turning block t+3's codes into operands in LDS, and of loading block t+4's. Block t+3
     // goes where block t-1 was, whose last reads lie before the barrier that ended tile t-1. The
     // barrier that ends tile t publishes block t+3; K(t+2), read ahead here, was published by the
@@ -663,7 +711,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
             __builtin_amdgcn_sched_barrier(0);
         }
         uint64_t raise = __ballot(!(lt0 + lt1 <= kRaise));
-        if (__builtin_expect((raise | fresh) != 0, 0)) {
+        if (__builtin_expect((raise | fresh | static_cast<uint32_t>(unit.e ^ acc_unit)) != 0, 0)) {
             raise |= raise << 32 | raise >> 32;  // both lanes of a row; other rows keep their bits
             const float mx = row_max(x);
             const bool first = __builtin_amdgcn_inverse_ballot_w64(fresh) && mx != kNegInf;
@@ -673,8 +721,10 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
             fresh &= __ballot(mx == kNegInf);
             m += dm;
             l *= alpha;
+            const float to = alpha * unit.from(acc_unit);
+            acc_unit = unit.e;
 #pragma unroll
-            for (int d = 0; d < DB; ++d) acc[d] *= alpha;
+            for (int d = 0; d < DB; ++d) acc[d] *= to;
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -685,8 +735,9 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
         // (as one fma the compiler kept two copies of O: 200 registers spilled)
         l += pin(pin(lt0 + lt1) * iv);
         const float c = score_factor(cq, ks);
-        const float add = __builtin_amdgcn_logf(vs) - m;
-        iv = uniform_f(__builtin_amdgcn_rcpf(vs));
+        if (__builtin_expect(!unit.holds(vs), 0)) unit.move(vs);
+        const float share = vs * unit.inverse(), add = __builtin_amdgcn_logf(share) - m;
+        iv = uniform_f(__builtin_amdgcn_rcpf(share));
         if (__builtin_expect(cnt[(u + 1) & 3] < kCacheBlock, 0)) mask_tile(nx, cnt[(u + 1) & 3]);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -735,11 +786,11 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
     __syncthreads();
 
     // ---- the rows, through the wave's share of the LDS so that they are stored whole: O over
-    // the row sum, or a part's O as it is (fp32)
+    // the row sum (a part's: in fp32)
     l += __shfl_xor(l, 32);
     const bool part_rows = s.split >= 0;
     float* const part = part_rows ? part_at<D, kTileRows>(a, s.split, s.part) : nullptr;
-    const float inv = part_rows ? 1.f : 1.f / l;
+    const float inv = __uint_as_float(static_cast<uint32_t>(acc_unit) << 23) / l;
     if (busy) {
         constexpr int CPR = D / 4;  // 16-byte chunks of an fp32 row
         static_assert(kTileRows * D * 4 <= 2 * NBUF * TILEB, "output rows must fit the LDS");
@@ -813,9 +864,19 @@ __global__ __launch_bounds__(kMergeThreads) void attn_kv8_merge_kernel(const Kv8
     const bool ok = q0 + r < q1;
     const float* const p = part_at<D, ROWS>(a, split, 0);
     constexpr int64_t step = ROWS * (D + 2);
-    // one pass: the sum so far is rescaled where a part raises the maximum
+    // one pass: O is the mean of the parts so far, by their shares of the row sum
     float top = kNegInf, sum = 0.f;
     f32x4_t o{};
+    auto add = [&](float mi, float li, f32x4_t oi) __attribute__((always_inline)) {
+        const float nm = fmaxf(top, mi);
+        const float keep = top == kNegInf ? 0.f : sum * __builtin_amdgcn_exp2f(top - nm);
+        const float take = li * __builtin_amdgcn_exp2f(mi - nm);
+        top = nm;
+        sum = keep + take;
+        const float inv = __builtin_amdgcn_rcpf(sum), old = keep * inv, now = take * inv;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = fmaf(now, oi[e], o[e] * old);
+    };
     if (ok) {
         for (int i0 = pg; i0 < a.parts; i0 += U * PG) {
             float mi[U], li[U];
@@ -831,13 +892,7 @@ __global__ __launch_bounds__(kMergeThreads) void attn_kv8_merge_kernel(const Kv8
             for (int u = 0; u < U; ++u) {
                 // (a part with only scores of -inf has a sum of 0 and any maximum)
                 if (i0 + u * PG >= a.parts || li[u] == 0.f) continue;
-                const float nm = fmaxf(top, mi[u]);
-                const float keep = top == kNegInf ? 0.f : __builtin_amdgcn_exp2f(top - nm);
-                const float take = __builtin_amdgcn_exp2f(mi[u] - nm);
-                top = nm;
-                sum = fmaf(take, li[u], sum * keep);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = fmaf(take, oi[u][e], o[e] * keep);
+                add(mi[u], li[u], oi[u]);
             }
         }
     }
@@ -849,20 +904,13 @@ __global__ __launch_bounds__(kMergeThreads) void attn_kv8_merge_kernel(const Kv8
         if (pg != 0) return;
 #pragma unroll
         for (int i = 1; i < PG; ++i) {
-            const float li = lsums[tid + i * TPR], mi = tops[tid + i * TPR];
+            const float li = lsums[tid + i * TPR];
             if (li == 0.f) continue;
-            const float nm = fmaxf(top, mi);
-            const float keep = top == kNegInf ? 0.f : __builtin_amdgcn_exp2f(top - nm);
-            const float take = __builtin_amdgcn_exp2f(mi - nm);
-            top = nm;
-            sum = fmaf(take, li, sum * keep);
-            const f32x4_t oi = sums[tid + i * TPR];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = fmaf(take, oi[e], o[e] * keep);
+            add(tops[tid + i * TPR], li, sums[tid + i * TPR]);
         }
     }
     if (!ok) return;
-    o *= 1.f / sum;
+    if (sum == 0.f) o *= 1.f / sum;  // only scores of -inf: NaN
     const int64_t at = row_at(a, bat, kvh, q0 + r) * D + d;
     if constexpr (OF32) {
         *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.o) + at) = o;

@@ -1,9 +1,15 @@
-"""Attention over the 8-bit cache where sizes differ widely: K with a channel far
-above the others, rows of q with a common part.
+"""Attention over the 8-bit cache where sizes differ widely: blocks of V
+of any finite size, K with a channel far above the others, rows of q with a common part.
 
-The bounds are those of test_gpu_kv8.py's header. Scores are below 30 and the sums
-behind them are either of products whose sizes add up to less than 30 as well, or
-exact (said where).
+The bounds are those of test_gpu_kv8.py's header, which hold for any such input:
+P is off by 2^-11 of each weight that fp16 holds as a normal number, whatever its
+block's scale (include/tm.h: to 2^-60 of the largest), so the output of every
+dimension by 2^-11 sum_j p_j |v_j| of that dimension. The weights here are above
+2^-14 of their row's largest, whose P is 2^8 times the quotient of two blocks' shares of
+their units, 2^-4 at least: 2^8 * 2^-14 * 2^-4 = 2^-10, a normal fp16 number. Scores are
+below 30 and the sums behind them are either of products whose sizes add up to less
+than 30 as well, or exact (said where); with the share of 2^-12 for them the bound is
+(2^-11 + 2^-12) sum_j p_j |v_j| again. The log-sum-exp: 1e-4.
 """
 import pytest
 import torch
@@ -27,6 +33,43 @@ def put(tm, D, H, k, v):  # noqa: F811
     cache = make(tm, 1, H, H, D, k.shape[1], 1, 0)
     tm.tm_kv8_append(cache, 0, bf16(k).cuda(), bf16(v).cuda())
     return cache
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n_q,H,blocks,tiles", FORMS)
+@pytest.mark.parametrize("sizes", [
+    (0.0, 2.0 ** 68),
+    (2.0 ** 68, 0.0),
+    (2.0 ** 76, 0.0, 1.0, 2.0 ** 76, 0.0),
+    (1.0, 2.0 ** 100, 1e-9, 0.0, 2.0 ** 40, 2.0 ** 124, 1e-30, 1e6),
+    (2.0 ** -55, 2.0 ** 10, 0.0, 2.0 ** 124, 0.0),
+])
+def test_row_sums_count_every_key_beside_values_of_any_size(tm, D, n_q, H, blocks, tiles, sizes):  # noqa: F811
+    """Scores of a few units, V blocks of these sizes in turn: each key has its share of the row sum."""
+    n = blocks * BLOCK
+    assert in_tiles(1, H, n_q, [n], D) == tiles
+    g = torch.Generator().manual_seed(31)
+    k, v = torch.randn((1, n, H, D), generator=g), torch.randn((1, n, H, D), generator=g)
+    for i in range(blocks):
+        v[:, BLOCK * i:BLOCK * (i + 1)] *= sizes[i % len(sizes)]
+    check_attention(tm, put(tm, D, H, k, v), 0, queries(1, n_q, H, D, g), f"{sizes}")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n_q,H,blocks,tiles", FORMS)
+@pytest.mark.parametrize("large,small", [(1e6, 1e-2), (1e6, 1e-9), (2.0 ** 40, 2.0 ** -18), (3e38, 1e30)])
+@pytest.mark.parametrize("at", [0, 5])
+def test_dimensions_that_only_blocks_of_small_values_have(tm, D, n_q, H, blocks, tiles, large, small, at):  # noqa: F811
+    """Every eighth block of V is large in dimension 0 and zero elsewhere; the other dimensions are
+    held to the bound of the small values alone."""
+    n = blocks * BLOCK
+    assert in_tiles(1, H, n_q, [n], D) == tiles
+    g = torch.Generator().manual_seed(32)
+    k, v = torch.randn((1, n, H, D), generator=g), torch.randn((1, n, H, D), generator=g) * small / 4
+    for i in range(at, blocks, 8):
+        v[:, BLOCK * i:BLOCK * (i + 1)] = 0
+        v[:, BLOCK * i:BLOCK * (i + 1), :, 0] = large
+    check_attention(tm, put(tm, D, H, k, v), 0, queries(1, n_q, H, D, g), f"{large} {small}")
 
 
 @pytest.mark.parametrize("D", [64, 128])
