@@ -429,8 +429,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_kv8_few_kernel(const Kv8AttnA
         const float base = m == kNegInf ? 0.f : m;
         float less = add - base;
         // `less` is rounded at the size of m. Scores so large that it shows take their steps one by one,
-        // which leaves the difference from the maximum exact.
-        if (__builtin_expect(__ballot(fabsf(base) > kLargeScore) != 0, 0)) {
+        // which leaves the difference from the maximum exact (in the lanes of those rows alone: the
+        // others keep their bits).
+        if (__builtin_expect(fabsf(base) > kLargeScore, 0)) {
 #pragma unroll
             for (int e = 0; e < 32; ++e) x[e / 16][e % 16] = fmaf(x[e / 16][e % 16], c, add) - base;
             c = 1.f;

@@ -1,5 +1,6 @@
 """Attention over the 8-bit cache where sizes differ widely: blocks of V
-of any finite size, K with a channel far above the others, rows of q with a common part.
+of any finite size, K with a channel far above the others, rows of q with a common
+part, and scores of one row far above its neighbours'.
 
 The bounds are those of test_gpu_kv8.py's header, which hold for any such input:
 P is off by 2^-11 of each weight that fp16 holds as a normal number, whatever its
@@ -101,3 +102,22 @@ def test_rows_of_q_with_a_common_part(tm, D, n_q, H, blocks, tiles, common):  # 
     k = (k - k.mean(-1, keepdim=True)) * 0.3
     q = torch.round(common + torch.randn((1, n_q, H, D), generator=g))
     check_attention(tm, put(tm, D, H, k, v), 0, bf16(q).cuda(), f"common {common}")
+
+
+@pytest.mark.parametrize("D,H", [(64, 1), (128, 1), (64, 250), (128, 200)])
+def test_a_row_does_not_depend_on_far_larger_scores_beside_it(tm, D, H):  # noqa: F811
+    """Scores of some thousand units in one row of 32: the others keep their bits."""
+    n, n_q = 640, 256
+    assert in_tiles(1, H, n_q, [n], D) == (H > 1)
+    g = torch.Generator().manual_seed(35)
+    k, v = torch.randn((1, n, H, D), generator=g), torch.randn((1, n, H, D), generator=g)
+    cache = put(tm, D, H, k, v)
+    q = queries(1, n_q, H, D, g)
+    want = tm.tm_kv8_attn_fwd(cache, q, 0, o_f32=True)
+    other = q.clone()
+    other[0, 5::32] = 400 * bf16(k)[0, n - 1].cuda()
+    got = tm.tm_kv8_attn_fwd(cache, other, 0, o_f32=True)
+    keep = torch.ones(n_q, dtype=torch.bool, device="cuda")
+    keep[5::32] = False
+    assert torch.equal(got[0, keep], want[0, keep])
+    assert torch.isfinite(got).all()
