@@ -1233,6 +1233,7 @@ tm_status write_chunk8(tm_kv8_cache* cache, int32_t chunk, const void* q, const 
         if (!std::isfinite(eps) || eps < 0.f) return fail(TM_E_ARG, "eps must be finite and >= 0");
         if ((st = check(q, q_bytes, "q")) != TM_OK) return st;
         if ((st = check(q_out, q_bytes, "q_out")) != TM_OK) return st;
+        if (overlaps(q, q_bytes, cache->pool, z.bytes())) return fail(TM_E_ARG, "q overlaps the cache's pool");
         if (q_out != q && overlaps(q_out, q_bytes, q, q_bytes))
             return fail(TM_E_ARG, "q_out overlaps q without being q");
         if (overlaps(q_out, q_bytes, k, kv_bytes) || overlaps(q_out, q_bytes, v, kv_bytes) ||
