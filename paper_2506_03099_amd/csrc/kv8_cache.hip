@@ -335,9 +335,8 @@ __global__ __launch_bounds__(kKv8Threads) void kv8_read_kernel(const Kv8ReadArgs
                 const uint32_t w = tile[x][r * PITCH + (run_of<EB, D>(g, 4 * i * EB / 16) + 4 * i % (16 / EB)) / 4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    // (code + 128) * s - 128 * s: the product and the difference are exact in the fma
-                    const float s = x == 0 ? sk : sv;
-                    v[4 * i + e] = fmaf(static_cast<float>((w >> (8 * e)) & 0xFFu), s, -128.f * s);
+                    // (128 off before the product: 128 scales of the largest values are past fp32)
+                    v[4 * i + e] = (static_cast<float>((w >> (8 * e)) & 0xFFu) - 128.f) * (x == 0 ? sk : sv);
                 }
             }
             store_row<EB, D>((x == 0 ? a.k_out : a.v_out) + first + t * stride, g, v);

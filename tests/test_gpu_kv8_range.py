@@ -1,6 +1,6 @@
-"""Attention over the 8-bit cache where sizes differ widely: blocks of V
+"""The 8-bit cache and the attention over it where sizes differ widely: blocks of V
 of any finite size, K with a channel far above the others, rows of q with a common
-part, and scores of one row far above its neighbours'.
+part, scores of one row far above its neighbours', and the largest finite values.
 
 The bounds are those of test_gpu_kv8.py's header, which hold for any such input:
 P is off by 2^-11 of each weight that fp16 holds as a normal number, whatever its
@@ -15,7 +15,7 @@ than 30 as well, or exact (said where); with the share of 2^-12 for them the bou
 import pytest
 import torch
 
-from test_gpu_kv8 import BLOCK, bf16, check_attention, in_tiles, make, queries, tm  # noqa: F401
+from test_gpu_kv8 import BLOCK, bf16, check_attention, held32, in_tiles, make, queries, tm  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -121,3 +121,19 @@ def test_a_row_does_not_depend_on_far_larger_scores_beside_it(tm, D, H):  # noqa
     keep[5::32] = False
     assert torch.equal(got[0, keep], want[0, keep])
     assert torch.isfinite(got).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_the_largest_finite_values_read_back(tm, D, dtype):  # noqa: F811
+    n = 3 * BLOCK
+    top = float(torch.finfo(torch.bfloat16).max)
+    g = torch.Generator().manual_seed(36)
+    x = bf16((2 * torch.rand((1, n, 2, D), generator=g) - 1) * top)
+    x[:, 0, :, 0], x[:, BLOCK, :, 0] = top, -top
+    assert torch.isfinite(x).all()
+    cache = make(tm, 1, 2, 2, D, n, 1, 0)
+    tm.tm_kv8_append(cache, 0, x.cuda(), x.cuda())
+    want = torch.from_numpy(held32(x.float().numpy())).to(dtype)
+    for y in tm.tm_kv8_read(cache, 0, dtype):
+        assert torch.equal(y.cpu(), want)
