@@ -927,13 +927,13 @@ __global__ __launch_bounds__(kMergeThreads) void attn_kv8_merge_kernel(const Kv8
 template <int D, bool OF32>
 hipError_t launch(const Kv8AttnArgs& a, hipStream_t s) {
     const int64_t total = static_cast<int64_t>(a.n_tiles) * a.B * a.Hk, split = total - a.n_whole;
+    // (no more than one split tile a CU: the split is there for the CUs that a round leaves idle)
+    if (split > kCUs) return hipErrorInvalidValue;
     const unsigned grid = static_cast<unsigned>(a.n_whole + split * a.parts);
     const hipError_t e = a.few == 4   ? launch_with(attn_kv8_few_kernel<D, OF32, 4>, dim3(grid), 256, s, a)
                          : a.few == 8 ? launch_with(attn_kv8_few_kernel<D, OF32, 8>, dim3(grid), 512, s, a)
                                       : launch_with(attn_kv8_tile_kernel<D, OF32>, dim3(grid), kTileThreads, s, a);
     if (e != hipSuccess || split == 0) return e;
-    // (no more than one split tile a CU: the split is there for the CUs that a round leaves idle)
-    if (split > kCUs) return hipErrorInvalidValue;
     const int rows = min(a.rows, a.few ? kKv8FewRows : kTileRows);
     auto wgs = [&](int rpw) { return dim3((rows + rpw - 1) / rpw, static_cast<unsigned>(split)); };
     constexpr int kOne = kMergeThreads / (D / 4), kEight = kOne / 8;  // rows of a workgroup

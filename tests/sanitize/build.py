@@ -17,6 +17,7 @@ ROOT = os.path.dirname(os.path.dirname(HERE))
 PKG = os.path.join(ROOT, "paper_2506_03099_amd")
 DRIVER = os.path.join(HERE, "host_abi_driver")
 KV8_DRIVER = os.path.join(HERE, "host_kv8_driver")
+KV8_LAYOUT_DRIVER = os.path.join(HERE, "host_kv8_layout_driver")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 
 SAN = ["-fsanitize=address,undefined", "-fno-sanitize-recover=undefined", "-fno-omit-frame-pointer"]
@@ -27,7 +28,7 @@ CXXFLAGS = ["-std=c++17", "-O1", "-g", "-D__HIP_PLATFORM_AMD__", "-I", os.path.j
 def build(verbose: bool = False) -> str:
     if not os.path.exists(os.path.join(PKG, "libtm.so")):
         raise RuntimeError("libtm.so must be built first")
-    for driver in (DRIVER, KV8_DRIVER):
+    for driver in (DRIVER, KV8_DRIVER, KV8_LAYOUT_DRIVER):
         obj = driver + ".o"
         cmd = ["g++", *CXXFLAGS, *SAN, "-c", driver + ".cpp", "-o", obj]
         if verbose:
