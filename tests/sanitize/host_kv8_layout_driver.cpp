@@ -28,10 +28,10 @@ int refused_launch() {
     a.n_q = a.rows = a.n_tiles = 1;
     a.n_whole = 0;
     a.parts = 2;
-    a.n_kblocks = 48;
+    a.n_kblocks = 50;
     a.n_ranges = 1;
-    a.range_keys[0] = 48 * 64;
-    a.n_blocks = 48;
+    a.range_keys[0] = 50 * 64;
+    a.n_blocks = 50;
     const hipError_t e = tmk::launch_attn_kv8(a, 128, nullptr);
     if (e != hipErrorInvalidValue) {
         std::fprintf(stderr, "a launch of 257 split tiles: %s\n", hipGetErrorString(e));
