@@ -175,10 +175,11 @@ __device__ __forceinline__ float scale_q(const u32x4_t (&raw)[D / 16], float sca
 }
 
 // The factor of a tile's scores from that of the row's q and the scale of K. (Not zero, as a tiny
-// row's may be: a masked score of -inf is still to be scaled.)
+// row's may be: a masked score of -inf is still to be scaled; nor infinite, as that of large rows: a
+// score of zero still is one. NaN stays.)
 __device__ __forceinline__ float score_factor(float cq, float ks) {
-    const float c = cq * ks;
-    return c < FLT_MIN ? FLT_MIN : c;
+    const float c = cq * ks, low = c < FLT_MIN ? FLT_MIN : c;
+    return low > FLT_MAX ? FLT_MAX : low;
 }
 
 // The unit of O: 2^(e - 127), moved where a block's scale of V lies outside [1/8, 2) of it, by the whole

@@ -124,6 +124,20 @@ def test_a_row_does_not_depend_on_far_larger_scores_beside_it(tm, D, H):  # noqa
 
 
 @pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n_q,H,blocks,tiles", FORMS)
+def test_large_rows_whose_products_are_zero(tm, D, n_q, H, blocks, tiles):  # noqa: F811
+    """q and K of 1e30 in dimensions apart from each other's: every score is exactly zero."""
+    n = blocks * BLOCK
+    assert in_tiles(1, H, n_q, [n], D) == tiles
+    g = torch.Generator().manual_seed(37)
+    k, v = torch.randn((1, n, H, D), generator=g) * 1e30, torch.randn((1, n, H, D), generator=g)
+    k[..., ::2] = 0
+    q = torch.randn((1, n_q, H, D), generator=g) * 1e30
+    q[..., 1::2] = 0
+    check_attention(tm, put(tm, D, H, k, v), 0, bf16(q).cuda(), "zero products")
+
+
+@pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_the_largest_finite_values_read_back(tm, D, dtype):  # noqa: F811
     n = 3 * BLOCK
