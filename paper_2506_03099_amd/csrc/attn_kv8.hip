@@ -397,8 +397,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_kv8_few_kernel(const Kv8AttnA
         if (__builtin_expect(!unit.holds(vs), 0)) {
             const int was = unit.e;
             unit.move(vs);
+            if (was != 0) {
+                const float to = unit.from(was);
 #pragma unroll
-            for (int d = 0; d < DB; ++d) acc[d] *= unit.from(was);
+                for (int d = 0; d < DB; ++d) acc[d] *= to;
+            }
         }
         const float share = vs * unit.inverse();
         const float iv = __builtin_amdgcn_rcpf(share), add = __builtin_amdgcn_logf(share);
@@ -484,7 +487,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_kv8_few_kernel(const Kv8AttnA
             f[w] = __builtin_amdgcn_exp2f(rows_m[w][r] - base);
             sum = fmaf(f[w], rows_l[w][r], sum);
         }
-        const float inv = 1.f / sum;
+        // (a part with only scores of -inf: zeros, which count for nothing in the merge)
+        const float inv = part != nullptr && sum == 0.f ? 0.f : 1.f / sum;
         f32x4_t o{};
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
@@ -684,7 +688,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
     // ---- iteration t, with x = x(t) and nx receiving S(t+1); u = t % 4. Stage 1: the score
     // MFMAs of tile t+1, each with its share of P(t). Check: a lane's sum of P beyond the bound
     // (or not a number) raises m to the tile's maximum less the headroom, rescales O and the row
-    // sum and forms P(t) again; O also follows there where P(t) is in another unit. Stage 2: the P V MFMAs of tile t, each with its share of x(t+1),
+    // sum and forms P(t) again. O follows P(t) where that is in another unit. Stage 2: the P V MFMAs of tile t, each with its share of x(t+1),
     // of turning block t+3's codes into operands in LDS, and of loading block t+4's. Block t+3
     // goes where block t-1 was, whose last reads lie before the barrier that ended tile t-1. The
     // barrier that ends tile t publishes block t+3; K(t+2), read ahead here, was published by the
@@ -713,26 +717,31 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
             __builtin_amdgcn_sched_barrier(0);
         }
         uint64_t raise = __ballot(!(lt0 + lt1 <= kRaise));
+        // (one branch for all of it on the way past: two take 0.5% longer)
         if (__builtin_expect((raise | fresh | static_cast<uint32_t>(unit.e ^ acc_unit)) != 0, 0)) {
-            raise |= raise << 32 | raise >> 32;  // both lanes of a row; other rows keep their bits
-            const float mx = row_max(x);
-            const bool first = __builtin_amdgcn_inverse_ballot_w64(fresh) && mx != kNegInf;
-            const float up = __builtin_amdgcn_inverse_ballot_w64(raise) ? fmaxf(below(mx), 0.f) : 0.f;
-            const float dm = first ? below(mx) : up;
-            const float alpha = first ? 1.f : __builtin_amdgcn_exp2f(-dm);  // (sum and O are still 0)
-            fresh &= __ballot(mx == kNegInf);
-            m += dm;
-            l *= alpha;
-            const float to = alpha * unit.from(acc_unit);
+            const float to = unit.from(acc_unit);
             acc_unit = unit.e;
 #pragma unroll
             for (int d = 0; d < DB; ++d) acc[d] *= to;
+            if ((raise | fresh) != 0) {
+                raise |= raise << 32 | raise >> 32;  // both lanes of a row; other rows keep their bits
+                const float mx = row_max(x);
+                const bool first = __builtin_amdgcn_inverse_ballot_w64(fresh) && mx != kNegInf;
+                const float up = __builtin_amdgcn_inverse_ballot_w64(raise) ? fmaxf(below(mx), 0.f) : 0.f;
+                const float dm = first ? below(mx) : up;
+                const float alpha = first ? 1.f : __builtin_amdgcn_exp2f(-dm);  // (sum and O are still 0)
+                fresh &= __ballot(mx == kNegInf);
+                m += dm;
+                l *= alpha;
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
+                for (int d = 0; d < DB; ++d) acc[d] *= alpha;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) x[kb][i] -= dm;
+                for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int e = 0; e < 32; e += 2) form_p2(x, pf, e, (e & 2) ? lt1 : lt0);
+                    for (int i = 0; i < 16; ++i) x[kb][i] -= dm;
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) form_p2(x, pf, e, (e & 2) ? lt1 : lt0);
+            }
         }
         // (as one fma the compiler kept two copies of O: 200 registers spilled)
         l += pin(pin(lt0 + lt1) * iv);
@@ -792,7 +801,7 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
     l += __shfl_xor(l, 32);
     const bool part_rows = s.split >= 0;
     float* const part = part_rows ? part_at<D, kTileRows>(a, s.split, s.part) : nullptr;
-    const float inv = __uint_as_float(static_cast<uint32_t>(acc_unit) << 23) / l;
+    const float inv = part_rows && l == 0.f ? 0.f : __uint_as_float(static_cast<uint32_t>(acc_unit) << 23) / l;
     if (busy) {
         constexpr int CPR = D / 4;  // 16-byte chunks of an fp32 row
         static_assert(kTileRows * D * 4 <= 2 * NBUF * TILEB, "output rows must fit the LDS");
@@ -869,15 +878,25 @@ __global__ __launch_bounds__(kMergeThreads) void attn_kv8_merge_kernel(const Kv8
     // one pass: O is the mean of the parts so far, by their shares of the row sum
     float top = kNegInf, sum = 0.f;
     f32x4_t o{};
-    auto add = [&](float mi, float li, f32x4_t oi) __attribute__((always_inline)) {
-        const float nm = fmaxf(top, mi);
-        const float keep = top == kNegInf ? 0.f : sum * __builtin_amdgcn_exp2f(top - nm);
-        const float take = li * __builtin_amdgcn_exp2f(mi - nm);
-        top = nm;
-        sum = keep + take;
-        const float inv = __builtin_amdgcn_rcpf(sum), old = keep * inv, now = take * inv;
+    // (a part without a finite score has a sum of 0, any maximum and zeros)
+    auto add = [&](const float (&mi)[U], const float (&li)[U], const f32x4_t (&oi)[U]) __attribute__((always_inline)) {
+        float nm = top, share[U];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = fmaf(now, oi[e], o[e] * old);
+        for (int u = 0; u < U; ++u) nm = fmaxf(nm, li[u] == 0.f ? kNegInf : mi[u]);
+        const float keep = sum == 0.f ? 0.f : sum * __builtin_amdgcn_exp2f(top - nm);
+        sum = keep;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            share[u] = li[u] == 0.f ? 0.f : li[u] * __builtin_amdgcn_exp2f(mi[u] - nm);
+            sum += share[u];
+        }
+        top = nm;
+        const float inv = sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum);
+        o *= keep * inv;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = fmaf(share[u] * inv, oi[u][e], o[e]);
     };
     if (ok) {
         for (int i0 = pg; i0 < a.parts; i0 += U * PG) {
@@ -887,15 +906,10 @@ __global__ __launch_bounds__(kMergeThreads) void attn_kv8_merge_kernel(const Kv8
             for (int u = 0; u < U; ++u) {  // (past the end: the last part again, which then counts for nothing)
                 const float* const pi = p + min(i0 + u * PG, a.parts - 1) * step;
                 mi[u] = pi[ROWS * D + 2 * r];
-                li[u] = pi[ROWS * D + 2 * r + 1];
+                li[u] = i0 + u * PG < a.parts ? pi[ROWS * D + 2 * r + 1] : 0.f;
                 oi[u] = *reinterpret_cast<const f32x4_t*>(pi + r * D + d);
             }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                // (a part with only scores of -inf has a sum of 0 and any maximum)
-                if (i0 + u * PG >= a.parts || li[u] == 0.f) continue;
-                add(mi[u], li[u], oi[u]);
-            }
+            add(mi, li, oi);
         }
     }
     if constexpr (PG > 1) {
@@ -904,11 +918,18 @@ __global__ __launch_bounds__(kMergeThreads) void attn_kv8_merge_kernel(const Kv8
         tops[tid] = top;
         __syncthreads();
         if (pg != 0) return;
+        static_assert(PG == 2 * U, "the others' sums, in two steps");
 #pragma unroll
-        for (int i = 1; i < PG; ++i) {
-            const float li = lsums[tid + i * TPR];
-            if (li == 0.f) continue;
-            add(tops[tid + i * TPR], li, sums[tid + i * TPR]);
+        for (int i = 0; i < PG; i += U) {
+            float mi[U], li[U];
+            f32x4_t oi[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                mi[u] = tops[tid + (i + u) * TPR];
+                li[u] = i + u == 0 ? 0.f : lsums[tid + (i + u) * TPR];  // (its own are there)
+                oi[u] = sums[tid + (i + u) * TPR];
+            }
+            add(mi, li, oi);
         }
     }
     if (!ok) return;
