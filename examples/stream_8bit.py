@@ -5,7 +5,7 @@ One attention layer of the chunked student, with synthetic projections:
 - serving: for every chunk, ``tm_qkv8_produce`` RMS-normalises the chunk's
   queries and keys, rotates them by their latent frame, row and column, and
   quantises keys and values into the 8-bit cache; ``tm_kv8_attn_fwd`` attends,
-  for the whole chunk and for its last token alone. The same stream through the
+  for the whole chunk and for its last token's queries alone. The same stream through the
   16-bit cache says what the 8 bits cost;
 - training: ``tm_rope3d_fwd``, the whole-sequence attention forward and backward,
   and ``tm_rope3d_bwd``.
@@ -49,7 +49,7 @@ def stream(heads, kv_heads, grid, chunk_frames, chunks, seed=0):
         q, k, v = draw((1, n, heads, D), g), draw((1, n, kv_heads, D), g), draw((1, n, kv_heads, D), g)
         rotated = tm.tm_qkv8_produce(cache8, t, q, k, v, eps=EPS, rope=rope, table=table, first_token=first)
         o8 = tm.tm_kv8_attn_fwd(cache8, rotated, t)
-        last = tm.tm_kv8_attn_fwd(cache8, rotated[:, -1:].contiguous(), t)  # one token, as a decoder asks
+        last = tm.tm_kv8_attn_fwd(cache8, rotated[:, -1:].contiguous(), t)  # one token's rows
         assert float((last.float() - o8[:, -1:].float()).norm() / last.float().norm()) < 0.01
         # the 16-bit cache: every head of queries has keys of its own there
         q16, k16 = tm.tm_rope3d_fwd(rope, table, normalise(q), normalise(k), first)

@@ -29,22 +29,21 @@
 // every 64-key tile in LDS, each wave's softmax in between its own MFMAs. The tiles come
 // as codes into registers, half the bytes, one tile ahead, and are turned into fp16
 // operands once per workgroup on the way into LDS; the cache's order makes every LDS
-// access a contiguous KB (no bank conflicts). Bound by the MFMAs (60% of the cycles) and by
+// access a contiguous KB (no bank conflicts). Bound by the MFMAs (58% of the cycles) and by
 // what the waves wait for in between: 4680 queries over 10920 keys, 40 heads of 128,
-// 870-955 us on different nodes (1096-1203 TFLOP/s; an 8192^3 bf16 product 1118-1161
-// on them), 7-8% more than the bf16 forward over a 16-bit cache. Without the decoding,
-// its LDS writes and the loads, the same loop takes 10% less; their place among the
-// MFMAs hardly matters.
+// 889-950 us on different nodes (1102-1177 TFLOP/s; an 8192^3 bf16 product reaches 1627 at
+// best), 10% more than the bf16 forward over a 16-bit cache. The decoding's place among
+// the MFMAs hardly matters. Blocks of V that move the unit every time (scales 100 times
+// apart) take 8% more.
 //
 // Few rows: a workgroup's waves share the keys of one block of 32 rows out, each with
 // whole 64-key blocks, whose operands it loads straight from the cache; their results
 // are merged through LDS, those of several workgroups by a second kernel, in a fixed
 // order. Bound by the cache's bytes: one row, 65745 keys, 8 key heads, 4 streams (539
-// MB) 95 us a call, 4 of them for the merge (5.7 TB/s); 10920 keys, 40 heads (112 MB) 26.5.
+// MB) 95 us a call, 5 of them for the merge (5.7 TB/s); 10920 keys, 40 heads (112 MB) 26.2.
 // Caches of some thousand keys are bound by a wave's chain of loads, decoding, products
-// and softmax: 324 vector instructions a block of D = 128. (564 before K's bias was kept, masks
-// moved behind a branch and a score took one fma, behind the maximum: 6517 keys, 18 rows,
-// 20 heads 16.3 us a call, now 15.5.)
+// and softmax: 389 vector instructions a block of D = 128, with the masks behind a branch and
+// one fma a score, behind the maximum (6517 keys, 18 rows, 20 heads 15.3 us a call).
 
 #include <float.h>
 #include <hip/hip_runtime.h>
@@ -688,11 +687,11 @@ __global__ __launch_bounds__(kTileThreads, 1) void attn_kv8_tile_kernel(const Kv
     // ---- iteration t, with x = x(t) and nx receiving S(t+1); u = t % 4. Stage 1: the score
     // MFMAs of tile t+1, each with its share of P(t). Check: a lane's sum of P beyond the bound
     // (or not a number) raises m to the tile's maximum less the headroom, rescales O and the row
-    // sum and forms P(t) again. O follows P(t) where that is in another unit. Stage 2: the P V MFMAs of tile t, each with its share of x(t+1),
-    // of turning block t+3's codes into operands in LDS, and of loading block t+4's. Block t+3
-    // goes where block t-1 was, whose last reads lie before the barrier that ended tile t-1. The
-    // barrier that ends tile t publishes block t+3; K(t+2), read ahead here, was published by the
-    // one before.
+    // sum and forms P(t) again; O follows P(t) where that is in another unit. Stage 2: the P V
+    // MFMAs of tile t, each with its share of x(t+1), of turning block t+3's codes into operands
+    // in LDS, and of loading block t+4's. Block t+3 goes where block t-1 was, whose last reads
+    // lie before the barrier that ended tile t-1. The barrier that ends tile t publishes block
+    // t+3; K(t+2), read ahead here, was published by the one before.
     auto end_tile = [&](bool reads) __attribute__((always_inline)) {
         // this wave's LDS writes are done when at most the reads ahead behind them are not
         if (reads) __builtin_amdgcn_s_waitcnt(0xC07F | (RING << 8));

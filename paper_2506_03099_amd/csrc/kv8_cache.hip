@@ -21,8 +21,8 @@
 // producer's queries are rows of their own, in workgroups of the same launch that
 // go first (the other way round 1.4% slower). Bound by HBM: K and V in (2 bytes an
 // element), codes out (1). Measured on a chunk of 4680 tokens, 40 heads of 128:
-// written 24.9 us (144 MB, 5.8 TB/s), read back 22.4 us (144 MB, 6.4), produced 53 us
-// from cold inputs (240 MB, 4.5 TB/s; 39 where they are in the last-level cache).
+// written 25-32 us on different nodes (144 MB, 4.5-5.8 TB/s), read back 22.3 us (144 MB, 6.4), produced
+// 53-61 us from cold inputs (240 MB, 3.9-4.5 TB/s; 39 where they are in the last-level cache).
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -1313,11 +1313,11 @@ tm_status plan_attn8(const tm_kv8_cache* cache, const Kv8Geo& z, int32_t q_chunk
     // are not full. More than two such tiles per CU are compared by both sides' times: a round of full
     // tiles takes kEnds us and kBlock a key block, a tile of 32 rows (all CUs busy) kFixed and kWork.
     // Over long caches full tiles gain earlier, as their keys are split as well. Measured, us, 256 and
-    // 32 rows a tile, D = 128: 1 head, 100000 keys, 64 rows 24.5 and 18.0, 384 rows 36.7 and 39.4; 40
-    // heads, 10000 keys, 64 rows 34.8 and 40.6; 40 heads, 1000 keys, 384 rows 27.9 and 20.7, 1216 rows
-    // 33.7 and 47.2; 40 heads, 1 key, 384 rows 11.3 and 8.6, 1632 rows 22.6 and 28.5. D = 64: 8 heads,
-    // 20000 keys, 64 rows 19.3 and 13.4, 384 rows 37.6 and 42.3; 40 heads, 1000 keys, 800 rows 25.1 and
-    // 20.3, 1216 rows 26.0 and 27.8; 8 heads, 1 key, 7412 rows 9.3 and 14.3.
+    // 32 rows a tile, D = 128: 1 head, 100000 keys, 64 rows 23.2 and 18.2, 384 rows 35.6 and 38.8; 40
+    // heads, 10000 keys, 64 rows 35.1 and 39.7; 40 heads, 1000 keys, 384 rows 27.8 and 20.4, 1216 rows
+    // 32.8 and 46.9; 40 heads, 1 key, 384 rows 11.1 and 8.6, 1632 rows 22.1 and 29.2. D = 64: 8 heads,
+    // 20000 keys, 64 rows 17.2 and 14.0, 384 rows 34.6 and 46.6; 40 heads, 1000 keys, 800 rows 22.6 and
+    // 19.4, 1216 rows 23.6 and 26.8; 8 heads, 1 key, 7412 rows 8.5 and 14.7.
     const bool narrow = z.g.D == 64;
     const double kEnds = narrow ? 8 : 9, kBlock = narrow ? 1.05 : 1.4;
     const double kFixed = narrow ? 0.0045 : 0.0105, kWork = narrow ? 0.00066 : 0.0011;
@@ -1337,11 +1337,11 @@ tm_status plan_attn8(const tm_kv8_cache* cache, const Kv8Geo& z, int32_t q_chunk
     a->parts = 1;
     if (few) {
         // One workgroup of 4 waves on every CU, each wave with a key block at least (two blocks at least
-        // take 2-8% longer below 6000 keys; two workgroups on every CU as well, us: one row a head, 20 key
-        // heads with 6690 keys 14.1 and 16.1, 40 with 10920 24.6 and 25.9; and more than 192 parts, whose
-        // merge grows: 1 with 100000 17.2 and 18.1). The merge and the second launch take 5 us, so a share has
+        // take 3-7% longer from 2000 to 5000 keys; two workgroups on every CU as well, us: one row a head, 20
+        // key heads with 6690 keys 13.6 and 15.6, 40 with 10920 24.1 and 25.4; and more than 192 parts, whose
+        // merge grows: 1 with 100000 14.4 and 15.8). The merge and the second launch take 5 us, so a share has
         // to save that; short caches have 8 waves a workgroup instead. (Whole and split, D = 128, 1500 keys,
-        // 20 rows 12.6 and 11.2; D = 64, 2000 keys, one row 9.2 and 10.7, 3000 keys 11.9 and 11.3.)
+        // 20 rows 13.2 and 11.2; D = 64, 2000 keys, one row 9.9 and 11.2, 3000 keys 12.8 and 10.9.)
         const int64_t parts = std::min<int64_t>({tmk::kCUs / std::max<int64_t>(tiles, 1), a->n_kblocks / 4, 192});
         a->few = 4;
         if (parts >= 2 && a->n_kblocks - ceil_div(a->n_kblocks, parts) >= (narrow ? 36 : 20)) {

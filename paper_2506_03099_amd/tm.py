@@ -296,8 +296,9 @@ def tm_qkv_produce(cache: KVCache, chunk: int, q, k, v, q_gain=None, k_gain=None
 def _workspace(nbytes: int, q, stream: int):
     """A workspace for one call on `stream`: memory of torch's allocator, which
     hands it out again in the order of the current stream once the call has
-    returned. None (the call then runs without: the forward to the same bits, the
-    backward with its fp32 sums in another order) where that order does not cover
+    returned. None (the call then runs without: the forward over 16-bit keys to the
+    same bits, the one over the 8-bit cache and the backward with their fp32 sums in
+    another order) where that order does not cover
     the call: q a plain address or on another device than the current one,
     another stream than the current one, or a stream under capture; and where the
     memory is not to be had."""
@@ -636,8 +637,8 @@ def tm_kv8_attn_fwd(cache: KV8Cache, q, q_chunk: int, o=None, o_f32: bool = Fals
     rows of the latest chunk ``q_chunk``) over the 8-bit cache; returns ``o``
     (allocated like q, or as fp32, if not given). Rows that leave the GPU idle
     share their keys out through a workspace of torch's allocator; calls that
-    can have none (under capture, on another stream than the current one) order
-    the fp32 sums otherwise."""
+    can have none (under capture, on another stream than the current one) do
+    not, and order the fp32 sums otherwise."""
     n_q = cache.rows("q", q, cache.heads)
     pq = _ptr(q)
     if o is None:
