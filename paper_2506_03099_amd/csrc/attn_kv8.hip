@@ -185,7 +185,7 @@ __device__ __forceinline__ float score_factor(float cq, float ks) {
 // wave, as a block's scale is the same in every lane. O follows by an exact factor, unless that takes it
 // past the ends of fp32: so the unit is kept within 2^-kDown of the largest so far (O is at most 2^15 *
 // 127 * 2^30 in it), and a block further down counts as one of 1/8 of that, off by less than 2^-60 of the
-// largest value. Scales are 2^-67 / 127 at least, so normal numbers, or NaN, which moves nothing.
+// largest value. Scales are 2^-60 / 127 at least, so normal numbers, or NaN, which moves nothing.
 struct Unit {
     static constexpr int kDown = 64;
     int e = 0;    // (0: no block yet, and O is zero)
