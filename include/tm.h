@@ -453,6 +453,112 @@ tm_status tm_kv8_attn_fwd(const tm_kv8_cache* cache, const void* q, int32_t q_ch
                           void* o, int32_t o_f32, float* lse, void* workspace,
                           size_t workspace_bytes, hipStream_t stream);
 
+/* The rest of a block of the student around its attention (paper Sec. 4.1: the
+ * student keeps the blocks of its WAN2.1 teacher, whose branches are normalised,
+ * modulated by the timestep's vectors, and gated into the residual stream): the
+ * norms before and after a branch, and the linear layers that a branch consists of.
+ *
+ * Modulations (gates, scales, shifts) are fp32 [B, groups, width], one row for each
+ * group of group_tokens tokens (a latent frame; 1: a token): token row i of a call
+ * is the token at position first_token + i, of group (first_token + i) /
+ * group_tokens, which must be one of the groups (else TM_E_SHAPE); their gradients
+ * have zeros for groups without a token in the call. group_tokens = 0: one group,
+ * whatever the position. Widths are multiples of 8; fp32 vectors are 16-byte
+ * aligned like everything else. No output may overlap anything but where said. */
+typedef enum tm_norm { TM_NORM_NONE = 0, TM_NORM_LAYER = 1, TM_NORM_RMS = 2 } tm_norm;
+typedef enum tm_act { TM_ACT_NONE = 0, TM_ACT_GELU = 1, TM_ACT_SILU = 2 } tm_act;
+
+typedef struct tm_block_norm_desc {
+    int32_t batch;        /* B >= 1 */
+    int32_t width;        /* E: a multiple of 8, at most 20480 */
+    int32_t pre;          /* tm_norm of the stream, before the next branch */
+    int32_t post;         /* tm_norm of the branch's output y */
+    int32_t dtype;        /* tm_dtype of y and h */
+    int32_t stream_dtype; /* tm_dtype of x and r */
+    int32_t groups;       /* >= 1 */
+    int32_t group_tokens; /* >= 1, or 0 with one group */
+    float eps;            /* >= 0, of both norms */
+} tm_block_norm_desc;
+
+/* Rows of E, all arithmetic in fp32, each output rounded once:
+ *     r = x + gate * (post(y) * post_weight)
+ *     h = (pre(r) * pre_weight + pre_bias) * (1 + scale) + shift
+ * with layer(v) = (v - mean v) / sqrt(var v + eps), rms(v) = v / sqrt(mean v^2 + eps),
+ * and r as it is before its rounding. x, r: [B, n_tok, E] in stream_dtype (r may be x
+ * itself); y, h: [B, n_tok, E] in dtype; post_weight, pre_weight, pre_bias: fp32 [E];
+ * gate, scale, shift: fp32 [B, groups, E].
+ * NULL leaves out: y (then r, gate and post_weight are NULL as well, post is
+ * TM_NORM_NONE, and x stands for r), gate, any weight, pre_bias, scale and shift (both or neither).
+ * With pre TM_NORM_NONE there is no h: it and what belongs to it are NULL. n_tok = 0
+ * launches nothing. */
+tm_status tm_block_norm_fwd(const tm_block_norm_desc* desc, int32_t n_tok, int64_t first_token,
+                            const void* x, const void* y, const float* gate,
+                            const float* post_weight, const float* pre_weight,
+                            const float* pre_bias, const float* scale, const float* shift, void* r,
+                            void* h, hipStream_t stream);
+
+/* Backward pass: from the gradients dh of h and dr of r (what reaches r by other ways; NULL:
+ * none, not without pre), those of the inputs: dx (of x; in stream_dtype; may be dr
+ * itself), dy (in dtype; may be y or dh itself if y is given), dgate, dscale, dshift (fp32 [B, groups,
+ * E]), dpost_weight, dpre_weight, dpre_bias (fp32 [E]). r is the forward's r (x without
+ * y), y and the vectors its inputs (shift has no part in it). r and dh are NULL without
+ * pre, dy without y. The gradient of a vector that the forward did not have is NULL, and any other
+ * one may be (not wanted); dscale and dshift also need scale. Sums over rows are in fp32 and in a fixed order. n_tok = 0 writes zeros to
+ * the vectors' gradients.
+ * workspace: device memory of tm_block_norm_bwd_workspace() bytes (0 on invalid arguments),
+ * 16-byte aligned; needed where a vector's gradient is wanted. */
+size_t tm_block_norm_bwd_workspace(const tm_block_norm_desc* desc, int32_t n_tok, int64_t first_token);
+tm_status tm_block_norm_bwd(const tm_block_norm_desc* desc, int32_t n_tok, int64_t first_token,
+                            const void* r, const void* dh, const void* dr, const void* y,
+                            const float* gate, const float* post_weight, const float* pre_weight,
+                            const float* pre_bias, const float* scale, void* dx, void* dy,
+                            float* dgate, float* dpost_weight, float* dpre_weight, float* dpre_bias,
+                            float* dscale, float* dshift, void* workspace, size_t workspace_bytes,
+                            hipStream_t stream);
+
+typedef struct tm_linear_desc {
+    int32_t batch;        /* B >= 1 */
+    int32_t in_width;     /* K: a multiple of 8, at most 2^18 */
+    int32_t out_width;    /* N: likewise */
+    int32_t act;          /* tm_act; GELU in its tanh form */
+    int32_t out_dtype;    /* tm_dtype of o, residual and dout */
+    int32_t groups;       /* >= 1, of the gate */
+    int32_t group_tokens; /* >= 1, or 0 with one group */
+} tm_linear_desc;
+
+/* A linear layer with what follows it:
+ *     z = x W^T + bias,   o = residual + gate * act(z)
+ * x: bf16 [B, n_tok, K], weight W: bf16 [N, K], bias: fp32 [N], gate: fp32 [B, groups, N],
+ * residual, o: [B, n_tok, N] in out_dtype (o may be the residual itself). Sums and
+ * everything after them are in fp32, o is rounded once. bias, gate and residual may be
+ * NULL; pre, if not NULL, gets z in bf16 [B, n_tok, N], for the backward pass.
+ * n_tok = 0 launches nothing. workspace: device memory, 16-byte aligned, or NULL: where
+ * tiles leave CUs idle their sums are shared out through it; with fewer than tm_linear_fwd_workspace()
+ * bytes (0: the call needs none; also on invalid arguments) they are not, and the fp32
+ * sums are ordered otherwise. Either way the result is deterministic. */
+size_t tm_linear_fwd_workspace(const tm_linear_desc* desc, int32_t n_tok);
+tm_status tm_linear_fwd(const tm_linear_desc* desc, int32_t n_tok, int64_t first_token,
+                        const void* x, const void* weight, const float* bias, const float* gate,
+                        const void* residual, void* pre, void* o, void* workspace,
+                        size_t workspace_bytes, hipStream_t stream);
+
+/* Backward pass: from the gradient dout of o ([B, n_tok, N] in out_dtype, also the
+ * residual's gradient), with dz = dout * gate * act'(pre):
+ *     dx = dz W (bf16 [B, n_tok, K]),   dweight = dz^T x (bf16 [N, K]),
+ *     dbias = sums of dz over rows (fp32 [N]),
+ *     dgate = sums of dout * act(pre) over each group's rows (fp32 [B, groups, N]).
+ * Any of them may be NULL (not wanted; dgate where the forward had no gate). x is
+ * needed for dweight, weight for dx, pre (the forward's, bf16) with an activation and for
+ * dgate; else they may be NULL. dz is rounded to bf16 for the two products (not with at
+ * most 16 rows in all), sums over rows take it in fp32. All orders are fixed.
+ * n_tok = 0 writes zeros to dweight, dbias and dgate. workspace: device memory of
+ * tm_linear_bwd_workspace() bytes (0 on invalid arguments, or where none is needed), 16-byte aligned. */
+size_t tm_linear_bwd_workspace(const tm_linear_desc* desc, int32_t n_tok, int64_t first_token);
+tm_status tm_linear_bwd(const tm_linear_desc* desc, int32_t n_tok, int64_t first_token,
+                        const void* x, const void* weight, const void* dout, const float* gate,
+                        const void* pre, void* dx, void* dweight, float* dbias, float* dgate,
+                        void* workspace, size_t workspace_bytes, hipStream_t stream);
+
 /* Message of the last failing call on this thread ("" if none). */
 const char* tm_last_error(void);
 

@@ -1,0 +1,426 @@
+// The norms before and after a branch of a block, with gate, residual and modulation, for gfx950.
+//
+//     z = post(y) post_weight,  r = x + gate z,  h = (pre(r) pre_weight + pre_bias) (1 + scale) + shift
+// and the gradients of that.
+//
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "tm_device.h"
+#include "tm_internal.h"
+
+namespace tmk {
+namespace {
+
+typedef __attribute__((address_space(3))) float lds_float;
+
+// Four neighbouring elements of a row in memory, and as fp32.
+template <typename T>
+struct Four;
+template <>
+struct Four<float> {
+    typedef f32x4_t raw;
+};
+template <>
+struct Four<__bf16> {
+    typedef bf16x4_t raw;
+};
+template <typename T>
+__device__ __forceinline__ f32x4_t as_f32(typename Four<T>::raw v) {
+    return f32x4_t{static_cast<float>(v[0]), static_cast<float>(v[1]), static_cast<float>(v[2]), static_cast<float>(v[3])};
+}
+template <typename T>
+__device__ __forceinline__ typename Four<T>::raw load4(const void* p, int64_t at) {
+    return *reinterpret_cast<const typename Four<T>::raw*>(static_cast<const T*>(p) + at);
+}
+template <typename T>
+__device__ __forceinline__ void store4(void* p, int64_t at, f32x4_t v) {
+    typename Four<T>::raw w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = static_cast<T>(v[e]);
+    *reinterpret_cast<typename Four<T>::raw*>(static_cast<T*>(p) + at) = w;
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+    return v;
+}
+
+constexpr int kMaxWaves = 16;
+
+// Sums of N values over the workgroup, the same in every lane, in a fixed order. `slots`: N * kMaxWaves
+// floats that no wave of the workgroup still reads.
+template <int N>
+__device__ __forceinline__ void group_sum(float (&v)[N], lds_float* slots, int waves, int wave, int lane) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = wave_sum(v[k]);
+    if (waves == 1) return;
+    if (lane == 0) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) slots[k * kMaxWaves + wave] = v[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        float s = 0.f;
+        for (int w = 0; w < waves; ++w) s += slots[k * kMaxWaves + w];
+        v[k] = s;
+    }
+}
+
+// One row per workgroup, four neighbouring elements a lane, U times.
+template <typename S, typename A, int U>
+__global__ __launch_bounds__(1024) void block_norm_kernel(const BlockNormArgs a) {
+    __shared__ float smem[4 * kMaxWaves];
+    lds_float* const L = (lds_float*)smem;
+    const int T = blockDim.x, waves = T / 64, tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int row = blockIdx.x;
+    const int64_t base = static_cast<int64_t>(row) * a.E;
+    const int64_t mod = a.tg.row(row) * a.E;
+    f32x4_t x[U];
+    bool in[U];
+    int col[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        col[u] = (u * T + tid) * 4;
+        in[u] = col[u] < a.E;
+        x[u] = in[u] ? as_f32<S>(load4<S>(a.x, base + col[u])) : f32x4_t{};
+    }
+    // Normalised values of v over the row, in place: (v - mean) / sqrt(var + eps) with the variance from the
+    // centred values, or v / sqrt(mean of squares + eps); zeros stay where the row has ended.
+    auto normalise = [&](f32x4_t (&v)[U], int kind, lds_float* slots) __attribute__((always_inline)) {
+        if (kind == kNormLayer) {
+            float s[1] = {0.f};
+#pragma unroll
+            for (int u = 0; u < U; ++u) s[0] += (v[u][0] + v[u][1]) + (v[u][2] + v[u][3]);
+            group_sum(s, slots, waves, wave, lane);
+            const float mean = s[0] * a.inv_E;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[u][e] = in[u] ? v[u][e] - mean : 0.f;
+        }
+        float q[1] = {0.f};
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) q[0] = fmaf(v[u][e], v[u][e], q[0]);
+        group_sum(q, slots + kMaxWaves, waves, wave, lane);
+        const float by = 1.f / sqrtf(fmaf(q[0], a.inv_E, a.eps));
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[u][e] *= by;
+    };
+    if (a.y != nullptr) {
+        f32x4_t z[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) z[u] = in[u] ? as_f32<A>(load4<A>(a.y, base + col[u])) : f32x4_t{};
+        if (a.post != kNormNone) normalise(z, a.post, L);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (!in[u]) continue;
+            f32x4_t g = f32x4_t{1.f, 1.f, 1.f, 1.f};
+            if (a.post_weight != nullptr) g = load4<float>(a.post_weight, col[u]);
+            if (a.gate != nullptr) g *= load4<float>(a.gate, mod + col[u]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[u][e] = fmaf(g[e], z[u][e], x[u][e]);
+            store4<S>(a.r, base + col[u], x[u]);
+        }
+    }
+    if (a.pre == kNormNone) return;
+    normalise(x, a.pre, L + 2 * kMaxWaves);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (!in[u]) continue;
+        f32x4_t m = x[u];
+        if (a.pre_weight != nullptr) m *= load4<float>(a.pre_weight, col[u]);
+        if (a.pre_bias != nullptr) m += load4<float>(a.pre_bias, col[u]);
+        if (a.scale != nullptr) {
+            const f32x4_t sc = load4<float>(a.scale, mod + col[u]), sh = load4<float>(a.shift, mod + col[u]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m[e] = fmaf(m[e], sc[e], m[e]) + sh[e];
+        }
+        store4<A>(a.h, base + col[u], m);
+    }
+}
+
+// One part of the rows (of one group) per workgroup, one row after the other; each lane keeps the sums over
+// rows of its columns.
+template <typename S, typename A, int U>
+__global__ __launch_bounds__(1024) void block_norm_bwd_kernel(const BlockNormBwdArgs a) {
+    __shared__ float smem[2 * 8 * kMaxWaves];
+    const int T = blockDim.x, waves = T / 64, tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int32_t b, t0, t1;
+    int64_t mod;
+    a.parts.of(blockIdx.x, b, mod, t0, t1);
+    const bool has_pre = a.pre != kNormNone, has_y = a.y != nullptr, has_dr = a.dr != nullptr;
+    int col[U];
+    bool in[U];
+    f32x4_t by_pre[U], by_post[U];  // (1 + scale) pre_weight, gate post_weight
+    f32x4_t sum_dh[U], sum_dhn[U], sum_av[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        col[u] = (u * T + tid) * 4;
+        in[u] = col[u] < a.E;
+        const f32x4_t one = f32x4_t{1.f, 1.f, 1.f, 1.f};
+        by_pre[u] = by_post[u] = one;
+        if (in[u]) {
+            if (a.scale != nullptr) by_pre[u] += load4<float>(a.scale, mod * a.E + col[u]);
+            if (a.pre_weight != nullptr) by_pre[u] *= load4<float>(a.pre_weight, col[u]);
+            if (a.gate != nullptr) by_post[u] = load4<float>(a.gate, mod * a.E + col[u]);
+            if (a.post_weight != nullptr) by_post[u] *= load4<float>(a.post_weight, col[u]);
+        }
+        sum_dh[u] = sum_dhn[u] = sum_av[u] = f32x4_t{};
+    }
+    typename Four<S>::raw r_next[U], dr_next[U];
+    typename Four<A>::raw dh_next[U], y_next[U];
+    auto load_row = [&](int t) __attribute__((always_inline)) {
+        const int64_t base = (static_cast<int64_t>(b) * a.parts.n + t) * a.E;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            r_next[u] = dr_next[u] = typename Four<S>::raw{};
+            dh_next[u] = y_next[u] = typename Four<A>::raw{};
+            if (!in[u]) continue;
+            if (has_pre) {
+                r_next[u] = load4<S>(a.r, base + col[u]);
+                dh_next[u] = load4<A>(a.dh, base + col[u]);
+            }
+            if (has_dr) dr_next[u] = load4<S>(a.dr, base + col[u]);
+            if (has_y) y_next[u] = load4<A>(a.y, base + col[u]);
+        }
+    };
+    if (t0 < t1) load_row(t0);
+    for (int t = t0; t < t1; ++t) {
+        // (sums of a row in slots that the row before does not use: a wave may still read those)
+        lds_float* const L = (lds_float*)smem + (t & 1) * 8 * kMaxWaves;
+        const int64_t base = (static_cast<int64_t>(b) * a.parts.n + t) * a.E;
+        f32x4_t r[U], dx[U], dh[U], y[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            r[u] = as_f32<S>(r_next[u]);
+            dx[u] = as_f32<S>(dr_next[u]);
+            dh[u] = as_f32<A>(dh_next[u]);
+            y[u] = as_f32<A>(y_next[u]);
+        }
+        if (t + 1 < t1) load_row(t + 1);
+        const bool pre_layer = a.pre == kNormLayer, post_layer = a.post == kNormLayer;
+        float mean_t = 0.f;
+        if (pre_layer || post_layer) {
+            float s[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[0] += r[u][e];
+                    s[1] = fmaf(dh[u][e], by_pre[u][e], s[1]);
+                    s[2] += y[u][e];
+                }
+            group_sum(s, L, waves, wave, lane);
+            mean_t = pre_layer ? s[1] * a.inv_E : 0.f;
+            const float mr = pre_layer ? s[0] * a.inv_E : 0.f, my = post_layer ? s[2] * a.inv_E : 0.f;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    r[u][e] = in[u] ? r[u][e] - mr : 0.f;
+                    y[u][e] = in[u] ? y[u][e] - my : 0.f;
+                }
+        }
+        float post_by = 1.f;
+        if (has_pre || a.post != kNormNone) {
+            float s[3] = {0.f, 0.f, 0.f};  // squares of r and y, and t r
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[0] = fmaf(r[u][e], r[u][e], s[0]);
+                    s[1] = fmaf(dh[u][e] * by_pre[u][e], r[u][e], s[1]);
+                    s[2] = fmaf(y[u][e], y[u][e], s[2]);
+                }
+            group_sum(s, L + 3 * kMaxWaves, waves, wave, lane);
+            if (has_pre) {
+                const float by = 1.f / sqrtf(fmaf(s[0], a.inv_E, a.eps));
+                const float along = s[1] * by * a.inv_E;  // mean of t n
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float n = r[u][e] * by, d = dh[u][e];
+                        sum_dh[u][e] += d;
+                        sum_dhn[u][e] = fmaf(d, n, sum_dhn[u][e]);
+                        dx[u][e] = fmaf(by, fmaf(d, by_pre[u][e], -mean_t) - n * along, dx[u][e]);
+                    }
+            }
+            if (a.post != kNormNone) post_by = 1.f / sqrtf(fmaf(s[2], a.inv_E, a.eps));
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (in[u]) store4<S>(a.dx, base + col[u], dx[u]);
+        if (!has_y) continue;
+        float mean_u = 0.f, along = 0.f;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                y[u][e] *= post_by;
+                sum_av[u][e] = fmaf(dx[u][e], y[u][e], sum_av[u][e]);
+                dx[u][e] = in[u] ? dx[u][e] * by_post[u][e] : 0.f;
+            }
+        if (a.post != kNormNone) {
+            float s[2] = {0.f, 0.f};
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[0] += dx[u][e];
+                    s[1] = fmaf(dx[u][e], y[u][e], s[1]);
+                }
+            group_sum(s, L + 6 * kMaxWaves, waves, wave, lane);
+            mean_u = post_layer ? s[0] * a.inv_E : 0.f;
+            along = s[1] * a.inv_E;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            f32x4_t d;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) d[e] = post_by * ((dx[u][e] - mean_u) - y[u][e] * along);
+            if (in[u]) store4<A>(a.dy, base + col[u], d);
+        }
+    }
+    if (a.part == nullptr) return;
+    float* out = a.part + static_cast<int64_t>(blockIdx.x) * kNormSums * a.E;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (!in[u]) continue;
+        store4<float>(out, col[u], sum_dh[u]);
+        store4<float>(out, a.E + col[u], sum_dhn[u]);
+        store4<float>(out, 2 * a.E + col[u], sum_av[u]);
+    }
+}
+
+// Columns [64 i, + 64) of one sum, LANES threads a column, which share out the parts. The first workgroups
+// take the totals.
+template <int LANES>
+__global__ __launch_bounds__(64 * LANES) void column_sums_kernel(const ColumnSums a) {
+    __shared__ float sums[2][LANES][64];
+    const int blocks = (a.E + 63) / 64;
+    const int e = static_cast<int>(blockIdx.x % blocks) * 64 + threadIdx.x % 64;
+    const int l = threadIdx.x / 64;
+    const int64_t which = blockIdx.x / blocks;
+    const int64_t stride = static_cast<int64_t>(a.vectors) * a.E;
+    const bool in = e < a.E;
+    float s = 0.f, s_w = 0.f;
+    if (which < a.n_total) {
+        const TotalSum& o = a.total[which];
+        const float* at = a.part + static_cast<int64_t>(o.v) * a.E + e;
+        const int n = a.parts.count();
+        if (in) {
+            for (int i = l; i < n; i += LANES) {
+                const int g = i / a.parts.per_group, b = g / a.parts.touched;
+                const int64_t mod = static_cast<int64_t>(b) * a.parts.groups + a.parts.g0 + g % a.parts.touched;
+                const float by = o.mod != nullptr ? o.mod[mod * a.E + e] + o.add : 1.f;
+                s = fmaf(at[i * stride], by, s);
+            }
+        }
+        sums[0][l][threadIdx.x % 64] = s;
+        __syncthreads();
+        if (l > 0 || !in) return;
+        s = 0.f;
+        for (int i = 0; i < LANES; ++i) s += sums[0][i][threadIdx.x];
+        o.out[e] = s;
+        return;
+    }
+    const int64_t rows = static_cast<int64_t>(a.parts.B) * a.parts.groups;
+    const int64_t row = (which - a.n_total) % rows;
+    const GroupSum& o = a.group[(which - a.n_total) / rows];
+    const int b = static_cast<int>(row / a.parts.groups), j = static_cast<int>(row % a.parts.groups) - a.parts.g0;
+    if (in && j >= 0 && j < a.parts.touched) {
+        const int first = (b * a.parts.touched + j) * a.parts.per_group;
+        for (int i = l; i < a.parts.per_group; i += LANES) {
+            const float* at = a.part + (first + i) * stride + e;
+            s += at[static_cast<int64_t>(o.v) * a.E];
+            if (o.w >= 0) s_w += at[static_cast<int64_t>(o.w) * a.E];
+        }
+    }
+    sums[0][l][threadIdx.x % 64] = s;
+    sums[1][l][threadIdx.x % 64] = s_w;
+    __syncthreads();
+    if (l > 0 || !in) return;
+    s = s_w = 0.f;
+    for (int i = 0; i < LANES; ++i) {
+        s += sums[0][i][threadIdx.x];
+        s_w += sums[1][i][threadIdx.x];
+    }
+    if (o.mul != nullptr) s *= o.mul[e];
+    if (o.w >= 0) s = fmaf(s_w, o.mul_w[e], s);
+    o.out[row * a.E + e] = s;
+}
+
+// Elements a lane takes at a time, and lanes of a row.
+void row_shape(int E, int* U, int* threads) {
+    const int fours = E / 4;
+    *U = fours <= 256 ? 1 : fours <= 2 * 1024 ? 2 : 5;
+    *threads = ((fours + *U - 1) / *U + 63) / 64 * 64;
+}
+
+}  // namespace
+
+hipError_t launch_block_norm(const BlockNormArgs& a, bool stream_f32, bool act_f32, hipStream_t s) {
+    int U, threads;
+    row_shape(a.E, &U, &threads);
+#define TM_NORM_CASE(U_)                                                                                   \
+    if (U == U_) {                                                                                         \
+        if (stream_f32)                                                                                    \
+            return act_f32 ? launch_with(block_norm_kernel<float, float, U_>, dim3(a.rows), threads, s, a)     \
+                           : launch_with(block_norm_kernel<float, __bf16, U_>, dim3(a.rows), threads, s, a);   \
+        return act_f32 ? launch_with(block_norm_kernel<__bf16, float, U_>, dim3(a.rows), threads, s, a)        \
+                       : launch_with(block_norm_kernel<__bf16, __bf16, U_>, dim3(a.rows), threads, s, a);      \
+    }
+    TM_NORM_CASE(1)
+    TM_NORM_CASE(2)
+    TM_NORM_CASE(5)
+#undef TM_NORM_CASE
+    return hipErrorInvalidValue;
+}
+
+hipError_t launch_block_norm_bwd(const BlockNormBwdArgs& a, bool stream_f32, bool act_f32, hipStream_t s) {
+    int U, threads;
+    row_shape(a.E, &U, &threads);
+    const dim3 grid(a.parts.count());
+#define TM_NORM_CASE(U_)                                                                                 \
+    if (U == U_) {                                                                                       \
+        if (stream_f32)                                                                                  \
+            return act_f32 ? launch_with(block_norm_bwd_kernel<float, float, U_>, grid, threads, s, a)       \
+                           : launch_with(block_norm_bwd_kernel<float, __bf16, U_>, grid, threads, s, a);     \
+        return act_f32 ? launch_with(block_norm_bwd_kernel<__bf16, float, U_>, grid, threads, s, a)          \
+                       : launch_with(block_norm_bwd_kernel<__bf16, __bf16, U_>, grid, threads, s, a);        \
+    }
+    TM_NORM_CASE(1)
+    TM_NORM_CASE(2)
+    TM_NORM_CASE(5)
+#undef TM_NORM_CASE
+    return hipErrorInvalidValue;
+}
+
+hipError_t launch_column_sums(const ColumnSums& a, hipStream_t s) {
+    const int blocks = (a.E + 63) / 64;
+    const int64_t rows = static_cast<int64_t>(a.parts.B) * a.parts.groups;
+    // a column's few parts need few threads
+    ColumnSums t = a, g = a;
+    t.n_group = 0;
+    g.n_total = 0;
+    if (a.n_total > 0) {
+        const hipError_t e = launch_with(column_sums_kernel<16>, dim3(blocks * a.n_total), 1024, s, t);
+        if (e != hipSuccess) return e;
+    }
+    if (a.n_group == 0) return hipSuccess;
+    const dim3 grid(static_cast<unsigned>(blocks * a.n_group * rows));
+    return a.parts.per_group <= 4 ? launch_with(column_sums_kernel<1>, grid, 64, s, g)
+                                  : launch_with(column_sums_kernel<16>, grid, 1024, s, g);
+}
+
+}  // namespace tmk

@@ -1,0 +1,693 @@
+// Linear layers with bias, activation, gate and residual for gfx950, forward and backward.
+//
+//     z = x W^T + bias,  o = residual + gate * act(z);
+//     dz = dout gate act'(z),  dx = dz W,  dW = dz^T x,  dbias = sums of dz,  dgate = sums of dout act(z).
+//
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "tm_device.h"
+#include "tm_internal.h"
+
+namespace tmk {
+namespace {
+
+typedef __attribute__((address_space(3))) unsigned char lds_u8;
+typedef __attribute__((address_space(3))) bf16x8_t lds_bf16x8_t;
+typedef __attribute__((address_space(3))) bf16x4_t lds_bf16x4_t;
+typedef __attribute__((address_space(3))) f32x4_t lds_f32x4_t;
+
+// ---------------------------------------------------------------------------
+// An element's way from the sum of its products to the output
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ float sigmoid(float x) {
+    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * x));
+}
+
+// gelu(z) = z sigmoid(2 c (z + a z^3)), c = sqrt(2 / pi), a = 0.044715: the tanh form, (1 + tanh u) / 2 = sigmoid(2 u).
+constexpr float kGelu2C = 1.5957691216057308f, kGeluA = 0.044715f;
+__device__ __forceinline__ float activate(float z, int act) {
+    if (act == kActGelu) return z * sigmoid(kGelu2C * (z + kGeluA * z * z * z));
+    if (act == kActSilu) return z * sigmoid(z);
+    return z;
+}
+
+__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
+    const f32x4_t lo = *reinterpret_cast<const f32x4_t*>(p), hi = *reinterpret_cast<const f32x4_t*>(p + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[e] = lo[e];
+        x[4 + e] = hi[e];
+    }
+}
+__device__ __forceinline__ void load8(const __bf16* p, float (&x)[8]) {
+    const bf16x8_t v = *reinterpret_cast<const bf16x8_t*>(p);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = static_cast<float>(v[e]);
+}
+__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+    *reinterpret_cast<f32x4_t*>(p) = f32x4_t{x[0], x[1], x[2], x[3]};
+    *reinterpret_cast<f32x4_t*>(p + 4) = f32x4_t{x[4], x[5], x[6], x[7]};
+}
+__device__ __forceinline__ void store8(__bf16* p, const float (&x)[8]) {
+    bf16x8_t v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = static_cast<__bf16>(x[e]);
+    *reinterpret_cast<bf16x8_t*>(p) = v;
+}
+
+// Columns [col, col + 8) of row `row`: z holds the sums of products plus bias.
+__device__ __forceinline__ void finish8(const LinearEpilogue& ep, int N, int row, int col, float (&z)[8]) {
+    const int64_t at = static_cast<int64_t>(row) * N + col;
+    if (ep.pre != nullptr) store8(static_cast<__bf16*>(ep.pre) + at, z);
+    if (ep.act != kActNone) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] = activate(z[e], ep.act);
+    }
+    if (ep.gate != nullptr) {
+        float g[8];
+        load8(ep.gate + ep.tg.row(row) * N + col, g);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] *= g[e];
+    }
+    if (ep.residual != nullptr) {
+        float r[8];
+        if (ep.o_f32)
+            load8(static_cast<const float*>(ep.residual) + at, r);
+        else
+            load8(static_cast<const __bf16*>(ep.residual) + at, r);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] += r[e];
+    }
+    if (ep.o_f32)
+        store8(static_cast<float*>(ep.o) + at, z);
+    else
+        store8(static_cast<__bf16*>(ep.o) + at, z);
+}
+
+// ---------------------------------------------------------------------------
+// The matrix product
+// ---------------------------------------------------------------------------
+constexpr int kSlots = 4;  // stages in LDS: one read, two arriving, one just left
+
+// One operand's part of a stage, T rows (its m or n) by 32 k, 64 * T bytes, in LDS.
+// k side by side: rows of 64 bytes, 16-byte chunk c of row r at c ^ (r >> 2) % 4, so that the 16 rows that
+// one cycle of a read covers lie in 16 different bank groups. A lane's operand of the MFMA, 8 k, is a chunk.
+// TRANS: rows of one k and T elements, chunk c of row k at c ^ 4 (k % 4), so that the 4 rows by 64 bytes
+// of a cycle of the transposing read lie apart. A lane's operand is two of these reads, 4 k each.
+template <int T, bool TRANS>
+struct Tile {
+    static constexpr int kBytes = 64 * T;
+    static constexpr int kLoads = kBytes / 4096;    // 1-KB direct loads per wave
+    static constexpr int kChunks = TRANS ? T / 8 : 4;  // of a row
+    uint32_t voff[kLoads];
+
+    static __device__ __forceinline__ int swizzle(int row) { return TRANS ? 4 * (row & 3) : (row >> 2) & 3; }
+
+    // Byte offsets in memory, from the stage's first element, of the chunks that this lane brings;
+    // `rows`: of m (n) that exist from the tile's first one on. Past them the last ones come again.
+    __device__ __forceinline__ void init(int wave, int lane, int64_t ld, int rows) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int ch = (i * 4 + wave) * 64 + lane;
+            const int row = ch / kChunks, c = (ch % kChunks) ^ swizzle(row);
+            if (TRANS)
+                voff[i] = static_cast<uint32_t>(row * ld + min(c * 8, rows - 8) * 2);
+            else
+                voff[i] = static_cast<uint32_t>(min(row, rows - 1) * ld + c * 16);
+        }
+    }
+
+    // The last stage of the sum, of which only `left` < 32 k exist: through registers, zeros behind them.
+    __device__ __forceinline__ void load_rest(const unsigned char* base, lds_u8* lds, int wave, int lane, int left) const {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int ch = (i * 4 + wave) * 64 + lane;
+            const int row = ch / kChunks, c = (ch % kChunks) ^ swizzle(row);
+            f32x4_t v = f32x4_t{};
+            if ((TRANS ? row : c * 8) < left) v = *reinterpret_cast<const f32x4_t*>(base + voff[i]);
+            *(lds_f32x4_t*)(lds + ch * 16) = v;
+        }
+    }
+
+    // LDS offset of a lane's operand of rows [first + 32 i, + 32), k-step 0; at() of the others.
+    static __device__ __forceinline__ uint32_t frag0(int first, int lane) {
+        const int l32 = lane & 31, hw = lane >> 5;
+        if (!TRANS) return (first + l32) * 64 + ((hw ^ swizzle(l32)) << 4);
+        const int grp = lane >> 4, gi = lane & 15, k = 8 * hw + (gi >> 2);
+        return k * (2 * T) + ((first * 2) ^ (swizzle(k) << 4)) + (2 * (grp & 1) + ((gi & 3) >> 1)) * 16 + (gi & 1) * 8;
+    }
+    static __device__ __forceinline__ bf16x8_t frag(const lds_u8* lds, uint32_t at0, int i, int kk) {
+        if (!TRANS) return *(const lds_bf16x8_t*)(lds + (at0 ^ (kk << 5)) + i * 32 * 64);
+        const lds_u8* p = lds + (at0 ^ (i << 6)) + kk * 16 * (2 * T);
+        const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t*)p);
+        const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t*)(p + 4 * (2 * T)));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+};
+
+// Units [first, last) of the stages of all split tiles that workgroup w of W takes.
+__device__ __forceinline__ int64_t share_begin(int64_t units, int w, int W) { return units * w / W; }
+
+template <int N>
+__device__ __forceinline__ void wait_and_meet() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+template <int BT, bool AT, bool BTR>
+__global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const GemmArgs a) {
+    constexpr int WT = BT / 2;      // a wave's rows and columns
+    constexpr int F = WT / 32;      // its 32-wide blocks, either way
+    using TA = Tile<BT, AT>;
+    using TB = Tile<BT, BTR>;
+    constexpr int SLOT = TA::kBytes + TB::kBytes;
+    constexpr int LOADS = TA::kLoads + TB::kLoads;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[kSlots * SLOT];
+    lds_u8* const L = (lds_u8*)smem;
+    const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(L));
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = (wave & 1) * WT, wn = (wave >> 1) * WT;
+    const int l32 = lane & 31, hw = lane >> 5;
+
+    const bool split = static_cast<int>(blockIdx.x) >= a.whole;
+    const int sw = blockIdx.x - a.whole;
+    const int64_t units = static_cast<int64_t>(a.tiles_m * a.tiles_n - a.whole) * a.stages;
+    int64_t u = 0, u_end = 1;
+    int id = 0;
+    if (split) {
+        u = share_begin(units, sw, a.split_wgs);
+        u_end = share_begin(units, sw + 1, a.split_wgs);
+    } else {
+        id = xcd_logical_id(blockIdx.x, a.whole);
+    }
+    const uint32_t fa = TA::frag0(wm, lane), fb = TB::frag0(wn, lane) + TA::kBytes;
+    const int rest = a.K % kGemmDepth;
+
+    for (int seg = 0; u < u_end; ++seg) {
+        int s0 = 0, s1 = a.stages;
+        if (split) {
+            id = a.whole + static_cast<int>(u / a.stages);
+            s0 = static_cast<int>(u % a.stages);
+            s1 = static_cast<int>(min(static_cast<int64_t>(a.stages), s0 + (u_end - u)));
+        }
+        u += split ? s1 - s0 : 1;
+        // tiles in bands of 8 rows of tiles, so that those at work at one time share rows and columns
+        constexpr int BAND = 8;
+        const int per = BAND * a.tiles_n, band = id / per, in = id % per;
+        const int high = min(BAND, a.tiles_m - band * BAND);
+        const int m0 = (band * BAND + in % high) * BT, n0 = in / high * BT;
+
+        TA ta;
+        TB tb;
+        ta.init(wave, lane, a.lda, a.M - m0);
+        tb.init(wave, lane, a.ldb, a.N - n0);
+        // stage 0 is what K leaves over 32, if anything, so that all later ones are whole
+        auto base_a = [&](int s) __attribute__((always_inline)) {
+            const int64_t k = rest ? (s == 0 ? a.K - rest : (s - 1) * kGemmDepth) : s * kGemmDepth;
+            return uniform_ptr(a.a + (AT ? k * a.lda + m0 * int64_t(2) : m0 * a.lda + k * 2));
+        };
+        auto base_b = [&](int s) __attribute__((always_inline)) {
+            const int64_t k = rest ? (s == 0 ? a.K - rest : (s - 1) * kGemmDepth) : s * kGemmDepth;
+            return uniform_ptr(a.b + (BTR ? k * a.ldb + n0 * int64_t(2) : n0 * a.ldb + k * 2));
+        };
+        // load j of stage s into a slot
+        auto issue = [&](const void* pa, const void* pb, uint32_t slot, int j) __attribute__((always_inline)) {
+            const bool is_a = j < TA::kLoads;
+            const int i = is_a ? j : j - TA::kLoads;
+            lds_dma16(is_a ? pa : pb, is_a ? ta.voff[i] : tb.voff[i],
+                      lds_base + slot + (is_a ? 0 : TA::kBytes) + (i * 4 + wave) * 1024);
+        };
+        const int n = s1 - s0;
+        // (the slots of the last segment: all waves are through with them)
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+        for (int s = 0; s < kSlots - 1; ++s) {
+            if (s < n) {
+                const void* pa = base_a(s0 + s);
+                const void* pb = base_b(s0 + s);
+                if (rest != 0 && s0 + s == 0) {
+                    ta.load_rest(static_cast<const unsigned char*>(pa), L + s * SLOT, wave, lane, rest);
+                    tb.load_rest(static_cast<const unsigned char*>(pb), L + s * SLOT + TA::kBytes, wave, lane, rest);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < LOADS; ++j) issue(pa, pb, s * SLOT, j);
+                }
+            }
+        }
+        if (n >= kSlots - 1)
+            wait_and_meet<2 * LOADS>();
+        else
+            wait_and_meet<0>();
+
+        f32x16_t acc[F][F];
+#pragma unroll
+        for (int i = 0; i < F; ++i)
+#pragma unroll
+            for (int j = 0; j < F; ++j) acc[i][j] = f32x16_t{};
+        // a wave's operands of k-steps 0 and 1 of a stage; operand f: A's first block, B's blocks, A's others
+        bf16x8_t af[2][F], bf[2][F];
+        auto read = [&](const lds_u8* p, int kk, int f) __attribute__((always_inline)) {
+            if (f == 0)
+                af[kk][0] = TA::frag(p, fa, 0, kk);
+            else if (f <= F)
+                bf[kk][f - 1] = TB::frag(p, fb, f - 1, kk);
+            else
+                af[kk][f - F] = TA::frag(p, fa, f - F, kk);
+        };
+#pragma unroll
+        for (int f = 0; f < 2 * F; ++f) read(L, 0, f);
+        // Stage at slot `at`: the MFMAs of k-step 0, under them the reads of k-step 1 and the loads of the
+        // stage three ahead into the slot that was left last; the wait for the next stage; the MFMAs of
+        // k-step 1, under them the reads of the next stage's k-step 0.
+        auto stage = [&](auto more, int s, uint32_t at) __attribute__((always_inline)) {
+            constexpr bool MORE = decltype(more)::value;
+            const lds_u8* p = L + at;
+            const uint32_t next = at + SLOT == kSlots * SLOT ? 0 : at + SLOT;
+            const uint32_t left = at == 0 ? (kSlots - 1) * SLOT : at - SLOT;
+            const void *pa = nullptr, *pb = nullptr;
+            if (MORE) {
+                pa = base_a(s + kSlots - 1);
+                pb = base_b(s + kSlots - 1);
+            }
+            constexpr int MEET = F * F - F;  // MFMA of k-step 0 that the wait comes behind
+#pragma unroll
+            for (int m = 0; m < F * F; ++m) {
+                acc[m / F][m % F] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[0][m % F], af[0][m / F], acc[m / F][m % F], 0, 0, 0);
+                if (F == 4) {
+                    if (m < 2 * F) read(p, 1, m);
+                    if (MORE && m < LOADS) issue(pa, pb, left, m);
+                } else if (m < F) {
+                    read(p, 1, 2 * m);
+                    read(p, 1, 2 * m + 1);
+                    if (MORE) {
+                        issue(pa, pb, left, 2 * m);
+                        issue(pa, pb, left, 2 * m + 1);
+                    }
+                }
+                if (m == MEET) {
+                    if (MORE)
+                        wait_and_meet<2 * LOADS>();
+                    else
+                        wait_and_meet<0>();
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            const lds_u8* q = L + next;
+#pragma unroll
+            for (int m = 0; m < F * F; ++m) {
+                acc[m / F][m % F] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[1][m % F], af[1][m / F], acc[m / F][m % F], 0, 0, 0);
+                if (m < 2 * F) read(q, 0, m);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        uint32_t at = 0;
+        int s = s0;
+        for (; s + kSlots - 1 < s1; ++s) {
+            stage(std::true_type{}, s, at);
+            at = at + SLOT == kSlots * SLOT ? 0 : at + SLOT;
+        }
+        for (; s < s1; ++s) {
+            stage(std::false_type{}, s, at);
+            at = at + SLOT == kSlots * SLOT ? 0 : at + SLOT;
+        }
+
+        // Register 4 g + e of acc[i][j]: row wm + 32 i + l32, column wn + 32 j + 8 g + 4 hw + e. Through the
+        // wave's own share of LDS (chunk c of row r at c ^ r % 16), 32 rows at a time, into whole rows.
+        constexpr int ROWB = WT * 4, LPR = WT / 8, RPP = 64 / LPR;
+        lds_u8* const own = L + wave * (32 * ROWB);
+        const int col = n0 + wn + (lane % LPR) * 8;
+        float bias[8] = {};
+        if (!split && a.ep.bias != nullptr && col < a.N) load8(a.ep.bias + col, bias);
+        float* part = split ? a.part + (static_cast<int64_t>(sw) * 2 + seg) * (BT * BT) : nullptr;
+#pragma unroll
+        for (int i = 0; i < F; ++i) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+            for (int j = 0; j < F; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *(lds_f32x4_t*)(own + l32 * ROWB + (((8 * j + 2 * g + hw) ^ (l32 & 15)) << 4)) =
+                        f32x4_t{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll 2
+            for (int p = 0; p < 32 / RPP; ++p) {
+                const int r = p * RPP + lane / LPR, c = 2 * (lane % LPR);
+                const f32x4_t lo = *(const lds_f32x4_t*)(own + r * ROWB + ((c ^ (r & 15)) << 4));
+                const f32x4_t hi = *(const lds_f32x4_t*)(own + r * ROWB + (((c + 1) ^ (r & 15)) << 4));
+                float z[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                const int in_tile = wm + 32 * i + r;
+                if (split) {
+                    store8(part + in_tile * BT + wn + (lane % LPR) * 8, z);
+                } else if (m0 + in_tile < a.M && col < a.N) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[e] += bias[e];
+                    finish8(a.ep, a.N, m0 + in_tile, col, z);
+                }
+            }
+        }
+    }
+}
+
+// The split tiles' sums of products from their parts, in the order of k, and the rest of the way. A thread
+// takes 8 columns of a row.
+template <int BT>
+__global__ __launch_bounds__(256) void gemm_merge_kernel(const GemmArgs a) {
+    constexpr int LPR = BT / 8, ROWS = 256 / LPR, PER = BT / ROWS;
+    const int t = blockIdx.x / PER, id = a.whole + t;
+    constexpr int BAND = 8;
+    const int per = BAND * a.tiles_n, band = id / per, in = id % per;
+    const int high = min(BAND, a.tiles_m - band * BAND);
+    const int r = (blockIdx.x % PER) * ROWS + threadIdx.x / LPR, c = (threadIdx.x % LPR) * 8;
+    const int row = (band * BAND + in % high) * BT + r, col = in / high * BT + c;
+    if (row >= a.M || col >= a.N) return;
+    const int64_t units = static_cast<int64_t>(a.tiles_m * a.tiles_n - a.whole) * a.stages;
+    const int64_t u0 = static_cast<int64_t>(t) * a.stages, u1 = u0 + a.stages;
+    const int W = a.split_wgs;
+    int w = static_cast<int>(u0 * W / units);
+    while (share_begin(units, w + 1, W) <= u0) ++w;
+    float z[8] = {};
+    if (a.ep.bias != nullptr) load8(a.ep.bias + col, z);
+    float sum[8] = {};
+    for (; w < W; ++w) {
+        const int64_t b = share_begin(units, w, W);
+        if (b >= u1) break;
+        float x[8];
+        load8(a.part + (static_cast<int64_t>(w) * 2 + (b < u0 ? 1 : 0)) * (BT * BT) + r * BT + c, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += x[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e] += sum[e];
+    finish8(a.ep, a.N, row, col, z);
+}
+
+template <int BT, bool AT, bool BTR>
+hipError_t launch_tiles(const GemmArgs& a, hipStream_t s) {
+    const int rest = a.tiles_m * a.tiles_n - a.whole;
+    hipError_t e = launch_with(gemm_kernel<BT, AT, BTR>, dim3(a.whole + (rest ? a.split_wgs : 0)), 256, s, a);
+    if (e != hipSuccess || rest == 0) return e;
+    constexpr int PER = BT / (256 / (BT / 8));
+    return launch_with(gemm_merge_kernel<BT>, dim3(rest * PER), 256, s, a);
+}
+
+// ---------------------------------------------------------------------------
+// Few rows: W streams by once
+// ---------------------------------------------------------------------------
+// A workgroup takes 16 columns of the output (rows of W) and its NW waves share K in runs of 64:
+// v_mfma_f32_16x16x32_bf16 with W as the first operand and the rows of x as the second. A lane brings
+// 32 neighbouring bytes of its row of W, the k of two MFMAs, so that 4 lanes read a whole line; which k an
+// operand's element is does not matter as long as x's are the same. Rows that do not exist repeat the last one.
+template <int NW>
+__global__ __launch_bounds__(NW * 64) void few_rows_kernel(const FewRowsArgs a) {
+    __shared__ float sums[NW][16][17];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n0 = blockIdx.x * 16;
+    const int64_t K = a.K;
+    const __bf16* w = static_cast<const __bf16*>(a.w) + min(n0 + (lane & 15), a.N - 1) * K + (lane >> 4) * 16;
+    const __bf16* x = static_cast<const __bf16*>(a.x) + min(lane & 15, a.rows - 1) * K + (lane >> 4) * 16;
+    f32x4_t acc[2] = {f32x4_t{}, f32x4_t{}};
+    const int whole = a.K / 64;
+    constexpr int U = 4;
+    int i = wave;
+    for (; i + (U - 1) * NW < whole; i += U * NW) {
+        bf16x8_t wf[U][2], xf[U][2];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) wf[u][h] = *reinterpret_cast<const bf16x8_t*>(w + (i + u * NW) * 64 + h * 8);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) xf[u][h] = *reinterpret_cast<const bf16x8_t*>(x + (i + u * NW) * 64 + h * 8);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                acc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[u][h], xf[u][h], acc[h], 0, 0, 0);
+    }
+    // the runs that are left, the last one perhaps with its first k only
+    for (; i * 64 < a.K; i += NW) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            bf16x8_t wf = bf16x8_t{}, xf = bf16x8_t{};
+            if (i * 64 + (lane >> 4) * 16 + h * 8 < a.K) {
+                wf = *reinterpret_cast<const bf16x8_t*>(w + i * 64 + h * 8);
+                xf = *reinterpret_cast<const bf16x8_t*>(x + i * 64 + h * 8);
+            }
+            acc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, xf, acc[h], 0, 0, 0);
+        }
+    }
+    // register e of a lane: column 4 (lane / 16) + e, row lane % 16
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sums[wave][lane & 15][4 * (lane >> 4) + e] = acc[0][e] + acc[1][e];
+    __syncthreads();
+    if (tid >= 256) return;
+    const int row = tid >> 4, col = n0 + (tid & 15);
+    if (row >= a.rows || col >= a.N) return;
+    float z = a.ep.bias != nullptr ? a.ep.bias[col] : 0.f, sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < NW; ++v) sum += sums[v][row][tid & 15];
+    z += sum;
+    const int64_t at = static_cast<int64_t>(row) * a.N + col;
+    if (a.ep.pre != nullptr) static_cast<__bf16*>(a.ep.pre)[at] = static_cast<__bf16>(z);
+    z = activate(z, a.ep.act);
+    if (a.ep.gate != nullptr) z *= a.ep.gate[a.ep.tg.row(row) * a.N + col];
+    if (a.ep.residual != nullptr)
+        z += a.ep.o_f32 ? static_cast<const float*>(a.ep.residual)[at]
+                        : static_cast<float>(static_cast<const __bf16*>(a.ep.residual)[at]);
+    if (a.ep.o_f32)
+        static_cast<float*>(a.ep.o)[at] = z;
+    else
+        static_cast<__bf16*>(a.ep.o)[at] = static_cast<__bf16>(z);
+}
+
+// ---------------------------------------------------------------------------
+// Backward: the gradient of the sums of products, and its sums over rows
+// ---------------------------------------------------------------------------
+// d/dz of the activation: gelu with s = sigmoid(u), u = 2 c (z + a z^3): s + z s (1 - s) u'; silu: s + z s (1 - s).
+// (z s (1 - s) is 0 wherever s is 0 or 1, also where u' has grown past all bounds.)
+__device__ __forceinline__ void activate_both(float z, int act, float& value, float& slope) {
+    value = z;
+    slope = 1.f;
+    if (act == kActNone) return;
+    const float u = act == kActGelu ? kGelu2C * (z + kGeluA * z * z * z) : z;
+    const float du = act == kActGelu ? kGelu2C * (1.f + 3.f * kGeluA * z * z) : 1.f;
+    const float s = sigmoid(u), c = sigmoid(-u);
+    value = z * s;
+    const float t = s * c;
+    slope = t > 0.f ? fmaf(z * t, du, s) : s;
+}
+
+// One part of the rows per workgroup and 256 columns: 32 lanes of 8 columns, 8 rows at a time.
+__global__ __launch_bounds__(256) void linear_dz_kernel(const LinearDzArgs a) {
+    __shared__ float sums[8][256];
+    int32_t b, t0, t1;
+    int64_t mod;
+    a.parts.of(blockIdx.x, b, mod, t0, t1);
+    const int lane = threadIdx.x % 32, line = threadIdx.x / 32;
+    const int col = blockIdx.y * 256 + lane * 8;
+    const bool in = col < a.N;
+    float gate[8], sum_dz[8] = {}, sum_u[8] = {};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) gate[e] = 1.f;
+    if (in && a.gate != nullptr) load8(a.gate + mod * a.N + col, gate);
+    if (in) {
+#pragma unroll 2
+        for (int t = t0 + line; t < t1; t += 8) {
+            const int64_t row = static_cast<int64_t>(b) * a.parts.n + t, at = row * a.N + col;
+            float d[8], z[8] = {};
+            if (a.dout_f32)
+                load8(static_cast<const float*>(a.dout) + at, d);
+            else
+                load8(static_cast<const __bf16*>(a.dout) + at, d);
+            if (a.pre != nullptr) load8(static_cast<const __bf16*>(a.pre) + at, z);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float value, slope;
+                activate_both(z[e], a.act, value, slope);
+                sum_u[e] = fmaf(d[e], value, sum_u[e]);
+                d[e] *= gate[e] * slope;
+                sum_dz[e] += d[e];
+            }
+            if (a.dz != nullptr) store8(static_cast<__bf16*>(a.dz) + at, d);
+            if (a.dz_few != nullptr) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) a.dz_few[static_cast<int64_t>(col + e) * a.R + row] = d[e];
+            }
+        }
+        // (the rows that fill dz_few up to R)
+        if (a.dz_few != nullptr && blockIdx.x == 0) {
+            for (int row = a.parts.B * a.parts.n + line; row < a.R; row += 8)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) a.dz_few[static_cast<int64_t>(col + e) * a.R + row] = 0.f;
+        }
+    }
+    if (a.part == nullptr) return;
+    float* out = a.part + static_cast<int64_t>(blockIdx.x) * kLinearSums * a.N;
+    for (int v = 0; v < (a.gate_sums ? 2 : 1); ++v) {
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sums[line][lane * 8 + e] = v == 0 ? sum_dz[e] : sum_u[e];
+        __syncthreads();
+        const int c = blockIdx.y * 256 + threadIdx.x;
+        if (c < a.N) {
+            float s = 0.f;
+#pragma unroll
+            for (int l = 0; l < 8; ++l) s += sums[l][threadIdx.x];
+            out[v * a.N + c] = s;
+        }
+    }
+}
+
+// dx of R rows: 512 columns per wave, the 4 waves of a workgroup and the shares of the grid deal out N; the
+// gradients are the same in every lane. In fp32: with so few rows nothing would average the roundings of dz.
+template <int R>
+__global__ __launch_bounds__(256) void few_rows_dx_kernel(const FewRowsBwdArgs a) {
+    __shared__ float sums[3][64][9];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = blockIdx.x * 512 + lane * 8;
+    const int piece = blockIdx.y * 4 + wave, pieces = a.shares * 4;
+    const int n0 = static_cast<int>(static_cast<int64_t>(a.N) * piece / pieces);
+    const int n1 = static_cast<int>(static_cast<int64_t>(a.N) * (piece + 1) / pieces);
+    float acc[R][8];
+#pragma unroll
+    for (int m = 0; m < R; ++m)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[m][e] = 0.f;
+    const __bf16* w = static_cast<const __bf16*>(a.w) + min(col, a.K - 8);
+#pragma unroll 4
+    for (int n = n0; n < n1; ++n) {
+        float x[8];
+        load8(w + static_cast<int64_t>(n) * a.K, x);
+        const float* g = a.dz + static_cast<int64_t>(n) * R;
+#pragma unroll
+        for (int m = 0; m < R; ++m)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[m][e] = fmaf(g[m], x[e], acc[m][e]);
+    }
+#pragma unroll
+    for (int m = 0; m < R; ++m) {
+        __syncthreads();
+        if (wave > 0) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sums[wave - 1][lane][e] = acc[m][e];
+        }
+        __syncthreads();
+        if (wave == 0 && col < a.K) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                acc[m][e] = ((acc[m][e] + sums[0][lane][e]) + sums[1][lane][e]) + sums[2][lane][e];
+            store8(a.part + (static_cast<int64_t>(blockIdx.y) * R + m) * a.K + col, acc[m]);
+        }
+    }
+}
+
+__global__ __launch_bounds__(256) void few_rows_dx_merge_kernel(const FewRowsBwdArgs a) {
+    const int64_t at = blockIdx.x * int64_t(256) + threadIdx.x;  // groups of 8 columns
+    const int per = a.K / 8;
+    if (at >= static_cast<int64_t>(a.rows) * per) return;
+    const int64_t row = at / per, col = at % per * 8;
+    float s[8] = {};
+#pragma unroll 4
+    for (int p = 0; p < a.shares; ++p) {
+        float x[8];
+        load8(a.part + (static_cast<int64_t>(p) * a.R + row) * a.K + col, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] += x[e];
+    }
+    store8(static_cast<__bf16*>(a.dx) + row * a.K + col, s);
+}
+
+// dW of R rows: 8 columns a lane, whose R values of x stay in registers over kDwRows rows of dW.
+constexpr int kDwRows = 16;
+template <int R>
+__global__ __launch_bounds__(256) void few_rows_dw_kernel(const FewRowsBwdArgs a) {
+    const int col = (blockIdx.x * 256 + threadIdx.x) * 8;
+    if (col >= a.K) return;
+    float x[R][8];
+#pragma unroll
+    for (int m = 0; m < R; ++m) load8(static_cast<const __bf16*>(a.x) + min(m, a.rows - 1) * static_cast<int64_t>(a.K) + col, x[m]);
+    const int n1 = min(a.N, (static_cast<int>(blockIdx.y) + 1) * kDwRows);
+    for (int n = blockIdx.y * kDwRows; n < n1; ++n) {
+        const float* g = a.dz + static_cast<int64_t>(n) * R;
+        float d[8] = {};
+#pragma unroll
+        for (int m = 0; m < R; ++m) {
+            if (m < a.rows) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) d[e] = fmaf(g[m], x[m][e], d[e]);
+            }
+        }
+        store8(static_cast<__bf16*>(a.dw) + static_cast<int64_t>(n) * a.K + col, d);
+    }
+}
+
+__global__ __launch_bounds__(256) void zero_kernel(uint32_t* p, int64_t n) {
+    for (int64_t i = blockIdx.x * int64_t(256) + threadIdx.x; i < n; i += gridDim.x * int64_t(256)) p[i] = 0;
+}
+
+}  // namespace
+
+hipError_t launch_gemm(const GemmArgs& a, int tile, bool a_trans, bool b_trans, hipStream_t s) {
+#define TM_GEMM_CASE(T_, A_, B_) \
+    if (tile == T_ && a_trans == A_ && b_trans == B_) return launch_tiles<T_, A_, B_>(a, s);
+    TM_GEMM_CASE(256, false, false)
+    TM_GEMM_CASE(128, false, false)
+    TM_GEMM_CASE(256, false, true)
+    TM_GEMM_CASE(128, false, true)
+    TM_GEMM_CASE(256, true, true)
+    TM_GEMM_CASE(128, true, true)
+#undef TM_GEMM_CASE
+    return hipErrorInvalidValue;
+}
+
+hipError_t launch_few_rows(const FewRowsArgs& a, hipStream_t s) {
+    const dim3 grid((a.N + 15) / 16);
+    // as many waves as there is work for: 4 a workgroup where the workgroups fill the CUs
+    return grid.x >= 4 * kCUs ? launch_with(few_rows_kernel<4>, grid, 256, s, a)
+                              : launch_with(few_rows_kernel<16>, grid, 1024, s, a);
+}
+
+hipError_t launch_linear_dz(const LinearDzArgs& a, hipStream_t s) {
+    return launch_with(linear_dz_kernel, dim3(a.parts.count(), (a.N + 255) / 256), 256, s, a);
+}
+
+template <int R>
+static hipError_t launch_few_bwd(const FewRowsBwdArgs& a, hipStream_t s) {
+    hipError_t e = hipSuccess;
+    if (a.dx != nullptr) {
+        e = launch_with(few_rows_dx_kernel<R>, dim3((a.K + 511) / 512, a.shares), 256, s, a);
+        if (e != hipSuccess) return e;
+        e = launch_with(few_rows_dx_merge_kernel, dim3((static_cast<unsigned>(a.rows) * (a.K / 8) + 255) / 256), 256, s, a);
+        if (e != hipSuccess) return e;
+    }
+    if (a.dw != nullptr)
+        e = launch_with(few_rows_dw_kernel<R>, dim3((a.K + 2047) / 2048, (a.N + kDwRows - 1) / kDwRows), 256, s, a);
+    return e;
+}
+
+hipError_t launch_few_rows_bwd(const FewRowsBwdArgs& a, hipStream_t s) {
+    switch (a.R) {
+        case 1: return launch_few_bwd<1>(a, s);
+        case 2: return launch_few_bwd<2>(a, s);
+        case 4: return launch_few_bwd<4>(a, s);
+        case 8: return launch_few_bwd<8>(a, s);
+        case 16: return launch_few_bwd<16>(a, s);
+    }
+    return hipErrorInvalidValue;
+}
+
+hipError_t launch_zero(void* p, int64_t n, hipStream_t s) {
+    if (n == 0) return hipSuccess;
+    const int64_t blocks = (n + 255) / 256;
+    hipLaunchKernelGGL(zero_kernel, dim3(static_cast<unsigned>(blocks < 4096 ? blocks : 4096)), dim3(256), 0, s,
+                       static_cast<uint32_t*>(p), n);
+    return hipGetLastError();
+}
+
+}  // namespace tmk

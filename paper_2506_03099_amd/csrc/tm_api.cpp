@@ -19,6 +19,7 @@
 #include <cstdarg>
 #include <cstdint>
 #include <cstdio>
+#include <initializer_list>
 #include <new>
 #include <utility>
 
@@ -1535,6 +1536,589 @@ tm_status tm_kv8_attn_fwd(const tm_kv8_cache* cache, const void* q, int32_t q_ch
                           int32_t o_f32, float* lse, void* workspace, size_t workspace_bytes,
                           hipStream_t stream) {
     return attn8(cache, q, q_chunk, n_q, o, o_f32 != 0, lse, workspace, workspace_bytes, stream);
+}
+
+}  // extern "C"
+
+// ---- the block around the attention: norms with gate and residual, linear layers
+
+namespace {
+
+// What the tensors of one call cover, to check them and that no output overlaps anything.
+class Spans {
+    struct Span {
+        const void* p;
+        size_t bytes;
+        const char* name;
+        bool out;
+    };
+    Span span_[24];
+    int n_ = 0;
+    PtrChecks check_;
+
+public:
+    // The pointer of a tensor of the call (null: not there).
+    tm_status add(const void* p, size_t bytes, const char* name, bool out = false) {
+        if (p == nullptr) return TM_OK;
+        const tm_status st = check_(p, bytes, name);
+        if (st != TM_OK) return st;
+        span_[n_++] = Span{p, bytes, name, out};
+        return TM_OK;
+    }
+    // No output overlaps another tensor, but for those that are the same as the tensor named.
+    tm_status apart(std::initializer_list<std::pair<const void*, const void*>> same) const {
+        for (int i = 0; i < n_; ++i) {
+            if (!span_[i].out) continue;
+            for (int j = 0; j < n_; ++j) {
+                if (i == j || (span_[j].out && j < i)) continue;
+                if (!overlaps(span_[i].p, span_[i].bytes, span_[j].p, span_[j].bytes)) continue;
+                bool fine = false;
+                for (const auto& s : same)
+                    fine |= span_[i].p == s.first && span_[j].p == s.second && s.first == s.second && !span_[j].out;
+                if (!fine) return fail(TM_E_ARG, "%s overlaps %s", span_[i].name, span_[j].name);
+            }
+        }
+        return TM_OK;
+    }
+};
+
+// The rows of a call and the rows of its modulations.
+struct Run {
+    int64_t B, n, rows, groups;
+    int64_t len, f0, g0, touched;  // as in RowParts
+};
+
+tm_status check_run(int32_t batch, int32_t groups, int32_t group_tokens, int32_t n_tok, int64_t first_token, Run* r) {
+    if (batch < 1 || batch > 65535) return fail(TM_E_SHAPE, "batch must be in [1, 65535]");
+    if (groups < 1 || group_tokens < 0) return fail(TM_E_SHAPE, "groups must be >= 1 and group_tokens >= 0");
+    if (group_tokens == 0 && groups != 1) return fail(TM_E_SHAPE, "group_tokens 0 goes with one group");
+    if (n_tok < 0) return fail(TM_E_SHAPE, "n_tok must be >= 0");
+    if (first_token < 0 || first_token > kMaxTokens || n_tok > kMaxTokens - first_token)
+        return fail(TM_E_SHAPE, "positions must lie in [0, 2^30]");
+    r->B = batch;
+    r->n = n_tok;
+    r->rows = r->B * r->n;
+    r->groups = groups;
+    if (r->rows > kMaxTokens) return fail(TM_E_SHAPE, "more than 2^30 rows");
+    r->len = std::max<int64_t>(r->n, 1);
+    r->f0 = r->g0 = 0;
+    r->touched = 1;
+    if (group_tokens > 0) {
+        const int64_t last = n_tok > 0 ? (first_token + n_tok - 1) / group_tokens : 0;
+        if (last >= groups)
+            return fail(TM_E_SHAPE, "tokens from %lld on lie past the %d groups of %d",
+                        static_cast<long long>(first_token), groups, group_tokens);
+        r->g0 = n_tok > 0 ? first_token / group_tokens : 0;
+        r->touched = last - r->g0 + 1;
+        if (r->touched > 1) {
+            r->len = group_tokens;
+            r->f0 = first_token % group_tokens;
+        }
+    }
+    return TM_OK;
+}
+
+tmk::TokenGroups token_groups(const Run& r) {
+    tmk::TokenGroups t;
+    t.n = int32_t(r.n);
+    t.groups = int32_t(r.groups);
+    t.f0 = int32_t(r.f0);
+    t.g0 = int32_t(r.g0);
+    t.by_n = tmk::FastDiv(uint32_t(std::max<int64_t>(r.n, 1)));
+    t.by_group = tmk::FastDiv(r.touched > 1 ? uint32_t(r.len) : 0x7fffffffu);
+    return t;
+}
+
+// About `want` parts, none of them of fewer than `least` rows where a group has that many.
+tmk::RowParts row_parts(const Run& r, int64_t want, int64_t least) {
+    tmk::RowParts p{};
+    p.B = int32_t(r.B);
+    p.n = int32_t(r.n);
+    p.len = int32_t(r.len);
+    p.f0 = int32_t(r.f0);
+    p.touched = int32_t(r.touched);
+    p.g0 = int32_t(r.g0);
+    p.groups = int32_t(r.groups);
+    const int64_t rows = std::min(std::max(ceil_div(r.rows, want), least), r.len);
+    p.per_group = int32_t(ceil_div(r.len, rows));
+    p.rows_per_part = int32_t(ceil_div(r.len, p.per_group));
+    return p;
+}
+
+tm_status check_modulation(int64_t B, int64_t groups, int64_t width) {
+    if (B * groups > (int64_t(1) << 30) / width)
+        return fail(TM_E_SHAPE, "modulations of more than 2^30 elements");
+    return TM_OK;
+}
+
+struct NormGeo {
+    Run run;
+    int64_t E;
+    size_t act, stream;  // bytes of an element
+    tmk::RowParts parts;
+    size_t part_bytes;
+};
+
+tm_status check_norm(const tm_block_norm_desc* d, int32_t n_tok, int64_t first_token, NormGeo* g) {
+    if (d == nullptr) return fail(TM_E_ARG, "descriptor is NULL");
+    if ((d->dtype != TM_F32 && d->dtype != TM_BF16) || (d->stream_dtype != TM_F32 && d->stream_dtype != TM_BF16))
+        return fail(TM_E_DTYPE, "dtypes %d, %d are neither TM_F32 nor TM_BF16", d->dtype, d->stream_dtype);
+    if (d->width < 8 || d->width % 8 != 0 || d->width > tmk::kMaxNormWidth)
+        return fail(TM_E_SHAPE, "width %d is no multiple of 8 in [8, %d]", d->width, tmk::kMaxNormWidth);
+    if (d->pre < TM_NORM_NONE || d->pre > TM_NORM_RMS || d->post < TM_NORM_NONE || d->post > TM_NORM_RMS)
+        return fail(TM_E_ARG, "unknown norm");
+    if (!std::isfinite(d->eps) || d->eps < 0.f) return fail(TM_E_ARG, "eps must be finite and >= 0");
+    tm_status st = check_run(d->batch, d->groups, d->group_tokens, n_tok, first_token, &g->run);
+    if (st != TM_OK) return st;
+    g->E = d->width;
+    if ((st = check_modulation(d->batch, d->groups, g->E)) != TM_OK) return st;
+    g->act = d->dtype == TM_BF16 ? 2 : 4;
+    g->stream = d->stream_dtype == TM_BF16 ? 2 : 4;
+    // two workgroups a CU, but 8 rows at least to share a part's sums
+    g->parts = row_parts(g->run, 2 * tmk::kCUs, 8);
+    g->part_bytes = size_t(g->parts.count()) * tmk::kNormSums * size_t(g->E) * 4;
+    return TM_OK;
+}
+
+// Which of a block norm's tensors go together.
+tm_status check_norm_set(const tm_block_norm_desc* d, const void* y, const void* gate, const void* post_weight,
+                         const void* pre_weight, const void* pre_bias, const void* scale) {
+    if (y == nullptr && (gate != nullptr || post_weight != nullptr || d->post != TM_NORM_NONE))
+        return fail(TM_E_ARG, "gate, post_weight and post need y");
+    if (d->pre == TM_NORM_NONE && (pre_weight != nullptr || pre_bias != nullptr || scale != nullptr))
+        return fail(TM_E_ARG, "pre_weight, pre_bias, scale and shift need a norm before the block");
+    if (y == nullptr && d->pre == TM_NORM_NONE) return fail(TM_E_ARG, "neither y nor a norm: nothing to do");
+    return TM_OK;
+}
+
+constexpr size_t kAlign = 256;
+size_t aligned(size_t n) { return (n + kAlign - 1) / kAlign * kAlign; }
+
+// A linear layer's sizes, checked.
+struct LinearGeo {
+    Run run;
+    int64_t K, N;
+    size_t out;  // bytes of an element of o
+};
+
+tm_status check_linear(const tm_linear_desc* d, int32_t n_tok, int64_t first_token, LinearGeo* g) {
+    if (d == nullptr) return fail(TM_E_ARG, "descriptor is NULL");
+    if (d->out_dtype != TM_F32 && d->out_dtype != TM_BF16)
+        return fail(TM_E_DTYPE, "out_dtype %d is neither TM_F32 nor TM_BF16", d->out_dtype);
+    constexpr int32_t kMost = 1 << 18;
+    for (const int32_t w : {d->in_width, d->out_width})
+        if (w < 8 || w % 8 != 0 || w > kMost) return fail(TM_E_SHAPE, "width %d is no multiple of 8 in [8, 2^18]", w);
+    if (d->act < TM_ACT_NONE || d->act > TM_ACT_SILU) return fail(TM_E_ARG, "unknown activation");
+    tm_status st = check_run(d->batch, d->groups, d->group_tokens, n_tok, first_token, &g->run);
+    if (st != TM_OK) return st;
+    g->K = d->in_width;
+    g->N = d->out_width;
+    if ((st = check_modulation(d->batch, d->groups, g->N)) != TM_OK) return st;
+    g->out = d->out_dtype == TM_BF16 ? 2 : 4;
+    return TM_OK;
+}
+
+// Tiles of a product of M x N sums of K, and how many of them are split.
+struct GemmPlan {
+    int tile;
+    int64_t tiles_m, tiles_n, stages, whole, split_wgs;
+    size_t part_bytes() const {
+        return tiles_m * tiles_n == whole ? 0 : size_t(split_wgs) * 2 * size_t(tile) * size_t(tile) * 4;
+    }
+};
+
+GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool may_split) {
+    GemmPlan best{};
+    double best_cost = 0;
+    for (const int tile : {256, 128}) {
+        GemmPlan p{};
+        p.tile = tile;
+        p.tiles_m = ceil_div(M, tile);
+        p.tiles_n = ceil_div(N, tile);
+        p.stages = ceil_div(K, tmk::kGemmDepth);
+        const int64_t tiles = p.tiles_m * p.tiles_n;
+        const int64_t at_once = tile == 256 ? tmk::kCUs : 2 * tmk::kCUs;
+        // cycles of a stage with the chip full, and beside the stages: a tile's start and end, a merge's launch
+        const double stage = tile == 256 ? 1100 : 700, ends = tile == 256 ? 8000 : 5000, merge = 12000;
+        p.whole = tiles;
+        double cost = double(ceil_div(tiles, at_once)) * (double(p.stages) * stage + ends);
+        const int64_t rest = tiles % at_once;
+        // (at least 8 stages a workgroup)
+        const int64_t wgs = std::min(at_once, rest * p.stages / 8);
+        if (may_split && rest > 0 && wgs > rest) {
+            const double with = double(tiles / at_once) * (double(p.stages) * stage + ends) +
+                                double(rest * p.stages) / double(wgs) * stage + ends + merge;
+            if (with < cost) {
+                cost = with;
+                p.whole = tiles - rest;
+                p.split_wgs = wgs;
+            }
+        }
+        if (best.tile == 0 || cost < best_cost) {
+            best = p;
+            best_cost = cost;
+        }
+    }
+    return best;
+}
+
+tm_status check_tiles(const GemmPlan& p) {
+    if (p.tiles_m * p.tiles_n > (int64_t(1) << 24)) return fail(TM_E_SHAPE, "rows * width too large");
+    return TM_OK;
+}
+
+tmk::GemmArgs gemm_args(const GemmPlan& p, const void* a, const void* b, int64_t M, int64_t N, int64_t K, int64_t lda,
+                        int64_t ldb, void* part) {
+    tmk::GemmArgs g{};
+    g.a = static_cast<const unsigned char*>(a);
+    g.b = static_cast<const unsigned char*>(b);
+    g.lda = lda * 2;
+    g.ldb = ldb * 2;
+    g.M = int32_t(M);
+    g.N = int32_t(N);
+    g.K = int32_t(K);
+    g.tiles_m = int32_t(p.tiles_m);
+    g.tiles_n = int32_t(p.tiles_n);
+    g.stages = int32_t(p.stages);
+    g.whole = int32_t(p.whole);
+    g.split_wgs = int32_t(p.split_wgs);
+    g.part = static_cast<float*>(part);
+    return g;
+}
+
+// The backward's workspace, in this order.
+struct LinearBwdPlan {
+    bool few;
+    int32_t R;       // few rows: 1, 2, 4, 8 or 16
+    int32_t shares;  // of N, for dx
+    tmk::RowParts parts;
+    GemmPlan dx, dw;
+    size_t dz_bytes, sums_bytes, gemm_bytes;
+    size_t total() const { return dz_bytes + sums_bytes + gemm_bytes; }
+};
+
+LinearBwdPlan plan_linear_bwd(const LinearGeo& g) {
+    LinearBwdPlan p{};
+    const int64_t rows = g.run.rows;
+    p.few = rows <= tmk::kFewRows;
+    const int64_t blocks = ceil_div(g.N, 256);
+    p.parts = row_parts(g.run, std::max<int64_t>(1, 8 * tmk::kCUs / blocks), 32);
+    p.sums_bytes = aligned(size_t(p.parts.count()) * tmk::kLinearSums * size_t(g.N) * 4);
+    if (p.few) {
+        p.R = 1;
+        while (p.R < rows) p.R *= 2;
+        // four workgroups a CU, 16 columns of a wave at least
+        p.shares = int32_t(std::max<int64_t>(1, std::min(ceil_div(4 * tmk::kCUs, ceil_div(g.K, 512)), g.N / 64)));
+        p.dz_bytes = aligned(size_t(p.R) * size_t(g.N) * 4);
+        p.gemm_bytes = aligned(size_t(p.shares) * size_t(p.R) * size_t(g.K) * 4);
+    } else {
+        p.dz_bytes = aligned(size_t(rows) * size_t(g.N) * 2);
+        p.dx = plan_gemm(rows, g.K, g.N, true);
+        p.dw = plan_gemm(g.N, g.K, rows, true);
+        p.gemm_bytes = aligned(std::max(p.dx.part_bytes(), p.dw.part_bytes()));
+    }
+    return p;
+}
+
+#define TM_LAUNCH(call, what)                                                                      \
+    do {                                                                                           \
+        const hipError_t e_ = (call);                                                              \
+        if (e_ != hipSuccess) return fail(TM_E_DEVICE, what " launch: %s", hipGetErrorString(e_)); \
+    } while (0)
+
+}  // namespace
+
+extern "C" {
+
+tm_status tm_block_norm_fwd(const tm_block_norm_desc* desc, int32_t n_tok, int64_t first_token, const void* x,
+                            const void* y, const float* gate, const float* post_weight, const float* pre_weight,
+                            const float* pre_bias, const float* scale, const float* shift, void* r, void* h,
+                            hipStream_t stream) {
+    NormGeo g;
+    tm_status st = check_norm(desc, n_tok, first_token, &g);
+    if (st != TM_OK) return st;
+    if (n_tok == 0) return TM_OK;  // (of nothing, tensors have no address)
+    if ((st = check_norm_set(desc, y, gate, post_weight, pre_weight, pre_bias, scale)) != TM_OK) return st;
+    if ((scale == nullptr) != (shift == nullptr)) return fail(TM_E_ARG, "scale and shift: both or neither");
+    if ((r != nullptr) != (y != nullptr)) return fail(TM_E_ARG, "r goes with y");
+    if ((h != nullptr) != (desc->pre != TM_NORM_NONE)) return fail(TM_E_ARG, "h goes with a norm before the block");
+    if (x == nullptr) return fail(TM_E_ARG, "x is NULL");
+    const size_t elems = size_t(g.run.rows) * size_t(g.E), vec = size_t(g.E) * 4, mod = size_t(g.run.B * g.run.groups) * vec;
+    Spans t;
+    if ((st = t.add(x, elems * g.stream, "x")) != TM_OK || (st = t.add(y, elems * g.act, "y")) != TM_OK ||
+        (st = t.add(gate, mod, "gate")) != TM_OK || (st = t.add(post_weight, vec, "post_weight")) != TM_OK ||
+        (st = t.add(pre_weight, vec, "pre_weight")) != TM_OK || (st = t.add(pre_bias, vec, "pre_bias")) != TM_OK ||
+        (st = t.add(scale, mod, "scale")) != TM_OK || (st = t.add(shift, mod, "shift")) != TM_OK ||
+        (st = t.add(r, elems * g.stream, "r", true)) != TM_OK || (st = t.add(h, elems * g.act, "h", true)) != TM_OK ||
+        (st = t.apart({{r, x}})) != TM_OK)
+        return st;
+    tmk::BlockNormArgs a{};
+    a.x = x;
+    a.y = y;
+    a.gate = gate;
+    a.post_weight = post_weight;
+    a.pre_weight = pre_weight;
+    a.pre_bias = pre_bias;
+    a.scale = scale;
+    a.shift = shift;
+    a.r = r;
+    a.h = h;
+    a.E = int32_t(g.E);
+    a.rows = int32_t(g.run.rows);
+    a.pre = desc->pre;
+    a.post = desc->post;
+    a.eps = desc->eps;
+    a.inv_E = 1.f / float(g.E);
+    a.tg = token_groups(g.run);
+    TM_LAUNCH(tmk::launch_block_norm(a, desc->stream_dtype == TM_F32, desc->dtype == TM_F32, stream), "block norm");
+    return TM_OK;
+}
+
+size_t tm_block_norm_bwd_workspace(const tm_block_norm_desc* desc, int32_t n_tok, int64_t first_token) {
+    NormGeo g;
+    return check_norm(desc, n_tok, first_token, &g) == TM_OK && n_tok > 0 ? g.part_bytes : 0;
+}
+
+tm_status tm_block_norm_bwd(const tm_block_norm_desc* desc, int32_t n_tok, int64_t first_token, const void* r,
+                            const void* dh, const void* dr, const void* y, const float* gate, const float* post_weight,
+                            const float* pre_weight, const float* pre_bias, const float* scale, void* dx, void* dy,
+                            float* dgate, float* dpost_weight, float* dpre_weight, float* dpre_bias, float* dscale,
+                            float* dshift, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    NormGeo g;
+    tm_status st = check_norm(desc, n_tok, first_token, &g);
+    if (st != TM_OK) return st;
+    if (n_tok > 0) {  // (of nothing, tensors have no address)
+        if ((st = check_norm_set(desc, y, gate, post_weight, pre_weight, pre_bias, scale)) != TM_OK) return st;
+        const bool has_pre = desc->pre != TM_NORM_NONE;
+        if (has_pre ? (r == nullptr || dh == nullptr) : (r != nullptr || dh != nullptr))
+            return fail(TM_E_ARG, "r and dh go with a norm before the block");
+        if (!has_pre && dr == nullptr) return fail(TM_E_ARG, "dr is NULL without a norm before the block");
+        if (dx == nullptr) return fail(TM_E_ARG, "dx is NULL");
+        if ((dy != nullptr) != (y != nullptr)) return fail(TM_E_ARG, "dy goes with y");
+    }
+    if ((dgate != nullptr && gate == nullptr) || (dpost_weight != nullptr && post_weight == nullptr) ||
+        (dpre_weight != nullptr && pre_weight == nullptr) || (dpre_bias != nullptr && pre_bias == nullptr) ||
+        ((dscale != nullptr || dshift != nullptr) && scale == nullptr))
+        return fail(TM_E_ARG, "the gradient of a vector that is not there");
+    const size_t elems = size_t(g.run.rows) * size_t(g.E), vec = size_t(g.E) * 4, mod = size_t(g.run.B * g.run.groups) * vec;
+    const bool sums = dgate != nullptr || dpost_weight != nullptr || dpre_weight != nullptr || dpre_bias != nullptr ||
+                      dscale != nullptr || dshift != nullptr;
+    const size_t need = sums && n_tok > 0 ? g.part_bytes : 0;
+    if (need > 0 && (workspace == nullptr || workspace_bytes < need))
+        return fail(TM_E_ARG, "workspace of %zu bytes needed", need);
+    Spans t;
+    if (n_tok > 0 &&
+        ((st = t.add(r, elems * g.stream, "r")) != TM_OK || (st = t.add(dh, elems * g.act, "dh")) != TM_OK ||
+         (st = t.add(dr, elems * g.stream, "dr")) != TM_OK || (st = t.add(y, elems * g.act, "y")) != TM_OK ||
+         (st = t.add(dx, elems * g.stream, "dx", true)) != TM_OK || (st = t.add(dy, elems * g.act, "dy", true)) != TM_OK ||
+         (need > 0 && (st = t.add(workspace, need, "workspace", true)) != TM_OK)))
+        return st;
+    if ((st = t.add(gate, mod, "gate")) != TM_OK || (st = t.add(post_weight, vec, "post_weight")) != TM_OK ||
+        (st = t.add(pre_weight, vec, "pre_weight")) != TM_OK || (st = t.add(pre_bias, vec, "pre_bias")) != TM_OK ||
+        (st = t.add(scale, mod, "scale")) != TM_OK || (st = t.add(dgate, mod, "dgate", true)) != TM_OK ||
+        (st = t.add(dpost_weight, vec, "dpost_weight", true)) != TM_OK ||
+        (st = t.add(dpre_weight, vec, "dpre_weight", true)) != TM_OK ||
+        (st = t.add(dpre_bias, vec, "dpre_bias", true)) != TM_OK ||
+        (st = t.add(dscale, mod, "dscale", true)) != TM_OK || (st = t.add(dshift, mod, "dshift", true)) != TM_OK ||
+        (st = t.apart({{dx, dr}, {dy, y}, {dy, dh}})) != TM_OK)
+        return st;
+    if (n_tok == 0) {
+        for (float* p : {dgate, dscale, dshift})
+            if (p != nullptr) TM_LAUNCH(tmk::launch_zero(p, int64_t(mod / 4), stream), "zero");
+        for (float* p : {dpost_weight, dpre_weight, dpre_bias})
+            if (p != nullptr) TM_LAUNCH(tmk::launch_zero(p, g.E, stream), "zero");
+        return TM_OK;
+    }
+    tmk::BlockNormBwdArgs a{};
+    a.r = r;
+    a.dh = dh;
+    a.dr = dr;
+    a.y = y;
+    a.gate = gate;
+    a.post_weight = post_weight;
+    a.pre_weight = pre_weight;
+    a.scale = scale;
+    a.dx = dx;
+    a.dy = dy;
+    a.part = need > 0 ? static_cast<float*>(workspace) : nullptr;
+    a.E = int32_t(g.E);
+    a.pre = desc->pre;
+    a.post = desc->post;
+    a.eps = desc->eps;
+    a.inv_E = 1.f / float(g.E);
+    a.parts = g.parts;
+    TM_LAUNCH(tmk::launch_block_norm_bwd(a, desc->stream_dtype == TM_F32, desc->dtype == TM_F32, stream),
+              "block norm backward");
+    if (!sums) return TM_OK;
+    // sums 0: dh, 1: dh pre(r), 2: dx post(y)
+    tmk::ColumnSums c{};
+    c.part = a.part;
+    c.vectors = tmk::kNormSums;
+    c.E = a.E;
+    c.parts = g.parts;
+    if (dscale != nullptr) c.group[c.n_group++] = {dscale, pre_weight, pre_bias, 1, pre_bias != nullptr ? 0 : -1};
+    if (dshift != nullptr) c.group[c.n_group++] = {dshift, nullptr, nullptr, 0, -1};
+    if (dgate != nullptr) c.group[c.n_group++] = {dgate, post_weight, nullptr, 2, -1};
+    if (dpre_weight != nullptr) c.total[c.n_total++] = {dpre_weight, scale, 1.f, 1};
+    if (dpre_bias != nullptr) c.total[c.n_total++] = {dpre_bias, scale, 1.f, 0};
+    if (dpost_weight != nullptr) c.total[c.n_total++] = {dpost_weight, gate, 0.f, 2};
+    TM_LAUNCH(tmk::launch_column_sums(c, stream), "column sums");
+    return TM_OK;
+}
+
+size_t tm_linear_fwd_workspace(const tm_linear_desc* desc, int32_t n_tok) {
+    LinearGeo g;
+    // (the groups, which the position matters for, do not count here)
+    tm_linear_desc d{};
+    if (desc != nullptr) {
+        d = *desc;
+        d.groups = 1;
+        d.group_tokens = 0;
+    }
+    if (check_linear(desc == nullptr ? nullptr : &d, n_tok, 0, &g) != TM_OK || g.run.rows <= tmk::kFewRows) return 0;
+    const GemmPlan p = plan_gemm(g.run.rows, g.N, g.K, true);
+    return check_tiles(p) == TM_OK ? p.part_bytes() : 0;
+}
+
+tm_status tm_linear_fwd(const tm_linear_desc* desc, int32_t n_tok, int64_t first_token, const void* x,
+                        const void* weight, const float* bias, const float* gate, const void* residual, void* pre,
+                        void* o, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    LinearGeo g;
+    tm_status st = check_linear(desc, n_tok, first_token, &g);
+    if (st != TM_OK) return st;
+    if (n_tok == 0) return TM_OK;
+    if (x == nullptr || weight == nullptr || o == nullptr) return fail(TM_E_ARG, "x, weight or o is NULL");
+    const bool few = g.run.rows <= tmk::kFewRows;
+    GemmPlan p{};
+    if (!few) {
+        p = plan_gemm(g.run.rows, g.N, g.K, true);
+        if (p.part_bytes() > 0 && (workspace == nullptr || workspace_bytes < p.part_bytes()))
+            p = plan_gemm(g.run.rows, g.N, g.K, false);
+        if ((st = check_tiles(p)) != TM_OK) return st;
+    }
+    const size_t outs = size_t(g.run.rows) * size_t(g.N);
+    Spans t;
+    if ((st = t.add(x, size_t(g.run.rows) * size_t(g.K) * 2, "x")) != TM_OK ||
+        (st = t.add(weight, size_t(g.N) * size_t(g.K) * 2, "weight")) != TM_OK ||
+        (st = t.add(bias, size_t(g.N) * 4, "bias")) != TM_OK ||
+        (st = t.add(gate, size_t(g.run.B * g.run.groups) * size_t(g.N) * 4, "gate")) != TM_OK ||
+        (st = t.add(residual, outs * g.out, "residual")) != TM_OK || (st = t.add(pre, outs * 2, "pre", true)) != TM_OK ||
+        (st = t.add(o, outs * g.out, "o", true)) != TM_OK ||
+        (p.part_bytes() > 0 && (st = t.add(workspace, p.part_bytes(), "workspace", true)) != TM_OK) ||
+        (st = t.apart({{o, residual}})) != TM_OK)
+        return st;
+    tmk::LinearEpilogue ep{};
+    ep.bias = bias;
+    ep.gate = gate;
+    ep.residual = residual;
+    ep.pre = pre;
+    ep.o = o;
+    ep.act = desc->act;
+    ep.o_f32 = desc->out_dtype == TM_F32;
+    ep.tg = token_groups(g.run);
+    if (few) {
+        const tmk::FewRowsArgs a{x, weight, int32_t(g.run.rows), int32_t(g.K), int32_t(g.N), ep};
+        TM_LAUNCH(tmk::launch_few_rows(a, stream), "linear");
+        return TM_OK;
+    }
+    tmk::GemmArgs a = gemm_args(p, x, weight, g.run.rows, g.N, g.K, g.K, g.K, workspace);
+    a.ep = ep;
+    TM_LAUNCH(tmk::launch_gemm(a, p.tile, false, false, stream), "linear");
+    return TM_OK;
+}
+
+size_t tm_linear_bwd_workspace(const tm_linear_desc* desc, int32_t n_tok, int64_t first_token) {
+    LinearGeo g;
+    return check_linear(desc, n_tok, first_token, &g) == TM_OK && n_tok > 0 ? plan_linear_bwd(g).total() : 0;
+}
+
+tm_status tm_linear_bwd(const tm_linear_desc* desc, int32_t n_tok, int64_t first_token, const void* x,
+                        const void* weight, const void* dout, const float* gate, const void* pre, void* dx,
+                        void* dweight, float* dbias, float* dgate, void* workspace, size_t workspace_bytes,
+                        hipStream_t stream) {
+    LinearGeo g;
+    tm_status st = check_linear(desc, n_tok, first_token, &g);
+    if (st != TM_OK) return st;
+    if (dgate != nullptr && gate == nullptr) return fail(TM_E_ARG, "dgate without gate");
+    if (n_tok > 0 && dout == nullptr) return fail(TM_E_ARG, "dout is NULL");
+    if (dx != nullptr && weight == nullptr) return fail(TM_E_ARG, "dx needs weight");
+    if (n_tok > 0 && dweight != nullptr && x == nullptr) return fail(TM_E_ARG, "dweight needs x");
+    if (n_tok > 0 && pre == nullptr && (desc->act != TM_ACT_NONE || dgate != nullptr))
+        return fail(TM_E_ARG, "an activation and dgate need pre");
+    const size_t outs = size_t(g.run.rows) * size_t(g.N), ins = size_t(g.run.rows) * size_t(g.K) * 2;
+    const size_t w_bytes = size_t(g.N) * size_t(g.K) * 2, mod = size_t(g.run.B * g.run.groups) * size_t(g.N) * 4;
+    LinearBwdPlan p{};
+    if (n_tok > 0) {
+        p = plan_linear_bwd(g);
+        if (!p.few && ((st = check_tiles(p.dx)) != TM_OK || (st = check_tiles(p.dw)) != TM_OK)) return st;
+        if (workspace == nullptr || workspace_bytes < p.total())
+            return fail(TM_E_ARG, "workspace of %zu bytes needed", p.total());
+    }
+    Spans t;
+    if (n_tok > 0 && ((st = t.add(x, ins, "x")) != TM_OK || (st = t.add(dout, outs * g.out, "dout")) != TM_OK ||
+                      (st = t.add(pre, outs * 2, "pre")) != TM_OK || (st = t.add(dx, ins, "dx", true)) != TM_OK ||
+                      (st = t.add(workspace, p.total(), "workspace", true)) != TM_OK))
+        return st;
+    if ((st = t.add(weight, w_bytes, "weight")) != TM_OK || (st = t.add(gate, mod, "gate")) != TM_OK ||
+        (st = t.add(dweight, w_bytes, "dweight", true)) != TM_OK ||
+        (st = t.add(dbias, size_t(g.N) * 4, "dbias", true)) != TM_OK || (st = t.add(dgate, mod, "dgate", true)) != TM_OK ||
+        (st = t.apart({})) != TM_OK)
+        return st;
+    if (n_tok == 0) {
+        if (dweight != nullptr) TM_LAUNCH(tmk::launch_zero(dweight, int64_t(w_bytes / 4), stream), "zero");
+        if (dbias != nullptr) TM_LAUNCH(tmk::launch_zero(dbias, g.N, stream), "zero");
+        if (dgate != nullptr) TM_LAUNCH(tmk::launch_zero(dgate, int64_t(mod / 4), stream), "zero");
+        return TM_OK;
+    }
+    unsigned char* ws = static_cast<unsigned char*>(workspace);
+    void* const part = ws + p.dz_bytes + p.sums_bytes;
+    const bool products = dx != nullptr || dweight != nullptr;
+    // dout is dz where nothing lies between and it has bf16 already
+    const bool direct = !p.few && desc->act == TM_ACT_NONE && gate == nullptr && desc->out_dtype == TM_BF16;
+    const bool sums = dbias != nullptr || dgate != nullptr;
+    tmk::LinearDzArgs z{};
+    z.dout = dout;
+    z.pre = desc->act != TM_ACT_NONE || dgate != nullptr ? pre : nullptr;
+    z.gate = gate;
+    z.dz = products && !p.few && !direct ? ws : nullptr;
+    z.dz_few = products && p.few ? reinterpret_cast<float*>(ws) : nullptr;
+    z.part = sums ? reinterpret_cast<float*>(ws + p.dz_bytes) : nullptr;
+    z.N = int32_t(g.N);
+    z.act = desc->act;
+    z.dout_f32 = desc->out_dtype == TM_F32;
+    z.gate_sums = dgate != nullptr;
+    z.R = p.R;
+    z.parts = p.parts;
+    if (z.dz != nullptr || z.dz_few != nullptr || z.part != nullptr)
+        TM_LAUNCH(tmk::launch_linear_dz(z, stream), "linear backward");
+    if (sums) {
+        tmk::ColumnSums c{};
+        c.part = z.part;
+        c.vectors = tmk::kLinearSums;
+        c.E = z.N;
+        c.parts = p.parts;
+        if (dbias != nullptr) c.total[c.n_total++] = {dbias, nullptr, 0.f, 0};
+        if (dgate != nullptr) c.group[c.n_group++] = {dgate, nullptr, nullptr, 1, -1};
+        TM_LAUNCH(tmk::launch_column_sums(c, stream), "column sums");
+    }
+    if (p.few) {
+        const tmk::FewRowsBwdArgs a{z.dz_few, x, weight, dx, dweight, static_cast<float*>(part), int32_t(g.run.rows), p.R,
+                                    int32_t(g.K), int32_t(g.N), p.shares};
+        TM_LAUNCH(tmk::launch_few_rows_bwd(a, stream), "linear backward");
+        return TM_OK;
+    }
+    const void* dz = direct ? dout : ws;
+    if (dx != nullptr) {
+        tmk::GemmArgs a = gemm_args(p.dx, dz, weight, g.run.rows, g.K, g.N, g.N, g.K, part);
+        a.ep.o = dx;
+        TM_LAUNCH(tmk::launch_gemm(a, p.dx.tile, false, true, stream), "linear backward");
+    }
+    if (dweight != nullptr) {
+        tmk::GemmArgs a = gemm_args(p.dw, dz, x, g.N, g.K, g.run.rows, g.N, g.K, part);
+        a.ep.o = dweight;
+        TM_LAUNCH(tmk::launch_gemm(a, p.dw.tile, true, true, stream), "linear backward");
+    }
+    return TM_OK;
 }
 
 }  // extern "C"

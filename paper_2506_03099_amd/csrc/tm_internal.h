@@ -325,4 +325,181 @@ constexpr int kKv8FewRows = 32;  // rows of a tile where rows are few
 constexpr int kKv8MaxParts = 256;
 hipError_t launch_attn_kv8(Kv8AttnArgs a, int head_dim, hipStream_t s);
 
+// Which row of a modulation [B, groups, width] a token row takes: token i of batch element b is at
+// position first + i, group (first + i) / group_tokens, of which the host keeps the quotient of first
+// (g0) and its remainder (f0). Without groups by_group divides by 2^31 - 1, which leaves 0.
+struct TokenGroups {
+    int32_t n, groups;
+    int32_t f0, g0;
+    FastDiv by_n, by_group;
+    __device__ __forceinline__ int64_t row(int32_t r) const {
+        const int32_t b = by_n.of(r);
+        return int64_t(b) * groups + g0 + by_group.of(f0 + (r - b * n));
+    }
+};
+
+// Linear layers. An element of the output from the sum z of its products: + bias, kept in pre (bf16) if
+// wanted, through the activation, times the token's gate, + residual, rounded once.
+constexpr int kActNone = 0, kActGelu = 1, kActSilu = 2;
+struct LinearEpilogue {
+    const float* bias;     // [N] or null
+    const float* gate;     // [B, groups, N] or null
+    const void* residual;  // [rows, N], of o's type, or null
+    void* pre;             // [rows, N] bf16, or null
+    void* o;               // [rows, N]
+    int32_t act, o_f32;
+    TokenGroups tg;
+};
+
+// C[m, n] = sum over k of A(m, k) B(n, k), bf16 operands, fp32 sums. An operand's rows in memory are its m
+// (n), k side by side, or its k, m (n) side by side (TRANS).
+struct GemmArgs {
+    const unsigned char* a;
+    const unsigned char* b;
+    int64_t lda, ldb;   // bytes from row to row in memory
+    int32_t M, N, K;
+    int32_t tiles_m, tiles_n;
+    int32_t stages;     // of kGemmDepth k each, the last one's first k only
+    int32_t whole;      // tiles that a workgroup takes alone; the others' stages are dealt out
+    int32_t split_wgs;  // to this many workgroups in equal shares
+    float* part;        // [split_wgs][2][tile][tile], or null where none is split
+    LinearEpilogue ep;
+};
+constexpr int kGemmDepth = 32;
+hipError_t launch_gemm(const GemmArgs& a, int tile, bool a_trans, bool b_trans, hipStream_t s);
+
+// Token rows in parts that lie in one group each, for sums over a group's rows: group j of those that the
+// run touches holds tokens [j * len - f0, (j + 1) * len - f0) of each batch element, cut to [0, n), and
+// part p of it the rows_per_part from p * rows_per_part on (none, at the run's ends).
+struct RowParts {
+    int32_t B, n;
+    int32_t len, f0;        // tokens of a group (n without groups), and of the first one before the run
+    int32_t touched;        // groups of the run
+    int32_t per_group;      // parts
+    int32_t rows_per_part;
+    int32_t g0, groups;     // the first one's index, of how many
+    __host__ __device__ int32_t count() const { return B * touched * per_group; }
+    // part `i`: its batch element, the modulation's row of its group, its tokens [t0, t1)
+    __device__ __forceinline__ void of(int32_t i, int32_t& b, int64_t& mod, int32_t& t0, int32_t& t1) const {
+        const int32_t p = i % per_group, j = i / per_group % touched;
+        b = i / per_group / touched;
+        mod = int64_t(b) * groups + g0 + j;
+        const int64_t at = int64_t(j) * len - f0;
+        const int64_t lo = at + int64_t(p) * rows_per_part;
+        const int64_t hi = lo + rows_per_part < at + len ? lo + rows_per_part : at + len;
+        t0 = static_cast<int32_t>(lo > 0 ? (lo < n ? lo : n) : 0);
+        t1 = static_cast<int32_t>(hi > 0 ? (hi < n ? hi : n) : 0);
+    }
+};
+
+// Sums over rows from those over the parts, part [parts][vectors][E]: per group into out [B, groups, E] (zeros
+// for groups outside the run), sum v times mul (null: 1) plus sum w times mul_w (w < 0: without); in total
+// over all parts into out [E], sum v times what mod [B, groups, E] has for its group plus add (null: 1).
+struct GroupSum {
+    float* out;
+    const float* mul;
+    const float* mul_w;
+    int32_t v, w;
+};
+struct TotalSum {
+    float* out;
+    const float* mod;
+    float add;
+    int32_t v;
+};
+struct ColumnSums {
+    const float* part;
+    int32_t vectors, E;
+    RowParts parts;
+    int32_t n_group, n_total;
+    GroupSum group[3];
+    TotalSum total[3];
+};
+hipError_t launch_column_sums(const ColumnSums& a, hipStream_t s);
+
+// Norms around a block (rows of E): z = post(y) * post_weight, r = x + gate * z, m = pre(r) * pre_weight +
+// pre_bias, h = m * (1 + scale) + shift. Null vectors are ones (weights, gate) or zeros.
+constexpr int kNormNone = 0, kNormLayer = 1, kNormRms = 2;
+constexpr int kMaxNormWidth = 20480;
+struct BlockNormArgs {
+    const void* x;  // backward: r
+    const void* y;
+    const float* gate;
+    const float* post_weight;
+    const float* pre_weight;
+    const float* pre_bias;
+    const float* scale;
+    const float* shift;
+    void* r;
+    void* h;
+    int32_t E, rows;
+    int32_t pre, post;
+    float eps, inv_E;
+    TokenGroups tg;
+};
+hipError_t launch_block_norm(const BlockNormArgs& a, bool stream_f32, bool act_f32, hipStream_t s);
+
+// Its backward: dx, dy, and per part the sums over rows of dh, of dh * pre(r) and of dx * post(y).
+constexpr int kNormSums = 3;
+struct BlockNormBwdArgs {
+    const void* r;   // null without pre
+    const void* dh;  // null without pre
+    const void* dr;  // or null: zeros
+    const void* y;   // or null
+    const float* gate;
+    const float* post_weight;
+    const float* pre_weight;
+    const float* scale;
+    void* dx;
+    void* dy;     // null without y
+    float* part;  // [parts][kNormSums][E], or null: no sums wanted
+    int32_t E, pre, post;
+    float eps, inv_E;
+    RowParts parts;
+};
+hipError_t launch_block_norm_bwd(const BlockNormBwdArgs& a, bool stream_f32, bool act_f32, hipStream_t s);
+
+// o = epilogue(x W^T) for at most kFewRows rows x [rows, K], W [N, K] bf16: W streams by once.
+constexpr int kFewRows = 16;
+struct FewRowsArgs {
+    const void* x;
+    const void* w;
+    int32_t rows, K, N;
+    LinearEpilogue ep;
+};
+hipError_t launch_few_rows(const FewRowsArgs& a, hipStream_t s);
+
+// dz = dout * gate * act'(pre) of a linear layer's rows, in bf16 [rows, N] (dz) or, of at most kFewRows rows,
+// in fp32 [N][R] (dz_few, rows past the last one zero), and per part the sums over rows of dz and of
+// dout * act(pre).
+constexpr int kLinearSums = 2;
+struct LinearDzArgs {
+    const void* dout;
+    const void* pre;    // bf16, or null
+    const float* gate;  // or null
+    void* dz;           // or null
+    float* dz_few;      // or null
+    float* part;        // [parts][kLinearSums][N], or null
+    int32_t N, act, dout_f32, gate_sums;
+    int32_t R;          // of dz_few
+    RowParts parts;
+};
+hipError_t launch_linear_dz(const LinearDzArgs& a, hipStream_t s);
+
+// dx = dz W and dW = dz^T x for at most kFewRows rows, from dz_few with R = 1, 2, 4, 8 or 16.
+struct FewRowsBwdArgs {
+    const float* dz;  // [N][R]
+    const void* x;    // [rows, K]
+    const void* w;    // [N, K]
+    void* dx;         // or null
+    void* dw;         // or null
+    float* part;      // of dx: [shares][R][K]
+    int32_t rows, R, K, N;
+    int32_t shares;   // of N that dx's sums are dealt out to
+};
+hipError_t launch_few_rows_bwd(const FewRowsBwdArgs& a, hipStream_t s);
+
+// n elements of 4 bytes to zero (a fill kernel: it may be captured).
+hipError_t launch_zero(void* p, int64_t n, hipStream_t s);
+
 }  // namespace tmk

@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -83,6 +84,38 @@ class tm_rope_desc(ctypes.Structure):
     ]
 
 
+TM_NORM_NONE, TM_NORM_LAYER, TM_NORM_RMS = 0, 1, 2
+TM_ACT_NONE, TM_ACT_GELU, TM_ACT_SILU = 0, 1, 2
+_NORM_CODE = {"none": TM_NORM_NONE, None: TM_NORM_NONE, "layer": TM_NORM_LAYER, "rms": TM_NORM_RMS}
+_ACT_CODE = {"none": TM_ACT_NONE, None: TM_ACT_NONE, "gelu": TM_ACT_GELU, "silu": TM_ACT_SILU}
+
+
+class tm_block_norm_desc(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32),
+        ("width", ctypes.c_int32),
+        ("pre", ctypes.c_int32),
+        ("post", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("stream_dtype", ctypes.c_int32),
+        ("groups", ctypes.c_int32),
+        ("group_tokens", ctypes.c_int32),
+        ("eps", ctypes.c_float),
+    ]
+
+
+class tm_linear_desc(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32),
+        ("in_width", ctypes.c_int32),
+        ("out_width", ctypes.c_int32),
+        ("act", ctypes.c_int32),
+        ("out_dtype", ctypes.c_int32),
+        ("groups", ctypes.c_int32),
+        ("group_tokens", ctypes.c_int32),
+    ]
+
+
 class TMError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"{STATUS_NAMES.get(status, status)}: {message}")
@@ -104,6 +137,8 @@ def lib() -> ctypes.CDLL:
         D = ctypes.POINTER(tm_attn_desc)
         AD = ctypes.POINTER(tm_audio_desc)
         RD = ctypes.POINTER(tm_rope_desc)
+        ND = ctypes.POINTER(tm_block_norm_desc)
+        LD = ctypes.POINTER(tm_linear_desc)
         rope = [RD, P, ctypes.c_int32, ctypes.c_int32, ctypes.c_int64, P, ctypes.c_int32, P,
                 ctypes.c_int32, P, P, P]
         sig = {
@@ -159,6 +194,16 @@ def lib() -> ctypes.CDLL:
             "tm_kv8_attn_workspace": (ctypes.c_size_t, [P, ctypes.c_int32, ctypes.c_int32]),
             "tm_kv8_attn_fwd": (ctypes.c_int, [P, P, ctypes.c_int32, ctypes.c_int32, P, ctypes.c_int32,
                                                P, P, ctypes.c_size_t, P]),
+            "tm_block_norm_fwd": (ctypes.c_int, [ND, ctypes.c_int32, ctypes.c_int64] + [P] * 11),
+            "tm_block_norm_bwd_workspace": (ctypes.c_size_t, [ND, ctypes.c_int32, ctypes.c_int64]),
+            "tm_block_norm_bwd": (ctypes.c_int, [ND, ctypes.c_int32, ctypes.c_int64] + [P] * 18
+                                  + [ctypes.c_size_t, P]),
+            "tm_linear_fwd_workspace": (ctypes.c_size_t, [LD, ctypes.c_int32]),
+            "tm_linear_fwd": (ctypes.c_int, [LD, ctypes.c_int32, ctypes.c_int64] + [P] * 8
+                              + [ctypes.c_size_t, P]),
+            "tm_linear_bwd_workspace": (ctypes.c_size_t, [LD, ctypes.c_int32, ctypes.c_int64]),
+            "tm_linear_bwd": (ctypes.c_int, [LD, ctypes.c_int32, ctypes.c_int64] + [P] * 10
+                              + [ctypes.c_size_t, P]),
             "tm_last_error": (ctypes.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -659,3 +704,209 @@ def tm_kv8_attn_fwd(cache: KV8Cache, q, q_chunk: int, o=None, o_f32: bool = Fals
         pw = None if ws is None else ws.data_ptr()
     _check(_lib.tm_kv8_attn_fwd(cache.handle, pq, q_chunk, n_q, po, o_f32, pl, pw, n, stream))
     return o
+
+
+def _own_workspace(nbytes: int, given, like, stream: int):
+    """The workspace that a backward call cannot do without: the caller's, or memory of torch's allocator
+    (under capture, of the graph's pool), whose order is that of the current stream."""
+    if nbytes == 0:
+        return None
+    if given is not None:
+        if given.numel() * given.element_size() < nbytes:
+            raise TMError(TM_E_ARG, f"workspace is smaller than {nbytes} bytes")
+        return given
+    if like.get_device() != torch._C._cuda_getDevice() or stream != _current_stream():
+        raise TMError(TM_E_ARG, "on another stream or device than the current one, pass a workspace of "
+                                f"{nbytes} bytes")
+    return torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+
+
+def _rows(name, t, B, width, dtype) -> int:
+    """n of a tensor that has to be [B, n, width] of the descriptor."""
+    shape = t.shape
+    if len(shape) != 3 or shape[0] != B or shape[2] != width or t.dtype != dtype:
+        raise TMError(TM_E_SHAPE, f"{name} is not {dtype} [{B}, n, {width}]")
+    return shape[1]
+
+
+def _given(name, t, shape, dtype=torch.float32):
+    """The address of a tensor that may be missing."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype != dtype:
+        raise TMError(TM_E_SHAPE, f"{name} is not {dtype} {list(shape)}")
+    return _ptr(t)
+
+
+def _grad(name, t, wanted, shape, device, dtype=torch.float32):
+    """A gradient and its address: the caller's tensor, a new one if it is None, nothing if it is False or
+    there is nothing that it would be the gradient of."""
+    if t is False or not wanted:
+        if t is not False and t is not None:
+            raise TMError(TM_E_ARG, f"{name} is the gradient of a tensor that is not there")
+        return None, None
+    if t is None:
+        t = torch.empty(shape, dtype=dtype, device=device)
+        return t, t.data_ptr()
+    _expect(name, t, shape, dtype)
+    return t, _ptr(t)
+
+
+def make_block_norm_desc(batch, width, pre="layer", post="none", dtype="bf16", stream_dtype="f32", eps=1e-6,
+                         groups=1, group_tokens=0) -> tm_block_norm_desc:
+    """``pre``, ``post``: "none", "layer" or "rms"; ``dtype`` of y and h, ``stream_dtype`` of x and r."""
+    return tm_block_norm_desc(batch, width, _NORM_CODE.get(pre, pre), _NORM_CODE.get(post, post), _dtype(dtype),
+                              _dtype(stream_dtype), groups, group_tokens, eps)
+
+
+def tm_block_norm_fwd(desc: tm_block_norm_desc, x, y=None, gate=None, post_weight=None, pre_weight=None,
+                      pre_bias=None, scale=None, shift=None, first_token: int = 0, r=None, h=None, stream=None):
+    """r = x + gate * (post(y) * post_weight) and h = (pre(r) * pre_weight + pre_bias) * (1 + scale) + shift;
+    returns (r, h), allocated if not given: r is None without y (x stands for it), h without pre."""
+    B, E = desc.batch, desc.width
+    act, st = _TORCH_DTYPE.get(desc.dtype), _TORCH_DTYPE.get(desc.stream_dtype)
+    n = _rows("x", x, B, E, st)
+    mod, vec, shape = (B, desc.groups, E), (E,), x.shape
+    px, py, pr, ph = _ptr(x), None, None, None
+    if y is not None:
+        py = _given("y", y, shape, act)
+        if r is None:
+            r = torch.empty_like(x)
+            pr = r.data_ptr()
+        else:
+            pr = _given("r", r, shape, st)
+    elif r is not None:
+        raise TMError(TM_E_ARG, "r goes with y")
+    if desc.pre != TM_NORM_NONE:
+        if h is None:
+            h = torch.empty_like(x) if act == st else torch.empty(shape, dtype=act, device=x.device)
+            ph = h.data_ptr()
+        else:
+            ph = _given("h", h, shape, act)
+    elif h is not None:
+        raise TMError(TM_E_ARG, "h goes with a norm before the block")
+    _check(lib().tm_block_norm_fwd(
+        ctypes.byref(desc), n, first_token, px, py, _given("gate", gate, mod), _given("post_weight", post_weight, vec),
+        _given("pre_weight", pre_weight, vec), _given("pre_bias", pre_bias, vec), _given("scale", scale, mod),
+        _given("shift", shift, mod), pr, ph, _stream(stream)))
+    return r, h
+
+
+class BlockNormGrads(NamedTuple):
+    """Gradients of ``tm_block_norm_fwd``'s inputs; None where the forward had no such input."""
+    dx: torch.Tensor
+    dy: torch.Tensor | None
+    dgate: torch.Tensor | None
+    dpost_weight: torch.Tensor | None
+    dpre_weight: torch.Tensor | None
+    dpre_bias: torch.Tensor | None
+    dscale: torch.Tensor | None
+    dshift: torch.Tensor | None
+
+
+def tm_block_norm_bwd(desc: tm_block_norm_desc, r, dh=None, dr=None, y=None, gate=None, post_weight=None,
+                      pre_weight=None, pre_bias=None, scale=None, shift=None, first_token: int = 0, dx=None, dy=None,
+                      dgate=None, dpost_weight=None, dpre_weight=None, dpre_bias=None, dscale=None, dshift=None,
+                      workspace=None, stream=None) -> BlockNormGrads:
+    """Gradients of the block norm's inputs from dh and dr (None: r goes nowhere else), the forward's ``r`` (x
+    without y) and its inputs. Each gradient is allocated if not given, and left out with False. ``workspace``: a tensor of ``tm_block_norm_bwd_workspace`` bytes (allocated if
+    not given; needed on another stream than the current one)."""
+    B, E = desc.batch, desc.width
+    act, st = _TORCH_DTYPE.get(desc.dtype), _TORCH_DTYPE.get(desc.stream_dtype)
+    has_pre = desc.pre != TM_NORM_NONE
+    like = r if has_pre else dr
+    if like is None:
+        raise TMError(TM_E_ARG, "r is missing" if has_pre else "dr is missing without a norm before the block")
+    n = _rows("r" if has_pre else "dr", like, B, E, st)
+    shape, mod, vec, dev = like.shape, (B, desc.groups, E), (E,), like.device
+    if (scale is None) != (shift is None):
+        raise TMError(TM_E_ARG, "scale and shift: both or neither")
+    ins = [_ptr(r) if has_pre else None, _given("dh", dh, shape, act), _given("dr", dr, shape, st),
+           _given("y", y, shape, act), _given("gate", gate, mod), _given("post_weight", post_weight, vec),
+           _given("pre_weight", pre_weight, vec), _given("pre_bias", pre_bias, vec), _given("scale", scale, mod)]
+    _given("shift", shift, mod)
+    if dx is False or dy is False:
+        raise TMError(TM_E_ARG, "dx and dy are always formed")
+    grads = [_grad("dx", dx, True, shape, dev, st), _grad("dy", dy, y is not None, shape, dev, act),
+             _grad("dgate", dgate, gate is not None, mod, dev),
+             _grad("dpost_weight", dpost_weight, post_weight is not None, vec, dev),
+             _grad("dpre_weight", dpre_weight, pre_weight is not None, vec, dev),
+             _grad("dpre_bias", dpre_bias, pre_bias is not None, vec, dev),
+             _grad("dscale", dscale, scale is not None, mod, dev),
+             _grad("dshift", dshift, scale is not None, mod, dev)]
+    d, stream = ctypes.byref(desc), _stream(stream)
+    nbytes, ws = 0, None
+    if any(p is not None for _, p in grads[2:]):
+        nbytes = lib().tm_block_norm_bwd_workspace(d, n, first_token)
+        ws = _own_workspace(nbytes, workspace, like, stream)
+    _check(lib().tm_block_norm_bwd(d, n, first_token, *ins, *[p for _, p in grads], _ptr(ws), nbytes, stream))
+    return BlockNormGrads(*[t for t, _ in grads])
+
+
+def make_linear_desc(batch, in_width, out_width, act="none", out_dtype="bf16", groups=1,
+                     group_tokens=0) -> tm_linear_desc:
+    """``act``: "none", "gelu" (its tanh form) or "silu"."""
+    return tm_linear_desc(batch, in_width, out_width, _ACT_CODE.get(act, act), _dtype(out_dtype), groups,
+                          group_tokens)
+
+
+def tm_linear_fwd(desc: tm_linear_desc, x, weight, bias=None, gate=None, residual=None, first_token: int = 0, o=None,
+                  pre=None, workspace=None, stream=None):
+    """o = residual + gate * act(x W^T + bias) of bf16 ``x`` [B, n_tok, K] and ``weight`` [N, K]; returns ``o``
+    (allocated if not given). ``pre`` (bf16 [B, n_tok, N]), if given, gets x W^T + bias for the backward pass.
+    Sizes that leave CUs idle share their sums out through ``workspace`` (a tensor of ``tm_linear_fwd_workspace``
+    bytes) or memory of torch's allocator; calls that have neither (under capture, on another stream than the
+    current one) order the fp32 sums otherwise."""
+    B, K, N = desc.batch, desc.in_width, desc.out_width
+    out = _TORCH_DTYPE.get(desc.out_dtype)
+    n = _rows("x", x, B, K, torch.bfloat16)
+    shape = (B, n, N)
+    px, pw = _ptr(x), _given("weight", weight, (N, K), torch.bfloat16)
+    if o is None:
+        o = torch.empty(shape, dtype=out, device=x.device)
+        po = o.data_ptr()
+    else:
+        po = _given("o", o, shape, out)
+    pb, pg = _given("bias", bias, (N,)), _given("gate", gate, (B, desc.groups, N))
+    pr, pp = _given("residual", residual, shape, out), _given("pre", pre, shape, torch.bfloat16)
+    d, stream = ctypes.byref(desc), _stream(stream)
+    L = lib()
+    nbytes, ws = L.tm_linear_fwd_workspace(d, n), None
+    if nbytes:
+        if workspace is None:
+            ws = _workspace(nbytes, x, stream)
+        elif workspace.numel() * workspace.element_size() < nbytes:
+            raise TMError(TM_E_ARG, f"workspace is smaller than {nbytes} bytes")
+        else:
+            ws = workspace
+    _check(L.tm_linear_fwd(d, n, first_token, px, pw, pb, pg, pr, pp, po, _ptr(ws), nbytes, stream))
+    return o
+
+
+class LinearGrads(NamedTuple):
+    """Gradients of ``tm_linear_fwd``'s inputs; None where the forward had no such input or it is not wanted.
+    (The residual's is the output's.)"""
+    dx: torch.Tensor | None
+    dweight: torch.Tensor | None
+    dbias: torch.Tensor | None
+    dgate: torch.Tensor | None
+
+
+def tm_linear_bwd(desc: tm_linear_desc, x, weight, dout, gate=None, pre=None, first_token: int = 0, dx=None,
+                  dweight=None, dbias=None, dgate=None, workspace=None, stream=None) -> LinearGrads:
+    """Gradients from that of the output, ``dout``. ``pre``: the forward's (not needed without activation and
+    gate). Each gradient is allocated if not given, and left out with False (the bias' for a layer without).
+    ``workspace``: a tensor of ``tm_linear_bwd_workspace`` bytes (allocated if not given; needed on another
+    stream than the current one)."""
+    B, K, N = desc.batch, desc.in_width, desc.out_width
+    n = _rows("dout", dout, B, N, _TORCH_DTYPE.get(desc.out_dtype))
+    xs, mod, dev, bf16 = (B, n, K), (B, desc.groups, N), dout.device, torch.bfloat16
+    px, pw = _given("x", x, xs, bf16), _given("weight", weight, (N, K), bf16)
+    pd, pg, pp = _ptr(dout), _given("gate", gate, mod), _given("pre", pre, (B, n, N), bf16)
+    grads = [_grad("dx", dx, True, xs, dev, bf16), _grad("dweight", dweight, True, (N, K), dev, bf16),
+             _grad("dbias", dbias, True, (N,), dev), _grad("dgate", dgate, gate is not None, mod, dev)]
+    d, stream = ctypes.byref(desc), _stream(stream)
+    nbytes = lib().tm_linear_bwd_workspace(d, n, first_token)
+    ws = _own_workspace(nbytes, workspace, dout, stream)
+    _check(lib().tm_linear_bwd(d, n, first_token, px, pw, pd, pg, pp, *[p for _, p in grads], _ptr(ws), nbytes, stream))
+    return LinearGrads(*[t for t, _ in grads])
