@@ -90,21 +90,21 @@ __device__ __forceinline__ void finish8(const LinearEpilogue& ep, int N, int row
 // ---------------------------------------------------------------------------
 // The matrix product
 // ---------------------------------------------------------------------------
-constexpr int kSlots = 4;  // stages in LDS: one read, two arriving, one just left
+constexpr int kSlots = 5;  // operands' parts of stages in LDS: two that are read, the next two and one more arriving
 
-// One operand's part of a stage, T rows (its m or n) by 32 k, 64 * T bytes, in LDS.
-// k side by side: rows of 64 bytes, 16-byte chunk c of row r at c ^ (r >> 2) % 4, so that the 16 rows that
+// One operand's part of a stage, T rows (its m or n) by 64 k, 128 * T bytes, in LDS.
+// k side by side: rows of 128 bytes, 16-byte chunk c of row r at c ^ (r >> 1) % 8, so that the 16 rows that
 // one cycle of a read covers lie in 16 different bank groups. A lane's operand of the MFMA, 8 k, is a chunk.
 // TRANS: rows of one k and T elements, chunk c of row k at c ^ 4 (k % 4), so that the 4 rows by 64 bytes
 // of a cycle of the transposing read lie apart. A lane's operand is two of these reads, 4 k each.
 template <int T, bool TRANS>
 struct Tile {
-    static constexpr int kBytes = 64 * T;
+    static constexpr int kBytes = 2 * kGemmDepth * T;
     static constexpr int kLoads = kBytes / 4096;    // 1-KB direct loads per wave
-    static constexpr int kChunks = TRANS ? T / 8 : 4;  // of a row
+    static constexpr int kChunks = TRANS ? T / 8 : kGemmDepth / 8;  // of a row
     uint32_t voff[kLoads];
 
-    static __device__ __forceinline__ int swizzle(int row) { return TRANS ? 4 * (row & 3) : (row >> 2) & 3; }
+    static __device__ __forceinline__ int swizzle(int row) { return TRANS ? 4 * (row & 3) : (row >> 1) & 7; }
 
     // Byte offsets in memory, from the stage's first element, of the chunks that this lane brings;
     // `rows`: of m (n) that exist from the tile's first one on. Past them the last ones come again.
@@ -120,7 +120,7 @@ struct Tile {
         }
     }
 
-    // The last stage of the sum, of which only `left` < 32 k exist: through registers, zeros behind them.
+    // The last stage of the sum, of which only `left` < 64 k exist: through registers, zeros behind them.
     __device__ __forceinline__ void load_rest(const unsigned char* base, lds_u8* lds, int wave, int lane, int left) const {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
@@ -135,12 +135,12 @@ struct Tile {
     // LDS offset of a lane's operand of rows [first + 32 i, + 32), k-step 0; at() of the others.
     static __device__ __forceinline__ uint32_t frag0(int first, int lane) {
         const int l32 = lane & 31, hw = lane >> 5;
-        if (!TRANS) return (first + l32) * 64 + ((hw ^ swizzle(l32)) << 4);
+        if (!TRANS) return (first + l32) * (2 * kGemmDepth) + ((hw ^ swizzle(l32)) << 4);
         const int grp = lane >> 4, gi = lane & 15, k = 8 * hw + (gi >> 2);
         return k * (2 * T) + ((first * 2) ^ (swizzle(k) << 4)) + (2 * (grp & 1) + ((gi & 3) >> 1)) * 16 + (gi & 1) * 8;
     }
     static __device__ __forceinline__ bf16x8_t frag(const lds_u8* lds, uint32_t at0, int i, int kk) {
-        if (!TRANS) return *(const lds_bf16x8_t*)(lds + (at0 ^ (kk << 5)) + i * 32 * 64);
+        if (!TRANS) return *(const lds_bf16x8_t*)(lds + (at0 ^ (kk << 5)) + i * 32 * (2 * kGemmDepth));
         const lds_u8* p = lds + (at0 ^ (i << 6)) + kk * 16 * (2 * T);
         const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t*)p);
         const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t*)(p + 4 * (2 * T)));
@@ -162,8 +162,9 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const Gemm
     constexpr int F = WT / 32;      // its 32-wide blocks, either way
     using TA = Tile<BT, AT>;
     using TB = Tile<BT, BTR>;
-    constexpr int SLOT = TA::kBytes + TB::kBytes;
-    constexpr int LOADS = TA::kLoads + TB::kLoads;
+    constexpr int SLOT = TA::kBytes;
+    constexpr int LOADS = TA::kLoads;
+    static_assert(TB::kBytes == SLOT && TB::kLoads == LOADS, "both operands' parts take one slot");
     __shared__ __attribute__((aligned(1024))) unsigned char smem[kSlots * SLOT];
     lds_u8* const L = (lds_u8*)smem;
     const uint32_t lds_base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(L));
@@ -183,7 +184,7 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const Gemm
     } else {
         id = xcd_logical_id(blockIdx.x, a.whole);
     }
-    const uint32_t fa = TA::frag0(wm, lane), fb = TB::frag0(wn, lane) + TA::kBytes;
+    const uint32_t fa = TA::frag0(wm, lane), fb = TB::frag0(wn, lane);
     const int rest = a.K % kGemmDepth;
 
     for (int seg = 0; u < u_end; ++seg) {
@@ -204,7 +205,7 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const Gemm
         TB tb;
         ta.init(wave, lane, a.lda, a.M - m0);
         tb.init(wave, lane, a.ldb, a.N - n0);
-        // stage 0 is what K leaves over 32, if anything, so that all later ones are whole
+        // stage 0 is what K leaves over 64, if anything, so that all later ones are whole
         auto base_a = [&](int s) __attribute__((always_inline)) {
             const int64_t k = rest ? (s == 0 ? a.K - rest : (s - 1) * kGemmDepth) : s * kGemmDepth;
             return uniform_ptr(a.a + (AT ? k * a.lda + m0 * int64_t(2) : m0 * a.lda + k * 2));
@@ -213,106 +214,117 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const Gemm
             const int64_t k = rest ? (s == 0 ? a.K - rest : (s - 1) * kGemmDepth) : s * kGemmDepth;
             return uniform_ptr(a.b + (BTR ? k * a.ldb + n0 * int64_t(2) : n0 * a.ldb + k * 2));
         };
-        // load j of stage s into a slot
-        auto issue = [&](const void* pa, const void* pb, uint32_t slot, int j) __attribute__((always_inline)) {
-            const bool is_a = j < TA::kLoads;
-            const int i = is_a ? j : j - TA::kLoads;
-            lds_dma16(is_a ? pa : pb, is_a ? ta.voff[i] : tb.voff[i],
-                      lds_base + slot + (is_a ? 0 : TA::kBytes) + (i * 4 + wave) * 1024);
+        // load j of an operand's part from p into the slot at `slot`
+        auto issue = [&](bool is_a, const void* p, uint32_t slot, int j) __attribute__((always_inline)) {
+            lds_dma16(p, is_a ? ta.voff[j] : tb.voff[j], lds_base + slot + (j * 4 + wave) * 1024);
+        };
+        auto ahead = [](uint32_t slot, int by) __attribute__((always_inline)) {
+            const uint32_t x = slot + by * SLOT;
+            return x >= kSlots * SLOT ? x - kSlots * SLOT : x;
         };
         const int n = s1 - s0;
         // (the slots of the last segment: all waves are through with them)
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        // A and B of the first stage, A and half of B of the second
+        constexpr int HALF = LOADS / 2;
+        if (rest != 0 && s0 == 0) {
+            ta.load_rest(static_cast<const unsigned char*>(base_a(0)), L, wave, lane, rest);
+            tb.load_rest(static_cast<const unsigned char*>(base_b(0)), L + SLOT, wave, lane, rest);
+        } else {
+            const void *pa = base_a(s0), *pb = base_b(s0);
 #pragma unroll
-        for (int s = 0; s < kSlots - 1; ++s) {
-            if (s < n) {
-                const void* pa = base_a(s0 + s);
-                const void* pb = base_b(s0 + s);
-                if (rest != 0 && s0 + s == 0) {
-                    ta.load_rest(static_cast<const unsigned char*>(pa), L + s * SLOT, wave, lane, rest);
-                    tb.load_rest(static_cast<const unsigned char*>(pb), L + s * SLOT + TA::kBytes, wave, lane, rest);
-                } else {
+            for (int j = 0; j < LOADS; ++j) issue(true, pa, 0, j);
 #pragma unroll
-                    for (int j = 0; j < LOADS; ++j) issue(pa, pb, s * SLOT, j);
-                }
-            }
+            for (int j = 0; j < LOADS; ++j) issue(false, pb, SLOT, j);
         }
-        if (n >= kSlots - 1)
-            wait_and_meet<2 * LOADS>();
-        else
+        if (n > 1) {
+            const void *pa = base_a(s0 + 1), *pb = base_b(s0 + 1);
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) issue(true, pa, 2 * SLOT, j);
+#pragma unroll
+            for (int j = 0; j < HALF; ++j) issue(false, pb, 3 * SLOT, j);
+            wait_and_meet<LOADS + HALF>();
+        } else {
             wait_and_meet<0>();
+        }
 
         f32x16_t acc[F][F];
 #pragma unroll
         for (int i = 0; i < F; ++i)
 #pragma unroll
             for (int j = 0; j < F; ++j) acc[i][j] = f32x16_t{};
-        // a wave's operands of k-steps 0 and 1 of a stage; operand f: A's first block, B's blocks, A's others
+        // a wave's operands of two k-steps; operand f: A's first block, B's blocks, A's others
         bf16x8_t af[2][F], bf[2][F];
-        auto read = [&](const lds_u8* p, int kk, int f) __attribute__((always_inline)) {
+        auto read = [&](const lds_u8* pa, const lds_u8* pb, int kk, int f) __attribute__((always_inline)) {
             if (f == 0)
-                af[kk][0] = TA::frag(p, fa, 0, kk);
+                af[kk & 1][0] = TA::frag(pa, fa, 0, kk);
             else if (f <= F)
-                bf[kk][f - 1] = TB::frag(p, fb, f - 1, kk);
+                bf[kk & 1][f - 1] = TB::frag(pb, fb, f - 1, kk);
             else
-                af[kk][f - F] = TA::frag(p, fa, f - F, kk);
+                af[kk & 1][f - F] = TA::frag(pa, fa, f - F, kk);
         };
 #pragma unroll
-        for (int f = 0; f < 2 * F; ++f) read(L, 0, f);
-        // Stage at slot `at`: the MFMAs of k-step 0, under them the reads of k-step 1 and the loads of the
-        // stage three ahead into the slot that was left last; the wait for the next stage; the MFMAs of
-        // k-step 1, under them the reads of the next stage's k-step 0.
-        auto stage = [&](auto more, int s, uint32_t at) __attribute__((always_inline)) {
-            constexpr bool MORE = decltype(more)::value;
-            const lds_u8* p = L + at;
-            const uint32_t next = at + SLOT == kSlots * SLOT ? 0 : at + SLOT;
-            const uint32_t left = at == 0 ? (kSlots - 1) * SLOT : at - SLOT;
-            const void *pa = nullptr, *pb = nullptr;
-            if (MORE) {
-                pa = base_a(s + kSlots - 1);
-                pb = base_b(s + kSlots - 1);
+        for (int f = 0; f < 2 * F; ++f) read(L, L + SLOT, 0, f);
+        // Stage s, A in the slot at `at`, B in the one behind it: the MFMAs of its four k-steps, under those of
+        // each the reads of the next one and half a part's loads, evenly. Near the end of the third one, when the
+        // wave's last reads of the stage are through, the wait for the next stage; its slots are free behind it.
+        // Loads run 1.2 (B) to 1.7 stages ahead: the second half of B of s + 1, A of s + 2, half of B of s + 2.
+        auto stage = [&](auto have1, auto have2, int s, uint32_t at) __attribute__((always_inline)) {
+            constexpr bool ONE = decltype(have1)::value, TWO = decltype(have2)::value;
+            const void *pb = nullptr, *pa2 = nullptr, *pb2 = nullptr;
+            if (ONE) pb = base_b(s + 1);
+            if (TWO) {
+                pa2 = base_a(s + 2);
+                pb2 = base_b(s + 2);
             }
-            constexpr int MEET = F * F - F;  // MFMA of k-step 0 that the wait comes behind
+            const uint32_t a1 = ahead(at, 2), b1 = ahead(at, 3), a2 = ahead(at, 4);
+            constexpr int M = F * F;
 #pragma unroll
-            for (int m = 0; m < F * F; ++m) {
-                acc[m / F][m % F] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[0][m % F], af[0][m / F], acc[m / F][m % F], 0, 0, 0);
-                if (F == 4) {
-                    if (m < 2 * F) read(p, 1, m);
-                    if (MORE && m < LOADS) issue(pa, pb, left, m);
-                } else if (m < F) {
-                    read(p, 1, 2 * m);
-                    read(p, 1, 2 * m + 1);
-                    if (MORE) {
-                        issue(pa, pb, left, 2 * m);
-                        issue(pa, pb, left, 2 * m + 1);
+            for (int kk = 0; kk < 4; ++kk) {
+                auto load = [&](int j) __attribute__((always_inline)) {
+                    if (kk == 0 && ONE) issue(false, pb, b1, HALF + j);
+                    if (kk == 1 && TWO) issue(true, pa2, a2, j);
+                    if (kk == 2 && TWO) issue(true, pa2, a2, HALF + j);
+                    if (kk == 3 && TWO) issue(false, pb2, at, j);
+                };
+                const lds_u8* pa = L + (kk == 3 ? a1 : at);
+                const lds_u8* pbk = L + (kk == 3 ? b1 : ahead(at, 1));
+#pragma unroll
+                for (int m = 0; m < M; ++m) {
+                    acc[m / F][m % F] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[kk & 1][m % F], af[kk & 1][m / F], acc[m / F][m % F], 0, 0, 0);
+                    if (F == 4) {
+                        if (kk == 2) {
+                            if (m % 4 != 3 && m / 4 * 3 + m % 4 < 2 * F) read(pa, pbk, kk + 1, m / 4 * 3 + m % 4);
+                            if (m == 3 || m == 7 || m == 10 || m == 11) load(m == 3 ? 0 : m == 7 ? 1 : m - 8);
+                        } else {
+                            if (m % 2 == 0) read(pa, pbk, (kk + 1) & 3, m / 2);
+                            if (m % 4 == 1) load(m / 4);
+                        }
+                    } else if (kk == 2) {
+                        if (m < F) {
+                            read(pa, pbk, kk + 1, 2 * m);
+                            read(pa, pbk, kk + 1, 2 * m + 1);
+                            load(m);
+                        }
+                    } else {
+                        read(pa, pbk, (kk + 1) & 3, m);
+                        if (m % 2 == 1) load(m / 2);
                     }
+                    if (kk == 2 && m == (F == 4 ? 13 : 2)) {
+                        if (TWO)
+                            wait_and_meet<LOADS>();
+                        else
+                            wait_and_meet<0>();
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                if (m == MEET) {
-                    if (MORE)
-                        wait_and_meet<2 * LOADS>();
-                    else
-                        wait_and_meet<0>();
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            const lds_u8* q = L + next;
-#pragma unroll
-            for (int m = 0; m < F * F; ++m) {
-                acc[m / F][m % F] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[1][m % F], af[1][m / F], acc[m / F][m % F], 0, 0, 0);
-                if (m < 2 * F) read(q, 0, m);
-                __builtin_amdgcn_sched_barrier(0);
             }
         };
         uint32_t at = 0;
         int s = s0;
-        for (; s + kSlots - 1 < s1; ++s) {
-            stage(std::true_type{}, s, at);
-            at = at + SLOT == kSlots * SLOT ? 0 : at + SLOT;
-        }
-        for (; s < s1; ++s) {
-            stage(std::false_type{}, s, at);
-            at = at + SLOT == kSlots * SLOT ? 0 : at + SLOT;
-        }
+        for (; s + 2 < s1; ++s, at = ahead(at, 2)) stage(std::true_type{}, std::true_type{}, s, at);
+        for (; s + 1 < s1; ++s, at = ahead(at, 2)) stage(std::true_type{}, std::false_type{}, s, at);
+        stage(std::false_type{}, std::false_type{}, s, at);
 
         // Register 4 g + e of acc[i][j]: row wm + 32 i + l32, column wn + 32 j + 8 g + 4 hw + e. Through the
         // wave's own share of LDS (chunk c of row r at c ^ r % 16), 32 rows at a time, into whole rows.

@@ -1739,12 +1739,12 @@ GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool may_split) {
         const int64_t tiles = p.tiles_m * p.tiles_n;
         const int64_t at_once = tile == 256 ? tmk::kCUs : 2 * tmk::kCUs;
         // cycles of a stage with the chip full, and beside the stages: a tile's start and end, a merge's launch
-        const double stage = tile == 256 ? 1100 : 700, ends = tile == 256 ? 8000 : 5000, merge = 12000;
+        const double stage = tile == 256 ? 2200 : 1400, ends = tile == 256 ? 8000 : 5000, merge = 12000;
         p.whole = tiles;
         double cost = double(ceil_div(tiles, at_once)) * (double(p.stages) * stage + ends);
         const int64_t rest = tiles % at_once;
-        // (at least 8 stages a workgroup)
-        const int64_t wgs = std::min(at_once, rest * p.stages / 8);
+        // (at least 4 stages a workgroup)
+        const int64_t wgs = std::min(at_once, rest * p.stages / 4);
         if (may_split && rest > 0 && wgs > rest) {
             const double with = double(tiles / at_once) * (double(p.stages) * stage + ends) +
                                 double(rest * p.stages) / double(wgs) * stage + ends + merge;

@@ -365,7 +365,7 @@ struct GemmArgs {
     float* part;        // [split_wgs][2][tile][tile], or null where none is split
     LinearEpilogue ep;
 };
-constexpr int kGemmDepth = 32;
+constexpr int kGemmDepth = 64;
 hipError_t launch_gemm(const GemmArgs& a, int tile, bool a_trans, bool b_trans, hipStream_t s);
 
 // Token rows in parts that lie in one group each, for sums over a group's rows: group j of those that the
