@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "tm_device.h"
@@ -28,9 +29,13 @@ __device__ __forceinline__ float sigmoid(float x) {
 
 // gelu(z) = z sigmoid(2 c (z + a z^3)), c = sqrt(2 / pi), a = 0.044715: the tanh form, (1 + tanh u) / 2 = sigmoid(2 u).
 constexpr float kGelu2C = 1.5957691216057308f, kGeluA = 0.044715f;
-__device__ __forceinline__ float activate(float z, int act) {
-    if (act == kActGelu) return z * sigmoid(kGelu2C * (z + kGeluA * z * z * z));
-    if (act == kActSilu) return z * sigmoid(z);
+template <int ACT>
+__device__ __forceinline__ float activate(float z) {
+    if (ACT == kActGelu) {
+        constexpr float k1 = -1.4426950408889634f * kGelu2C, k3 = k1 * kGeluA;
+        return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * fmaf(k3, z * z, k1)));
+    }
+    if (ACT == kActSilu) return z * sigmoid(z);
     return z;
 }
 
@@ -58,33 +63,48 @@ __device__ __forceinline__ void store8(__bf16* p, const float (&x)[8]) {
     *reinterpret_cast<bf16x8_t*>(p) = v;
 }
 
-// Columns [col, col + 8) of row `row`: z holds the sums of products plus bias.
-__device__ __forceinline__ void finish8(const LinearEpilogue& ep, int N, int row, int col, float (&z)[8]) {
-    const int64_t at = static_cast<int64_t>(row) * N + col;
+// Eight neighbours at element `at` of the output, `mod` of the gate: z holds the sums of products plus bias.
+template <int ACT, bool F32>
+__device__ __forceinline__ void finish8(const LinearEpilogue& ep, int64_t at, int64_t mod, float (&z)[8]) {
     if (ep.pre != nullptr) store8(static_cast<__bf16*>(ep.pre) + at, z);
-    if (ep.act != kActNone) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) z[e] = activate(z[e], ep.act);
-    }
+    for (int e = 0; e < 8; ++e) z[e] = activate<ACT>(z[e]);
     if (ep.gate != nullptr) {
         float g[8];
-        load8(ep.gate + ep.tg.row(row) * N + col, g);
+        load8(ep.gate + mod, g);
 #pragma unroll
         for (int e = 0; e < 8; ++e) z[e] *= g[e];
     }
     if (ep.residual != nullptr) {
         float r[8];
-        if (ep.o_f32)
+        if (F32)
             load8(static_cast<const float*>(ep.residual) + at, r);
         else
             load8(static_cast<const __bf16*>(ep.residual) + at, r);
 #pragma unroll
         for (int e = 0; e < 8; ++e) z[e] += r[e];
     }
-    if (ep.o_f32)
+    if (F32)
         store8(static_cast<float*>(ep.o) + at, z);
     else
         store8(static_cast<__bf16*>(ep.o) + at, z);
+}
+
+// body(activation, whether the output is fp32) with both known to the compiler
+template <typename Body>
+__device__ __forceinline__ void by_kind(const LinearEpilogue& ep, const Body& body) {
+    auto typed = [&](auto act) __attribute__((always_inline)) {
+        if (ep.o_f32)
+            body(act, std::true_type{});
+        else
+            body(act, std::false_type{});
+    };
+    if (ep.act == kActGelu)
+        typed(std::integral_constant<int, kActGelu>{});
+    else if (ep.act == kActSilu)
+        typed(std::integral_constant<int, kActSilu>{});
+    else
+        typed(std::integral_constant<int, kActNone>{});
 }
 
 // ---------------------------------------------------------------------------
@@ -132,12 +152,18 @@ struct Tile {
         }
     }
 
-    // LDS offset of a lane's operand of rows [first + 32 i, + 32), k-step 0; at() of the others.
-    static __device__ __forceinline__ uint32_t frag0(int first, int lane) {
+    // LDS offset of a lane's operand of rows [first, + 32), k-step 0. `perm`: lane l brings row k_perm(l), so
+    // that 8 registers of the result in a row are 8 neighbours (of the transposing read's columns, the four
+    // that each address stands for change places).
+    static __device__ __forceinline__ uint32_t frag0(int first, int lane, bool perm) {
         const int l32 = lane & 31, hw = lane >> 5;
-        if (!TRANS) return (first + l32) * (2 * kGemmDepth) + ((hw ^ swizzle(l32)) << 4);
+        if (!TRANS) {
+            const int row = perm ? k_perm(l32) : l32;
+            return (first + row) * (2 * kGemmDepth) + ((hw ^ swizzle(row)) << 4);
+        }
         const int grp = lane >> 4, gi = lane & 15, k = 8 * hw + (gi >> 2);
-        return k * (2 * T) + ((first * 2) ^ (swizzle(k) << 4)) + (2 * (grp & 1) + ((gi & 3) >> 1)) * 16 + (gi & 1) * 8;
+        const int four = perm ? 2 * (gi & 1) + ((gi >> 1) & 1) : gi & 3;
+        return k * (2 * T) + ((first * 2) ^ (swizzle(k) << 4)) + (2 * (grp & 1) + (four >> 1)) * 16 + (four & 1) * 8;
     }
     static __device__ __forceinline__ bf16x8_t frag(const lds_u8* lds, uint32_t at0, int i, int kk) {
         if (!TRANS) return *(const lds_bf16x8_t*)(lds + (at0 ^ (kk << 5)) + i * 32 * (2 * kGemmDepth));
@@ -156,14 +182,25 @@ __device__ __forceinline__ void wait_and_meet() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-template <int BT, bool AT, bool BTR>
+// The first row and column of tile t: tiles go in bands of 8 rows of tiles, so that those at work at one time
+// share rows and columns.
+__device__ __forceinline__ void tile_at(const GemmArgs& a, int t, int tile, int& m0, int& n0) {
+    constexpr int BAND = 8;
+    const int per = BAND * a.tiles_n, band = t / per, in = t % per;
+    const int high = min(BAND, a.tiles_m - band * BAND);
+    m0 = (band * BAND + in % high) * tile;
+    n0 = in / high * tile;
+}
+
+// FULL: with all of the epilogue; else the sums are the output, in bf16.
+template <int BT, bool AT, bool BTR, bool FULL>
 __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const GemmArgs a) {
     constexpr int WT = BT / 2;      // a wave's rows and columns
     constexpr int F = WT / 32;      // its 32-wide blocks, either way
     using TA = Tile<BT, AT>;
     using TB = Tile<BT, BTR>;
     constexpr int SLOT = TA::kBytes;
-    constexpr int LOADS = TA::kLoads;
+    constexpr int LOADS = TA::kLoads, HALF = LOADS / 2;
     static_assert(TB::kBytes == SLOT && TB::kLoads == LOADS, "both operands' parts take one slot");
     __shared__ __attribute__((aligned(1024))) unsigned char smem[kSlots * SLOT];
     lds_u8* const L = (lds_u8*)smem;
@@ -171,195 +208,271 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const Gemm
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = (wave & 1) * WT, wn = (wave >> 1) * WT;
-    const int l32 = lane & 31, hw = lane >> 5;
-
-    const bool split = static_cast<int>(blockIdx.x) >= a.whole;
-    const int sw = blockIdx.x - a.whole;
-    const int64_t units = static_cast<int64_t>(a.tiles_m * a.tiles_n - a.whole) * a.stages;
-    int64_t u = 0, u_end = 1;
-    int id = 0;
-    if (split) {
-        u = share_begin(units, sw, a.split_wgs);
-        u_end = share_begin(units, sw + 1, a.split_wgs);
-    } else {
-        id = xcd_logical_id(blockIdx.x, a.whole);
-    }
-    const uint32_t fa = TA::frag0(wm, lane), fb = TB::frag0(wn, lane);
+    const uint32_t fa = TA::frag0(wm, lane, false), fb = TB::frag0(wn, lane, true);
     const int rest = a.K % kGemmDepth;
 
-    for (int seg = 0; u < u_end; ++seg) {
-        int s0 = 0, s1 = a.stages;
-        if (split) {
-            id = a.whole + static_cast<int>(u / a.stages);
-            s0 = static_cast<int>(u % a.stages);
-            s1 = static_cast<int>(min(static_cast<int64_t>(a.stages), s0 + (u_end - u)));
-        }
-        u += split ? s1 - s0 : 1;
-        // tiles in bands of 8 rows of tiles, so that those at work at one time share rows and columns
-        constexpr int BAND = 8;
-        const int per = BAND * a.tiles_n, band = id / per, in = id % per;
-        const int high = min(BAND, a.tiles_m - band * BAND);
-        const int m0 = (band * BAND + in % high) * BT, n0 = in / high * BT;
-
-        TA ta;
-        TB tb;
-        ta.init(wave, lane, a.lda, a.M - m0);
-        tb.init(wave, lane, a.ldb, a.N - n0);
-        // stage 0 is what K leaves over 64, if anything, so that all later ones are whole
-        auto base_a = [&](int s) __attribute__((always_inline)) {
-            const int64_t k = rest ? (s == 0 ? a.K - rest : (s - 1) * kGemmDepth) : s * kGemmDepth;
-            return uniform_ptr(a.a + (AT ? k * a.lda + m0 * int64_t(2) : m0 * a.lda + k * 2));
-        };
-        auto base_b = [&](int s) __attribute__((always_inline)) {
-            const int64_t k = rest ? (s == 0 ? a.K - rest : (s - 1) * kGemmDepth) : s * kGemmDepth;
-            return uniform_ptr(a.b + (BTR ? k * a.ldb + n0 * int64_t(2) : n0 * a.ldb + k * 2));
-        };
-        // load j of an operand's part from p into the slot at `slot`
-        auto issue = [&](bool is_a, const void* p, uint32_t slot, int j) __attribute__((always_inline)) {
-            lds_dma16(p, is_a ? ta.voff[j] : tb.voff[j], lds_base + slot + (j * 4 + wave) * 1024);
-        };
-        auto ahead = [](uint32_t slot, int by) __attribute__((always_inline)) {
-            const uint32_t x = slot + by * SLOT;
-            return x >= kSlots * SLOT ? x - kSlots * SLOT : x;
-        };
-        const int n = s1 - s0;
-        // (the slots of the last segment: all waves are through with them)
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        // A and B of the first stage, A and half of B of the second
-        constexpr int HALF = LOADS / 2;
-        if (rest != 0 && s0 == 0) {
-            ta.load_rest(static_cast<const unsigned char*>(base_a(0)), L, wave, lane, rest);
-            tb.load_rest(static_cast<const unsigned char*>(base_b(0)), L + SLOT, wave, lane, rest);
+    // What a workgroup does, one after the other: whole tiles, those of its XCD dealt out to its XCD's
+    // workgroups, then its share of the split ones' stages (of at most two tiles).
+    struct Work {
+        int m0, n0, s0, s1;
+        float* part;
+    };
+    const int per_xcd = a.whole / 8, over = a.whole % 8, xcd = blockIdx.x % 8;
+    const int first = xcd * per_xcd + min(xcd, over), end = first + per_xcd + (xcd < over ? 1 : 0);
+    const int stride = (static_cast<int>(gridDim.x) - xcd + 7) / 8;
+    int id = first + static_cast<int>(blockIdx.x) / 8, seg = 0;
+    const int64_t units = static_cast<int64_t>(a.tiles_m * a.tiles_n - a.whole) * a.stages;
+    int64_t u = 0, u_end = 0;
+    if (units > 0 && static_cast<int>(blockIdx.x) < a.split_wgs) {
+        u = share_begin(units, blockIdx.x, a.split_wgs);
+        u_end = share_begin(units, blockIdx.x + 1, a.split_wgs);
+    }
+    auto next_work = [&](Work& w) __attribute__((always_inline)) {
+        int t;
+        if (id < end) {
+            t = id;
+            id += stride;
+            w.s0 = 0;
+            w.s1 = a.stages;
+            w.part = nullptr;
+        } else if (u < u_end) {
+            t = a.whole + static_cast<int>(u / a.stages);
+            w.s0 = static_cast<int>(u % a.stages);
+            w.s1 = static_cast<int>(min(static_cast<int64_t>(a.stages), w.s0 + (u_end - u)));
+            w.part = a.part + (static_cast<int64_t>(blockIdx.x) * 2 + seg) * (BT * BT);
+            u += w.s1 - w.s0;
+            ++seg;
         } else {
-            const void *pa = base_a(s0), *pb = base_b(s0);
+            return false;
+        }
+        tile_at(a, t, BT, w.m0, w.n0);
+        return true;
+    };
+
+    // stage 0 is what K leaves over 64, if anything, so that all later ones are whole
+    auto first_k = [&](int s) __attribute__((always_inline)) {
+        return static_cast<int64_t>(rest ? (s == 0 ? a.K - rest : (s - 1) * kGemmDepth) : s * kGemmDepth);
+    };
+    auto base_a = [&](const Work& w, int s) __attribute__((always_inline)) {
+        const int64_t k = first_k(s);
+        return uniform_ptr(a.a + (AT ? k * a.lda + w.m0 * int64_t(2) : w.m0 * a.lda + k * 2));
+    };
+    auto base_b = [&](const Work& w, int s) __attribute__((always_inline)) {
+        const int64_t k = first_k(s);
+        return uniform_ptr(a.b + (BTR ? k * a.ldb + w.n0 * int64_t(2) : w.n0 * a.ldb + k * 2));
+    };
+    TA ta;
+    TB tb;
+    // load j of an operand's part from p into the slot at `slot`
+    auto issue = [&](bool is_a, const void* p, uint32_t slot, int j) __attribute__((always_inline)) {
+        lds_dma16(p, is_a ? ta.voff[j] : tb.voff[j], lds_base + slot + (j * 4 + wave) * 1024);
+    };
+    auto ahead = [](uint32_t slot, int by) __attribute__((always_inline)) {
+        const uint32_t x = slot + by * SLOT;
+        return x >= kSlots * SLOT ? x - kSlots * SLOT : x;
+    };
+    // The first loads of a tile: A and B of its first stage, A and half of B of the second.
+    auto begin = [&](const Work& w) __attribute__((always_inline)) {
+        const int lane = fresh_thread_index() & 63;  // (what follows from it is not kept from tile to tile)
+        ta.init(wave, lane, a.lda, a.M - w.m0);
+        tb.init(wave, lane, a.ldb, a.N - w.n0);
+        const void *pa = base_a(w, w.s0), *pb = base_b(w, w.s0);
+        if (rest != 0 && w.s0 == 0) {
+            ta.load_rest(static_cast<const unsigned char*>(pa), L, wave, lane, rest);
+            tb.load_rest(static_cast<const unsigned char*>(pb), L + SLOT, wave, lane, rest);
+        } else {
 #pragma unroll
             for (int j = 0; j < LOADS; ++j) issue(true, pa, 0, j);
 #pragma unroll
             for (int j = 0; j < LOADS; ++j) issue(false, pb, SLOT, j);
         }
-        if (n > 1) {
-            const void *pa = base_a(s0 + 1), *pb = base_b(s0 + 1);
+        if (w.s1 - w.s0 > 1) {
+            pa = base_a(w, w.s0 + 1);
+            pb = base_b(w, w.s0 + 1);
 #pragma unroll
             for (int j = 0; j < LOADS; ++j) issue(true, pa, 2 * SLOT, j);
 #pragma unroll
             for (int j = 0; j < HALF; ++j) issue(false, pb, 3 * SLOT, j);
-            wait_and_meet<LOADS + HALF>();
+        }
+    };
+
+    f32x16_t acc[F][F];
+    // a wave's operands of two k-steps; operand f: A's first block, B's blocks, A's others
+    bf16x8_t af[2][F], bf[2][F];
+    auto read = [&](const lds_u8* pa, const lds_u8* pb, int kk, int f) __attribute__((always_inline)) {
+        if (f == 0)
+            af[kk & 1][0] = TA::frag(pa, fa, 0, kk);
+        else if (f <= F)
+            bf[kk & 1][f - 1] = TB::frag(pb, fb, f - 1, kk);
+        else
+            af[kk & 1][f - F] = TA::frag(pa, fa, f - F, kk);
+    };
+    // Stage s, A in the slot at `at`, B in the one behind it: the MFMAs of its four k-steps, under those of
+    // each the reads of the next one and half a part's loads, evenly. Near the end of the third one, when the
+    // wave's last reads of the stage are through, the wait for the next stage; its slots are free behind it.
+    // Loads run 1.2 (B) to 1.7 stages ahead: the second half of B of s + 1, A of s + 2, half of B of s + 2.
+    auto stage = [&](auto have1, auto have2, const Work& w, int s, uint32_t at) __attribute__((always_inline)) {
+        constexpr bool ONE = decltype(have1)::value, TWO = decltype(have2)::value;
+        const void *pb = nullptr, *pa2 = nullptr, *pb2 = nullptr;
+        if (ONE) pb = base_b(w, s + 1);
+        if (TWO) {
+            pa2 = base_a(w, s + 2);
+            pb2 = base_b(w, s + 2);
+        }
+        const uint32_t a1 = ahead(at, 2), b1 = ahead(at, 3), a2 = ahead(at, 4);
+        constexpr int M = F * F;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+            auto load = [&](int j) __attribute__((always_inline)) {
+                if (kk == 0 && ONE) issue(false, pb, b1, HALF + j);
+                if (kk == 1 && TWO) issue(true, pa2, a2, j);
+                if (kk == 2 && TWO) issue(true, pa2, a2, HALF + j);
+                if (kk == 3 && TWO) issue(false, pb2, at, j);
+            };
+            // (behind the last stage there is none to read of)
+            auto next_read = [&](const lds_u8* qa, const lds_u8* qb, int of, int f) __attribute__((always_inline)) {
+                if (of < 3 || ONE) read(qa, qb, (of + 1) & 3, f);
+            };
+            const lds_u8* pa = L + (kk == 3 ? a1 : at);
+            const lds_u8* pbk = L + (kk == 3 ? b1 : ahead(at, 1));
+#pragma unroll
+            for (int m = 0; m < M; ++m) {
+                acc[m / F][m % F] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[kk & 1][m % F], af[kk & 1][m / F], acc[m / F][m % F], 0, 0, 0);
+                if (F == 4) {
+                    if (kk == 2) {
+                        if (m % 4 != 3 && m / 4 * 3 + m % 4 < 2 * F) read(pa, pbk, kk + 1, m / 4 * 3 + m % 4);
+                        if (m == 3 || m == 7 || m == 10 || m == 11) load(m == 3 ? 0 : m == 7 ? 1 : m - 8);
+                    } else {
+                        if (m % 2 == 0) next_read(pa, pbk, kk, m / 2);
+                        if (m % 4 == 1) load(m / 4);
+                    }
+                } else if (kk == 2) {
+                    if (m < F) {
+                        read(pa, pbk, kk + 1, 2 * m);
+                        read(pa, pbk, kk + 1, 2 * m + 1);
+                        load(m);
+                    }
+                } else {
+                    next_read(pa, pbk, kk, m);
+                    if (m % 2 == 1) load(m / 2);
+                }
+                if (kk == 2 && m == (F == 4 ? 13 : 2)) {
+                    if (TWO)
+                        wait_and_meet<LOADS>();
+                    else
+                        wait_and_meet<0>();
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    };
+
+    // A tile's sums are read where they are used: the compiler would copy many of them at once, and spill them.
+    auto here = [&](f32x16_t& x) __attribute__((always_inline)) {
+        if (BT == 256)
+            asm volatile("" : "+a"(x));
+        else
+            asm volatile("" : "+v"(x));
+    };
+    // Register 8 h + e of acc[i][j]: row wm + 32 i + l32, column wn + 32 j + 16 h + 8 hw + e (by B's order of
+    // rows in the MFMA): a lane has 8 neighbours, the wave's store 32 bytes of each of 32 rows, and nothing goes
+    // through LDS, where the next tile's first loads arrive meanwhile.
+    auto finish = [&](const Work& w) __attribute__((always_inline)) {
+        const int lane = fresh_thread_index() & 63, l32 = lane & 31, hw = lane >> 5;
+        const int row0 = w.m0 + wm + l32, col0 = w.n0 + wn + 8 * hw;
+        if (w.part != nullptr) {
+            float* out = w.part + (wm + l32) * BT + wn + 8 * hw;
+#pragma unroll
+            for (int i = 0; i < F; ++i)
+#pragma unroll
+                for (int j = 0; j < 2 * F; ++j) {
+                    float z[8];
+                    if (j % 2 == 0) here(acc[i][j / 2]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[e] = acc[i][j / 2][8 * (j % 2) + e];
+                    store8(out + i * 32 * BT + 16 * j, z);
+                }
+            return;
+        }
+        if (!FULL) {
+#pragma unroll
+            for (int i = 0; i < F; ++i) {
+                if (row0 + 32 * i >= a.M) break;
+                __bf16* out = static_cast<__bf16*>(a.ep.o) + static_cast<int64_t>(row0 + 32 * i) * a.N + col0;
+#pragma unroll
+                for (int j = 0; j < 2 * F; ++j) {
+                    if (col0 + 16 * j >= a.N) break;
+                    float z[8];
+                    if (j % 2 == 0) here(acc[i][j / 2]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[e] = acc[i][j / 2][8 * (j % 2) + e];
+                    store8(out + 16 * j, z);
+                }
+            }
+            return;
+        }
+        by_kind(a.ep, [&](auto act, auto f32) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < F; ++i) {
+                const int row = row0 + 32 * i;
+                if (row >= a.M) break;
+                const int64_t at = static_cast<int64_t>(row) * a.N + col0;
+                const int64_t mod = a.ep.gate != nullptr ? a.ep.tg.row(row) * a.N + col0 : 0;
+#pragma unroll
+                for (int j = 0; j < 2 * F; ++j) {
+                    if (col0 + 16 * j >= a.N) break;
+                    float z[8];
+                    if (j % 2 == 0) here(acc[i][j / 2]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[e] = acc[i][j / 2][8 * (j % 2) + e];
+                    finish8<decltype(act)::value, decltype(f32)::value>(a.ep, at + 16 * j, mod + 16 * j, z);
+                }
+            }
+        });
+    };
+
+    Work w, next;
+    if (!next_work(w)) return;
+    begin(w);
+    // Vector-memory operations that follow begin()'s loads of the first stage: those of the second, and behind
+    // them the stores of the tile before, where all of its rows and columns exist (they complete in order).
+    bool stores = false;
+    constexpr int STORES = 2 * F * F;
+    for (;;) {
+        // the sums start from the bias (a split tile's get it where its parts are joined)
+        const int hw = (fresh_thread_index() & 63) >> 5;
+#pragma unroll
+        for (int j = 0; j < 2 * F; ++j) {
+            float bias[8] = {};
+            const int col = w.n0 + wn + 16 * j + 8 * hw;
+            if (FULL && a.ep.bias != nullptr && w.part == nullptr && col < a.N) load8(a.ep.bias + col, bias);
+#pragma unroll
+            for (int i = 0; i < F; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) acc[i][j / 2][8 * (j % 2) + e] = bias[e];
+        }
+        if (w.s1 - w.s0 > 1) {
+            if (stores)
+                wait_and_meet<LOADS + HALF + STORES>();
+            else
+                wait_and_meet<LOADS + HALF>();
         } else {
             wait_and_meet<0>();
         }
-
-        f32x16_t acc[F][F];
-#pragma unroll
-        for (int i = 0; i < F; ++i)
-#pragma unroll
-            for (int j = 0; j < F; ++j) acc[i][j] = f32x16_t{};
-        // a wave's operands of two k-steps; operand f: A's first block, B's blocks, A's others
-        bf16x8_t af[2][F], bf[2][F];
-        auto read = [&](const lds_u8* pa, const lds_u8* pb, int kk, int f) __attribute__((always_inline)) {
-            if (f == 0)
-                af[kk & 1][0] = TA::frag(pa, fa, 0, kk);
-            else if (f <= F)
-                bf[kk & 1][f - 1] = TB::frag(pb, fb, f - 1, kk);
-            else
-                af[kk & 1][f - F] = TA::frag(pa, fa, f - F, kk);
-        };
 #pragma unroll
         for (int f = 0; f < 2 * F; ++f) read(L, L + SLOT, 0, f);
-        // Stage s, A in the slot at `at`, B in the one behind it: the MFMAs of its four k-steps, under those of
-        // each the reads of the next one and half a part's loads, evenly. Near the end of the third one, when the
-        // wave's last reads of the stage are through, the wait for the next stage; its slots are free behind it.
-        // Loads run 1.2 (B) to 1.7 stages ahead: the second half of B of s + 1, A of s + 2, half of B of s + 2.
-        auto stage = [&](auto have1, auto have2, int s, uint32_t at) __attribute__((always_inline)) {
-            constexpr bool ONE = decltype(have1)::value, TWO = decltype(have2)::value;
-            const void *pb = nullptr, *pa2 = nullptr, *pb2 = nullptr;
-            if (ONE) pb = base_b(s + 1);
-            if (TWO) {
-                pa2 = base_a(s + 2);
-                pb2 = base_b(s + 2);
-            }
-            const uint32_t a1 = ahead(at, 2), b1 = ahead(at, 3), a2 = ahead(at, 4);
-            constexpr int M = F * F;
-#pragma unroll
-            for (int kk = 0; kk < 4; ++kk) {
-                auto load = [&](int j) __attribute__((always_inline)) {
-                    if (kk == 0 && ONE) issue(false, pb, b1, HALF + j);
-                    if (kk == 1 && TWO) issue(true, pa2, a2, j);
-                    if (kk == 2 && TWO) issue(true, pa2, a2, HALF + j);
-                    if (kk == 3 && TWO) issue(false, pb2, at, j);
-                };
-                const lds_u8* pa = L + (kk == 3 ? a1 : at);
-                const lds_u8* pbk = L + (kk == 3 ? b1 : ahead(at, 1));
-#pragma unroll
-                for (int m = 0; m < M; ++m) {
-                    acc[m / F][m % F] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[kk & 1][m % F], af[kk & 1][m / F], acc[m / F][m % F], 0, 0, 0);
-                    if (F == 4) {
-                        if (kk == 2) {
-                            if (m % 4 != 3 && m / 4 * 3 + m % 4 < 2 * F) read(pa, pbk, kk + 1, m / 4 * 3 + m % 4);
-                            if (m == 3 || m == 7 || m == 10 || m == 11) load(m == 3 ? 0 : m == 7 ? 1 : m - 8);
-                        } else {
-                            if (m % 2 == 0) read(pa, pbk, (kk + 1) & 3, m / 2);
-                            if (m % 4 == 1) load(m / 4);
-                        }
-                    } else if (kk == 2) {
-                        if (m < F) {
-                            read(pa, pbk, kk + 1, 2 * m);
-                            read(pa, pbk, kk + 1, 2 * m + 1);
-                            load(m);
-                        }
-                    } else {
-                        read(pa, pbk, (kk + 1) & 3, m);
-                        if (m % 2 == 1) load(m / 2);
-                    }
-                    if (kk == 2 && m == (F == 4 ? 13 : 2)) {
-                        if (TWO)
-                            wait_and_meet<LOADS>();
-                        else
-                            wait_and_meet<0>();
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            }
-        };
         uint32_t at = 0;
-        int s = s0;
-        for (; s + 2 < s1; ++s, at = ahead(at, 2)) stage(std::true_type{}, std::true_type{}, s, at);
-        for (; s + 1 < s1; ++s, at = ahead(at, 2)) stage(std::true_type{}, std::false_type{}, s, at);
-        stage(std::false_type{}, std::false_type{}, s, at);
-
-        // Register 4 g + e of acc[i][j]: row wm + 32 i + l32, column wn + 32 j + 8 g + 4 hw + e. Through the
-        // wave's own share of LDS (chunk c of row r at c ^ r % 16), 32 rows at a time, into whole rows.
-        constexpr int ROWB = WT * 4, LPR = WT / 8, RPP = 64 / LPR;
-        lds_u8* const own = L + wave * (32 * ROWB);
-        const int col = n0 + wn + (lane % LPR) * 8;
-        float bias[8] = {};
-        if (!split && a.ep.bias != nullptr && col < a.N) load8(a.ep.bias + col, bias);
-        float* part = split ? a.part + (static_cast<int64_t>(sw) * 2 + seg) * (BT * BT) : nullptr;
-#pragma unroll
-        for (int i = 0; i < F; ++i) {
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll
-            for (int j = 0; j < F; ++j)
-#pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    *(lds_f32x4_t*)(own + l32 * ROWB + (((8 * j + 2 * g + hw) ^ (l32 & 15)) << 4)) =
-                        f32x4_t{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll 2
-            for (int p = 0; p < 32 / RPP; ++p) {
-                const int r = p * RPP + lane / LPR, c = 2 * (lane % LPR);
-                const f32x4_t lo = *(const lds_f32x4_t*)(own + r * ROWB + ((c ^ (r & 15)) << 4));
-                const f32x4_t hi = *(const lds_f32x4_t*)(own + r * ROWB + (((c + 1) ^ (r & 15)) << 4));
-                float z[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-                const int in_tile = wm + 32 * i + r;
-                if (split) {
-                    store8(part + in_tile * BT + wn + (lane % LPR) * 8, z);
-                } else if (m0 + in_tile < a.M && col < a.N) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) z[e] += bias[e];
-                    finish8(a.ep, a.N, m0 + in_tile, col, z);
-                }
-            }
-        }
+        int s = w.s0;
+        for (; s + 2 < w.s1; ++s, at = ahead(at, 2)) stage(std::true_type{}, std::true_type{}, w, s, at);
+        for (; s + 1 < w.s1; ++s, at = ahead(at, 2)) stage(std::true_type{}, std::false_type{}, w, s, at);
+        stage(std::false_type{}, std::false_type{}, w, s, at);
+        // (since the last stage's wait no wave reads LDS)
+        const bool more = next_work(next);
+        if (more) begin(next);
+        finish(w);
+        if (!more) return;
+        stores = w.m0 + wm + WT <= a.M && w.n0 + wn + WT <= a.N;
+        w = next;
     }
 }
 
@@ -369,11 +482,10 @@ template <int BT>
 __global__ __launch_bounds__(256) void gemm_merge_kernel(const GemmArgs a) {
     constexpr int LPR = BT / 8, ROWS = 256 / LPR, PER = BT / ROWS;
     const int t = blockIdx.x / PER, id = a.whole + t;
-    constexpr int BAND = 8;
-    const int per = BAND * a.tiles_n, band = id / per, in = id % per;
-    const int high = min(BAND, a.tiles_m - band * BAND);
+    int m0, n0;
+    tile_at(a, id, BT, m0, n0);
     const int r = (blockIdx.x % PER) * ROWS + threadIdx.x / LPR, c = (threadIdx.x % LPR) * 8;
-    const int row = (band * BAND + in % high) * BT + r, col = in / high * BT + c;
+    const int row = m0 + r, col = n0 + c;
     if (row >= a.M || col >= a.N) return;
     const int64_t units = static_cast<int64_t>(a.tiles_m * a.tiles_n - a.whole) * a.stages;
     const int64_t u0 = static_cast<int64_t>(t) * a.stages, u1 = u0 + a.stages;
@@ -393,13 +505,18 @@ __global__ __launch_bounds__(256) void gemm_merge_kernel(const GemmArgs a) {
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) z[e] += sum[e];
-    finish8(a.ep, a.N, row, col, z);
+    const int64_t at = static_cast<int64_t>(row) * a.N + col, mod = a.ep.gate != nullptr ? a.ep.tg.row(row) * a.N + col : 0;
+    by_kind(a.ep, [&](auto act, auto f32) __attribute__((always_inline)) {
+        finish8<decltype(act)::value, decltype(f32)::value>(a.ep, at, mod, z);
+    });
 }
 
 template <int BT, bool AT, bool BTR>
 hipError_t launch_tiles(const GemmArgs& a, hipStream_t s) {
     const int rest = a.tiles_m * a.tiles_n - a.whole;
-    hipError_t e = launch_with(gemm_kernel<BT, AT, BTR>, dim3(a.whole + (rest ? a.split_wgs : 0)), 256, s, a);
+    // as many workgroups as the chip holds at a time; each takes one tile after the other
+    const int most = BT == 256 ? kCUs : 2 * kCUs;
+    hipError_t e = launch_with(gemm_kernel<BT, AT, BTR, !BTR>, dim3(std::min(most, std::max(a.whole, rest ? a.split_wgs : 0))), 256, s, a);
     if (e != hipSuccess || rest == 0) return e;
     constexpr int PER = BT / (256 / (BT / 8));
     return launch_with(gemm_merge_kernel<BT>, dim3(rest * PER), 256, s, a);
@@ -466,7 +583,7 @@ __global__ __launch_bounds__(NW * 64) void few_rows_kernel(const FewRowsArgs a) 
     z += sum;
     const int64_t at = static_cast<int64_t>(row) * a.N + col;
     if (a.ep.pre != nullptr) static_cast<__bf16*>(a.ep.pre)[at] = static_cast<__bf16>(z);
-    z = activate(z, a.ep.act);
+    z = a.ep.act == kActGelu ? activate<kActGelu>(z) : a.ep.act == kActSilu ? activate<kActSilu>(z) : z;
     if (a.ep.gate != nullptr) z *= a.ep.gate[a.ep.tg.row(row) * a.N + col];
     if (a.ep.residual != nullptr)
         z += a.ep.o_f32 ? static_cast<const float*>(a.ep.residual)[at]
