@@ -63,24 +63,18 @@ __device__ __forceinline__ void store8(__bf16* p, const float (&x)[8]) {
     *reinterpret_cast<bf16x8_t*>(p) = v;
 }
 
-// Eight neighbours at element `at` of the output, `mod` of the gate: z holds the sums of products plus bias.
+// Eight neighbours at element `at` of the output: z holds the sums of products plus bias, g the gate, r the
+// residual (which the caller loads, well ahead).
 template <int ACT, bool F32>
-__device__ __forceinline__ void finish8(const LinearEpilogue& ep, int64_t at, int64_t mod, float (&z)[8]) {
+__device__ __forceinline__ void finish8(const LinearEpilogue& ep, int64_t at, float (&z)[8], const float (&g)[8], const float (&r)[8]) {
     if (ep.pre != nullptr) store8(static_cast<__bf16*>(ep.pre) + at, z);
 #pragma unroll
     for (int e = 0; e < 8; ++e) z[e] = activate<ACT>(z[e]);
     if (ep.gate != nullptr) {
-        float g[8];
-        load8(ep.gate + mod, g);
 #pragma unroll
         for (int e = 0; e < 8; ++e) z[e] *= g[e];
     }
     if (ep.residual != nullptr) {
-        float r[8];
-        if (F32)
-            load8(static_cast<const float*>(ep.residual) + at, r);
-        else
-            load8(static_cast<const __bf16*>(ep.residual) + at, r);
 #pragma unroll
         for (int e = 0; e < 8; ++e) z[e] += r[e];
     }
@@ -88,6 +82,13 @@ __device__ __forceinline__ void finish8(const LinearEpilogue& ep, int64_t at, in
         store8(static_cast<float*>(ep.o) + at, z);
     else
         store8(static_cast<__bf16*>(ep.o) + at, z);
+}
+template <bool F32>
+__device__ __forceinline__ void load_residual(const LinearEpilogue& ep, int64_t at, float (&r)[8]) {
+    if (F32)
+        load8(static_cast<const float*>(ep.residual) + at, r);
+    else
+        load8(static_cast<const __bf16*>(ep.residual) + at, r);
 }
 
 // body(activation, whether the output is fp32) with both known to the compiler
@@ -271,7 +272,7 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const Gemm
         const uint32_t x = slot + by * SLOT;
         return x >= kSlots * SLOT ? x - kSlots * SLOT : x;
     };
-    // The first loads of a tile: A and B of its first stage, A and half of B of the second.
+    // The first loads of a tile: A and B of its first two stages.
     auto begin = [&](const Work& w) __attribute__((always_inline)) {
         const int lane = fresh_thread_index() & 63;  // (what follows from it is not kept from tile to tile)
         ta.init(wave, lane, a.lda, a.M - w.m0);
@@ -292,7 +293,7 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const Gemm
 #pragma unroll
             for (int j = 0; j < LOADS; ++j) issue(true, pa, 2 * SLOT, j);
 #pragma unroll
-            for (int j = 0; j < HALF; ++j) issue(false, pb, 3 * SLOT, j);
+            for (int j = 0; j < LOADS; ++j) issue(false, pb, 3 * SLOT, j);
         }
     };
 
@@ -308,13 +309,13 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const Gemm
             af[kk & 1][f - F] = TA::frag(pa, fa, f - F, kk);
     };
     // Stage s, A in the slot at `at`, B in the one behind it: the MFMAs of its four k-steps, under those of
-    // each the reads of the next one and half a part's loads, evenly. Near the end of the third one, when the
+    // each the reads of the next one, and loads. Near the end of the third one, when the
     // wave's last reads of the stage are through, the wait for the next stage; its slots are free behind it.
-    // Loads run 1.2 (B) to 1.7 stages ahead: the second half of B of s + 1, A of s + 2, half of B of s + 2.
+    // Loads: A of s + 2 under the first two k-steps, B of s + 2 under the last, all at once, since it has the
+    // shorter time, little less than a stage, until it is waited for.
     auto stage = [&](auto have1, auto have2, const Work& w, int s, uint32_t at) __attribute__((always_inline)) {
         constexpr bool ONE = decltype(have1)::value, TWO = decltype(have2)::value;
-        const void *pb = nullptr, *pa2 = nullptr, *pb2 = nullptr;
-        if (ONE) pb = base_b(w, s + 1);
+        const void *pa2 = nullptr, *pb2 = nullptr;
         if (TWO) {
             pa2 = base_a(w, s + 2);
             pb2 = base_b(w, s + 2);
@@ -324,10 +325,9 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const Gemm
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
             auto load = [&](int j) __attribute__((always_inline)) {
-                if (kk == 0 && ONE) issue(false, pb, b1, HALF + j);
-                if (kk == 1 && TWO) issue(true, pa2, a2, j);
-                if (kk == 2 && TWO) issue(true, pa2, a2, HALF + j);
                 if (kk == 3 && TWO) issue(false, pb2, at, j);
+                if (kk == 0 && TWO) issue(true, pa2, a2, j);
+                if (kk == 1 && TWO) issue(true, pa2, a2, HALF + j);
             };
             // (behind the last stage there is none to read of)
             auto next_read = [&](const lds_u8* qa, const lds_u8* qb, int of, int f) __attribute__((always_inline)) {
@@ -341,20 +341,20 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const Gemm
                 if (F == 4) {
                     if (kk == 2) {
                         if (m % 4 != 3 && m / 4 * 3 + m % 4 < 2 * F) read(pa, pbk, kk + 1, m / 4 * 3 + m % 4);
-                        if (m == 3 || m == 7 || m == 10 || m == 11) load(m == 3 ? 0 : m == 7 ? 1 : m - 8);
                     } else {
                         if (m % 2 == 0) next_read(pa, pbk, kk, m / 2);
-                        if (m % 4 == 1) load(m / 4);
+                        if (kk == 3 && m % 2 == 1) load(m / 2);
+                        if (kk < 2 && m % 4 == 1) load(m / 4);
                     }
                 } else if (kk == 2) {
                     if (m < F) {
                         read(pa, pbk, kk + 1, 2 * m);
                         read(pa, pbk, kk + 1, 2 * m + 1);
-                        load(m);
                     }
                 } else {
                     next_read(pa, pbk, kk, m);
-                    if (m % 2 == 1) load(m / 2);
+                    if (kk == 3) load(m);
+                    if (kk < 2 && m % 2 == 1) load(m / 2);
                 }
                 if (kk == 2 && m == (F == 4 ? 13 : 2)) {
                     if (TWO)
@@ -417,7 +417,20 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const Gemm
                 const int row = row0 + 32 * i;
                 if (row >= a.M) break;
                 const int64_t at = static_cast<int64_t>(row) * a.N + col0;
-                const int64_t mod = a.ep.gate != nullptr ? a.ep.tg.row(row) * a.N + col0 : 0;
+                // gate and residual of a row of blocks at once
+                constexpr bool F32 = decltype(f32)::value;
+                float g[2 * F][8], r[2 * F][8];
+                if (a.ep.gate != nullptr) {
+                    const int64_t mod = a.ep.tg.row(row) * a.N + col0;
+#pragma unroll
+                    for (int j = 0; j < 2 * F; ++j)
+                        if (col0 + 16 * j < a.N) load8(a.ep.gate + mod + 16 * j, g[j]);
+                }
+                if (a.ep.residual != nullptr) {
+#pragma unroll
+                    for (int j = 0; j < 2 * F; ++j)
+                        if (col0 + 16 * j < a.N) load_residual<F32>(a.ep, at + 16 * j, r[j]);
+                }
 #pragma unroll
                 for (int j = 0; j < 2 * F; ++j) {
                     if (col0 + 16 * j >= a.N) break;
@@ -425,7 +438,7 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const Gemm
                     if (j % 2 == 0) here(acc[i][j / 2]);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) z[e] = acc[i][j / 2][8 * (j % 2) + e];
-                    finish8<decltype(act)::value, decltype(f32)::value>(a.ep, at + 16 * j, mod + 16 * j, z);
+                    finish8<decltype(act)::value, F32>(a.ep, at + 16 * j, z, g[j], r[j]);
                 }
             }
         });
@@ -453,9 +466,9 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const Gemm
         }
         if (w.s1 - w.s0 > 1) {
             if (stores)
-                wait_and_meet<LOADS + HALF + STORES>();
+                wait_and_meet<2 * LOADS + STORES>();
             else
-                wait_and_meet<LOADS + HALF>();
+                wait_and_meet<2 * LOADS>();
         } else {
             wait_and_meet<0>();
         }
@@ -505,9 +518,12 @@ __global__ __launch_bounds__(256) void gemm_merge_kernel(const GemmArgs a) {
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) z[e] += sum[e];
-    const int64_t at = static_cast<int64_t>(row) * a.N + col, mod = a.ep.gate != nullptr ? a.ep.tg.row(row) * a.N + col : 0;
+    const int64_t at = static_cast<int64_t>(row) * a.N + col;
     by_kind(a.ep, [&](auto act, auto f32) __attribute__((always_inline)) {
-        finish8<decltype(act)::value, decltype(f32)::value>(a.ep, at, mod, z);
+        float g[8], r[8];
+        if (a.ep.gate != nullptr) load8(a.ep.gate + a.ep.tg.row(row) * a.N + col, g);
+        if (a.ep.residual != nullptr) load_residual<decltype(f32)::value>(a.ep, at, r);
+        finish8<decltype(act)::value, decltype(f32)::value>(a.ep, at, z, g, r);
     });
 }
 
