@@ -21,6 +21,7 @@
 #include <cstdio>
 #include <initializer_list>
 #include <new>
+#include <numeric>
 #include <utility>
 
 #include "tm.h"
@@ -1721,11 +1722,23 @@ tm_status check_linear(const tm_linear_desc* d, int32_t n_tok, int64_t first_tok
 // Tiles of a product of M x N sums of K, and how many of them are split.
 struct GemmPlan {
     int tile;
-    int64_t tiles_m, tiles_n, stages, whole, split_wgs;
-    size_t part_bytes() const {
-        return tiles_m * tiles_n == whole ? 0 : size_t(split_wgs) * 2 * size_t(tile) * size_t(tile) * 4;
-    }
+    int64_t tiles_m, tiles_n, stages, whole, groups, shares;  // as in GemmArgs
+    size_t part_bytes() const { return size_t(groups * shares) * 2 * size_t(tile) * size_t(tile) * 4; }
 };
+
+// Workgroups that share out `rest` tiles, and in how many groups: at most `most`, with 1/8 less if that makes groups
+// enough for an XCD's 32 workgroups to go through the same k.
+void plan_shares(int64_t rest, int64_t most, GemmPlan* p) {
+    int64_t best = 0;
+    for (int64_t w = most; w >= rest && w >= most - most / 8; --w) {
+        const int64_t g = std::gcd(rest, w);
+        if (std::min<int64_t>(g, 32) > best) {
+            best = std::min<int64_t>(g, 32);
+            p->groups = g;
+            p->shares = w / g;
+        }
+    }
+}
 
 GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool may_split) {
     GemmPlan best{};
@@ -1746,12 +1759,14 @@ GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool may_split) {
         // (at least 4 stages a workgroup)
         const int64_t wgs = std::min(at_once, rest * p.stages / 4);
         if (may_split && rest > 0 && wgs > rest) {
+            GemmPlan q = p;
+            q.whole = tiles - rest;
+            plan_shares(rest, wgs, &q);
             const double with = double(tiles / at_once) * (double(p.stages) * stage + ends) +
-                                double(rest * p.stages) / double(wgs) * stage + ends + merge;
+                                double(rest * p.stages) / double(q.groups * q.shares) * stage + ends + merge;
             if (with < cost) {
                 cost = with;
-                p.whole = tiles - rest;
-                p.split_wgs = wgs;
+                p = q;
             }
         }
         if (best.tile == 0 || cost < best_cost) {
@@ -1781,7 +1796,8 @@ tmk::GemmArgs gemm_args(const GemmPlan& p, const void* a, const void* b, int64_t
     g.tiles_n = int32_t(p.tiles_n);
     g.stages = int32_t(p.stages);
     g.whole = int32_t(p.whole);
-    g.split_wgs = int32_t(p.split_wgs);
+    g.groups = int32_t(p.groups);
+    g.shares = int32_t(p.shares);
     g.part = static_cast<float*>(part);
     return g;
 }

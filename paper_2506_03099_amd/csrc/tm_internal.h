@@ -361,8 +361,9 @@ struct GemmArgs {
     int32_t tiles_m, tiles_n;
     int32_t stages;     // of kGemmDepth k each, the last one's first k only
     int32_t whole;      // tiles that a workgroup takes alone; the others' stages are dealt out
-    int32_t split_wgs;  // to this many workgroups in equal shares
-    float* part;        // [split_wgs][2][tile][tile], or null where none is split
+    int32_t groups;     // in so many groups of as many tiles each (group i: tiles whole + i, + groups, ...),
+    int32_t shares;     // each to this many workgroups in equal shares, at most a tile's stages each
+    float* part;        // [shares][groups][2][tile][tile], or null where none is split
     LinearEpilogue ep;
 };
 constexpr int kGemmDepth = 64;

@@ -214,18 +214,16 @@ void split_checks() {
                 EXPECT(rest >= 0);
                 if (rest == 0) continue;
                 ++split;
-                const int64_t units = rest * p.stages, W = p.split_wgs;
-                EXPECT(W >= rest && W <= units);
-                int64_t slots = 0;
+                const int64_t per_group = rest / p.groups, units = per_group * p.stages, W = p.shares;
+                EXPECT(per_group * p.groups == rest && W >= per_group && W <= units);
+                EXPECT(p.groups * W <= (p.tile == 256 ? 256 : 512));
                 for (int64_t w = 0; w < W; ++w) {
                     const int64_t u0 = units * w / W, u1 = units * (w + 1) / W;
                     EXPECT(u0 < u1);
-                    EXPECT((u1 - 1) / p.stages - u0 / p.stages <= 1);
-                    slots += (u1 - 1) / p.stages - u0 / p.stages + 1;
+                    EXPECT((u1 - 1) / p.stages - u0 / p.stages <= 1);  // its two partial tiles
                 }
-                EXPECT(slots <= 2 * W);
-                EXPECT(p.part_bytes() == size_t(2 * W) * size_t(p.tile) * size_t(p.tile) * 4);
-                for (int64_t t = 0; t < rest; ++t) {
+                EXPECT(p.part_bytes() == size_t(2 * p.groups * W) * size_t(p.tile) * size_t(p.tile) * 4);
+                for (int64_t t = 0; t < per_group; ++t) {
                     const int64_t u0 = t * p.stages, u1 = u0 + p.stages;
                     int64_t w = u0 * W / units;
                     EXPECT(units * w / W <= u0);
