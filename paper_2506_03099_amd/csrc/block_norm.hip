@@ -41,32 +41,53 @@ __device__ __forceinline__ void store4(void* p, int64_t at, f32x4_t v) {
     *reinterpret_cast<typename Four<T>::raw*>(static_cast<T*>(p) + at) = w;
 }
 
+// v of the lane that the DPP control CTRL names (0 where there is none, or where ROWS leaves the row out), added.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float add_dpp(float v) {
+    const int moved = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, true);
+    return v + __builtin_bit_cast(float, moved);
+}
+// The sum over 16 lanes in lane 15 of each row of them, and over the wave in lane 63: row_shr 1, 2, 4, 8, then
+// row_bcast 15 and 31. (A shuffle through LDS takes ten times as long as one of these steps, and a row's
+// statistics wait for three such sums, one after the other.)
+__device__ __forceinline__ float row_sum(float v) {
+    v = add_dpp<0x111, 0xf>(v);
+    v = add_dpp<0x112, 0xf>(v);
+    v = add_dpp<0x114, 0xf>(v);
+    return add_dpp<0x118, 0xf>(v);
+}
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
-    return v;
+    v = row_sum(v);
+    v = add_dpp<0x142, 0xa>(v);
+    return add_dpp<0x143, 0xc>(v);
+}
+__device__ __forceinline__ float lane_value(float v, int lane) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
 }
 
 constexpr int kMaxWaves = 16;
 
 // Sums of N values over the workgroup, the same in every lane, in a fixed order. `slots`: N * kMaxWaves
-// floats that no wave of the workgroup still reads.
+// floats that no wave of the workgroup still reads, zeros where there is no wave.
 template <int N>
 __device__ __forceinline__ void group_sum(float (&v)[N], lds_float* slots, int waves, int wave, int lane) {
 #pragma unroll
     for (int k = 0; k < N; ++k) v[k] = wave_sum(v[k]);
-    if (waves == 1) return;
-    if (lane == 0) {
+    if (waves == 1) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = lane_value(v[k], 63);
+        return;
+    }
+    if (lane == 63) {
 #pragma unroll
         for (int k = 0; k < N; ++k) slots[k * kMaxWaves + wave] = v[k];
     }
     __syncthreads();
+    float s[N];
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-        float s = 0.f;
-        for (int w = 0; w < waves; ++w) s += slots[k * kMaxWaves + w];
-        v[k] = s;
-    }
+    for (int k = 0; k < N; ++k) s[k] = slots[k * kMaxWaves + (lane & 15)];
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = lane_value(row_sum(s[k]), 15);
 }
 
 // One row per workgroup, four neighbouring elements a lane, U times.
@@ -77,6 +98,7 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(const BlockNormArgs a)
     const int T = blockDim.x, waves = T / 64, tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int row = blockIdx.x;
+    if (waves > 1 && tid < 4 * kMaxWaves) L[tid] = 0.f;
     const int64_t base = static_cast<int64_t>(row) * a.E;
     const int64_t mod = a.tg.row(row) * a.E;
     f32x4_t x[U];
@@ -88,6 +110,7 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(const BlockNormArgs a)
         in[u] = col[u] < a.E;
         x[u] = in[u] ? as_f32<S>(load4<S>(a.x, base + col[u])) : f32x4_t{};
     }
+    if (waves > 1) __syncthreads();  // the slots are clear
     // Normalised values of v over the row, in place: (v - mean) / sqrt(var + eps) with the variance from the
     // centred values, or v / sqrt(mean of squares + eps); zeros stay where the row has ended.
     auto normalise = [&](f32x4_t (&v)[U], int kind, lds_float* slots) __attribute__((always_inline)) {
@@ -154,6 +177,8 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(const BlockNormBwd
     __shared__ float smem[2 * 8 * kMaxWaves];
     const int T = blockDim.x, waves = T / 64, tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    for (int i = tid; i < 2 * 8 * kMaxWaves; i += T) ((lds_float*)smem)[i] = 0.f;  // no wave's slots stay so
+    __syncthreads();
     int32_t b, t0, t1;
     int64_t mod;
     a.parts.of(blockIdx.x, b, mod, t0, t1);
@@ -319,6 +344,7 @@ __global__ __launch_bounds__(64 * LANES) void column_sums_kernel(const ColumnSum
         const float* at = a.part + static_cast<int64_t>(o.v) * a.E + e;
         const int n = a.parts.count();
         if (in) {
+#pragma unroll 4
             for (int i = l; i < n; i += LANES) {
                 const int g = i / a.parts.per_group, b = g / a.parts.touched;
                 const int64_t mod = static_cast<int64_t>(b) * a.parts.groups + a.parts.g0 + g % a.parts.touched;
@@ -340,6 +366,7 @@ __global__ __launch_bounds__(64 * LANES) void column_sums_kernel(const ColumnSum
     const int b = static_cast<int>(row / a.parts.groups), j = static_cast<int>(row % a.parts.groups) - a.parts.g0;
     if (in && j >= 0 && j < a.parts.touched) {
         const int first = (b * a.parts.touched + j) * a.parts.per_group;
+#pragma unroll 4
         for (int i = l; i < a.parts.per_group; i += LANES) {
             const float* at = a.part + (first + i) * stride + e;
             s += at[static_cast<int64_t>(o.v) * a.E];

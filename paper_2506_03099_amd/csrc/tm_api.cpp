@@ -1630,7 +1630,7 @@ tmk::TokenGroups token_groups(const Run& r) {
     return t;
 }
 
-// About `want` parts, none of them of fewer than `least` rows where a group has that many.
+// At most `want` parts (but one for each group), of no fewer than `least` rows where a group has that many.
 tmk::RowParts row_parts(const Run& r, int64_t want, int64_t least) {
     tmk::RowParts p{};
     p.B = int32_t(r.B);
@@ -1640,8 +1640,7 @@ tmk::RowParts row_parts(const Run& r, int64_t want, int64_t least) {
     p.touched = int32_t(r.touched);
     p.g0 = int32_t(r.g0);
     p.groups = int32_t(r.groups);
-    const int64_t rows = std::min(std::max(ceil_div(r.rows, want), least), r.len);
-    p.per_group = int32_t(ceil_div(r.len, rows));
+    p.per_group = int32_t(std::max<int64_t>(1, std::min(want / (r.B * r.touched), ceil_div(r.len, least))));
     p.rows_per_part = int32_t(ceil_div(r.len, p.per_group));
     return p;
 }
@@ -1675,8 +1674,7 @@ tm_status check_norm(const tm_block_norm_desc* d, int32_t n_tok, int64_t first_t
     if ((st = check_modulation(d->batch, d->groups, g->E)) != TM_OK) return st;
     g->act = d->dtype == TM_BF16 ? 2 : 4;
     g->stream = d->stream_dtype == TM_BF16 ? 2 : 4;
-    // two workgroups a CU, but 8 rows at least to share a part's sums
-    g->parts = row_parts(g->run, 2 * tmk::kCUs, 8);
+    g->parts = row_parts(g->run, 2 * tmk::kCUs, 2);
     g->part_bytes = size_t(g->parts.count()) * tmk::kNormSums * size_t(g->E) * 4;
     return TM_OK;
 }
