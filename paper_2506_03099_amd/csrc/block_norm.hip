@@ -13,6 +13,7 @@ namespace tmk {
 namespace {
 
 typedef __attribute__((address_space(3))) float lds_float;
+typedef __attribute__((address_space(3))) f32x4_t lds_f32x4_t;
 
 // Four neighbouring elements of a row in memory, and as fp32.
 template <typename T>
@@ -174,7 +175,11 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(const BlockNormArgs a)
 // rows of its columns.
 template <typename S, typename A, int U>
 __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(const BlockNormBwdArgs a) {
+    // Rows of more than 8192 (U = 5) leave no registers for all of it: a sum lives in LDS, and the vectors are
+    // read anew for each row.
+    constexpr bool WIDE = U > 2;
     __shared__ float smem[2 * 8 * kMaxWaves];
+    __shared__ __attribute__((aligned(16))) float wide[WIDE ? kMaxNormWidth : 4];
     const int T = blockDim.x, waves = T / 64, tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     for (int i = tid; i < 2 * 8 * kMaxWaves; i += T) ((lds_float*)smem)[i] = 0.f;  // no wave's slots stay so
@@ -183,127 +188,146 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(const BlockNormBwd
     int64_t mod;
     a.parts.of(blockIdx.x, b, mod, t0, t1);
     const bool has_pre = a.pre != kNormNone, has_y = a.y != nullptr, has_dr = a.dr != nullptr;
+    const bool pre_layer = a.pre == kNormLayer, post_layer = a.post == kNormLayer;
     int col[U];
     bool in[U];
-    f32x4_t by_pre[U], by_post[U];  // (1 + scale) pre_weight, gate post_weight
-    f32x4_t sum_dh[U], sum_dhn[U], sum_av[U];
+    const f32x4_t one = f32x4_t{1.f, 1.f, 1.f, 1.f};
+    // (1 + scale) pre_weight and gate post_weight of a lane's columns
+    auto load_by_pre = [&](int u) __attribute__((always_inline)) {
+        f32x4_t v = one;
+        if (in[u]) {
+            if (a.scale != nullptr) v += load4<float>(a.scale, mod * a.E + col[u]);
+            if (a.pre_weight != nullptr) v *= load4<float>(a.pre_weight, col[u]);
+        }
+        return v;
+    };
+    auto load_by_post = [&](int u) __attribute__((always_inline)) {
+        f32x4_t v = one;
+        if (in[u]) {
+            if (a.gate != nullptr) v = load4<float>(a.gate, mod * a.E + col[u]);
+            if (a.post_weight != nullptr) v *= load4<float>(a.post_weight, col[u]);
+        }
+        return v;
+    };
+    f32x4_t by_pre_kept[WIDE ? 1 : U], by_post_kept[WIDE ? 1 : U];
+    f32x4_t sum_dh[WIDE ? 1 : U], sum_dhn[U], sum_av[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         col[u] = (u * T + tid) * 4;
         in[u] = col[u] < a.E;
-        const f32x4_t one = f32x4_t{1.f, 1.f, 1.f, 1.f};
-        by_pre[u] = by_post[u] = one;
-        if (in[u]) {
-            if (a.scale != nullptr) by_pre[u] += load4<float>(a.scale, mod * a.E + col[u]);
-            if (a.pre_weight != nullptr) by_pre[u] *= load4<float>(a.pre_weight, col[u]);
-            if (a.gate != nullptr) by_post[u] = load4<float>(a.gate, mod * a.E + col[u]);
-            if (a.post_weight != nullptr) by_post[u] *= load4<float>(a.post_weight, col[u]);
+        sum_dhn[u] = sum_av[u] = f32x4_t{};
+        if (WIDE) {
+            if (in[u]) *(lds_f32x4_t*)((lds_float*)wide + col[u]) = f32x4_t{};
+        } else {
+            by_pre_kept[u] = load_by_pre(u);
+            by_post_kept[u] = load_by_post(u);
+            sum_dh[u] = f32x4_t{};
         }
-        sum_dh[u] = sum_dhn[u] = sum_av[u] = f32x4_t{};
     }
-    typename Four<S>::raw r_next[U], dr_next[U];
-    typename Four<A>::raw dh_next[U], y_next[U];
-    auto load_row = [&](int t) __attribute__((always_inline)) {
-        const int64_t base = (static_cast<int64_t>(b) * a.parts.n + t) * a.E;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            r_next[u] = dr_next[u] = typename Four<S>::raw{};
-            dh_next[u] = y_next[u] = typename Four<A>::raw{};
-            if (!in[u]) continue;
-            if (has_pre) {
-                r_next[u] = load4<S>(a.r, base + col[u]);
-                dh_next[u] = load4<A>(a.dh, base + col[u]);
-            }
-            if (has_dr) dr_next[u] = load4<S>(a.dr, base + col[u]);
-            if (has_y) y_next[u] = load4<A>(a.y, base + col[u]);
-        }
-    };
-    if (t0 < t1) load_row(t0);
+    auto by_pre = [&](int u) __attribute__((always_inline)) { return WIDE ? load_by_pre(u) : by_pre_kept[WIDE ? 0 : u]; };
+    auto by_post = [&](int u) __attribute__((always_inline)) { return WIDE ? load_by_post(u) : by_post_kept[WIDE ? 0 : u]; };
     for (int t = t0; t < t1; ++t) {
         // (sums of a row in slots that the row before does not use: a wave may still read those)
         lds_float* const L = (lds_float*)smem + (t & 1) * 8 * kMaxWaves;
         const int64_t base = (static_cast<int64_t>(b) * a.parts.n + t) * a.E;
-        f32x4_t r[U], dx[U], dh[U], y[U];
+        // kept as they come, and turned into fp32 where they are used. (Loads a row ahead were no faster: 653 for
+        // 655 us for the 480p clip, with 31 registers more.)
+        typename Four<S>::raw r_raw[U], dr_raw[U];
+        typename Four<A>::raw dh_raw[U], y_raw[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            r[u] = as_f32<S>(r_next[u]);
-            dx[u] = as_f32<S>(dr_next[u]);
-            dh[u] = as_f32<A>(dh_next[u]);
-            y[u] = as_f32<A>(y_next[u]);
+            r_raw[u] = dr_raw[u] = typename Four<S>::raw{};
+            dh_raw[u] = y_raw[u] = typename Four<A>::raw{};
+            if (!in[u]) continue;
+            if (has_pre) {
+                r_raw[u] = load4<S>(a.r, base + col[u]);
+                dh_raw[u] = load4<A>(a.dh, base + col[u]);
+            }
+            if (has_dr) dr_raw[u] = load4<S>(a.dr, base + col[u]);
+            if (has_y) y_raw[u] = load4<A>(a.y, base + col[u]);
         }
-        if (t + 1 < t1) load_row(t + 1);
-        const bool pre_layer = a.pre == kNormLayer, post_layer = a.post == kNormLayer;
-        float mean_t = 0.f;
+        float mean_t = 0.f, mean_r = 0.f, mean_y = 0.f;
         if (pre_layer || post_layer) {
             float s[3] = {0.f, 0.f, 0.f};
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[0] += r[u][e];
-                    s[1] = fmaf(dh[u][e], by_pre[u][e], s[1]);
-                    s[2] += y[u][e];
-                }
+            for (int u = 0; u < U; ++u) {
+                const f32x4_t r = as_f32<S>(r_raw[u]), d = as_f32<A>(dh_raw[u]) * by_pre(u), y = as_f32<A>(y_raw[u]);
+                s[0] += (r[0] + r[1]) + (r[2] + r[3]);
+                s[1] += (d[0] + d[1]) + (d[2] + d[3]);
+                s[2] += (y[0] + y[1]) + (y[2] + y[3]);
+            }
             group_sum(s, L, waves, wave, lane);
-            mean_t = pre_layer ? s[1] * a.inv_E : 0.f;
-            const float mr = pre_layer ? s[0] * a.inv_E : 0.f, my = post_layer ? s[2] * a.inv_E : 0.f;
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    r[u][e] = in[u] ? r[u][e] - mr : 0.f;
-                    y[u][e] = in[u] ? y[u][e] - my : 0.f;
-                }
+            if (pre_layer) {
+                mean_r = s[0] * a.inv_E;
+                mean_t = s[1] * a.inv_E;
+            }
+            if (post_layer) mean_y = s[2] * a.inv_E;
         }
-        float post_by = 1.f;
+        // (zeros stay where the row has ended)
+        auto r_centred = [&](int u, int e) __attribute__((always_inline)) {
+            return in[u] ? static_cast<float>(r_raw[u][e]) - mean_r : 0.f;
+        };
+        auto y_centred = [&](int u, int e) __attribute__((always_inline)) {
+            return in[u] ? static_cast<float>(y_raw[u][e]) - mean_y : 0.f;
+        };
+        float pre_by = 1.f, post_by = 1.f, along_r = 0.f;
         if (has_pre || a.post != kNormNone) {
             float s[3] = {0.f, 0.f, 0.f};  // squares of r and y, and t r
 #pragma unroll
-            for (int u = 0; u < U; ++u)
+            for (int u = 0; u < U; ++u) {
+                const f32x4_t d = as_f32<A>(dh_raw[u]) * by_pre(u);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    s[0] = fmaf(r[u][e], r[u][e], s[0]);
-                    s[1] = fmaf(dh[u][e] * by_pre[u][e], r[u][e], s[1]);
-                    s[2] = fmaf(y[u][e], y[u][e], s[2]);
+                    const float r = r_centred(u, e), y = y_centred(u, e);
+                    s[0] = fmaf(r, r, s[0]);
+                    s[1] = fmaf(d[e], r, s[1]);
+                    s[2] = fmaf(y, y, s[2]);
                 }
+            }
             group_sum(s, L + 3 * kMaxWaves, waves, wave, lane);
             if (has_pre) {
-                const float by = 1.f / sqrtf(fmaf(s[0], a.inv_E, a.eps));
-                const float along = s[1] * by * a.inv_E;  // mean of t n
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float n = r[u][e] * by, d = dh[u][e];
-                        sum_dh[u][e] += d;
-                        sum_dhn[u][e] = fmaf(d, n, sum_dhn[u][e]);
-                        dx[u][e] = fmaf(by, fmaf(d, by_pre[u][e], -mean_t) - n * along, dx[u][e]);
-                    }
+                pre_by = 1.f / sqrtf(fmaf(s[0], a.inv_E, a.eps));
+                along_r = s[1] * pre_by * a.inv_E;  // mean of t n
             }
             if (a.post != kNormNone) post_by = 1.f / sqrtf(fmaf(s[2], a.inv_E, a.eps));
         }
+        f32x4_t dx[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (in[u]) store4<S>(a.dx, base + col[u], dx[u]);
-        if (!has_y) continue;
-        float mean_u = 0.f, along = 0.f;
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                y[u][e] *= post_by;
-                sum_av[u][e] = fmaf(dx[u][e], y[u][e], sum_av[u][e]);
-                dx[u][e] = in[u] ? dx[u][e] * by_post[u][e] : 0.f;
-            }
-        if (a.post != kNormNone) {
-            float s[2] = {0.f, 0.f};
-#pragma unroll
-            for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
+            dx[u] = as_f32<S>(dr_raw[u]);
+            if (has_pre) {
+                const f32x4_t d = as_f32<A>(dh_raw[u]), by = by_pre(u);
+                f32x4_t sum = WIDE ? f32x4_t{} : sum_dh[WIDE ? 0 : u];
+                if (WIDE && in[u]) sum = *(lds_f32x4_t*)((lds_float*)wide + col[u]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    s[0] += dx[u][e];
-                    s[1] = fmaf(dx[u][e], y[u][e], s[1]);
+                    const float n = r_centred(u, e) * pre_by;
+                    sum[e] += d[e];
+                    sum_dhn[u][e] = fmaf(d[e], n, sum_dhn[u][e]);
+                    dx[u][e] = fmaf(pre_by, fmaf(d[e], by[e], -mean_t) - n * along_r, dx[u][e]);
                 }
+                if (!WIDE)
+                    sum_dh[WIDE ? 0 : u] = sum;
+                else if (in[u])
+                    *(lds_f32x4_t*)((lds_float*)wide + col[u]) = sum;
+            }
+            if (in[u]) store4<S>(a.dx, base + col[u], dx[u]);
+        }
+        if (!has_y) continue;
+        float mean_u = 0.f, along = 0.f, s[2] = {0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const f32x4_t by = by_post(u);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float v = y_centred(u, e) * post_by;
+                sum_av[u][e] = fmaf(dx[u][e], v, sum_av[u][e]);
+                dx[u][e] = in[u] ? dx[u][e] * by[e] : 0.f;
+                s[0] += dx[u][e];
+                s[1] = fmaf(dx[u][e], v, s[1]);
+            }
+        }
+        if (a.post != kNormNone) {
             group_sum(s, L + 6 * kMaxWaves, waves, wave, lane);
             mean_u = post_layer ? s[0] * a.inv_E : 0.f;
             along = s[1] * a.inv_E;
@@ -312,7 +336,7 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(const BlockNormBwd
         for (int u = 0; u < U; ++u) {
             f32x4_t d;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) d[e] = post_by * ((dx[u][e] - mean_u) - y[u][e] * along);
+            for (int e = 0; e < 4; ++e) d[e] = post_by * ((dx[u][e] - mean_u) - y_centred(u, e) * post_by * along);
             if (in[u]) store4<A>(a.dy, base + col[u], d);
         }
     }
@@ -321,7 +345,7 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(const BlockNormBwd
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         if (!in[u]) continue;
-        store4<float>(out, col[u], sum_dh[u]);
+        store4<float>(out, col[u], WIDE ? *(lds_f32x4_t*)((lds_float*)wide + col[u]) : sum_dh[WIDE ? 0 : u]);
         store4<float>(out, a.E + col[u], sum_dhn[u]);
         store4<float>(out, 2 * a.E + col[u], sum_av[u]);
     }
