@@ -549,8 +549,8 @@ tm_status tm_linear_fwd(const tm_linear_desc* desc, int32_t n_tok, int64_t first
  *     dgate = sums of dout * act(pre) over each group's rows (fp32 [B, groups, N]).
  * Any of them may be NULL (not wanted; dgate where the forward had no gate). x is
  * needed for dweight, weight for dx, pre (the forward's, bf16) with an activation and for
- * dgate; else they may be NULL. dz is rounded to bf16 for the two products (not with at
- * most 16 rows in all), sums over rows take it in fp32. All orders are fixed.
+ * dgate; else they may be NULL. dz is rounded to bf16 for the two products (with at
+ * most 16 rows in all to 16 digits, with at most 4 not at all), sums over rows take it in fp32. All orders are fixed.
  * n_tok = 0 writes zeros to dweight, dbias and dgate. workspace: device memory of
  * tm_linear_bwd_workspace() bytes (0 on invalid arguments, or where none is needed), 16-byte aligned. */
 size_t tm_linear_bwd_workspace(const tm_linear_desc* desc, int32_t n_tok, int64_t first_token);

@@ -351,15 +351,15 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(const BlockNormBwd
     }
 }
 
-// Columns [64 i, + 64) of one sum, LANES threads a column, which share out the parts. The first workgroups
-// take the totals.
-template <int LANES>
-__global__ __launch_bounds__(64 * LANES) void column_sums_kernel(const ColumnSums a) {
-    __shared__ float sums[2][LANES][64];
-    const int blocks = (a.E + 63) / 64;
-    const int e = static_cast<int>(blockIdx.x % blocks) * 64 + threadIdx.x % 64;
-    const int l = threadIdx.x / 64;
-    const int64_t which = blockIdx.x / blocks;
+// COLS columns of one sum, LANES threads a column, which deal out the parts (8 loads of each in flight). The first
+// workgroups take the totals.
+template <int COLS, int LANES>
+__global__ __launch_bounds__(COLS * LANES) void column_sums_kernel(const ColumnSums a) {
+    __shared__ float sums[2][LANES][COLS];
+    const int blocks = (a.E + COLS - 1) / COLS;
+    const int c = threadIdx.x % COLS, l = threadIdx.x / COLS;
+    const int e = static_cast<int>(blockIdx.x % blocks) * COLS + c;
+    const int which = static_cast<int>(blockIdx.x / blocks);
     const int64_t stride = static_cast<int64_t>(a.vectors) * a.E;
     const bool in = e < a.E;
     float s = 0.f, s_w = 0.f;
@@ -368,47 +368,64 @@ __global__ __launch_bounds__(64 * LANES) void column_sums_kernel(const ColumnSum
         const float* at = a.part + static_cast<int64_t>(o.v) * a.E + e;
         const int n = a.parts.count();
         if (in) {
-#pragma unroll 4
-            for (int i = l; i < n; i += LANES) {
-                const int g = i / a.parts.per_group, b = g / a.parts.touched;
-                const int64_t mod = static_cast<int64_t>(b) * a.parts.groups + a.parts.g0 + g % a.parts.touched;
-                const float by = o.mod != nullptr ? o.mod[mod * a.E + e] + o.add : 1.f;
-                s = fmaf(at[i * stride], by, s);
+            if (o.mod != nullptr) {
+#pragma unroll 8
+                for (int i = l; i < n; i += LANES) {
+                    const int g = a.by_parts.of(i), b = a.by_touched.of(g);
+                    const int64_t mod = static_cast<int64_t>(b) * a.parts.groups + a.parts.g0 + (g - b * a.parts.touched);
+                    s = fmaf(at[i * stride], o.mod[mod * a.E + e] + o.add, s);
+                }
+            } else {
+#pragma unroll 8
+                for (int i = l; i < n; i += LANES) s += at[i * stride];
             }
         }
-        sums[0][l][threadIdx.x % 64] = s;
+        sums[0][l][c] = s;
         __syncthreads();
         if (l > 0 || !in) return;
         s = 0.f;
-        for (int i = 0; i < LANES; ++i) s += sums[0][i][threadIdx.x];
+#pragma unroll
+        for (int i = 0; i < LANES; ++i) s += sums[0][i][c];
         o.out[e] = s;
         return;
     }
-    const int64_t rows = static_cast<int64_t>(a.parts.B) * a.parts.groups;
-    const int64_t row = (which - a.n_total) % rows;
-    const GroupSum& o = a.group[(which - a.n_total) / rows];
-    const int b = static_cast<int>(row / a.parts.groups), j = static_cast<int>(row % a.parts.groups) - a.parts.g0;
+    const int rows = a.parts.B * a.parts.groups;
+    const int sum = (which - a.n_total) / rows, row = (which - a.n_total) % rows;
+    const GroupSum& o = a.group[sum];
+    const int b = row / a.parts.groups, j = row % a.parts.groups - a.parts.g0;
     if (in && j >= 0 && j < a.parts.touched) {
-        const int first = (b * a.parts.touched + j) * a.parts.per_group;
-#pragma unroll 4
-        for (int i = l; i < a.parts.per_group; i += LANES) {
-            const float* at = a.part + (first + i) * stride + e;
-            s += at[static_cast<int64_t>(o.v) * a.E];
-            if (o.w >= 0) s_w += at[static_cast<int64_t>(o.w) * a.E];
+        const float* at = a.part + static_cast<int64_t>((b * a.parts.touched + j) * a.parts.per_group) * stride + e;
+        const float* v = at + static_cast<int64_t>(o.v) * a.E;
+#pragma unroll 8
+        for (int i = l; i < a.parts.per_group; i += LANES) s += v[i * stride];
+        if (o.w >= 0) {
+            const float* w = at + static_cast<int64_t>(o.w) * a.E;
+#pragma unroll 8
+            for (int i = l; i < a.parts.per_group; i += LANES) s_w += w[i * stride];
         }
     }
-    sums[0][l][threadIdx.x % 64] = s;
-    sums[1][l][threadIdx.x % 64] = s_w;
-    __syncthreads();
-    if (l > 0 || !in) return;
-    s = s_w = 0.f;
-    for (int i = 0; i < LANES; ++i) {
-        s += sums[0][i][threadIdx.x];
-        s_w += sums[1][i][threadIdx.x];
+    if (LANES > 1) {
+        sums[0][l][c] = s;
+        sums[1][l][c] = s_w;
+        __syncthreads();
+        if (l > 0) return;
+        s = s_w = 0.f;
+#pragma unroll
+        for (int i = 0; i < LANES; ++i) {
+            s += sums[0][i][c];
+            s_w += sums[1][i][c];
+        }
     }
+    if (!in) return;
     if (o.mul != nullptr) s *= o.mul[e];
     if (o.w >= 0) s = fmaf(s_w, o.mul_w[e], s);
-    o.out[row * a.E + e] = s;
+    o.out[static_cast<int64_t>(row) * a.E + e] = s;
+}
+
+template <int COLS, int LANES>
+hipError_t launch_sums(const ColumnSums& a, int64_t sums, hipStream_t s) {
+    return launch_with(column_sums_kernel<COLS, LANES>, dim3(static_cast<unsigned>((a.E + COLS - 1) / COLS * sums)),
+                       COLS * LANES, s, a);
 }
 
 // Elements a lane takes at a time, and lanes of a row.
@@ -458,20 +475,19 @@ hipError_t launch_block_norm_bwd(const BlockNormBwdArgs& a, bool stream_f32, boo
 }
 
 hipError_t launch_column_sums(const ColumnSums& a, hipStream_t s) {
-    const int blocks = (a.E + 63) / 64;
-    const int64_t rows = static_cast<int64_t>(a.parts.B) * a.parts.groups;
-    // a column's few parts need few threads
     ColumnSums t = a, g = a;
+    t.by_parts = g.by_parts = FastDiv(a.parts.per_group);
+    t.by_touched = g.by_touched = FastDiv(a.parts.touched);
     t.n_group = 0;
     g.n_total = 0;
     if (a.n_total > 0) {
-        const hipError_t e = launch_with(column_sums_kernel<16>, dim3(blocks * a.n_total), 1024, s, t);
+        const hipError_t e = a.parts.count() <= 4 ? launch_sums<64, 1>(t, a.n_total, s) : launch_sums<32, 32>(t, a.n_total, s);
         if (e != hipSuccess) return e;
     }
     if (a.n_group == 0) return hipSuccess;
-    const dim3 grid(static_cast<unsigned>(blocks * a.n_group * rows));
-    return a.parts.per_group <= 4 ? launch_with(column_sums_kernel<1>, grid, 64, s, g)
-                                  : launch_with(column_sums_kernel<16>, grid, 1024, s, g);
+    const int64_t sums = static_cast<int64_t>(a.n_group) * a.parts.B * a.parts.groups;
+    if (a.parts.per_group <= 4) return launch_sums<64, 1>(g, sums, s);
+    return a.parts.per_group <= 64 ? launch_sums<64, 4>(g, sums, s) : launch_sums<32, 32>(g, sums, s);
 }
 
 }  // namespace tmk

@@ -184,6 +184,14 @@ __device__ __forceinline__ int share_begin(const GemmArgs& a, int c) {
     return static_cast<int>(static_cast<int64_t>(per_group) * a.stages * c / a.shares);
 }
 
+// The share that takes stage u of a group.
+__device__ __forceinline__ int share_of(const GemmArgs& a, int u) {
+    const int per_group = (a.tiles_m * a.tiles_n - a.whole) / a.groups;
+    int c = static_cast<int>(static_cast<int64_t>(u) * a.shares / (per_group * a.stages));
+    while (share_begin(a, c + 1) <= u) ++c;
+    return c;
+}
+
 template <int N>
 __device__ __forceinline__ void wait_and_meet() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
@@ -199,7 +207,7 @@ __device__ __forceinline__ void tile_at(const GemmArgs& a, int t, int tile, int&
     n0 = in / high * tile;
 }
 
-// FULL: with all of the epilogue; else the sums are the output, in bf16.
+// FULL: with all of the epilogue; else the sums are the output.
 template <int BT, bool AT, bool BTR, bool FULL>
 __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const GemmArgs a) {
     constexpr int WT = BT / 2;      // a wave's rows and columns
@@ -391,7 +399,8 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const Gemm
         if (w.part != nullptr) {
             float* out = w.part + (wm + l32) * BT + wn + 8 * hw;
 #pragma unroll
-            for (int i = 0; i < F; ++i)
+            for (int i = 0; i < F; ++i) {
+                if (row0 + 32 * i >= a.M) break;
 #pragma unroll
                 for (int j = 0; j < 2 * F; ++j) {
                     float z[8];
@@ -400,13 +409,14 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const Gemm
                     for (int e = 0; e < 8; ++e) z[e] = acc[i][j / 2][8 * (j % 2) + e];
                     store8(out + i * 32 * BT + 16 * j, z);
                 }
+            }
             return;
         }
         if (!FULL) {
 #pragma unroll
             for (int i = 0; i < F; ++i) {
                 if (row0 + 32 * i >= a.M) break;
-                __bf16* out = static_cast<__bf16*>(a.ep.o) + static_cast<int64_t>(row0 + 32 * i) * a.N + col0;
+                const int64_t at = static_cast<int64_t>(row0 + 32 * i) * a.N + col0;
 #pragma unroll
                 for (int j = 0; j < 2 * F; ++j) {
                     if (col0 + 16 * j >= a.N) break;
@@ -414,7 +424,10 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const Gemm
                     if (j % 2 == 0) here(acc[i][j / 2]);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) z[e] = acc[i][j / 2][8 * (j % 2) + e];
-                    store8(out + 16 * j, z);
+                    if (a.ep.o_f32)
+                        store8(static_cast<float*>(a.ep.o) + at + 16 * j, z);
+                    else
+                        store8(static_cast<__bf16*>(a.ep.o) + at + 16 * j, z);
                 }
             }
             return;
@@ -508,18 +521,20 @@ __global__ __launch_bounds__(256) void gemm_merge_kernel(const GemmArgs a) {
     const int r = (blockIdx.x % PER) * ROWS + threadIdx.x / LPR, c = (threadIdx.x % LPR) * 8;
     const int row = m0 + r, col = n0 + c;
     if (row >= a.M || col >= a.N) return;
-    const int group = t % a.groups, per_group = (a.tiles_m * a.tiles_n - a.whole) / a.groups;
+    // The shares that hold stages [u0, u1) of the group: w0 to w1. Only the first can have begun in the tile before,
+    // so that this one is its second.
+    const int group = t % a.groups;
     const int u0 = t / a.groups * a.stages, u1 = u0 + a.stages;
-    int w = static_cast<int>(static_cast<int64_t>(u0) * a.shares / (per_group * a.stages));
-    while (share_begin(a, w + 1) <= u0) ++w;
-    float z[8] = {};
+    const int w0 = share_of(a, u0), w1 = share_of(a, u1 - 1);
+    const float* part = a.part + static_cast<int64_t>(w0 * a.groups + group) * 2 * (BT * BT) + r * BT + c;
+    const int64_t step = static_cast<int64_t>(a.groups) * 2 * (BT * BT);
+    float z[8] = {}, sum[8];
     if (a.ep.bias != nullptr) load8(a.ep.bias + col, z);
-    float sum[8] = {};
-    for (; w < a.shares; ++w) {
-        const int b = share_begin(a, w);
-        if (b >= u1) break;
+    load8(part + (share_begin(a, w0) < u0 ? BT * BT : 0), sum);
+#pragma unroll 4
+    for (int w = w0 + 1; w <= w1; ++w) {
         float x[8];
-        load8(a.part + (static_cast<int64_t>(w * a.groups + group) * 2 + (b < u0 ? 1 : 0)) * (BT * BT) + r * BT + c, x);
+        load8(part + (w - w0) * step, x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum[e] += x[e];
     }
@@ -666,6 +681,11 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(const LinearDzArgs a) {
                 sum_dz[e] += d[e];
             }
             if (a.dz != nullptr) store8(static_cast<__bf16*>(a.dz) + at, d);
+            if (a.dz_rest != nullptr) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) d[e] -= static_cast<float>(static_cast<__bf16>(d[e]));
+                store8(static_cast<__bf16*>(a.dz_rest) + at, d);
+            }
             if (a.dz_few != nullptr) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) a.dz_few[static_cast<int64_t>(col + e) * a.R + row] = d[e];
@@ -739,20 +759,30 @@ __global__ __launch_bounds__(256) void few_rows_dx_kernel(const FewRowsBwdArgs a
     }
 }
 
+// 32 groups of 8 columns per workgroup, 8 threads a group, which deal out the shares.
 __global__ __launch_bounds__(256) void few_rows_dx_merge_kernel(const FewRowsBwdArgs a) {
-    const int64_t at = blockIdx.x * int64_t(256) + threadIdx.x;  // groups of 8 columns
-    const int per = a.K / 8;
-    if (at >= static_cast<int64_t>(a.rows) * per) return;
-    const int64_t row = at / per, col = at % per * 8;
+    __shared__ float sums[8][32][9];
+    const int lane = threadIdx.x % 32, l = threadIdx.x / 32, per = a.K / 8;
+    const int at = blockIdx.x * 32 + lane;
+    const bool in = at < a.rows * per;
+    const int row = in ? at / per : 0, col = in ? at % per * 8 : 0;
     float s[8] = {};
 #pragma unroll 4
-    for (int p = 0; p < a.shares; ++p) {
+    for (int p = l; p < a.shares; p += 8) {
         float x[8];
         load8(a.part + (static_cast<int64_t>(p) * a.R + row) * a.K + col, x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) s[e] += x[e];
     }
-    store8(static_cast<__bf16*>(a.dx) + row * a.K + col, s);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sums[l][lane][e] = s[e];
+    __syncthreads();
+    if (l > 0 || !in) return;
+#pragma unroll
+    for (int k = 1; k < 8; ++k)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] += sums[k][lane][e];
+    store8(static_cast<__bf16*>(a.dx) + static_cast<int64_t>(row) * a.K + col, s);
 }
 
 // dW of R rows: 8 columns a lane, whose R values of x stay in registers over kDwRows rows of dW.
@@ -777,6 +807,27 @@ __global__ __launch_bounds__(256) void few_rows_dw_kernel(const FewRowsBwdArgs a
         }
         store8(static_cast<__bf16*>(a.dw) + static_cast<int64_t>(n) * a.K + col, d);
     }
+}
+
+// x twice, one behind the other (n groups of 8).
+__global__ __launch_bounds__(256) void twice_kernel(const TwiceArgs a) {
+    const int64_t i = blockIdx.x * int64_t(256) + threadIdx.x;
+    if (i >= a.n) return;
+    const f32x4_t v = static_cast<const f32x4_t*>(a.x)[i];
+    static_cast<f32x4_t*>(a.out)[i] = v;
+    static_cast<f32x4_t*>(a.out)[a.n + i] = v;
+}
+
+// out = a + b, b behind a (n groups of 8).
+__global__ __launch_bounds__(256) void halves_sum_kernel(const TwiceArgs a) {
+    const int64_t i = (blockIdx.x * int64_t(256) + threadIdx.x) * 8;
+    if (i >= a.n * 8) return;
+    float u[8], v[8];
+    load8(static_cast<const float*>(a.x) + i, u);
+    load8(static_cast<const float*>(a.x) + a.n * 8 + i, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) u[e] += v[e];
+    store8(static_cast<__bf16*>(a.out) + i, u);
 }
 
 __global__ __launch_bounds__(256) void zero_kernel(uint32_t* p, int64_t n) {
@@ -815,7 +866,7 @@ static hipError_t launch_few_bwd(const FewRowsBwdArgs& a, hipStream_t s) {
     if (a.dx != nullptr) {
         e = launch_with(few_rows_dx_kernel<R>, dim3((a.K + 511) / 512, a.shares), 256, s, a);
         if (e != hipSuccess) return e;
-        e = launch_with(few_rows_dx_merge_kernel, dim3((static_cast<unsigned>(a.rows) * (a.K / 8) + 255) / 256), 256, s, a);
+        e = launch_with(few_rows_dx_merge_kernel, dim3((static_cast<unsigned>(a.rows) * (a.K / 8) + 31) / 32), 256, s, a);
         if (e != hipSuccess) return e;
     }
     if (a.dw != nullptr)
@@ -828,10 +879,15 @@ hipError_t launch_few_rows_bwd(const FewRowsBwdArgs& a, hipStream_t s) {
         case 1: return launch_few_bwd<1>(a, s);
         case 2: return launch_few_bwd<2>(a, s);
         case 4: return launch_few_bwd<4>(a, s);
-        case 8: return launch_few_bwd<8>(a, s);
-        case 16: return launch_few_bwd<16>(a, s);
     }
     return hipErrorInvalidValue;
+}
+
+hipError_t launch_twice(const TwiceArgs& a, hipStream_t s) {
+    return launch_with(twice_kernel, dim3(static_cast<unsigned>((a.n + 255) / 256)), 256, s, a);
+}
+hipError_t launch_halves_sum(const TwiceArgs& a, hipStream_t s) {
+    return launch_with(halves_sum_kernel, dim3(static_cast<unsigned>((a.n + 255) / 256)), 256, s, a);
 }
 
 hipError_t launch_zero(void* p, int64_t n, hipStream_t s) {

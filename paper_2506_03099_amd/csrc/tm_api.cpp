@@ -1802,35 +1802,41 @@ tmk::GemmArgs gemm_args(const GemmPlan& p, const void* a, const void* b, int64_t
 
 // The backward's workspace, in this order.
 struct LinearBwdPlan {
-    bool few;
-    int32_t R;       // few rows: 1, 2, 4, 8 or 16
-    int32_t shares;  // of N, for dx
+    bool few;        // at most kFewRowsBwd rows
+    bool exact;      // at most kExactRows: dz in two parts, one behind the other, and x twice
+    int32_t R;       // few: 1, 2 or 4
+    int32_t shares;  // few: of N, for dx
     tmk::RowParts parts;
     GemmPlan dx, dw;
-    size_t dz_bytes, sums_bytes, gemm_bytes;
-    size_t total() const { return dz_bytes + sums_bytes + gemm_bytes; }
+    size_t dz_bytes, x2_bytes, dx2_bytes, sums_bytes, gemm_bytes;
+    size_t total() const { return dz_bytes + x2_bytes + dx2_bytes + sums_bytes + gemm_bytes; }
 };
 
 LinearBwdPlan plan_linear_bwd(const LinearGeo& g) {
     LinearBwdPlan p{};
     const int64_t rows = g.run.rows;
-    p.few = rows <= tmk::kFewRows;
+    p.few = rows <= tmk::kFewRowsBwd;
+    p.exact = !p.few && rows <= tmk::kExactRows;
     const int64_t blocks = ceil_div(g.N, 256);
     p.parts = row_parts(g.run, std::max<int64_t>(1, 8 * tmk::kCUs / blocks), 32);
     p.sums_bytes = aligned(size_t(p.parts.count()) * tmk::kLinearSums * size_t(g.N) * 4);
     if (p.few) {
-        p.R = 1;
-        while (p.R < rows) p.R *= 2;
+        p.R = rows <= 2 ? int32_t(rows) : 4;
         // four workgroups a CU, 16 columns of a wave at least
         p.shares = int32_t(std::max<int64_t>(1, std::min(ceil_div(4 * tmk::kCUs, ceil_div(g.K, 512)), g.N / 64)));
         p.dz_bytes = aligned(size_t(p.R) * size_t(g.N) * 4);
         p.gemm_bytes = aligned(size_t(p.shares) * size_t(p.R) * size_t(g.K) * 4);
-    } else {
-        p.dz_bytes = aligned(size_t(rows) * size_t(g.N) * 2);
-        p.dx = plan_gemm(rows, g.K, g.N, true);
-        p.dw = plan_gemm(g.N, g.K, rows, true);
-        p.gemm_bytes = aligned(std::max(p.dx.part_bytes(), p.dw.part_bytes()));
+        return p;
     }
+    const int64_t both = p.exact ? 2 * rows : rows;  // (either way one tile of rows, or one stage)
+    p.dz_bytes = aligned(size_t(both) * size_t(g.N) * 2);
+    if (p.exact) {
+        p.x2_bytes = aligned(size_t(both) * size_t(g.K) * 2);
+        p.dx2_bytes = aligned(size_t(both) * size_t(g.K) * 4);
+    }
+    p.dx = plan_gemm(both, g.K, g.N, true);
+    p.dw = plan_gemm(g.N, g.K, both, true);
+    p.gemm_bytes = aligned(std::max(p.dx.part_bytes(), p.dw.part_bytes()));
     return p;
 }
 
@@ -2085,18 +2091,23 @@ tm_status tm_linear_bwd(const tm_linear_desc* desc, int32_t n_tok, int64_t first
         return TM_OK;
     }
     unsigned char* ws = static_cast<unsigned char*>(workspace);
-    void* const part = ws + p.dz_bytes + p.sums_bytes;
+    unsigned char* const x2 = ws + p.dz_bytes;
+    unsigned char* const dx2 = x2 + p.x2_bytes;
+    unsigned char* const sums_at = dx2 + p.dx2_bytes;
+    void* const part = sums_at + p.sums_bytes;
     const bool products = dx != nullptr || dweight != nullptr;
     // dout is dz where nothing lies between and it has bf16 already
     const bool direct = !p.few && desc->act == TM_ACT_NONE && gate == nullptr && desc->out_dtype == TM_BF16;
+    const bool exact = p.exact && !direct;
     const bool sums = dbias != nullptr || dgate != nullptr;
     tmk::LinearDzArgs z{};
     z.dout = dout;
     z.pre = desc->act != TM_ACT_NONE || dgate != nullptr ? pre : nullptr;
     z.gate = gate;
     z.dz = products && !p.few && !direct ? ws : nullptr;
+    z.dz_rest = products && exact ? ws + outs * 2 : nullptr;
     z.dz_few = products && p.few ? reinterpret_cast<float*>(ws) : nullptr;
-    z.part = sums ? reinterpret_cast<float*>(ws + p.dz_bytes) : nullptr;
+    z.part = sums ? reinterpret_cast<float*>(sums_at) : nullptr;
     z.N = int32_t(g.N);
     z.act = desc->act;
     z.dout_f32 = desc->out_dtype == TM_F32;
@@ -2122,13 +2133,17 @@ tm_status tm_linear_bwd(const tm_linear_desc* desc, int32_t n_tok, int64_t first
         return TM_OK;
     }
     const void* dz = direct ? dout : ws;
+    const int64_t rows = exact ? 2 * g.run.rows : g.run.rows;
     if (dx != nullptr) {
-        tmk::GemmArgs a = gemm_args(p.dx, dz, weight, g.run.rows, g.K, g.N, g.N, g.K, part);
-        a.ep.o = dx;
+        tmk::GemmArgs a = gemm_args(p.dx, dz, weight, rows, g.K, g.N, g.N, g.K, part);
+        a.ep.o = exact ? dx2 : dx;
+        a.ep.o_f32 = exact;
         TM_LAUNCH(tmk::launch_gemm(a, p.dx.tile, false, true, stream), "linear backward");
+        if (exact) TM_LAUNCH(tmk::launch_halves_sum({dx2, dx, int64_t(ins / 16)}, stream), "linear backward");
     }
     if (dweight != nullptr) {
-        tmk::GemmArgs a = gemm_args(p.dw, dz, x, g.N, g.K, g.run.rows, g.N, g.K, part);
+        if (exact) TM_LAUNCH(tmk::launch_twice({x, x2, int64_t(ins / 16)}, stream), "linear backward");
+        tmk::GemmArgs a = gemm_args(p.dw, dz, exact ? x2 : x, g.N, g.K, rows, g.N, g.K, part);
         a.ep.o = dweight;
         TM_LAUNCH(tmk::launch_gemm(a, p.dw.tile, true, true, stream), "linear backward");
     }

@@ -415,6 +415,7 @@ struct ColumnSums {
     int32_t n_group, n_total;
     GroupSum group[3];
     TotalSum total[3];
+    FastDiv by_parts, by_touched;  // set by the launcher
 };
 hipError_t launch_column_sums(const ColumnSums& a, hipStream_t s);
 
@@ -470,7 +471,7 @@ struct FewRowsArgs {
 };
 hipError_t launch_few_rows(const FewRowsArgs& a, hipStream_t s);
 
-// dz = dout * gate * act'(pre) of a linear layer's rows, in bf16 [rows, N] (dz) or, of at most kFewRows rows,
+// dz = dout * gate * act'(pre) of a linear layer's rows, in bf16 [rows, N] (dz) or, of at most kFewRowsBwd rows,
 // in fp32 [N][R] (dz_few, rows past the last one zero), and per part the sums over rows of dz and of
 // dout * act(pre).
 constexpr int kLinearSums = 2;
@@ -479,6 +480,7 @@ struct LinearDzArgs {
     const void* pre;    // bf16, or null
     const float* gate;  // or null
     void* dz;           // or null
+    void* dz_rest;      // what dz's rounding left, in bf16, or null
     float* dz_few;      // or null
     float* part;        // [parts][kLinearSums][N], or null
     int32_t N, act, dout_f32, gate_sums;
@@ -487,7 +489,11 @@ struct LinearDzArgs {
 };
 hipError_t launch_linear_dz(const LinearDzArgs& a, hipStream_t s);
 
-// dx = dz W and dW = dz^T x for at most kFewRows rows, from dz_few with R = 1, 2, 4, 8 or 16.
+// dx = dz W and dW = dz^T x for at most kFewRowsBwd rows, from dz_few with R = 1, 2 or 4. More rows go through
+// the matrix instructions: as 8 + 8 digits (dz and dz_rest) up to kExactRows, where nothing would average
+// the roundings of dz.
+constexpr int kFewRowsBwd = 4;
+constexpr int kExactRows = 16;
 struct FewRowsBwdArgs {
     const float* dz;  // [N][R]
     const void* x;    // [rows, K]
@@ -499,6 +505,16 @@ struct FewRowsBwdArgs {
     int32_t shares;   // of N that dx's sums are dealt out to
 };
 hipError_t launch_few_rows_bwd(const FewRowsBwdArgs& a, hipStream_t s);
+
+// x twice into out, or (halves_sum) the sum of x's halves in fp32 into out in bf16; n: groups of 8 elements of x, or
+// of one half.
+struct TwiceArgs {
+    const void* x;
+    void* out;
+    int64_t n;
+};
+hipError_t launch_twice(const TwiceArgs& a, hipStream_t s);
+hipError_t launch_halves_sum(const TwiceArgs& a, hipStream_t s);
 
 // n elements of 4 bytes to zero (a fill kernel: it may be captured).
 hipError_t launch_zero(void* p, int64_t n, hipStream_t s);

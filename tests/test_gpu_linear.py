@@ -6,8 +6,10 @@ round) of the sum of magnitudes S = |x| |W|^T + |bias|, so z is within 2 (K + 8)
 below 1.13, its own arithmetic (two products, exp2 and rcp of 1 ulp each, and for gelu an argument that is off by
 4 u of itself, which its slope times z turns into at most 16 u of |z|) within 32 u |z|; gate, residual
 and the sums in fp32 another 4 u of their terms. Results in bf16 add half a step, 2^-8 of themselves.
-Backward: dz within 64 u of |dout gate| times (1 + |z|), rounded to bf16 for the products (2^-8 relative) unless
-there are at most 16 rows; a product of it within that times |W| (|x|), and 2 (terms + 8) u S. Roundings of
+Backward: dz within 64 u of |dout gate| times (1 + |z|), rounded to bf16 for the products (2^-8 relative). With 5 to 16
+rows dz goes into them as the sum of two bf16 numbers, hi = dz rounded and lo = dz - hi rounded: |dz - hi| <=
+2^-8 |dz|, so what lo's rounding leaves out is at most 2^-8 of that, 2^-16 |dz|; with up to 4 rows it is not rounded.
+A product of it is within that times |W| (|x|), and 2 (terms + 8) u S. Roundings of
 half a step at most have a root mean square of 2^-8 / sqrt(3) at most, and two of them, dz's and the result's,
 sqrt(2 / 3) 2^-8 of the result's norm: products are held to 2^-8 of their norm as well.
 """
@@ -94,10 +96,7 @@ def test_forward_and_backward(tm, B, n, K, N, act, out, parts, groups, group, fi
     value, z, d64 = value.detach(), z.detach(), dout.double()
     dz = d64 * gate * slope
     dzb = (64 * U if act != "none" else 4 * U) * (d64 * gate).abs() * (1 + z.abs())
-    if B * n > 16:
-        dzb_r = dzb + 2.0 ** -8 * dz.abs()
-    else:
-        dzb_r = dzb
+    dzb_r = dzb + (2.0 ** -8 if B * n > 16 else 2.0 ** -16 if B * n > 4 else 0) * dz.abs()
     flat, xf, w = dz.view(-1, N), p64["x"].view(-1, K), p64["weight"]
     held(got.dx, dz @ w, dzb_r @ w.abs() + 2 * (N + 8) * U * (dz.abs() @ w.abs()), "dx")
     held(got.dweight, flat.t() @ xf, dzb_r.view(-1, N).t() @ xf.abs() + 2 * (B * n + 8) * U * (flat.abs().t() @ xf.abs()),
