@@ -21,7 +21,6 @@
 #include <cstdio>
 #include <initializer_list>
 #include <new>
-#include <numeric>
 #include <utility>
 
 #include "tm.h"
@@ -1724,23 +1723,18 @@ struct GemmPlan {
     size_t part_bytes() const { return size_t(groups * shares) * 2 * size_t(tile) * size_t(tile) * 4; }
 };
 
-// Workgroups that share out `rest` tiles, and in how many groups: at most `most`, with 1/8 less if that makes groups
-// enough for an XCD's 32 workgroups to go through the same k.
-void plan_shares(int64_t rest, int64_t most, GemmPlan* p) {
-    int64_t best = 0;
-    for (int64_t w = most; w >= rest && w >= most - most / 8; --w) {
-        const int64_t g = std::gcd(rest, w);
-        if (std::min<int64_t>(g, 32) > best) {
-            best = std::min<int64_t>(g, 32);
-            p->groups = g;
-            p->shares = w / g;
-        }
-    }
+// What a round of `wgs` workgroups of `stages` stages each takes, in us. A stage of a 256 tile takes 0.97 us with few
+// workgroups at work and 1.4 with one on each CU; one of a 128 tile 0.45 and 0.55, and 0.95 with two on each. (From
+// 50 sizes from 130 to 9000 rows and 64 to 20480 wide, each with either tile, split and not: the choice by
+// these costs is 3% behind the best of the four.)
+double round_us(int tile, double wgs, double stages) {
+    const double f = wgs / tmk::kCUs;
+    return tile == 256 ? stages * (0.97 + 0.43 * f) + 8 : stages * (f <= 1 ? 0.45 + 0.1 * f : 0.55 + 0.4 * (f - 1)) + 4;
 }
 
 GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool may_split) {
     GemmPlan best{};
-    double best_cost = 0;
+    double best_us = 0;
     for (const int tile : {256, 128}) {
         GemmPlan p{};
         p.tile = tile;
@@ -1749,27 +1743,29 @@ GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool may_split) {
         p.stages = ceil_div(K, tmk::kGemmDepth);
         const int64_t tiles = p.tiles_m * p.tiles_n;
         const int64_t at_once = tile == 256 ? tmk::kCUs : 2 * tmk::kCUs;
-        // cycles of a stage with the chip full, and beside the stages: a tile's start and end, a merge's launch
-        const double stage = tile == 256 ? 2200 : 1400, ends = tile == 256 ? 8000 : 5000, merge = 12000;
-        p.whole = tiles;
-        double cost = double(ceil_div(tiles, at_once)) * (double(p.stages) * stage + ends);
         const int64_t rest = tiles % at_once;
-        // (at least 4 stages a workgroup)
-        const int64_t wgs = std::min(at_once, rest * p.stages / 4);
-        if (may_split && rest > 0 && wgs > rest) {
-            GemmPlan q = p;
-            q.whole = tiles - rest;
-            plan_shares(rest, wgs, &q);
-            const double with = double(tiles / at_once) * (double(p.stages) * stage + ends) +
-                                double(rest * p.stages) / double(q.groups * q.shares) * stage + ends + merge;
-            if (with < cost) {
-                cost = with;
-                p = q;
-            }
-        }
-        if (best.tile == 0 || cost < best_cost) {
+        const double whole_us = double(tiles / at_once) * round_us(tile, double(at_once), double(p.stages));
+        auto take = [&](double us) {
+            if (best.tile != 0 && us >= best_us) return;
             best = p;
-            best_cost = cost;
+            best_us = us;
+        };
+        p.whole = tiles;
+        take(whole_us + (rest ? round_us(tile, double(rest), double(p.stages)) : 0));
+        if (!may_split || rest == 0 || p.stages < 2) continue;
+        // The tiles of the last round shared out: `a` of them to each `shares` workgroups, in rest / a groups. The
+        // parts are written and read once, and joined by another launch.
+        p.whole = tiles - rest;
+        const double part_us = double(tile) * double(tile) * 8 * double(M) / double(p.tiles_m * tile) / 5.5e6;
+        for (int64_t a = 1; a <= 9 && a <= rest; ++a) {
+            if (rest % a != 0) continue;
+            p.groups = rest / a;
+            const int64_t most = std::min(at_once / p.groups, a * p.stages);
+            for (int64_t shares = most; shares > a && shares >= (a == 1 ? most / 8 : most - 1); shares -= a == 1 ? ceil_div(shares, 8) : 1) {
+                p.shares = shares;
+                take(whole_us + round_us(tile, double(p.groups * shares), double(ceil_div(a * p.stages, shares))) + 5 +
+                     double(p.groups * (shares + a - 1)) * part_us);
+            }
         }
     }
     return best;
