@@ -470,7 +470,7 @@ typedef enum tm_act { TM_ACT_NONE = 0, TM_ACT_GELU = 1, TM_ACT_SILU = 2 } tm_act
 
 typedef struct tm_block_norm_desc {
     int32_t batch;        /* B >= 1 */
-    int32_t width;        /* E: a multiple of 8, at most 20480 */
+    int32_t width;        /* E: a multiple of 8, at most 16384 */
     int32_t pre;          /* tm_norm of the stream, before the next branch */
     int32_t post;         /* tm_norm of the branch's output y */
     int32_t dtype;        /* tm_dtype of y and h */

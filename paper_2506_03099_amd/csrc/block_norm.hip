@@ -6,6 +6,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "tm_device.h"
 #include "tm_internal.h"
 
@@ -31,15 +33,33 @@ __device__ __forceinline__ f32x4_t as_f32(typename Four<T>::raw v) {
     return f32x4_t{static_cast<float>(v[0]), static_cast<float>(v[1]), static_cast<float>(v[2]), static_cast<float>(v[3])};
 }
 template <typename T>
-__device__ __forceinline__ typename Four<T>::raw load4(const void* p, int64_t at) {
-    return *reinterpret_cast<const typename Four<T>::raw*>(static_cast<const T*>(p) + at);
-}
-template <typename T>
-__device__ __forceinline__ void store4(void* p, int64_t at, f32x4_t v) {
+__device__ __forceinline__ typename Four<T>::raw as_raw(f32x4_t v) {
     typename Four<T>::raw w;
 #pragma unroll
     for (int e = 0; e < 4; ++e) w[e] = static_cast<T>(v[e]);
-    *reinterpret_cast<typename Four<T>::raw*>(static_cast<T*>(p) + at) = w;
+    return w;
+}
+// Element `col` on of a row that begins at element `row` of p: the row is the same in all lanes and stays in scalar
+// registers, the lane's part is a 32-bit offset.
+template <typename T, typename P>
+__device__ __forceinline__ auto* four_at(P* p, int64_t row, uint32_t col) {
+    using B = std::conditional_t<std::is_const_v<P>, const char, char>;
+    using R = std::conditional_t<std::is_const_v<P>, const typename Four<T>::raw, typename Four<T>::raw>;
+    return reinterpret_cast<R*>(reinterpret_cast<B*>(p) + row * static_cast<int64_t>(sizeof(T)) + col * static_cast<uint32_t>(sizeof(T)));
+}
+template <typename T>
+__device__ __forceinline__ typename Four<T>::raw load4(const void* p, int64_t row, uint32_t col) {
+    return *four_at<T>(p, row, col);
+}
+template <typename T>
+__device__ __forceinline__ void store4(void* p, int64_t row, uint32_t col, f32x4_t v) {
+    *four_at<T>(p, row, col) = as_raw<T>(v);
+}
+// The same past the caches' order of use (the forward's outputs: 56.7 for 59.7 us for the 480p chunk; the backward
+// writes the way it came, 640 for 648 us).
+template <typename T>
+__device__ __forceinline__ void store4_once(void* p, int64_t row, uint32_t col, f32x4_t v) {
+    __builtin_nontemporal_store(as_raw<T>(v), four_at<T>(p, row, col));
 }
 
 // v of the lane that the DPP control CTRL names (0 where there is none, or where ROWS leaves the row out), added.
@@ -109,7 +129,23 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(const BlockNormArgs a)
     for (int u = 0; u < U; ++u) {
         col[u] = (u * T + tid) * 4;
         in[u] = col[u] < a.E;
-        x[u] = in[u] ? as_f32<S>(load4<S>(a.x, base + col[u])) : f32x4_t{};
+        x[u] = in[u] ? as_f32<S>(load4<S>(a.x, base, col[u])) : f32x4_t{};
+    }
+    typename Four<A>::raw y_raw[U];
+    f32x4_t gate[U], scale[U], shift[U];
+    const f32x4_t one = f32x4_t{1.f, 1.f, 1.f, 1.f};
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        y_raw[u] = typename Four<A>::raw{};
+        gate[u] = one;
+        scale[u] = shift[u] = f32x4_t{};
+        if (!in[u]) continue;
+        if (a.y != nullptr) y_raw[u] = load4<A>(a.y, base, col[u]);
+        if (a.gate != nullptr) gate[u] = load4<float>(a.gate, mod, col[u]);
+        if (a.scale != nullptr) {
+            scale[u] = load4<float>(a.scale, mod, col[u]);
+            shift[u] = load4<float>(a.shift, mod, col[u]);
+        }
     }
     if (waves > 1) __syncthreads();  // the slots are clear
     // Normalised values of v over the row, in place: (v - mean) / sqrt(var + eps) with the variance from the
@@ -141,17 +177,16 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(const BlockNormArgs a)
     if (a.y != nullptr) {
         f32x4_t z[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) z[u] = in[u] ? as_f32<A>(load4<A>(a.y, base + col[u])) : f32x4_t{};
+        for (int u = 0; u < U; ++u) z[u] = as_f32<A>(y_raw[u]);
         if (a.post != kNormNone) normalise(z, a.post, L);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (!in[u]) continue;
-            f32x4_t g = f32x4_t{1.f, 1.f, 1.f, 1.f};
-            if (a.post_weight != nullptr) g = load4<float>(a.post_weight, col[u]);
-            if (a.gate != nullptr) g *= load4<float>(a.gate, mod + col[u]);
+            f32x4_t g = gate[u];
+            if (a.post_weight != nullptr) g *= load4<float>(a.post_weight, 0, col[u]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[u][e] = fmaf(g[e], z[u][e], x[u][e]);
-            store4<S>(a.r, base + col[u], x[u]);
+            store4_once<S>(a.r, base, col[u], x[u]);
         }
     }
     if (a.pre == kNormNone) return;
@@ -160,14 +195,13 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(const BlockNormArgs a)
     for (int u = 0; u < U; ++u) {
         if (!in[u]) continue;
         f32x4_t m = x[u];
-        if (a.pre_weight != nullptr) m *= load4<float>(a.pre_weight, col[u]);
-        if (a.pre_bias != nullptr) m += load4<float>(a.pre_bias, col[u]);
+        if (a.pre_weight != nullptr) m *= load4<float>(a.pre_weight, 0, col[u]);
+        if (a.pre_bias != nullptr) m += load4<float>(a.pre_bias, 0, col[u]);
         if (a.scale != nullptr) {
-            const f32x4_t sc = load4<float>(a.scale, mod + col[u]), sh = load4<float>(a.shift, mod + col[u]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) m[e] = fmaf(m[e], sc[e], m[e]) + sh[e];
+            for (int e = 0; e < 4; ++e) m[e] = fmaf(m[e], scale[u][e], m[e]) + shift[u][e];
         }
-        store4<A>(a.h, base + col[u], m);
+        store4_once<A>(a.h, base, col[u], m);
     }
 }
 
@@ -175,7 +209,7 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(const BlockNormArgs a)
 // rows of its columns.
 template <typename S, typename A, int U>
 __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(const BlockNormBwdArgs a) {
-    // Rows of more than 8192 (U = 5) leave no registers for all of it: a sum lives in LDS, and the vectors are
+    // Rows of more than 8192 (U = 4) leave no registers for all of it: a sum lives in LDS, and the vectors are
     // read anew for each row.
     constexpr bool WIDE = U > 2;
     __shared__ float smem[2 * 8 * kMaxWaves];
@@ -196,16 +230,16 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(const BlockNormBwd
     auto load_by_pre = [&](int u) __attribute__((always_inline)) {
         f32x4_t v = one;
         if (in[u]) {
-            if (a.scale != nullptr) v += load4<float>(a.scale, mod * a.E + col[u]);
-            if (a.pre_weight != nullptr) v *= load4<float>(a.pre_weight, col[u]);
+            if (a.scale != nullptr) v += load4<float>(a.scale, mod * a.E, col[u]);
+            if (a.pre_weight != nullptr) v *= load4<float>(a.pre_weight, 0, col[u]);
         }
         return v;
     };
     auto load_by_post = [&](int u) __attribute__((always_inline)) {
         f32x4_t v = one;
         if (in[u]) {
-            if (a.gate != nullptr) v = load4<float>(a.gate, mod * a.E + col[u]);
-            if (a.post_weight != nullptr) v *= load4<float>(a.post_weight, col[u]);
+            if (a.gate != nullptr) v = load4<float>(a.gate, mod * a.E, col[u]);
+            if (a.post_weight != nullptr) v *= load4<float>(a.post_weight, 0, col[u]);
         }
         return v;
     };
@@ -230,6 +264,10 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(const BlockNormBwd
         // (sums of a row in slots that the row before does not use: a wave may still read those)
         lds_float* const L = (lds_float*)smem + (t & 1) * 8 * kMaxWaves;
         const int64_t base = (static_cast<int64_t>(b) * a.parts.n + t) * a.E;
+        // (the columns anew for each row: the compiler would keep an address of each tensor for each of them)
+        const int lane_now = fresh_thread_index();
+#pragma unroll
+        for (int u = 0; u < U; ++u) col[u] = (u * T + lane_now) * 4;
         // kept as they come, and turned into fp32 where they are used. (Loads a row ahead were no faster: 653 for
         // 655 us for the 480p clip, with 31 registers more.)
         typename Four<S>::raw r_raw[U], dr_raw[U];
@@ -240,11 +278,11 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(const BlockNormBwd
             dh_raw[u] = y_raw[u] = typename Four<A>::raw{};
             if (!in[u]) continue;
             if (has_pre) {
-                r_raw[u] = load4<S>(a.r, base + col[u]);
-                dh_raw[u] = load4<A>(a.dh, base + col[u]);
+                r_raw[u] = load4<S>(a.r, base, col[u]);
+                dh_raw[u] = load4<A>(a.dh, base, col[u]);
             }
-            if (has_dr) dr_raw[u] = load4<S>(a.dr, base + col[u]);
-            if (has_y) y_raw[u] = load4<A>(a.y, base + col[u]);
+            if (has_dr) dr_raw[u] = load4<S>(a.dr, base, col[u]);
+            if (has_y) y_raw[u] = load4<A>(a.y, base, col[u]);
         }
         float mean_t = 0.f, mean_r = 0.f, mean_y = 0.f;
         if (pre_layer || post_layer) {
@@ -311,7 +349,7 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(const BlockNormBwd
                 else if (in[u])
                     *(lds_f32x4_t*)((lds_float*)wide + col[u]) = sum;
             }
-            if (in[u]) store4<S>(a.dx, base + col[u], dx[u]);
+            if (in[u]) store4<S>(a.dx, base, col[u], dx[u]);
         }
         if (!has_y) continue;
         float mean_u = 0.f, along = 0.f, s[2] = {0.f, 0.f};
@@ -337,7 +375,7 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(const BlockNormBwd
             f32x4_t d;
 #pragma unroll
             for (int e = 0; e < 4; ++e) d[e] = post_by * ((dx[u][e] - mean_u) - y_centred(u, e) * post_by * along);
-            if (in[u]) store4<A>(a.dy, base + col[u], d);
+            if (in[u]) store4<A>(a.dy, base, col[u], d);
         }
     }
     if (a.part == nullptr) return;
@@ -345,9 +383,9 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(const BlockNormBwd
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         if (!in[u]) continue;
-        store4<float>(out, col[u], WIDE ? *(lds_f32x4_t*)((lds_float*)wide + col[u]) : sum_dh[WIDE ? 0 : u]);
-        store4<float>(out, a.E + col[u], sum_dhn[u]);
-        store4<float>(out, 2 * a.E + col[u], sum_av[u]);
+        store4<float>(out, 0, col[u], WIDE ? *(lds_f32x4_t*)((lds_float*)wide + col[u]) : sum_dh[WIDE ? 0 : u]);
+        store4<float>(out, a.E, col[u], sum_dhn[u]);
+        store4<float>(out, 2 * a.E, col[u], sum_av[u]);
     }
 }
 
@@ -428,10 +466,15 @@ hipError_t launch_sums(const ColumnSums& a, int64_t sums, hipStream_t s) {
                        COLS * LANES, s, a);
 }
 
-// Elements a lane takes at a time, and lanes of a row.
-void row_shape(int E, int* U, int* threads) {
+// Fours of a row that a lane takes, and lanes of a row. Forward: more work a lane takes less time (5120 wide, 4680
+// rows: 55.4 us with 5, 59.9 with 2; 1024 wide: 42 with 2, 47 with 1) while there are lanes enough.
+// Backward: as few as the registers of its sums allow.
+void row_shape(int E, bool backward, int* U, int* threads) {
     const int fours = E / 4;
-    *U = fours <= 256 ? 1 : fours <= 2 * 1024 ? 2 : 5;
+    if (backward)
+        *U = fours <= 256 ? 1 : fours <= 2 * 1024 ? 2 : 4;
+    else
+        *U = fours <= 128 ? 1 : fours <= 512 ? 2 : 5;
     *threads = ((fours + *U - 1) / *U + 63) / 64 * 64;
 }
 
@@ -439,7 +482,7 @@ void row_shape(int E, int* U, int* threads) {
 
 hipError_t launch_block_norm(const BlockNormArgs& a, bool stream_f32, bool act_f32, hipStream_t s) {
     int U, threads;
-    row_shape(a.E, &U, &threads);
+    row_shape(a.E, false, &U, &threads);
 #define TM_NORM_CASE(U_)                                                                                   \
     if (U == U_) {                                                                                         \
         if (stream_f32)                                                                                    \
@@ -457,7 +500,7 @@ hipError_t launch_block_norm(const BlockNormArgs& a, bool stream_f32, bool act_f
 
 hipError_t launch_block_norm_bwd(const BlockNormBwdArgs& a, bool stream_f32, bool act_f32, hipStream_t s) {
     int U, threads;
-    row_shape(a.E, &U, &threads);
+    row_shape(a.E, true, &U, &threads);
     const dim3 grid(a.parts.count());
 #define TM_NORM_CASE(U_)                                                                                 \
     if (U == U_) {                                                                                       \
@@ -469,7 +512,7 @@ hipError_t launch_block_norm_bwd(const BlockNormBwdArgs& a, bool stream_f32, boo
     }
     TM_NORM_CASE(1)
     TM_NORM_CASE(2)
-    TM_NORM_CASE(5)
+    TM_NORM_CASE(4)
 #undef TM_NORM_CASE
     return hipErrorInvalidValue;
 }

@@ -422,7 +422,7 @@ hipError_t launch_column_sums(const ColumnSums& a, hipStream_t s);
 // Norms around a block (rows of E): z = post(y) * post_weight, r = x + gate * z, m = pre(r) * pre_weight +
 // pre_bias, h = m * (1 + scale) + shift. Null vectors are ones (weights, gate) or zeros.
 constexpr int kNormNone = 0, kNormLayer = 1, kNormRms = 2;
-constexpr int kMaxNormWidth = 20480;
+constexpr int kMaxNormWidth = 16384;
 struct BlockNormArgs {
     const void* x;  // backward: r
     const void* y;
