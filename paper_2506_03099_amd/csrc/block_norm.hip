@@ -427,12 +427,22 @@ __global__ __launch_bounds__(COLS * LANES) void column_sums_kernel(const ColumnS
         o.out[e] = s;
         return;
     }
-    const int rows = a.parts.B * a.parts.groups;
-    const int sum = (which - a.n_total) / rows, row = (which - a.n_total) % rows;
-    const GroupSum& o = a.group[sum];
-    const int b = row / a.parts.groups, j = row % a.parts.groups - a.parts.g0;
-    if (in && j >= 0 && j < a.parts.touched) {
-        const float* at = a.part + static_cast<int64_t>((b * a.parts.touched + j) * a.parts.per_group) * stride + e;
+    const int rows = a.parts.B * a.parts.touched;
+    if (which >= a.n_total + a.n_group * rows) {
+        // a group that the run does not touch: a workgroup for each, over all columns
+        const int left = a.parts.groups - a.parts.touched;
+        const int i = static_cast<int>(blockIdx.x) - blocks * (a.n_total + a.n_group * rows);
+        const int r = i % (a.parts.B * left), b = r / left, j = r % left;
+        float* out = a.group[i / (a.parts.B * left)].out +
+                     (static_cast<int64_t>(b) * a.parts.groups + (j < a.parts.g0 ? j : j + a.parts.touched)) * a.E;
+        for (int k = threadIdx.x; k < a.E; k += COLS * LANES) out[k] = 0.f;
+        return;
+    }
+    const int touched = (which - a.n_total) % rows;
+    const GroupSum& o = a.group[(which - a.n_total) / rows];
+    const int row = touched / a.parts.touched * a.parts.groups + a.parts.g0 + touched % a.parts.touched;
+    if (in) {
+        const float* at = a.part + static_cast<int64_t>(touched * a.parts.per_group) * stride + e;
         const float* v = at + static_cast<int64_t>(o.v) * a.E;
 #pragma unroll 8
         for (int i = l; i < a.parts.per_group; i += LANES) s += v[i * stride];
@@ -461,28 +471,18 @@ __global__ __launch_bounds__(COLS * LANES) void column_sums_kernel(const ColumnS
 }
 
 template <int COLS, int LANES>
-hipError_t launch_sums(const ColumnSums& a, int64_t sums, hipStream_t s) {
-    return launch_with(column_sums_kernel<COLS, LANES>, dim3(static_cast<unsigned>((a.E + COLS - 1) / COLS * sums)),
-                       COLS * LANES, s, a);
-}
-
-// Fours of a row that a lane takes, and lanes of a row. Forward: more work a lane takes less time (5120 wide, 4680
-// rows: 55.4 us with 5, 59.9 with 2; 1024 wide: 42 with 2, 47 with 1) while there are lanes enough.
-// Backward: as few as the registers of its sums allow.
-void row_shape(int E, bool backward, int* U, int* threads) {
-    const int fours = E / 4;
-    if (backward)
-        *U = fours <= 256 ? 1 : fours <= 2 * 1024 ? 2 : 4;
-    else
-        *U = fours <= 128 ? 1 : fours <= 512 ? 2 : 5;
-    *threads = ((fours + *U - 1) / *U + 63) / 64 * 64;
+hipError_t launch_sums(const ColumnSums& a, hipStream_t s) {
+    const int64_t sums = a.n_total + static_cast<int64_t>(a.n_group) * a.parts.B * a.parts.touched;
+    const int64_t zeros = static_cast<int64_t>(a.n_group) * a.parts.B * (a.parts.groups - a.parts.touched);
+    return launch_with(column_sums_kernel<COLS, LANES>,
+                       dim3(static_cast<unsigned>((a.E + COLS - 1) / COLS * sums + zeros)), COLS * LANES, s, a);
 }
 
 }  // namespace
 
 hipError_t launch_block_norm(const BlockNormArgs& a, bool stream_f32, bool act_f32, hipStream_t s) {
     int U, threads;
-    row_shape(a.E, false, &U, &threads);
+    block_norm_shape(a.E, false, &U, &threads);
 #define TM_NORM_CASE(U_)                                                                                   \
     if (U == U_) {                                                                                         \
         if (stream_f32)                                                                                    \
@@ -500,7 +500,7 @@ hipError_t launch_block_norm(const BlockNormArgs& a, bool stream_f32, bool act_f
 
 hipError_t launch_block_norm_bwd(const BlockNormBwdArgs& a, bool stream_f32, bool act_f32, hipStream_t s) {
     int U, threads;
-    row_shape(a.E, true, &U, &threads);
+    block_norm_shape(a.E, true, &U, &threads);
     const dim3 grid(a.parts.count());
 #define TM_NORM_CASE(U_)                                                                                 \
     if (U == U_) {                                                                                       \
@@ -524,13 +524,12 @@ hipError_t launch_column_sums(const ColumnSums& a, hipStream_t s) {
     t.n_group = 0;
     g.n_total = 0;
     if (a.n_total > 0) {
-        const hipError_t e = a.parts.count() <= 4 ? launch_sums<64, 1>(t, a.n_total, s) : launch_sums<32, 32>(t, a.n_total, s);
+        const hipError_t e = a.parts.count() <= 4 ? launch_sums<64, 1>(t, s) : launch_sums<32, 32>(t, s);
         if (e != hipSuccess) return e;
     }
     if (a.n_group == 0) return hipSuccess;
-    const int64_t sums = static_cast<int64_t>(a.n_group) * a.parts.B * a.parts.groups;
-    if (a.parts.per_group <= 4) return launch_sums<64, 1>(g, sums, s);
-    return a.parts.per_group <= 64 ? launch_sums<64, 4>(g, sums, s) : launch_sums<32, 32>(g, sums, s);
+    if (a.parts.per_group <= 4) return launch_sums<64, 1>(g, s);
+    return a.parts.per_group <= 64 ? launch_sums<64, 4>(g, s) : launch_sums<64, 16>(g, s);
 }
 
 }  // namespace tmk

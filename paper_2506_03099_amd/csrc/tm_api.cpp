@@ -1673,7 +1673,11 @@ tm_status check_norm(const tm_block_norm_desc* d, int32_t n_tok, int64_t first_t
     if ((st = check_modulation(d->batch, d->groups, g->E)) != TM_OK) return st;
     g->act = d->dtype == TM_BF16 ? 2 : 4;
     g->stream = d->stream_dtype == TM_BF16 ? 2 : 4;
-    g->parts = row_parts(g->run, 2 * tmk::kCUs, 2);
+    // Workgroups for 10 waves a CU (20, which fit, were 3 to 10% slower); no more than one to 8 rows, since the
+    // parts' sums are written and read too, unless CUs would have none.
+    const int waves = tmk::block_norm_bwd_waves(d->width);
+    const int64_t fill = tmk::kCUs * std::max(1, 10 / waves);
+    g->parts = row_parts(g->run, std::max<int64_t>(tmk::kCUs, std::min(fill, g->run.rows / 8)), 2);
     g->part_bytes = size_t(g->parts.count()) * tmk::kNormSums * size_t(g->E) * 4;
     return TM_OK;
 }
