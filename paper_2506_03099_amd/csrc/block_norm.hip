@@ -521,15 +521,16 @@ hipError_t launch_column_sums(const ColumnSums& a, hipStream_t s) {
     ColumnSums t = a, g = a;
     t.by_parts = g.by_parts = FastDiv(a.parts.per_group);
     t.by_touched = g.by_touched = FastDiv(a.parts.touched);
-    t.n_group = 0;
-    g.n_total = 0;
-    if (a.n_total > 0) {
+    // totals over many parts have a launch of their own, with more threads a column
+    if (a.n_total > 0 && (a.parts.count() > 512 || a.n_group == 0)) {
+        t.n_group = 0;
+        g.n_total = 0;
         const hipError_t e = a.parts.count() <= 4 ? launch_sums<64, 1>(t, s) : launch_sums<32, 32>(t, s);
-        if (e != hipSuccess) return e;
+        if (e != hipSuccess || a.n_group == 0) return e;
     }
-    if (a.n_group == 0) return hipSuccess;
-    if (a.parts.per_group <= 4) return launch_sums<64, 1>(g, s);
-    return a.parts.per_group <= 64 ? launch_sums<64, 4>(g, s) : launch_sums<64, 16>(g, s);
+    const int each = g.n_total > 0 ? a.parts.count() : a.parts.per_group;
+    if (each <= 4) return launch_sums<64, 1>(g, s);
+    return each <= 64 ? launch_sums<64, 4>(g, s) : launch_sums<64, 16>(g, s);
 }
 
 }  // namespace tmk

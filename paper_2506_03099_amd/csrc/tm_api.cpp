@@ -140,7 +140,7 @@ tm_status check_ptr(const void* p, size_t bytes, const char* name, size_t align 
 // earlier one needs no further look-up (three calls of the runtime, 0.35 us; a
 // caching allocator puts the tensors of a small call into one allocation).
 class PtrChecks {
-    static constexpr int kKept = 4;
+    static constexpr int kKept = 8;
     uintptr_t base_[kKept] = {};
     size_t size_[kKept] = {};
     int n_ = 0;

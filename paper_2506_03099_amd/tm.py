@@ -33,6 +33,7 @@ STATUS_NAMES = {0: "TM_OK", -1: "TM_E_ARG", -2: "TM_E_SHAPE", -3: "TM_E_DTYPE",
                 -4: "TM_E_ORDER", -5: "TM_E_CAPACITY", -6: "TM_E_DEVICE"}
 
 _TORCH_DTYPE = {TM_F32: torch.float32, TM_BF16: torch.bfloat16}
+_BF16 = torch.bfloat16
 _DTYPE_CODE = {torch.float32: TM_F32, torch.bfloat16: TM_BF16, "f32": TM_F32, "bf16": TM_BF16}
 
 
@@ -738,17 +739,19 @@ def _given(name, t, shape, dtype=torch.float32):
     return _ptr(t)
 
 
-def _grad(name, t, wanted, shape, device, dtype=torch.float32):
-    """A gradient and its address: the caller's tensor, a new one if it is None, nothing if it is False or
-    there is nothing that it would be the gradient of."""
-    if t is False or not wanted:
-        if t is not False and t is not None:
-            raise TMError(TM_E_ARG, f"{name} is the gradient of a tensor that is not there")
-        return None, None
+def _grad(name, t, of):
+    """The gradient of tensor ``of`` and its address: the caller's tensor, a new one like ``of`` if it is None,
+    nothing if it is False or there is no ``of``."""
     if t is None:
-        t = torch.empty(shape, dtype=dtype, device=device)
+        if of is None:
+            return None, None
+        t = torch.empty_like(of)
         return t, t.data_ptr()
-    _expect(name, t, shape, dtype)
+    if t is False:
+        return None, None
+    if of is None:
+        raise TMError(TM_E_ARG, f"{name} is the gradient of a tensor that is not there")
+    _expect(name, t, of.shape, of.dtype)
     return t, _ptr(t)
 
 
@@ -792,6 +795,9 @@ def tm_block_norm_fwd(desc: tm_block_norm_desc, x, y=None, gate=None, post_weigh
     return r, h
 
 
+_NO_SUMS = (None,) * 6
+
+
 class BlockNormGrads(NamedTuple):
     """Gradients of ``tm_block_norm_fwd``'s inputs; None where the forward had no such input."""
     dx: torch.Tensor
@@ -818,7 +824,7 @@ def tm_block_norm_bwd(desc: tm_block_norm_desc, r, dh=None, dr=None, y=None, gat
     if like is None:
         raise TMError(TM_E_ARG, "r is missing" if has_pre else "dr is missing without a norm before the block")
     n = _rows("r" if has_pre else "dr", like, B, E, st)
-    shape, mod, vec, dev = like.shape, (B, desc.groups, E), (E,), like.device
+    shape, mod, vec = like.shape, (B, desc.groups, E), (E,)
     if (scale is None) != (shift is None):
         raise TMError(TM_E_ARG, "scale and shift: both or neither")
     ins = [_ptr(r) if has_pre else None, _given("dh", dh, shape, act), _given("dr", dr, shape, st),
@@ -827,20 +833,23 @@ def tm_block_norm_bwd(desc: tm_block_norm_desc, r, dh=None, dr=None, y=None, gat
     _given("shift", shift, mod)
     if dx is False or dy is False:
         raise TMError(TM_E_ARG, "dx and dy are always formed")
-    grads = [_grad("dx", dx, True, shape, dev, st), _grad("dy", dy, y is not None, shape, dev, act),
-             _grad("dgate", dgate, gate is not None, mod, dev),
-             _grad("dpost_weight", dpost_weight, post_weight is not None, vec, dev),
-             _grad("dpre_weight", dpre_weight, pre_weight is not None, vec, dev),
-             _grad("dpre_bias", dpre_bias, pre_bias is not None, vec, dev),
-             _grad("dscale", dscale, scale is not None, mod, dev),
-             _grad("dshift", dshift, scale is not None, mod, dev)]
+    dx, pdx = _grad("dx", dx, like)
+    dy, pdy = _grad("dy", dy, y)
+    dgate, pdg = _grad("dgate", dgate, gate)
+    dpost_weight, pdp = _grad("dpost_weight", dpost_weight, post_weight)
+    dpre_weight, pdw = _grad("dpre_weight", dpre_weight, pre_weight)
+    dpre_bias, pdb = _grad("dpre_bias", dpre_bias, pre_bias)
+    dscale, pdc = _grad("dscale", dscale, scale)
+    dshift, pdh = _grad("dshift", dshift, scale)
     d, stream = ctypes.byref(desc), _stream(stream)
+    L = lib()
     nbytes, ws = 0, None
-    if any(p is not None for _, p in grads[2:]):
-        nbytes = lib().tm_block_norm_bwd_workspace(d, n, first_token)
+    if (pdg, pdp, pdw, pdb, pdc, pdh) != _NO_SUMS:
+        nbytes = L.tm_block_norm_bwd_workspace(d, n, first_token)
         ws = _own_workspace(nbytes, workspace, like, stream)
-    _check(lib().tm_block_norm_bwd(d, n, first_token, *ins, *[p for _, p in grads], _ptr(ws), nbytes, stream))
-    return BlockNormGrads(*[t for t, _ in grads])
+    _check(L.tm_block_norm_bwd(d, n, first_token, *ins, pdx, pdy, pdg, pdp, pdw, pdb, pdc, pdh, _ptr(ws), nbytes,
+                               stream))
+    return BlockNormGrads(dx, dy, dgate, dpost_weight, dpre_weight, dpre_bias, dscale, dshift)
 
 
 def make_linear_desc(batch, in_width, out_width, act="none", out_dtype="bf16", groups=1,
@@ -895,18 +904,27 @@ class LinearGrads(NamedTuple):
 def tm_linear_bwd(desc: tm_linear_desc, x, weight, dout, gate=None, pre=None, first_token: int = 0, dx=None,
                   dweight=None, dbias=None, dgate=None, workspace=None, stream=None) -> LinearGrads:
     """Gradients from that of the output, ``dout``. ``pre``: the forward's (not needed without activation and
-    gate). Each gradient is allocated if not given, and left out with False (the bias' for a layer without).
+    gate; x is needed for dweight and dx, weight for dx and dweight, and both may be None where neither is
+    wanted). Each gradient is allocated if not given, and left out with False (the bias' for a layer without).
     ``workspace``: a tensor of ``tm_linear_bwd_workspace`` bytes (allocated if not given; needed on another
     stream than the current one)."""
     B, K, N = desc.batch, desc.in_width, desc.out_width
     n = _rows("dout", dout, B, N, _TORCH_DTYPE.get(desc.out_dtype))
-    xs, mod, dev, bf16 = (B, n, K), (B, desc.groups, N), dout.device, torch.bfloat16
-    px, pw = _given("x", x, xs, bf16), _given("weight", weight, (N, K), bf16)
-    pd, pg, pp = _ptr(dout), _given("gate", gate, mod), _given("pre", pre, (B, n, N), bf16)
-    grads = [_grad("dx", dx, True, xs, dev, bf16), _grad("dweight", dweight, True, (N, K), dev, bf16),
-             _grad("dbias", dbias, True, (N,), dev), _grad("dgate", dgate, gate is not None, mod, dev)]
+    px, pw = _given("x", x, (B, n, K), _BF16), _given("weight", weight, (N, K), _BF16)
+    pd, pg, pp = _ptr(dout), _given("gate", gate, (B, desc.groups, N)), _given("pre", pre, (B, n, N), _BF16)
+    dx, pdx = _grad("dx", dx, x)
+    dweight, pdw = _grad("dweight", dweight, weight)
+    dgate, pdg = _grad("dgate", dgate, gate)
+    pdb = None
+    if dbias is None:
+        dbias = torch.empty((N,), dtype=torch.float32, device=dout.device)
+        pdb = dbias.data_ptr()
+    elif dbias is False:
+        dbias = None
+    else:
+        pdb = _given("dbias", dbias, (N,))
     d, stream = ctypes.byref(desc), _stream(stream)
     nbytes = lib().tm_linear_bwd_workspace(d, n, first_token)
     ws = _own_workspace(nbytes, workspace, dout, stream)
-    _check(lib().tm_linear_bwd(d, n, first_token, px, pw, pd, pg, pp, *[p for _, p in grads], _ptr(ws), nbytes, stream))
-    return LinearGrads(*[t for t, _ in grads])
+    _check(lib().tm_linear_bwd(d, n, first_token, px, pw, pd, pg, pp, pdx, pdw, pdb, pdg, _ptr(ws), nbytes, stream))
+    return LinearGrads(dx, dweight, dbias, dgate)

@@ -58,10 +58,10 @@ def test_linear_refuses_host_tensors_and_wrong_shapes(tm):
 
 def test_workspace_sizes(tm):
     lib = tm.lib()
-    # a run of 21 groups of 1560: about two parts a CU, three sums each
+    # a run of 21 groups of 1560: about a part for each CU, three sums each
     d = tm.make_block_norm_desc(1, 5120, groups=21, group_tokens=1560)
     n = lib.tm_block_norm_bwd_workspace(d, 32760, 0)
-    assert n % (3 * 5120 * 4) == 0 and 256 <= n // (3 * 5120 * 4) <= 1024
+    assert n % (3 * 5120 * 4) == 0 and 200 <= n // (3 * 5120 * 4) <= 1024
     assert lib.tm_block_norm_bwd_workspace(d, 32761, 0) == 0
     # dz in bf16 at least, and room for a round of split tiles beside it
     d = tm.make_linear_desc(1, 5120, 5120, "none", "f32", 21, 1560)
