@@ -1728,12 +1728,13 @@ struct GemmPlan {
 };
 
 // What a round of `wgs` workgroups of `stages` stages each takes, in us. A stage of a 256 tile takes 0.97 us with few
-// workgroups at work and 1.4 with one on each CU; one of a 128 tile 0.45 and 0.55, and 0.95 with two on each. (From
+// workgroups at work and 1.4 with one on each CU; one of a 128 tile 0.43 and 0.51, 0.72 once
+// some CUs have two, and 0.94 when all have. (From
 // 50 sizes from 130 to 9000 rows and 64 to 20480 wide, each with either tile, split and not: the choice by
-// these costs is 3% behind the best of the four.)
+// these costs is 0.8% behind the best of the four.)
 double round_us(int tile, double wgs, double stages) {
     const double f = wgs / tmk::kCUs;
-    return tile == 256 ? stages * (0.97 + 0.43 * f) + 8 : stages * (f <= 1 ? 0.45 + 0.1 * f : 0.55 + 0.4 * (f - 1)) + 4;
+    return tile == 256 ? stages * (0.97 + 0.43 * f) + 8 : stages * (f <= 1 ? 0.43 + 0.08 * f : 0.72 + 0.22 * (f - 1)) + 4;
 }
 
 GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool may_split) {
