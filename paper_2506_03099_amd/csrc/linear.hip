@@ -563,21 +563,27 @@ hipError_t launch_tiles(const GemmArgs& a, hipStream_t s) {
 // ---------------------------------------------------------------------------
 // Few rows: W streams by once
 // ---------------------------------------------------------------------------
-// A workgroup takes 16 columns of the output (rows of W) and its NW waves share K in runs of 64:
-// v_mfma_f32_16x16x32_bf16 with W as the first operand and the rows of x as the second. A lane brings
-// 32 neighbouring bytes of its row of W, the k of two MFMAs, so that 4 lanes read a whole line; which k an
-// operand's element is does not matter as long as x's are the same. Rows that do not exist repeat the last one.
-template <int NW>
+// A workgroup takes 16 / C columns of the output (rows of W) and its NW waves share K in runs of 64 C:
+// v_mfma_f32_16x16x32_bf16 with W as the first operand and the rows of x as the second. Of its 16 rows and
+// columns, C blocks of 16 / C take a run's C pieces of 64 each; the blocks on the diagonal hold the sums of
+// a piece, the others nothing of use. (One or a few rows leave columns over, and 16 columns a workgroup
+// leave CUs idle: 5120 columns are 320 workgroups for 256 CUs.) A lane brings 32 neighbouring bytes of its row of W,
+// the k of two MFMAs, so that 4 lanes read a whole line; which k an operand's element is does not matter as
+// long as x's are the same. Rows that do not exist repeat the last one.
+template <int NW, int C>
 __global__ __launch_bounds__(NW * 64) void few_rows_kernel(const FewRowsArgs a) {
+    constexpr int CO = 16 / C;  // columns, and the most rows
     __shared__ float sums[NW][16][17];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int n0 = blockIdx.x * 16;
+    const int n0 = blockIdx.x * CO;
     const int64_t K = a.K;
-    const __bf16* w = static_cast<const __bf16*>(a.w) + min(n0 + (lane & 15), a.N - 1) * K + (lane >> 4) * 16;
-    const __bf16* x = static_cast<const __bf16*>(a.x) + min(lane & 15, a.rows - 1) * K + (lane >> 4) * 16;
+    const int piece = (lane & 15) / CO, k0 = piece * 64 + (lane >> 4) * 16;
+    const __bf16* w = static_cast<const __bf16*>(a.w) + min(n0 + (lane & 15) % CO, a.N - 1) * K + k0;
+    const __bf16* x = static_cast<const __bf16*>(a.x) + min((lane & 15) % CO, a.rows - 1) * K + k0;
     f32x4_t acc[2] = {f32x4_t{}, f32x4_t{}};
-    const int whole = a.K / 64;
+    constexpr int RUN = 64 * C;
+    const int whole = a.K / RUN;
     constexpr int U = 4;
     int i = wave;
     for (; i + (U - 1) * NW < whole; i += U * NW) {
@@ -585,11 +591,11 @@ __global__ __launch_bounds__(NW * 64) void few_rows_kernel(const FewRowsArgs a) 
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) wf[u][h] = *reinterpret_cast<const bf16x8_t*>(w + (i + u * NW) * 64 + h * 8);
+            for (int h = 0; h < 2; ++h) wf[u][h] = *reinterpret_cast<const bf16x8_t*>(w + (i + u * NW) * RUN + h * 8);
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) xf[u][h] = *reinterpret_cast<const bf16x8_t*>(x + (i + u * NW) * 64 + h * 8);
+            for (int h = 0; h < 2; ++h) xf[u][h] = *reinterpret_cast<const bf16x8_t*>(x + (i + u * NW) * RUN + h * 8);
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -597,13 +603,13 @@ __global__ __launch_bounds__(NW * 64) void few_rows_kernel(const FewRowsArgs a) 
                 acc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[u][h], xf[u][h], acc[h], 0, 0, 0);
     }
     // the runs that are left, the last one perhaps with its first k only
-    for (; i * 64 < a.K; i += NW) {
+    for (; i * RUN < a.K; i += NW) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             bf16x8_t wf = bf16x8_t{}, xf = bf16x8_t{};
-            if (i * 64 + (lane >> 4) * 16 + h * 8 < a.K) {
-                wf = *reinterpret_cast<const bf16x8_t*>(w + i * 64 + h * 8);
-                xf = *reinterpret_cast<const bf16x8_t*>(x + i * 64 + h * 8);
+            if (i * RUN + k0 + h * 8 < a.K) {
+                wf = *reinterpret_cast<const bf16x8_t*>(w + i * RUN + h * 8);
+                xf = *reinterpret_cast<const bf16x8_t*>(x + i * RUN + h * 8);
             }
             acc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, xf, acc[h], 0, 0, 0);
         }
@@ -612,12 +618,14 @@ __global__ __launch_bounds__(NW * 64) void few_rows_kernel(const FewRowsArgs a) 
 #pragma unroll
     for (int e = 0; e < 4; ++e) sums[wave][lane & 15][4 * (lane >> 4) + e] = acc[0][e] + acc[1][e];
     __syncthreads();
-    if (tid >= 256) return;
-    const int row = tid >> 4, col = n0 + (tid & 15);
+    if (tid >= CO * CO) return;
+    const int row = tid / CO, c = tid % CO, col = n0 + c;
     if (row >= a.rows || col >= a.N) return;
     float z = a.ep.bias != nullptr ? a.ep.bias[col] : 0.f, sum = 0.f;
 #pragma unroll
-    for (int v = 0; v < NW; ++v) sum += sums[v][row][tid & 15];
+    for (int v = 0; v < NW; ++v)
+#pragma unroll
+        for (int q = 0; q < C; ++q) sum += sums[v][q * CO + row][q * CO + c];
     z += sum;
     const int64_t at = static_cast<int64_t>(row) * a.N + col;
     if (a.ep.pre != nullptr) static_cast<__bf16*>(a.ep.pre)[at] = static_cast<__bf16>(z);
@@ -853,10 +861,19 @@ hipError_t launch_gemm(const GemmArgs& a, int tile, bool a_trans, bool b_trans, 
 }
 
 hipError_t launch_few_rows(const FewRowsArgs& a, hipStream_t s) {
-    const dim3 grid((a.N + 15) / 16);
-    // as many waves as there is work for: 4 a workgroup where the workgroups fill the CUs
-    return grid.x >= 4 * kCUs ? launch_with(few_rows_kernel<4>, grid, 256, s, a)
-                              : launch_with(few_rows_kernel<16>, grid, 1024, s, a);
+    // The fewest columns a workgroup (and pieces of K) that leave 1024 workgroups, as far as the rows allow: one row
+    // of 5120 x 5120 14.2 us with 16, 11.1 with 8, 10.0 with 4; 20480 x 5120 51, 42, 37; 5120 x 20480 37, 39, 37;
+    // 2560 x 40960 39, 37, 45. Their four waves are sixteen where workgroups are few.
+    int pieces = 1;
+    while (pieces < 4 && a.rows * pieces * 2 <= 16 && a.N / 16 * pieces < 1024) pieces *= 2;
+    const int columns = 16 / pieces;
+    const dim3 grid((a.N + columns - 1) / columns);
+    const bool many = grid.x >= kCUs;
+    switch (pieces) {
+        case 1: return many ? launch_with(few_rows_kernel<4, 1>, grid, 256, s, a) : launch_with(few_rows_kernel<16, 1>, grid, 1024, s, a);
+        case 2: return many ? launch_with(few_rows_kernel<4, 2>, grid, 256, s, a) : launch_with(few_rows_kernel<16, 2>, grid, 1024, s, a);
+    }
+    return many ? launch_with(few_rows_kernel<4, 4>, grid, 256, s, a) : launch_with(few_rows_kernel<16, 4>, grid, 1024, s, a);
 }
 
 hipError_t launch_linear_dz(const LinearDzArgs& a, hipStream_t s) {
