@@ -1776,6 +1776,18 @@ GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool may_split) {
     return best;
 }
 
+// Whether a forward call of few rows goes by tiles all the same, if it has the workspace: each workgroup of the
+// few rows' form reads all of x, which costs more than tiles' padding from some 45 MB on with 9 to 16 rows
+// (16 rows of 5120 x 5120, 52 MB: 19.4 us, by tiles 16.4; 12 rows, 39 MB: 17.8 and 16.9) and 100 MB on with
+// 5 to 8 (8 of 5120 x 20480, 105 MB: 45.5 and 44.9; 5 of 20480 x 5120, 131 MB: 51 and 44; 8 of 5120 x 5120,
+// 52 MB: 15.5 and 16.0).
+bool tiles_for_few(const LinearGeo& g) {
+    const int64_t rows = g.run.rows;
+    if (rows <= 4) return false;
+    const double wgs = double(g.N) / (rows <= 8 && g.N < 16384 ? 8 : 16);
+    return wgs * double(rows) * double(g.K) * 2 >= (rows <= 8 ? 100e6 : 45e6);
+}
+
 tm_status check_tiles(const GemmPlan& p) {
     if (p.tiles_m * p.tiles_n > (int64_t(1) << 24)) return fail(TM_E_SHAPE, "rows * width too large");
     return TM_OK;
@@ -1996,7 +2008,9 @@ size_t tm_linear_fwd_workspace(const tm_linear_desc* desc, int32_t n_tok) {
         d.groups = 1;
         d.group_tokens = 0;
     }
-    if (check_linear(desc == nullptr ? nullptr : &d, n_tok, 0, &g) != TM_OK || g.run.rows <= tmk::kFewRows) return 0;
+    if (check_linear(desc == nullptr ? nullptr : &d, n_tok, 0, &g) != TM_OK ||
+        (g.run.rows <= tmk::kFewRows && !tiles_for_few(g)))
+        return 0;
     const GemmPlan p = plan_gemm(g.run.rows, g.N, g.K, true);
     return check_tiles(p) == TM_OK ? p.part_bytes() : 0;
 }
@@ -2009,11 +2023,15 @@ tm_status tm_linear_fwd(const tm_linear_desc* desc, int32_t n_tok, int64_t first
     if (st != TM_OK) return st;
     if (n_tok == 0) return TM_OK;
     if (x == nullptr || weight == nullptr || o == nullptr) return fail(TM_E_ARG, "x, weight or o is NULL");
-    const bool few = g.run.rows <= tmk::kFewRows;
+    bool few = g.run.rows <= tmk::kFewRows;
     GemmPlan p{};
-    if (!few) {
+    if (!few || tiles_for_few(g)) {
         p = plan_gemm(g.run.rows, g.N, g.K, true);
-        if (p.part_bytes() > 0 && (workspace == nullptr || workspace_bytes < p.part_bytes()))
+        const bool room = p.part_bytes() == 0 || (workspace != nullptr && workspace_bytes >= p.part_bytes());
+        few = few && !room;
+        if (few)
+            p = GemmPlan{};
+        else if (!room)
             p = plan_gemm(g.run.rows, g.N, g.K, false);
         if ((st = check_tiles(p)) != TM_OK) return st;
     }
