@@ -463,8 +463,9 @@ tm_status tm_kv8_attn_fwd(const tm_kv8_cache* cache, const void* q, int32_t q_ch
  * is the token at position first_token + i, of group (first_token + i) /
  * group_tokens, which must be one of the groups (else TM_E_SHAPE); their gradients
  * have zeros for groups without a token in the call. group_tokens = 0: one group,
- * whatever the position. Widths are multiples of 8; fp32 vectors are 16-byte
- * aligned like everything else. No output may overlap anything but where said. */
+ * whatever the position. At most 2^20 rows (batch * groups) and 2^30 elements of a modulation. Widths are multiples of 8; fp32 vectors are 16-byte
+ * aligned like everything else. No output may overlap anything but where said. Calls that
+ * overlap in time (other streams, graphs that run at once) need workspaces of their own. */
 typedef enum tm_norm { TM_NORM_NONE = 0, TM_NORM_LAYER = 1, TM_NORM_RMS = 2 } tm_norm;
 typedef enum tm_act { TM_ACT_NONE = 0, TM_ACT_GELU = 1, TM_ACT_SILU = 2 } tm_act;
 

@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "tm_device.h"
@@ -118,7 +119,7 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(const BlockNormArgs a)
     lds_float* const L = (lds_float*)smem;
     const int T = blockDim.x, waves = T / 64, tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int row = blockIdx.x;
+    const int row = a.row0 + blockIdx.x;
     if (waves > 1 && tid < 4 * kMaxWaves) L[tid] = 0.f;
     const int64_t base = static_cast<int64_t>(row) * a.E;
     const int64_t mod = a.tg.row(row) * a.E;
@@ -480,16 +481,27 @@ hipError_t launch_sums(const ColumnSums& a, hipStream_t s) {
 
 }  // namespace
 
+template <typename S, typename A, int U>
+static hipError_t launch_rows(BlockNormArgs a, int threads, hipStream_t s) {
+    // Thread numbers are 32 bits wide: very many rows take several launches.
+    const int most = static_cast<int>((int64_t(1) << 31) / threads);
+    for (int64_t at = 0; at < a.rows; at += most) {
+        a.row0 = static_cast<int32_t>(at);
+        const hipError_t e = launch_with(block_norm_kernel<S, A, U>, dim3(static_cast<unsigned>(std::min<int64_t>(most, a.rows - at))),
+                                         threads, s, a);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 hipError_t launch_block_norm(const BlockNormArgs& a, bool stream_f32, bool act_f32, hipStream_t s) {
     int U, threads;
     block_norm_shape(a.E, false, &U, &threads);
-#define TM_NORM_CASE(U_)                                                                                   \
-    if (U == U_) {                                                                                         \
-        if (stream_f32)                                                                                    \
-            return act_f32 ? launch_with(block_norm_kernel<float, float, U_>, dim3(a.rows), threads, s, a)     \
-                           : launch_with(block_norm_kernel<float, __bf16, U_>, dim3(a.rows), threads, s, a);   \
-        return act_f32 ? launch_with(block_norm_kernel<__bf16, float, U_>, dim3(a.rows), threads, s, a)        \
-                       : launch_with(block_norm_kernel<__bf16, __bf16, U_>, dim3(a.rows), threads, s, a);      \
+#define TM_NORM_CASE(U_)                                                                                             \
+    if (U == U_) {                                                                                                   \
+        if (stream_f32)                                                                                              \
+            return act_f32 ? launch_rows<float, float, U_>(a, threads, s) : launch_rows<float, __bf16, U_>(a, threads, s); \
+        return act_f32 ? launch_rows<__bf16, float, U_>(a, threads, s) : launch_rows<__bf16, __bf16, U_>(a, threads, s);   \
     }
     TM_NORM_CASE(1)
     TM_NORM_CASE(2)

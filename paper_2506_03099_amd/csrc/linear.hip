@@ -694,7 +694,10 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(const LinearDzArgs a) {
             if (a.dz != nullptr) store8(static_cast<__bf16*>(a.dz) + at, d);
             if (a.dz_rest != nullptr) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) d[e] -= static_cast<float>(static_cast<__bf16>(d[e]));
+                for (int e = 0; e < 8; ++e) {
+                    const float hi = static_cast<float>(static_cast<__bf16>(d[e]));
+                    d[e] = __builtin_isfinite(hi) ? d[e] - hi : 0.f;  // (no NaN beside an infinity)
+                }
                 store8(static_cast<__bf16*>(a.dz_rest) + at, d);
             }
             if (a.dz_few != nullptr) {

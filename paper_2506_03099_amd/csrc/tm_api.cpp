@@ -1645,8 +1645,8 @@ tmk::RowParts row_parts(const Run& r, int64_t want, int64_t least) {
 }
 
 tm_status check_modulation(int64_t B, int64_t groups, int64_t width) {
-    if (B * groups > (int64_t(1) << 30) / width)
-        return fail(TM_E_SHAPE, "modulations of more than 2^30 elements");
+    if (B * groups > (int64_t(1) << 20) || B * groups > (int64_t(1) << 30) / width)
+        return fail(TM_E_SHAPE, "modulations of more than 2^20 rows or 2^30 elements");
     return TM_OK;
 }
 

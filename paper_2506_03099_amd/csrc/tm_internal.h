@@ -435,6 +435,7 @@ struct BlockNormArgs {
     void* r;
     void* h;
     int32_t E, rows;
+    int32_t row0;  // of one launch; set by the launcher
     int32_t pre, post;
     float eps, inv_E;
     TokenGroups tg;

@@ -755,6 +755,17 @@ def _grad(name, t, of):
     return t, _ptr(t)
 
 
+def _formed(name, t, shape, dtype, like):
+    """A gradient that there always is, and its address: the caller's tensor, a new one if it is None, nothing if it
+    is False."""
+    if t is None:
+        t = torch.empty(shape, dtype=dtype, device=like.device)
+        return t, t.data_ptr()
+    if t is False:
+        return None, None
+    return t, _given(name, t, shape, dtype)
+
+
 def make_block_norm_desc(batch, width, pre="layer", post="none", dtype="bf16", stream_dtype="f32", eps=1e-6,
                          groups=1, group_tokens=0) -> tm_block_norm_desc:
     """``pre``, ``post``: "none", "layer" or "rms"; ``dtype`` of y and h, ``stream_dtype`` of x and r."""
@@ -904,25 +915,17 @@ class LinearGrads(NamedTuple):
 def tm_linear_bwd(desc: tm_linear_desc, x, weight, dout, gate=None, pre=None, first_token: int = 0, dx=None,
                   dweight=None, dbias=None, dgate=None, workspace=None, stream=None) -> LinearGrads:
     """Gradients from that of the output, ``dout``. ``pre``: the forward's (not needed without activation and
-    gate; x is needed for dweight and dx, weight for dx and dweight, and both may be None where neither is
-    wanted). Each gradient is allocated if not given, and left out with False (the bias' for a layer without).
+    gate; nor ``x`` without dweight and ``weight`` without dx). Each gradient is allocated if not given, and left out with False (the bias' for a layer without).
     ``workspace``: a tensor of ``tm_linear_bwd_workspace`` bytes (allocated if not given; needed on another
     stream than the current one)."""
     B, K, N = desc.batch, desc.in_width, desc.out_width
     n = _rows("dout", dout, B, N, _TORCH_DTYPE.get(desc.out_dtype))
     px, pw = _given("x", x, (B, n, K), _BF16), _given("weight", weight, (N, K), _BF16)
     pd, pg, pp = _ptr(dout), _given("gate", gate, (B, desc.groups, N)), _given("pre", pre, (B, n, N), _BF16)
-    dx, pdx = _grad("dx", dx, x)
-    dweight, pdw = _grad("dweight", dweight, weight)
+    dx, pdx = _formed("dx", dx, (B, n, K), _BF16, dout)
+    dweight, pdw = _formed("dweight", dweight, (N, K), _BF16, dout)
+    dbias, pdb = _formed("dbias", dbias, (N,), torch.float32, dout)
     dgate, pdg = _grad("dgate", dgate, gate)
-    pdb = None
-    if dbias is None:
-        dbias = torch.empty((N,), dtype=torch.float32, device=dout.device)
-        pdb = dbias.data_ptr()
-    elif dbias is False:
-        dbias = None
-    else:
-        pdb = _given("dbias", dbias, (N,))
     d, stream = ctypes.byref(desc), _stream(stream)
     nbytes = lib().tm_linear_bwd_workspace(d, n, first_token)
     ws = _own_workspace(nbytes, workspace, dout, stream)

@@ -89,6 +89,12 @@ void norm_checks() {
     EXPECT(norm_fwd(&d, 1, (int64_t(1) << 30) - 1) == TM_E_ARG);
     d = norm(16384, TM_NORM_LAYER, TM_NORM_NONE, 65535, INT_MAX, 1);
     EXPECT(norm_fwd(&d, 1, 0) == TM_E_SHAPE);
+    d = norm(8, TM_NORM_LAYER, TM_NORM_NONE, 1, 1 << 20, 1);
+    EXPECT(norm_fwd(&d, 1, 0) == TM_E_ARG);
+    d = norm(8, TM_NORM_LAYER, TM_NORM_NONE, 1, (1 << 20) + 1, 1);
+    EXPECT(norm_fwd(&d, 1, 0) == TM_E_SHAPE);
+    d = norm(2048, TM_NORM_LAYER, TM_NORM_NONE, 2, 1 << 19, 1);
+    EXPECT(norm_fwd(&d, 1, 0) == TM_E_SHAPE);
     // which tensors go together
     d = norm(64);
     EXPECT(norm_fwd(&d, 1, 0, nullptr, FAKE) == TM_E_ARG);

@@ -338,3 +338,15 @@ def test_captured_calls_and_other_streams(tm):
     side.synchronize()
     for a, b in zip(want, got):
         assert a is None or torch.equal(a, b)
+
+
+def test_more_rows_than_one_launch_takes(tm):
+    """Thread numbers are 32 bits: 2^25 rows of one wave each take a second launch."""
+    n, E = 2 ** 25 + 1000, 8
+    x = torch.randn((1000, E), device="cuda").repeat(n // 1000 + 1, 1)[:n].to(torch.bfloat16).view(1, n, E)
+    d = tm.make_block_norm_desc(1, E, "layer", "none", "bf16", "bf16")
+    _, h = tm.tm_block_norm_fwd(d, x)
+    _, want = tm.tm_block_norm_fwd(d, x[:, :1000].contiguous())
+    assert torch.equal(h[:, :1000], want)
+    at = (2 ** 25 // 1000) * 1000  # a multiple of the period, below the second launch's first row
+    assert torch.equal(h[:, at:at + 1000], want) and torch.equal(h[:, n - 500:], h[:, n - 500 - at:n - at])

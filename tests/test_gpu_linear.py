@@ -274,3 +274,56 @@ def test_captured_calls(tm, rows):
         for a, b in zip(want, got):
             assert torch.equal(a, b)
         tm.tm_linear_bwd(d, p["x"], p["weight"], dout, p["gate"], pre)
+
+
+@pytest.mark.parametrize("rows", [3, 8, 40])
+def test_infinite_gradients_stay_in_their_rows(tm, rows):
+    """An infinity in dout makes its row of dx and of dweight infinite, not NaN, and no other."""
+    K, N = 72, 136
+    p = make(1, rows, K, N, "f32", "", 1, 3)
+    p["weight"] = p["weight"].abs()  # no cancellation of infinities: sums are +inf
+    d = tm.make_linear_desc(1, K, N, "none", "f32")
+    dout = torch.randn((1, rows, N), device="cuda")
+    want = tm.tm_linear_bwd(d, p["x"], p["weight"], dout)
+    dout[0, 1, 5] = float("inf")
+    got = tm.tm_linear_bwd(d, p["x"], p["weight"], dout)
+    others = [i for i in range(rows) if i != 1]
+    assert torch.equal(got.dx[:, others], want.dx[:, others])
+    assert bool((got.dx[0, 1] == float("inf")).all())
+    cols = [i for i in range(N) if i != 5]
+    assert torch.equal(got.dweight[cols], want.dweight[cols])
+    assert bool((~got.dweight[5].isfinite()).all()) and not bool(got.dweight[5].isnan().any())
+
+
+def test_gradients_without_what_they_do_not_need(tm):
+    p = make(1, 40, 72, 200, "bf16", "", 1, 4)
+    d = tm.make_linear_desc(1, 72, 200)
+    dout = torch.randn((1, 40, 200), device="cuda").to(torch.bfloat16)
+    want = tm.tm_linear_bwd(d, p["x"], p["weight"], dout)
+    assert torch.equal(tm.tm_linear_bwd(d, None, p["weight"], dout, dweight=False).dx, want.dx)
+    assert torch.equal(tm.tm_linear_bwd(d, p["x"], None, dout, dx=False).dweight, want.dweight)
+    for args in ((None, p["weight"]), (p["x"], None)):
+        with pytest.raises(tm.TMError) as e:
+            tm.tm_linear_bwd(d, *args, dout)
+        assert e.value.status == tm.TM_E_ARG
+
+
+@pytest.mark.parametrize("n,K,N,act,out,parts", [(700, 2056, 7688, "gelu", "bf16", "bz"), (2900, 1032, 5128, "silu", "f32", "bgr"),
+                                                 (1500, 6000, 5000, "none", "f32", "br")])
+def test_large_tiles(tm, n, K, N, act, out, parts):
+    """Sizes that the 256-wide tiles take, several to a workgroup and some of them split, rows and columns that
+    end inside tiles, each kind of epilogue; held to the bounds above, sizes in fp32 (1.01 for its roundings)."""
+    p = make(1, n, K, N, out, parts, 5, n)
+    g = group_rows(1, n, 5, 600, 20, "cuda")
+    d = tm.make_linear_desc(1, K, N, act, out, 5, 600)
+    pre = torch.empty((1, n, N), dtype=torch.bfloat16, device="cuda") if "z" in parts else None
+    o = tm.tm_linear_fwd(d, p["x"], p["weight"], p["bias"], p["gate"], p["residual"], 20, pre=pre)
+    o64, z64 = linear(as64(p), act, g)
+    S = 1.01 * (p["x"].float().abs() @ p["weight"].float().abs().t() + p["bias"].abs()).double()
+    zb = 2 * (K + 8) * U * S
+    gate = p["gate"].double()[:, g] if p["gate"] is not None else torch.ones((), device="cuda", dtype=torch.float64)
+    held(o, o64, gate.abs() * (1.13 * zb + 32 * U * z64.abs()) + 4 * U * (
+        (gate * z64).abs() + (p["residual"].double().abs() if p["residual"] is not None else 0)), "o")
+    if pre is not None:
+        held(pre, z64, zb, "pre")
+    near(o, o64, "o")
