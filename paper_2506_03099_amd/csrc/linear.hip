@@ -141,15 +141,17 @@ struct Tile {
         }
     }
 
-    // The last stage of the sum, of which only `left` < 64 k exist: through registers, zeros behind them.
-    __device__ __forceinline__ void load_rest(const unsigned char* base, lds_u8* lds, int wave, int lane, int left) const {
+    // The stage of which only `left` < 64 k exist: direct loads in the lanes that have some (the others' 16 bytes of
+    // LDS are left alone by them), zeros written in the others.
+    __device__ __forceinline__ void load_rest(const void* base, lds_u8* lds, uint32_t lds_at, int wave, int lane, int left) const {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int ch = (i * 4 + wave) * 64 + lane;
             const int row = ch / kChunks, c = (ch % kChunks) ^ swizzle(row);
-            f32x4_t v = f32x4_t{};
-            if ((TRANS ? row : c * 8) < left) v = *reinterpret_cast<const f32x4_t*>(base + voff[i]);
-            *(lds_f32x4_t*)(lds + ch * 16) = v;
+            if ((TRANS ? row : c * 8) < left)
+                lds_dma16(base, voff[i], lds_at + (i * 4 + wave) * 1024);
+            else
+                *(lds_f32x4_t*)(lds + ch * 16) = f32x4_t{};
         }
     }
 
@@ -295,8 +297,8 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const Gemm
         tb.init(wave, lane, a.ldb, a.N - w.n0);
         const void *pa = base_a(w, w.s0), *pb = base_b(w, w.s0);
         if (rest != 0 && w.s0 == 0) {
-            ta.load_rest(static_cast<const unsigned char*>(pa), L, wave, lane, rest);
-            tb.load_rest(static_cast<const unsigned char*>(pb), L + SLOT, wave, lane, rest);
+            ta.load_rest(pa, L, lds_base, wave, lane, rest);
+            tb.load_rest(pb, L + SLOT, lds_base + SLOT, wave, lane, rest);
         } else {
 #pragma unroll
             for (int j = 0; j < LOADS; ++j) issue(true, pa, 0, j);

@@ -1780,10 +1780,11 @@ GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool may_split) {
 // few rows' form reads all of x, which costs more than tiles' padding from some 45 MB on with 9 to 16 rows
 // (16 rows of 5120 x 5120, 52 MB: 19.4 us, by tiles 16.4; 12 rows, 39 MB: 17.8 and 16.9) and 100 MB on with
 // 5 to 8 (8 of 5120 x 20480, 105 MB: 45.5 and 44.9; 5 of 20480 x 5120, 131 MB: 51 and 44; 8 of 5120 x 5120,
-// 52 MB: 15.5 and 16.0).
+// 52 MB: 15.5 and 16.0). A long K alone is too much for one workgroup too (some 26 GB/s of W each).
 bool tiles_for_few(const LinearGeo& g) {
     const int64_t rows = g.run.rows;
     if (rows <= 4) return false;
+    if (g.K >= (rows <= 8 ? 22000 : 11000)) return true;
     const double wgs = double(g.N) / (rows <= 8 && g.N < 16384 ? 8 : 16);
     return wgs * double(rows) * double(g.K) * 2 >= (rows <= 8 ? 100e6 : 45e6);
 }
