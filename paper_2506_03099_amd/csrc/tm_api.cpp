@@ -1727,14 +1727,14 @@ struct GemmPlan {
     size_t part_bytes() const { return size_t(groups * shares) * 2 * size_t(tile) * size_t(tile) * 4; }
 };
 
-// What a round of `wgs` workgroups of `stages` stages each takes, in us. A stage of a 256 tile takes 0.97 us with few
-// workgroups at work and 1.4 with one on each CU; one of a 128 tile 0.43 and 0.51, 0.72 once
+// What a round of `wgs` workgroups of `stages` stages each takes, in us. A stage of a 256 tile takes 0.94 us with few
+// workgroups at work and 1.36 with one on each CU; one of a 128 tile 0.43 and 0.51, 0.72 once
 // some CUs have two, and 0.94 when all have. (From
-// 50 sizes from 130 to 9000 rows and 64 to 20480 wide, each with either tile, split and not: the choice by
-// these costs is 0.8% behind the best of the four.)
+// 63 sizes from 15 to 32760 rows and 64 to 20480 wide, each with either tile, split and not: the choice by
+// these costs is 1% behind the best of the four in the mean.)
 double round_us(int tile, double wgs, double stages) {
     const double f = wgs / tmk::kCUs;
-    return tile == 256 ? stages * (0.97 + 0.43 * f) + 8 : stages * (f <= 1 ? 0.43 + 0.08 * f : 0.72 + 0.22 * (f - 1)) + 4;
+    return tile == 256 ? stages * (0.94 + 0.42 * f) + 11 : stages * (f <= 1 ? 0.43 + 0.08 * f : 0.72 + 0.22 * (f - 1)) + 4;
 }
 
 GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool may_split) {
