@@ -1,8 +1,19 @@
 // The norms before and after a branch of a block, with gate, residual and modulation, for gfx950.
 //
+// The student keeps the blocks of its WAN2.1 teacher (TalkingMachines, Sec. 4.1): a branch's output is gated by frame
+// into the residual stream, which is normalised and modulated by frame for the next branch.
 //     z = post(y) post_weight,  r = x + gate z,  h = (pre(r) pre_weight + pre_bias) (1 + scale) + shift
-// and the gradients of that.
+// with layer(v) = (v - mean) / sqrt(var + eps), rms(v) = v / sqrt(mean of squares + eps). Backward, with n = pre(r), v =
+// post(y), t = dh (1 + scale) pre_weight, u = dx gate post_weight:
+//     dx = dr + (t - mean t - n mean(t n)) / sigma_r,  dy = (u - mean u - v mean(u v)) / sigma_y
+// (the means of t and u for a layer norm only), and from the sums over a group's rows of dh, dh n and dx v the gradients of
+// all vectors.
 //
+// Bound by HBM: each element is read and written once, a row stays in registers between its sums, of which a layer norm
+// takes two, one after the other (the variance from centred values). Measured: 4680 x 5120 into an fp32
+// stream (287 MB) 58 us; 12150 x 1024 in bf16, both norms, (99 MB) 18 us; the backward of 32760 x 5120 (3.0 GB) 624 us,
+// 4.9 TB/s in the kernel (a device copy of that size: 4.8); one token 3 us.
+
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

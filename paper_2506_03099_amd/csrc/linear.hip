@@ -1,8 +1,17 @@
 // Linear layers with bias, activation, gate and residual for gfx950, forward and backward.
 //
+// The student keeps the blocks of its WAN2.1 teacher (TalkingMachines, Sec. 4.1): projections around the attention and
+// a feed-forward layer, gated by frame into the residual stream.
 //     z = x W^T + bias,  o = residual + gate * act(z);
 //     dz = dout gate act'(z),  dx = dz W,  dW = dz^T x,  dbias = sums of dz,  dgate = sums of dout act(z).
+// The three products differ in what lies side by side in memory: k of both operands (x W^T), k of the first (dz W), of
+// neither (dz^T x). One kernel takes all, with transposing LDS reads where k is not side by side.
 //
+// Bound by the matrix cores from a few hundred rows on, by HBM (the bytes of W) below. Measured, with their
+// epilogues: 4680 x 5120 x 20480, GELU, 781 us (1257 TFLOP/s, matrix cores busy for 76% of the cycles at 1.53 GHz,
+// where power holds the clock); 4680 x 20480 x 5120, gated into an fp32 stream, 777 us (82%); dx and dW of 32760 x 5120 x
+// 5120 1262 and 1272 us (1350 TFLOP/s); 130 rows of 5120 x 5120 24 us; one row of 5120 x 20480 32 us (6.6 TB/s).
+
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -111,6 +120,13 @@ __device__ __forceinline__ void by_kind(const LinearEpilogue& ep, const Body& bo
 // ---------------------------------------------------------------------------
 // The matrix product
 // ---------------------------------------------------------------------------
+// Why these tiles: a wave's 128 x 128 sums (16 MFMAs of 32x32x16 a k-step from 8 operands) take its SIMD's 256
+// accumulation registers and ask 64 KB of LDS reads and 32 KB of writes per 32 k of a workgroup, 3/4 of what LDS moves
+// in the MFMAs' time; 8 waves of 128 x 64 would ask 96 + 32 KB. So one wave a SIMD hides everything
+// itself: operands are read a k-step ahead, in an order that is fixed (sched_barrier), loads a stage and more.
+// Stages are 64 k deep since a row's 128 bytes are a line: at 32 k (64 bytes) the loads of 4680 x 5120 x
+// 20480 kept the L2 busy for longer than the MFMAs (951 us, at 64 831). Small products take 128 x 128 tiles, two
+// workgroups a CU, which LDS reads bound (768 cycles a stage for 512 of MFMAs) but which fill the CUs.
 constexpr int kSlots = 5;  // operands' parts of stages in LDS: two that are read, the next two and one more arriving
 
 // One operand's part of a stage, T rows (its m or n) by 64 k, 128 * T bytes, in LDS.
@@ -513,7 +529,7 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const Gemm
 }
 
 // The split tiles' sums of products from their parts, in the order of k, and the rest of the way. A thread
-// takes 8 columns of a row.
+// takes 8 columns of a row. Bound by the parts' bytes (124 tiles of 256 in 2 parts, 65 MB, with gate and residual: 23 us).
 template <int BT>
 __global__ __launch_bounds__(256) void gemm_merge_kernel(const GemmArgs a) {
     constexpr int LPR = BT / 8, ROWS = 256 / LPR, PER = BT / ROWS;
@@ -571,7 +587,8 @@ hipError_t launch_tiles(const GemmArgs& a, hipStream_t s) {
 // a piece, the others nothing of use. (One or a few rows leave columns over, and 16 columns a workgroup
 // leave CUs idle: 5120 columns are 320 workgroups for 256 CUs.) A lane brings 32 neighbouring bytes of its row of W,
 // the k of two MFMAs, so that 4 lanes read a whole line; which k an operand's element is does not matter as
-// long as x's are the same. Rows that do not exist repeat the last one.
+// long as x's are the same. Rows that do not exist repeat the last one. Bound by HBM up to 4 rows (one row: 5.2 to 6.6
+// TB/s from 5120 x 5120 to 5120 x 20480), by each workgroup's reads of x above.
 template <int NW, int C>
 __global__ __launch_bounds__(NW * 64) void few_rows_kernel(const FewRowsArgs a) {
     constexpr int CO = 16 / C;  // columns, and the most rows
@@ -662,7 +679,8 @@ __device__ __forceinline__ void activate_both(float z, int act, float& value, fl
     slope = rest > 0.f ? s * fmaf(z * rest, du, 1.f) : s;
 }
 
-// One part of the rows per workgroup and 256 columns: 32 lanes of 8 columns, 8 rows at a time.
+// One part of the rows per workgroup and 256 columns: 32 lanes of 8 columns, 8 rows at a time. Bound by HBM: 32760 x 5120
+// from fp32 1.34 GB in 265 us (5.1 TB/s); 5376 x 4096 with GELU 132 MB in 25 us, close to its arithmetic (17 us).
 __global__ __launch_bounds__(256) void linear_dz_kernel(const LinearDzArgs a) {
     __shared__ float sums[8][256];
     int32_t b, t0, t1;
@@ -732,7 +750,8 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(const LinearDzArgs a) {
 }
 
 // dx of R rows: 512 columns per wave, the 4 waves of a workgroup and the shares of the grid deal out N; the
-// gradients are the same in every lane. In fp32: with so few rows nothing would average the roundings of dz.
+// gradients are the same in every lane. In fp32: with so few rows nothing would average the roundings of dz. One row
+// of 5120 x 5120, dx and dW: 27 us for 105 MB.
 template <int R>
 __global__ __launch_bounds__(256) void few_rows_dx_kernel(const FewRowsBwdArgs a) {
     __shared__ float sums[3][64][9];
