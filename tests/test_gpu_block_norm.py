@@ -350,3 +350,21 @@ def test_more_rows_than_one_launch_takes(tm):
     assert torch.equal(h[:, :1000], want)
     at = (2 ** 25 // 1000) * 1000  # a multiple of the period, below the second launch's first row
     assert torch.equal(h[:, at:at + 1000], want) and torch.equal(h[:, n - 500:], h[:, n - 500 - at:n - at])
+
+
+def test_offsets_past_32_bits(tm):
+    """More than 2^31 elements: the last rows, forward and backward."""
+    n, E = 135000, 16000
+    x = torch.randn((1000, E), device="cuda").to(torch.bfloat16).repeat(n // 1000, 1).view(1, n, E)
+    d = tm.make_block_norm_desc(1, E, "rms", "none", "bf16", "bf16")
+    w = 1 + 0.2 * torch.randn((E,), device="cuda")
+    _, h = tm.tm_block_norm_fwd(d, x, pre_weight=w)
+    _, want = tm.tm_block_norm_fwd(d, x[:, :1000].contiguous(), pre_weight=w)
+    assert torch.equal(h[:, :1000], want) and torch.equal(h[:, -1000:], want)
+    got = tm.tm_block_norm_bwd(d, x, h, pre_weight=w)
+    part = tm.tm_block_norm_bwd(d, x[:, :1000].contiguous(), want, pre_weight=w)
+    assert torch.equal(got.dx[:, -1000:], part.dx)
+    # 135 times the period's sum, each within its terms' roundings
+    n64 = normed(x[0, :1000].double(), "rms", EPS)
+    t = want[0].double() * n64
+    held(got.dpre_weight, 135 * t.sum(0), (512 + n + 64) * U * 135 * t.abs().sum(0), "dpre_weight")

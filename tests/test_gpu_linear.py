@@ -327,3 +327,27 @@ def test_large_tiles(tm, n, K, N, act, out, parts):
     if pre is not None:
         held(pre, z64, zb, "pre")
     near(o, o64, "o")
+
+
+def test_offsets_past_32_bits(tm):
+    """More than 2^31 elements of output and of dout: the last rows, and sums that reach over all of them."""
+    n, K, N = 70000, 64, 32768
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn((1, n, K), generator=g, device="cuda").to(torch.bfloat16)
+    w = (torch.randn((N, K), generator=g, device="cuda") / 8).to(torch.bfloat16)
+    b = torch.randn((N,), generator=g, device="cuda")
+    d = tm.make_linear_desc(1, K, N, "silu", "bf16")
+    o = tm.tm_linear_fwd(d, x, w, b)
+    rows = torch.tensor([0, 1, 65535, 65536, n - 300, n - 1], device="cuda")
+    z = x[0, rows].double() @ w.double().t() + b.double()
+    S = x[0, rows].double().abs() @ w.double().abs().t() + b.double().abs()
+    held(o[0, rows], activate(z, "silu"), 1.13 * 2 * (K + 8) * U * S + 32 * U * z.abs(), "o")
+    # dout = o: dx of these rows, and dweight's columns of ones times a known sum
+    d = tm.make_linear_desc(1, K, N, "none", "bf16")
+    got = tm.tm_linear_bwd(d, x, w, o)
+    want = o[0, rows].double() @ w.double()
+    held(got.dx[0, rows], want, 2 * (N + 8) * U * (o[0, rows].double().abs() @ w.double().abs()), "dx")
+    cols = torch.tensor([0, 1, N - 1], device="cuda")
+    oc = o[0][:, cols].double()
+    held(got.dweight[cols], oc.t() @ x[0].double(), 2 * (n + 8) * U * (oc.abs().t() @ x[0].double().abs()), "dweight")
+    held(got.dbias[cols], oc.sum(0), (n + 8) * U * oc.abs().sum(0), "dbias")
