@@ -125,15 +125,15 @@ __device__ __forceinline__ void by_kind(const LinearEpilogue& ep, const Body& bo
 // in the MFMAs' time; 8 waves of 128 x 64 would ask 96 + 32 KB. So one wave a SIMD hides everything
 // itself: operands are read a k-step ahead, in an order that is fixed (sched_barrier), loads a stage and more.
 // Stages are 64 k deep since a row's 128 bytes are a line: at 32 k (64 bytes) the loads of 4680 x 5120 x
-// 20480 kept the L2 busy for longer than the MFMAs (951 us, at 64 831). Small products take 128 x 128 tiles, two
-// workgroups a CU, which LDS reads bound (768 cycles a stage for 512 of MFMAs) but which fill the CUs.
-constexpr int kSlots = 5;  // operands' parts of stages in LDS: two that are read, the next two and one more arriving
+// 20480 kept the L2 busy for longer than the MFMAs (951 us, at 64 831). Smaller products take tiles of 128 (LDS
+// reads bound them: 768 cycles a stage for 512 of MFMAs) or 64 (the reads' latency: 0.45 us a stage), which fill the CUs
+// (130 rows, 5120 x 5120: 22 us; 1000 x 1000 x 1000: 8.7 us in tiles of 64, 12.3 of 128).
 
 // One operand's part of a stage, T rows (its m or n) by 64 k, 128 * T bytes, in LDS.
 // k side by side: rows of 128 bytes, 16-byte chunk c of row r at c ^ (r >> 1) % 8, so that the 16 rows that
 // one cycle of a read covers lie in 16 different bank groups. A lane's operand of the MFMA, 8 k, is a chunk.
-// TRANS: rows of one k and T elements, chunk c of row k at c ^ 4 (k % 4), so that the 4 rows by 64 bytes
-// of a cycle of the transposing read lie apart. A lane's operand is two of these reads, 4 k each.
+// TRANS: rows of one k and T elements, chunk c of row k at c ^ 4 (k % 4) (T = 64: c ^ 4 (k / 2 % 2)), so that the 4 rows
+// by 64 bytes of a cycle of the transposing read lie apart. A lane's operand is two of these reads, 4 k each.
 template <int T, bool TRANS>
 struct Tile {
     static constexpr int kBytes = 2 * kGemmDepth * T;
@@ -141,7 +141,9 @@ struct Tile {
     static constexpr int kChunks = TRANS ? T / 8 : kGemmDepth / 8;  // of a row
     uint32_t voff[kLoads];
 
-    static __device__ __forceinline__ int swizzle(int row) { return TRANS ? 4 * (row & 3) : (row >> 1) & 7; }
+    static __device__ __forceinline__ int swizzle(int row) {
+        return !TRANS ? (row >> 1) & 7 : T == 64 ? 4 * ((row >> 1) & 1) : 4 * (row & 3);
+    }
 
     // Byte offsets in memory, from the stage's first element, of the chunks that this lane brings;
     // `rows`: of m (n) that exist from the tile's first one on. Past them the last ones come again.
@@ -225,15 +227,18 @@ __device__ __forceinline__ void tile_at(const GemmArgs& a, int t, int tile, int&
     n0 = in / high * tile;
 }
 
-// FULL: with all of the epilogue; else the sums are the output.
-template <int BT, bool AT, bool BTR, bool FULL>
-__global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const GemmArgs a) {
+// FULL: with all of the epilogue; else the sums are the output. Loads run AHEAD stages ahead of the MFMAs: 2, so
+// that LDS holds 1 workgroup of tiles of 256, 2 of 128 or 4 of 64, or 4, since a smaller tile's workgroup that has a
+// CU for itself waits for loads otherwise (512 rows, 5120 x 5120, 160 tiles of 128: 40.8 us with 2, 35.2 with 4).
+template <int BT, bool AT, bool BTR, bool FULL, int AHEAD>
+__global__ __launch_bounds__(256, gemm_per_cu(BT, AHEAD)) void gemm_kernel(const GemmArgs a) {
     constexpr int WT = BT / 2;      // a wave's rows and columns
     constexpr int F = WT / 32;      // its 32-wide blocks, either way
     using TA = Tile<BT, AT>;
     using TB = Tile<BT, BTR>;
     constexpr int SLOT = TA::kBytes;
     constexpr int LOADS = TA::kLoads, HALF = LOADS / 2;
+    constexpr int kSlots = 2 * AHEAD + 1;  // operands' parts of stages in LDS
     static_assert(TB::kBytes == SLOT && TB::kLoads == LOADS, "both operands' parts take one slot");
     __shared__ __attribute__((aligned(1024))) unsigned char smem[kSlots * SLOT];
     lds_u8* const L = (lds_u8*)smem;
@@ -306,29 +311,39 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const Gemm
         const uint32_t x = slot + by * SLOT;
         return x >= kSlots * SLOT ? x - kSlots * SLOT : x;
     };
-    // The first loads of a tile: A and B of its first two stages.
+    // The first loads of a tile: A and B of its first stages.
     auto begin = [&](const Work& w) __attribute__((always_inline)) {
         const int lane = fresh_thread_index() & 63;  // (what follows from it is not kept from tile to tile)
         ta.init(wave, lane, a.lda, a.M - w.m0);
         tb.init(wave, lane, a.ldb, a.N - w.n0);
-        const void *pa = base_a(w, w.s0), *pb = base_b(w, w.s0);
-        if (rest != 0 && w.s0 == 0) {
-            ta.load_rest(pa, L, lds_base, wave, lane, rest);
-            tb.load_rest(pb, L + SLOT, lds_base + SLOT, wave, lane, rest);
-        } else {
 #pragma unroll
-            for (int j = 0; j < LOADS; ++j) issue(true, pa, 0, j);
+        for (int p = 0; p < AHEAD; ++p) {
+            if (p >= w.s1 - w.s0) break;
+            const void *pa = base_a(w, w.s0 + p), *pb = base_b(w, w.s0 + p);
+            if (p == 0 && rest != 0 && w.s0 == 0) {
+                ta.load_rest(pa, L, lds_base, wave, lane, rest);
+                tb.load_rest(pb, L + SLOT, lds_base + SLOT, wave, lane, rest);
+                continue;
+            }
 #pragma unroll
-            for (int j = 0; j < LOADS; ++j) issue(false, pb, SLOT, j);
+            for (int j = 0; j < LOADS; ++j) issue(true, pa, 2 * p * SLOT, j);
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) issue(false, pb, (2 * p + 1) * SLOT, j);
         }
-        if (w.s1 - w.s0 > 1) {
-            pa = base_a(w, w.s0 + 1);
-            pb = base_b(w, w.s0 + 1);
-#pragma unroll
-            for (int j = 0; j < LOADS; ++j) issue(true, pa, 2 * SLOT, j);
-#pragma unroll
-            for (int j = 0; j < LOADS; ++j) issue(false, pb, 3 * SLOT, j);
-        }
+    };
+    // Waits until all but the last `left` stages' loads (and MORE later operations) are through, and for the
+    // other waves.
+    auto wait_but = [&](auto more, int left) __attribute__((always_inline)) {
+        constexpr int MORE = decltype(more)::value;
+        static_assert(2 * (AHEAD - 1) * LOADS + MORE < 64 && AHEAD <= 4, "s_waitcnt counts to 63");
+        if (AHEAD > 3 && left >= 3)
+            wait_and_meet<(AHEAD > 3 ? 6 : 0) * LOADS + MORE>();
+        else if (AHEAD > 2 && left == 2)
+            wait_and_meet<(AHEAD > 2 ? 4 : 0) * LOADS + MORE>();
+        else if (left >= 1)
+            wait_and_meet<2 * LOADS + MORE>();
+        else
+            wait_and_meet<MORE>();
     };
 
     f32x16_t acc[F][F];
@@ -345,16 +360,16 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const Gemm
     // Stage s, A in the slot at `at`, B in the one behind it: the MFMAs of its four k-steps, under those of
     // each the reads of the next one, and loads. Near the end of the third one, when the
     // wave's last reads of the stage are through, the wait for the next stage; its slots are free behind it.
-    // Loads: A of s + 2 under the first two k-steps, B of s + 2 under the last, all at once, since it has the
-    // shorter time, little less than a stage, until it is waited for.
+    // Loads: A of s + AHEAD under the first two k-steps, B under the last, all at once, since it has the shorter
+    // time until it is waited for.
     auto stage = [&](auto have1, auto have2, const Work& w, int s, uint32_t at) __attribute__((always_inline)) {
         constexpr bool ONE = decltype(have1)::value, TWO = decltype(have2)::value;
         const void *pa2 = nullptr, *pb2 = nullptr;
         if (TWO) {
-            pa2 = base_a(w, s + 2);
-            pb2 = base_b(w, s + 2);
+            pa2 = base_a(w, s + AHEAD);
+            pb2 = base_b(w, s + AHEAD);
         }
-        const uint32_t a1 = ahead(at, 2), b1 = ahead(at, 3), a2 = ahead(at, 4);
+        const uint32_t a1 = ahead(at, 2), b1 = ahead(at, 3), a2 = ahead(at, 2 * AHEAD);
         constexpr int M = F * F;
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
@@ -380,6 +395,11 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const Gemm
                         if (kk == 3 && m % 2 == 1) load(m / 2);
                         if (kk < 2 && m % 4 == 1) load(m / 4);
                     }
+                } else if (F == 1) {
+                    next_read(pa, pbk, kk, 0);
+                    next_read(pa, pbk, kk, 1);
+                    load(0);
+                    if (kk == 3) load(1);
                 } else if (kk == 2) {
                     if (m < F) {
                         read(pa, pbk, kk + 1, 2 * m);
@@ -390,11 +410,11 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const Gemm
                     if (kk == 3) load(m);
                     if (kk < 2 && m % 2 == 1) load(m / 2);
                 }
-                if (kk == 2 && m == (F == 4 ? 13 : 2)) {
+                if (kk == 2 && m == (F == 4 ? 13 : F == 2 ? 2 : 0)) {
                     if (TWO)
-                        wait_and_meet<LOADS>();
+                        wait_and_meet<(2 * AHEAD - 3) * LOADS>();
                     else
-                        wait_and_meet<0>();
+                        wait_but(std::integral_constant<int, 0>{}, w.s1 - 2 - s);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -503,19 +523,16 @@ __global__ __launch_bounds__(256, BT == 256 ? 1 : 2) void gemm_kernel(const Gemm
 #pragma unroll
                 for (int e = 0; e < 8; ++e) acc[i][j / 2][8 * (j % 2) + e] = bias[e];
         }
-        if (w.s1 - w.s0 > 1) {
-            if (stores)
-                wait_and_meet<2 * LOADS + STORES>();
-            else
-                wait_and_meet<2 * LOADS>();
-        } else {
-            wait_and_meet<0>();
-        }
+        const int later = min(AHEAD, w.s1 - w.s0) - 1;
+        if (stores)
+            wait_but(std::integral_constant<int, STORES>{}, later);
+        else
+            wait_but(std::integral_constant<int, 0>{}, later);
 #pragma unroll
         for (int f = 0; f < 2 * F; ++f) read(L, L + SLOT, 0, f);
         uint32_t at = 0;
         int s = w.s0;
-        for (; s + 2 < w.s1; ++s, at = ahead(at, 2)) stage(std::true_type{}, std::true_type{}, w, s, at);
+        for (; s + AHEAD < w.s1; ++s, at = ahead(at, 2)) stage(std::true_type{}, std::true_type{}, w, s, at);
         for (; s + 1 < w.s1; ++s, at = ahead(at, 2)) stage(std::true_type{}, std::false_type{}, w, s, at);
         stage(std::false_type{}, std::false_type{}, w, s, at);
         // (since the last stage's wait no wave reads LDS)
@@ -571,8 +588,12 @@ template <int BT, bool AT, bool BTR>
 hipError_t launch_tiles(const GemmArgs& a, hipStream_t s) {
     const int rest = a.tiles_m * a.tiles_n - a.whole;
     // as many workgroups as the chip holds at a time; each takes one tile after the other
-    const int most = BT == 256 ? kCUs : 2 * kCUs;
-    hipError_t e = launch_with(gemm_kernel<BT, AT, BTR, !BTR>, dim3(std::min(most, std::max(a.whole, a.groups * a.shares))), 256, s, a);
+    const int wgs = std::min(kCUs * gemm_per_cu(BT), std::max(a.whole, a.groups * a.shares));
+    hipError_t e = hipSuccess;
+    if (BT < 256 && wgs <= kCUs)
+        e = launch_with(gemm_kernel<BT, AT, BTR, !BTR, BT < 256 ? 4 : 2>, dim3(wgs), 256, s, a);
+    else
+        e = launch_with(gemm_kernel<BT, AT, BTR, !BTR, 2>, dim3(wgs), 256, s, a);
     if (e != hipSuccess || rest == 0) return e;
     constexpr int PER = BT / (256 / (BT / 8));
     return launch_with(gemm_merge_kernel<BT>, dim3(rest * PER), 256, s, a);
@@ -876,10 +897,13 @@ hipError_t launch_gemm(const GemmArgs& a, int tile, bool a_trans, bool b_trans, 
     if (tile == T_ && a_trans == A_ && b_trans == B_) return launch_tiles<T_, A_, B_>(a, s);
     TM_GEMM_CASE(256, false, false)
     TM_GEMM_CASE(128, false, false)
+    TM_GEMM_CASE(64, false, false)
     TM_GEMM_CASE(256, false, true)
     TM_GEMM_CASE(128, false, true)
+    TM_GEMM_CASE(64, false, true)
     TM_GEMM_CASE(256, true, true)
     TM_GEMM_CASE(128, true, true)
+    TM_GEMM_CASE(64, true, true)
 #undef TM_GEMM_CASE
     return hipErrorInvalidValue;
 }

@@ -1728,35 +1728,41 @@ struct GemmPlan {
 };
 
 // What a round of `wgs` workgroups of `stages` stages each takes, in us. A stage of a 256 tile takes 0.94 us with few
-// workgroups at work and 1.36 with one on each CU; one of a 128 tile 0.43 and 0.51, 0.72 once
-// some CUs have two, and 0.94 when all have. (From
-// 63 sizes from 15 to 32760 rows and 64 to 20480 wide, each with either tile, split and not: the choice by
-// these costs is 1% behind the best of the four in the mean.)
-double round_us(int tile, double wgs, double stages) {
+// workgroups at work and 1.36 with one on each CU; one of a 128 tile 0.34 and 0.44, 0.72 once some CUs have two, and
+// 0.94 when all have; one of a 64 tile 0.45, 0.51 with two on each CU and 0.81 with four. Rows that do not begin on
+// cache lines cost the smaller tiles up to 45% more when many workgroups read them.
+double round_us(int tile, double wgs, double stages, bool on_lines) {
     const double f = wgs / tmk::kCUs;
-    return tile == 256 ? stages * (0.94 + 0.42 * f) + 11 : stages * (f <= 1 ? 0.43 + 0.08 * f : 0.72 + 0.22 * (f - 1)) + 4;
+    if (tile == 256) return stages * (0.94 + 0.42 * f) + 11;
+    if (tile == 128) {
+        if (f > 1) return stages * (0.72 + 0.22 * (f - 1)) + 4;
+        return stages * (0.34 + 0.1 * f) * (on_lines ? 1 : 1 + 0.9 * std::min(f, 0.5)) + 5;
+    }
+    if (!on_lines && f > 1) stages *= 1 + 0.2 * std::min(f - 1, 1.5);
+    return stages * (f <= 2 ? 0.45 + 0.03 * f : 0.51 + 0.15 * (f - 2)) + 2.8;
 }
 
 GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool may_split) {
     GemmPlan best{};
     double best_us = 0;
-    for (const int tile : {256, 128}) {
+    for (const int tile : {256, 128, 64}) {
         GemmPlan p{};
         p.tile = tile;
         p.tiles_m = ceil_div(M, tile);
         p.tiles_n = ceil_div(N, tile);
         p.stages = ceil_div(K, tmk::kGemmDepth);
         const int64_t tiles = p.tiles_m * p.tiles_n;
-        const int64_t at_once = tile == 256 ? tmk::kCUs : 2 * tmk::kCUs;
+        const int64_t at_once = tmk::kCUs * tmk::gemm_per_cu(tile);
         const int64_t rest = tiles % at_once;
-        const double whole_us = double(tiles / at_once) * round_us(tile, double(at_once), double(p.stages));
+        auto round = [&](int64_t wgs, int64_t stages) { return round_us(tile, double(wgs), double(stages), K % 64 == 0); };
+        const double whole_us = double(tiles / at_once) * round(at_once, p.stages);
         auto take = [&](double us) {
             if (best.tile != 0 && us >= best_us) return;
             best = p;
             best_us = us;
         };
         p.whole = tiles;
-        take(whole_us + (rest ? round_us(tile, double(rest), double(p.stages)) : 0));
+        take(whole_us + (rest ? round(rest, p.stages) : 0));
         if (!may_split || rest == 0 || p.stages < 2) continue;
         // The tiles of the last round shared out: `a` of them to each `shares` workgroups, in rest / a groups. The
         // parts are written and read once, and joined by another launch.
@@ -1768,7 +1774,7 @@ GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool may_split) {
             const int64_t most = std::min(at_once / p.groups, a * p.stages);
             for (int64_t shares = most; shares > a && shares >= (a == 1 ? most / 8 : most - 1); shares -= a == 1 ? ceil_div(shares, 8) : 1) {
                 p.shares = shares;
-                take(whole_us + round_us(tile, double(p.groups * shares), double(ceil_div(a * p.stages, shares))) + 5 +
+                take(whole_us + round(p.groups * shares, ceil_div(a * p.stages, shares)) + 5 +
                      double(p.groups * (shares + a - 1)) * part_us);
             }
         }

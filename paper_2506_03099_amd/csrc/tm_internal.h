@@ -367,6 +367,8 @@ struct GemmArgs {
     LinearEpilogue ep;
 };
 constexpr int kGemmDepth = 64;
+// Workgroups of a CU at a time: LDS holds 2 * ahead + 1 parts of 128 * tile bytes for each.
+constexpr int gemm_per_cu(int tile, int ahead = 2) { return 160 * 1024 / ((2 * ahead + 1) * 128 * tile); }
 hipError_t launch_gemm(const GemmArgs& a, int tile, bool a_trans, bool b_trans, hipStream_t s);
 
 // Token rows in parts that lie in one group each, for sums over a group's rows: group j of those that the

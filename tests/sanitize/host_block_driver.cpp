@@ -222,7 +222,7 @@ void split_checks() {
                 ++split;
                 const int64_t per_group = rest / p.groups, units = per_group * p.stages, W = p.shares;
                 EXPECT(per_group * p.groups == rest && W >= per_group && W <= units);
-                EXPECT(p.groups * W <= (p.tile == 256 ? 256 : 512));
+                EXPECT(p.groups * W <= 256 * tmk::gemm_per_cu(p.tile));
                 for (int64_t w = 0; w < W; ++w) {
                     const int64_t u0 = units * w / W, u1 = units * (w + 1) / W;
                     EXPECT(u0 < u1);

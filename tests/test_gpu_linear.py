@@ -116,6 +116,20 @@ def test_forward_and_backward(tm, B, n, K, N, act, out, parts, groups, group, fi
         assert got.dgate is None
 
 
+# Tiles of 64, 128 and 256: of one to six stages (the loads run two or four ahead), the first one whole or what K
+# leaves over 64; workgroups that take one tile or several; tiles shared out, in shares of one stage and of parts
+# of two tiles.
+STAGES = [(140, 64, 16), (18, 128, 96), (82, 192, 24), (25, 256, 64), (27, 448, 24), (35, 72, 32), (32, 136, 16), (24, 232, 16),
+          (194, 72, 4336), (1676, 64, 4632), (2374, 128, 3376), (2382, 144, 3336), (8257, 208, 904), (174, 832, 16),
+          (66, 8968, 32), (18, 8784, 2688), (7905, 328, 472), (76, 9024, 2056), (136, 5408, 3392), (1025, 136, 3952),
+          (2308, 192, 3528), (3084, 256, 2720), (2482, 392, 4016)]
+
+
+@pytest.mark.parametrize("n,K,N", STAGES)
+def test_stages_rounds_and_shares(tm, n, K, N):
+    test_forward_and_backward(tm, 1, n, K, N, "gelu", "bf16", "bz", 1, 0, 5)
+
+
 def test_gradients_against_differences(tm):
     B, n, K, N, groups, group, first, act = 2, 7, 136, 72, 3, 4, 2, "gelu"
     p = make(B, n, K, N, "f32", "bgr", groups, 1)
@@ -147,7 +161,7 @@ def test_gradients_against_differences(tm):
 
 def test_few_rows_and_tiles_agree_and_in_place(tm):
     """The forms for few rows and for tiles on the same rows, with and without a workspace, in place."""
-    K, N = 1352, 776
+    K, N = 20008, 776  # long enough that tiles are split
     p = make(1, 40, K, N, "f32", "br", 1, 3)
     d = tm.make_linear_desc(1, K, N, "silu", "f32")
     whole = tm.tm_linear_fwd(d, p["x"], p["weight"], p["bias"], None, p["residual"])
