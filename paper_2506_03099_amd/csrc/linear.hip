@@ -865,16 +865,19 @@ __global__ __launch_bounds__(256) void few_rows_dw_kernel(const FewRowsBwdArgs a
     }
 }
 
-// x twice, one behind the other (n groups of 8).
+// x twice, one behind the other (n groups of 8), the second time for what dz's rounding left. Zeros stand there for
+// infinities and NaN, which dz's first part takes along alone: the parts' signs differ, or the second one is zero.
 __global__ __launch_bounds__(256) void twice_kernel(const TwiceArgs a) {
     const int64_t i = blockIdx.x * int64_t(256) + threadIdx.x;
     if (i >= a.n) return;
-    const f32x4_t v = static_cast<const f32x4_t*>(a.x)[i];
-    static_cast<f32x4_t*>(a.out)[i] = v;
-    static_cast<f32x4_t*>(a.out)[a.n + i] = v;
+    bf16x8_t v = static_cast<const bf16x8_t*>(a.x)[i];
+    static_cast<bf16x8_t*>(a.out)[i] = v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = __builtin_isfinite(static_cast<float>(v[e])) ? v[e] : static_cast<__bf16>(0.f);
+    static_cast<bf16x8_t*>(a.out)[a.n + i] = v;
 }
 
-// out = a + b, b behind a (n groups of 8).
+// out = a + b, b behind a (n groups of 8); a alone where it is no finite number (of an infinite weight, as above).
 __global__ __launch_bounds__(256) void halves_sum_kernel(const TwiceArgs a) {
     const int64_t i = (blockIdx.x * int64_t(256) + threadIdx.x) * 8;
     if (i >= a.n * 8) return;
@@ -882,7 +885,7 @@ __global__ __launch_bounds__(256) void halves_sum_kernel(const TwiceArgs a) {
     load8(static_cast<const float*>(a.x) + i, u);
     load8(static_cast<const float*>(a.x) + a.n * 8 + i, v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) u[e] += v[e];
+    for (int e = 0; e < 8; ++e) u[e] = __builtin_isfinite(u[e]) ? u[e] + v[e] : u[e];
     store8(static_cast<__bf16*>(a.out) + i, u);
 }
 

@@ -309,6 +309,25 @@ def test_infinite_gradients_stay_in_their_rows(tm, rows):
     assert bool((~got.dweight[5].isfinite()).all()) and not bool(got.dweight[5].isnan().any())
 
 
+@pytest.mark.parametrize("rows", [1, 3, 8, 16, 40])
+def test_infinite_inputs_of_the_backward(tm, rows):
+    """An infinity in weight makes its column of dx infinite, one in x its column of dweight, with the signs of dz,
+    whether dz goes into the products as one number or as two."""
+    K, N = 72, 136
+    p = make(1, rows, K, N, "f32", "", 1, 41)
+    p["weight"][7, 3] = float("inf")
+    p["x"][0, rows - 1, 9] = float("-inf")
+    d = tm.make_linear_desc(1, K, N, "none", "f32")
+    gen = torch.Generator(device="cuda").manual_seed(42)
+    dout = torch.randn((1, rows, N), generator=gen, device="cuda")
+    dout[0, :, 7] += 0.1 * torch.sign(dout[0, :, 7])
+    got = tm.tm_linear_bwd(d, p["x"], p["weight"], dout, dbias=False)
+    assert torch.equal(got.dx[0, :, 3].float(), torch.sign(dout[0, :, 7]) * float("inf"))
+    assert torch.equal(got.dweight[:, 9].float(), torch.sign(dout[0, rows - 1]) * float("-inf"))
+    columns = torch.arange(K, device="cuda")
+    assert bool(got.dx[..., columns != 3].isfinite().all()) and bool(got.dweight[:, columns != 9].isfinite().all())
+
+
 def test_gradients_without_what_they_do_not_need(tm):
     p = make(1, 40, 72, 200, "bf16", "", 1, 4)
     d = tm.make_linear_desc(1, 72, 200)
