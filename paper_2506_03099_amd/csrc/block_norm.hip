@@ -123,14 +123,17 @@ __device__ __forceinline__ void group_sum(float (&v)[N], lds_float* slots, int w
     for (int k = 0; k < N; ++k) v[k] = lane_value(row_sum(s[k]), 15);
 }
 
-// One row per workgroup, four neighbouring elements a lane, U times.
-template <typename S, typename A, int U>
-__global__ __launch_bounds__(1024) void block_norm_kernel(const BlockNormArgs a) {
+// One row per workgroup, four neighbouring elements a lane, U times. ROWS > 1: a row per wave, for rows so short that
+// starting a workgroup takes longer than its bytes (88311 rows of 128, bf16: 18.4 us, 22.2 with a workgroup each; of 256
+// fp32 to bf16 25.5 and 22.4, so these stay).
+template <typename S, typename A, int U, int ROWS>
+__global__ __launch_bounds__(ROWS > 1 ? ROWS * 64 : 1024) void block_norm_kernel(const BlockNormArgs a) {
     __shared__ float smem[4 * kMaxWaves];
     lds_float* const L = (lds_float*)smem;
-    const int T = blockDim.x, waves = T / 64, tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int row = a.row0 + blockIdx.x;
+    const int lane = threadIdx.x & 63, in_group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int T = ROWS > 1 ? 64 : blockDim.x, waves = T / 64, tid = ROWS > 1 ? lane : threadIdx.x;
+    const int wave = ROWS > 1 ? 0 : in_group, row = a.row0 + blockIdx.x * ROWS + (ROWS > 1 ? in_group : 0);
+    if (ROWS > 1 && row >= a.rows) return;
     if (waves > 1 && tid < 4 * kMaxWaves) L[tid] = 0.f;
     const int64_t base = static_cast<int64_t>(row) * a.E;
     const int64_t mod = a.tg.row(row) * a.E;
@@ -492,14 +495,14 @@ hipError_t launch_sums(const ColumnSums& a, hipStream_t s) {
 
 }  // namespace
 
-template <typename S, typename A, int U>
+template <typename S, typename A, int U, int ROWS>
 static hipError_t launch_rows(BlockNormArgs a, int threads, hipStream_t s) {
     // Thread numbers are 32 bits wide: very many rows take several launches.
-    const int most = static_cast<int>((int64_t(1) << 31) / threads);
+    const int64_t most = (int64_t(1) << 31) / threads;
     for (int64_t at = 0; at < a.rows; at += most) {
         a.row0 = static_cast<int32_t>(at);
-        const hipError_t e = launch_with(block_norm_kernel<S, A, U>, dim3(static_cast<unsigned>(std::min<int64_t>(most, a.rows - at))),
-                                         threads, s, a);
+        const int64_t groups = (std::min(most, a.rows - at) + ROWS - 1) / ROWS;
+        const hipError_t e = launch_with(block_norm_kernel<S, A, U, ROWS>, dim3(static_cast<unsigned>(groups)), threads * ROWS, s, a);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
@@ -508,15 +511,18 @@ static hipError_t launch_rows(BlockNormArgs a, int threads, hipStream_t s) {
 hipError_t launch_block_norm(const BlockNormArgs& a, bool stream_f32, bool act_f32, hipStream_t s) {
     int U, threads;
     block_norm_shape(a.E, false, &U, &threads);
-#define TM_NORM_CASE(U_)                                                                                             \
-    if (U == U_) {                                                                                                   \
+#define TM_NORM_CASE(U_, ROWS_)                                                                                      \
+    if (U == U_ && (ROWS_ == 1 || a.E <= 128)) {                                                                     \
         if (stream_f32)                                                                                              \
-            return act_f32 ? launch_rows<float, float, U_>(a, threads, s) : launch_rows<float, __bf16, U_>(a, threads, s); \
-        return act_f32 ? launch_rows<__bf16, float, U_>(a, threads, s) : launch_rows<__bf16, __bf16, U_>(a, threads, s);   \
+            return act_f32 ? launch_rows<float, float, U_, ROWS_>(a, threads, s)                                     \
+                           : launch_rows<float, __bf16, U_, ROWS_>(a, threads, s);                                   \
+        return act_f32 ? launch_rows<__bf16, float, U_, ROWS_>(a, threads, s)                                        \
+                       : launch_rows<__bf16, __bf16, U_, ROWS_>(a, threads, s);                                      \
     }
-    TM_NORM_CASE(1)
-    TM_NORM_CASE(2)
-    TM_NORM_CASE(5)
+    TM_NORM_CASE(1, 4)
+    TM_NORM_CASE(1, 1)
+    TM_NORM_CASE(2, 1)
+    TM_NORM_CASE(5, 1)
 #undef TM_NORM_CASE
     return hipErrorInvalidValue;
 }
@@ -540,20 +546,25 @@ hipError_t launch_block_norm_bwd(const BlockNormBwdArgs& a, bool stream_f32, boo
     return hipErrorInvalidValue;
 }
 
+// With so many parts to a sum.
+static hipError_t launch_for(int parts, const ColumnSums& a, hipStream_t s) {
+    if (parts <= 4) return launch_sums<64, 1>(a, s);
+    if (parts <= 64) return launch_sums<64, 4>(a, s);
+    return parts <= 512 ? launch_sums<64, 16>(a, s) : launch_sums<16, 64>(a, s);
+}
+
 hipError_t launch_column_sums(const ColumnSums& a, hipStream_t s) {
     ColumnSums t = a, g = a;
     t.by_parts = g.by_parts = FastDiv(a.parts.per_group);
     t.by_touched = g.by_touched = FastDiv(a.parts.touched);
-    // totals over many parts have a launch of their own, with more threads a column
-    if (a.n_total > 0 && (a.parts.count() > 512 || a.n_group == 0)) {
+    // totals over many parts have a launch of their own, with more threads a column, if the groups have few
+    if (a.n_total > 0 && (a.parts.count() > std::max(512, a.parts.per_group) || a.n_group == 0)) {
         t.n_group = 0;
         g.n_total = 0;
-        const hipError_t e = a.parts.count() <= 4 ? launch_sums<64, 1>(t, s) : launch_sums<32, 32>(t, s);
+        const hipError_t e = launch_for(a.parts.count(), t, s);
         if (e != hipSuccess || a.n_group == 0) return e;
     }
-    const int each = g.n_total > 0 ? a.parts.count() : a.parts.per_group;
-    if (each <= 4) return launch_sums<64, 1>(g, s);
-    return each <= 64 ? launch_sums<64, 4>(g, s) : launch_sums<64, 16>(g, s);
+    return launch_for(g.n_total > 0 ? a.parts.count() : a.parts.per_group, g, s);
 }
 
 }  // namespace tmk
