@@ -1674,14 +1674,15 @@ tm_status check_norm(const tm_block_norm_desc* d, int32_t n_tok, int64_t first_t
     g->act = d->dtype == TM_BF16 ? 2 : 4;
     g->stream = d->stream_dtype == TM_BF16 ? 2 : 4;
     // Workgroups for 10 waves a CU (20, which fit, were 3 to 10% slower), for 14 with a stream of half the bytes (10000
-    // rows of 4096: 120 us, 155 with 10; 20000 of 2048, fp32: 168 and 159) and 16 of rows up to 1024, whose lanes hold half as much
-    // (20000 of 1024, bf16 and fp32: 88 us, 115 with 10). No more than one to 8 rows, since the parts' sums are
-    // written and read too, unless CUs would have none.
+    // rows of 4096: 120 us, 155 with 10; 20000 of 2048, fp32: 168 and 159) and 16 of rows up to 1024, whose lanes hold
+    // half as much (20000 of 1024, bf16 and fp32: 88 us, 115 with 10). No more than one to 8 rows, since the parts' sums are
+    // written and read too, unless CUs would have fewer than two (3000 of 1024: 25.4 us, with one 28.1, with four 23.2,
+    // but 999 of 1000 in fp32 25.9, 26.9 and 28.7).
     int fours, lanes;
     tmk::block_norm_shape(d->width, true, &fours, &lanes);
     const int waves = lanes / 64, per_cu = fours == 1 ? 16 : d->stream_dtype == TM_BF16 ? 14 : 10;
     const int64_t fill = tmk::kCUs * std::max(1, (2 * per_cu + waves - 1) / (2 * waves));
-    g->parts = row_parts(g->run, std::max<int64_t>(tmk::kCUs, std::min(fill, g->run.rows / 8)), 2);
+    g->parts = row_parts(g->run, std::max<int64_t>(std::min<int64_t>(fill, 2 * tmk::kCUs), std::min(fill, g->run.rows / 8)), 2);
     g->part_bytes = size_t(g->parts.count()) * tmk::kNormSums * size_t(g->E) * 4;
     return TM_OK;
 }
