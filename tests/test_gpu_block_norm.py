@@ -99,7 +99,9 @@ def run_forward(tm, p, pre, post, act, stream, groups, group, first, **kw):
     return d, tm.tm_block_norm_fwd(d, p["x"], *[p[k] for k in NAMES[1:]], first, **kw)
 
 
-SHAPES = [(1, 1, 8, 1, 0, 0), (2, 9, 128, 3, 4, 1), (3, 5, 136, 1, 0, 0), (1, 67, 256, 1, 0, 3), (2, 6, 264, 1, 0, 0), (1, 1, 5120, 1, 0, 9), (2, 7, 64, 3, 4, 2), (3, 33, 1000, 5, 10, 7), (1, 130, 1024, 2, 100, 30),
+SHAPES = [(1, 1, 8, 1, 0, 0), (2, 9, 128, 3, 4, 1), (3, 5, 136, 1, 0, 0), (1, 67, 256, 1, 0, 3), (2, 6, 264, 1, 0, 0),
+          (2, 400, 264, 900, 1, 37), (2, 1500, 1032, 800, 2, 30), (1, 19000, 64, 600, 33, 100),
+          (1, 1, 5120, 1, 0, 9), (2, 7, 64, 3, 4, 2), (3, 33, 1000, 5, 10, 7), (1, 130, 1024, 2, 100, 30),
           (2, 5, 2056, 9, 1, 3), (1, 3, 16384, 1, 0, 0), (1, 9, 16376, 4, 3, 1), (2, 3, 8200, 1, 0, 0), (1, 300, 264, 1, 4000, 11)]
 SETS = [("layer", "none", "m"), ("layer", "none", "ygm"), ("rms", "rms", "ypw"), ("none", "layer", "ygp"),
         ("rms", "layer", "ygpwbm"), ("layer", "none", "wb"), ("layer", "rms", "yb"), ("none", "none", "yg")]
