@@ -387,9 +387,12 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(const BlockNormBwd
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            f32x4_t d;
+            f32x4_t d = dx[u];
+            // (without a norm dy is u, whatever y holds: a product of an infinite y with an `along` of 0 would be NaN)
+            if (a.post != kNormNone) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) d[e] = post_by * ((dx[u][e] - mean_u) - y_centred(u, e) * post_by * along);
+                for (int e = 0; e < 4; ++e) d[e] = post_by * ((dx[u][e] - mean_u) - y_centred(u, e) * post_by * along);
+            }
             if (in[u]) store4<A>(a.dy, base, col[u], d);
         }
     }

@@ -370,3 +370,28 @@ def test_offsets_past_32_bits(tm):
     n64 = normed(x[0, :1000].double(), "rms", EPS)
     t = want[0].double() * n64
     held(got.dpre_weight, 135 * t.sum(0), (512 + n + 64) * U * 135 * t.abs().sum(0), "dpre_weight")
+
+
+@pytest.mark.parametrize("pre", ["none", "layer"])
+@pytest.mark.parametrize("E", [136, 1032, 8200])
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+def test_gradient_of_an_output_that_no_norm_takes_does_not_read_it(tm, E, act, pre):
+    """Without a norm after the branch dy is gate * post_weight * dx: the same bits whatever y holds, an infinity or
+    a NaN too, and the sums over rows of the other columns stay as they are."""
+    B, n, groups, group = 1, 23, 3, 10
+    p = make(B, n, E, "f32", act, "ygp", groups, E)
+    d = tm.make_block_norm_desc(B, E, pre, "none", act, "f32", EPS, groups, group)
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    dr = torch.randn((B, n, E), generator=gen, device="cuda")
+    r, dh = (p["x"], torch.randn((B, n, E), generator=gen, device="cuda").to(DT[act])) if pre != "none" else (None, None)
+    want = tm.tm_block_norm_bwd(d, r, dh, dr, p["y"], p["gate"], p["post_weight"])
+    y = p["y"].clone()
+    cols = [3, 64, E - 1]
+    for row, col, v in zip((0, 11, n - 1), cols, ("inf", "-inf", "nan")):
+        y[0, row, col] = float(v)
+    got = tm.tm_block_norm_bwd(d, r, dh, dr, y, p["gate"], p["post_weight"])
+    assert bool(want.dy.isfinite().all()) and torch.equal(got.dy, want.dy) and torch.equal(got.dx, want.dx)
+    others = [c for c in range(E) if c not in cols]
+    assert torch.equal(got.dgate[..., others], want.dgate[..., others])
+    assert torch.equal(got.dpost_weight[others], want.dpost_weight[others])
+    assert not bool(got.dpost_weight[cols].isfinite().any())
