@@ -422,13 +422,13 @@ __global__ __launch_bounds__(COLS * LANES) void column_sums_kernel(const ColumnS
     if (which < a.n_total) {
         const TotalSum& o = a.total[which];
         const float* at = a.part + static_cast<int64_t>(o.v) * a.E + e;
-        const int n = a.parts.count();
+        const int n = a.parts.filled();
         if (in) {
             if (o.mod != nullptr) {
 #pragma unroll 8
                 for (int i = l; i < n; i += LANES) {
-                    const int g = a.by_parts.of(i), b = a.by_touched.of(g);
-                    const int64_t mod = static_cast<int64_t>(b) * a.parts.groups + a.parts.g0 + (g - b * a.parts.touched);
+                    const int b = a.by_each.of(i), j = a.by_parts.of(i - b * a.parts.each() + a.parts.before);
+                    const int64_t mod = static_cast<int64_t>(b) * a.parts.groups + a.parts.g0 + j;
                     s = fmaf(at[i * stride], o.mod[mod * a.E + e] + o.add, s);
                 }
             } else {
@@ -458,16 +458,17 @@ __global__ __launch_bounds__(COLS * LANES) void column_sums_kernel(const ColumnS
     }
     const int touched = (which - a.n_total) % rows;
     const GroupSum& o = a.group[(which - a.n_total) / rows];
-    const int row = touched / a.parts.touched * a.parts.groups + a.parts.g0 + touched % a.parts.touched;
+    const int b = touched / a.parts.touched, j = touched % a.parts.touched, row = b * a.parts.groups + a.parts.g0 + j;
     if (in) {
-        const float* at = a.part + static_cast<int64_t>(touched * a.parts.per_group) * stride + e;
-        const float* v = at + static_cast<int64_t>(o.v) * a.E;
+        int32_t i0, i1;
+        a.parts.of_group(b, j, i0, i1);
+        const float* v = a.part + static_cast<int64_t>(o.v) * a.E + e;
 #pragma unroll 8
-        for (int i = l; i < a.parts.per_group; i += LANES) s += v[i * stride];
+        for (int i = i0 + l; i < i1; i += LANES) s += v[i * stride];
         if (o.w >= 0) {
-            const float* w = at + static_cast<int64_t>(o.w) * a.E;
+            const float* w = a.part + static_cast<int64_t>(o.w) * a.E + e;
 #pragma unroll 8
-            for (int i = l; i < a.parts.per_group; i += LANES) s_w += w[i * stride];
+            for (int i = i0 + l; i < i1; i += LANES) s_w += w[i * stride];
         }
     }
     if (LANES > 1) {
@@ -501,10 +502,11 @@ __global__ __launch_bounds__(256) void group_sums_kernel(const ColumnSums a) {
     f32x4_t s = f32x4_t{}, s_w = f32x4_t{};
     if (j >= 0 && j < a.parts.touched) {
         const int64_t stride = static_cast<int64_t>(a.vectors) * a.E;
-        const int64_t at = static_cast<int64_t>((b * a.parts.touched + j) * a.parts.per_group) * stride;
-        for (int i = 0; i < a.parts.per_group; ++i) {
-            s += load4<float>(a.part, at + i * stride + static_cast<int64_t>(o.v) * a.E, col);
-            if (o.w >= 0) s_w += load4<float>(a.part, at + i * stride + static_cast<int64_t>(o.w) * a.E, col);
+        int32_t i0, i1;
+        a.parts.of_group(b, j, i0, i1);
+        for (int i = i0; i < i1; ++i) {
+            s += load4<float>(a.part, i * stride + static_cast<int64_t>(o.v) * a.E, col);
+            if (o.w >= 0) s_w += load4<float>(a.part, i * stride + static_cast<int64_t>(o.w) * a.E, col);
         }
         if (o.mul != nullptr) s *= load4<float>(o.mul, 0, col);
         if (o.w >= 0) {
@@ -561,7 +563,7 @@ hipError_t launch_block_norm(const BlockNormArgs& a, bool stream_f32, bool act_f
 hipError_t launch_block_norm_bwd(const BlockNormBwdArgs& a, bool stream_f32, bool act_f32, hipStream_t s) {
     int U, threads;
     block_norm_shape(a.E, true, &U, &threads);
-    const dim3 grid(a.parts.count());
+    const dim3 grid(a.parts.filled());
 #define TM_NORM_CASE(U_)                                                                                 \
     if (U == U_) {                                                                                       \
         if (stream_f32)                                                                                  \
@@ -590,20 +592,20 @@ static hipError_t launch_for(int parts, const ColumnSums& a, hipStream_t s) {
 hipError_t launch_column_sums(const ColumnSums& a, hipStream_t s) {
     ColumnSums t = a, g = a;
     t.by_parts = g.by_parts = FastDiv(a.parts.per_group);
-    t.by_touched = g.by_touched = FastDiv(a.parts.touched);
+    t.by_each = g.by_each = FastDiv(a.parts.each());
     // totals over many parts have a launch of their own, with more threads a column, if the groups have few
-    if (a.n_total > 0 && (a.parts.count() > std::max(512, a.parts.per_group) || a.n_group == 0)) {
+    if (a.n_total > 0 && (a.parts.filled() > std::max(512, a.parts.per_group) || a.n_group == 0)) {
         t.n_group = 0;
         g.n_total = 0;
-        const hipError_t e = launch_for(a.parts.count(), t, s);
+        const hipError_t e = launch_for(a.parts.filled(), t, s);
         if (e != hipSuccess || a.n_group == 0) return e;
     }
-    if (g.n_total == 0 && a.parts.per_group <= 4 && a.parts.count() > 512) {
+    if (g.n_total == 0 && a.parts.per_group <= 4 && a.parts.filled() > 512) {
         const int threads = std::min(256, (a.E / 4 + 63) / 64 * 64);
         const int64_t blocks = (a.E / 4 + threads - 1) / threads;
         return launch_with(group_sums_kernel, dim3(static_cast<unsigned>(blocks * a.n_group * a.parts.B * a.parts.groups)), threads, s, g);
     }
-    return launch_for(g.n_total > 0 ? a.parts.count() : a.parts.per_group, g, s);
+    return launch_for(g.n_total > 0 ? a.parts.filled() : a.parts.per_group, g, s);
 }
 
 }  // namespace tmk

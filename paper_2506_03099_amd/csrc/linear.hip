@@ -928,7 +928,7 @@ hipError_t launch_few_rows(const FewRowsArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_linear_dz(const LinearDzArgs& a, hipStream_t s) {
-    return launch_with(linear_dz_kernel, dim3(a.parts.count(), (a.N + 255) / 256), 256, s, a);
+    return launch_with(linear_dz_kernel, dim3(a.parts.filled(), (a.N + 255) / 256), 256, s, a);
 }
 
 template <int R>

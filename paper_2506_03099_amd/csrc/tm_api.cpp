@@ -1585,7 +1585,7 @@ public:
 // The rows of a call and the rows of its modulations.
 struct Run {
     int64_t B, n, rows, groups;
-    int64_t len, f0, g0, touched;  // as in RowParts
+    int64_t len, f0, g0, touched;  // as in RowParts, with whole groups' tokens
 };
 
 tm_status check_run(int32_t batch, int32_t groups, int32_t group_tokens, int32_t n_tok, int64_t first_token, Run* r) {
@@ -1629,18 +1629,44 @@ tmk::TokenGroups token_groups(const Run& r) {
     return t;
 }
 
-// At most `want` parts (but one for each group), of no fewer than `least` rows where a group has that many.
+// At most `want` parts (but one for each group), of no fewer than `least` rows where a group has that many: the fewest
+// rows a part whose parts that have a row are no more than that. (With as many for each group as for a full one a
+// run over the border of two long groups went through few parts: 4680 rows over the border of groups of 32760 through
+// 20 of 256, of 256 rows each, where 19 rows are enough.)
 tmk::RowParts row_parts(const Run& r, int64_t want, int64_t least) {
+    int64_t len = r.len, f0 = r.f0;
+    if (r.touched == 2) {  // of both groups no more than the run has of the longer one
+        const int64_t first = len - f0;
+        len = std::max(first, r.n - first);
+        f0 = len - first;
+    }
+    const int64_t last = f0 + std::max<int64_t>(r.n, 1) - 1 - (r.touched - 1) * len;  // the last row in its group
+    auto parts = [&](int64_t rows) { return (r.touched - 1) * ceil_div(len, rows) + last / rows - f0 / rows + 1; };
+    int64_t rows = len;
+    if (const int64_t each = want / (r.B * r.touched); each > 0) {
+        // enough where all groups are full; with fewer rows the run's ends may make up for it
+        int64_t lo = ceil_div(len, ceil_div(len, least));
+        rows = std::max(lo, ceil_div(len, each));
+        while (lo < rows && (f0 > 0 || last < len - 1)) {
+            const int64_t mid = (lo + rows) / 2;
+            if (r.B * parts(mid) <= want)
+                rows = mid;
+            else
+                lo = mid + 1;
+        }
+    }
     tmk::RowParts p{};
     p.B = int32_t(r.B);
     p.n = int32_t(r.n);
-    p.len = int32_t(r.len);
-    p.f0 = int32_t(r.f0);
+    p.len = int32_t(len);
+    p.f0 = int32_t(f0);
     p.touched = int32_t(r.touched);
     p.g0 = int32_t(r.g0);
     p.groups = int32_t(r.groups);
-    p.per_group = int32_t(std::max<int64_t>(1, std::min(want / (r.B * r.touched), ceil_div(r.len, least))));
-    p.rows_per_part = int32_t(ceil_div(r.len, p.per_group));
+    p.per_group = int32_t(ceil_div(len, rows));
+    p.rows_per_part = int32_t(rows);
+    p.before = int32_t(f0 / rows);
+    p.empty = int32_t(r.touched * p.per_group - parts(rows));
     return p;
 }
 
@@ -1654,7 +1680,7 @@ struct NormGeo {
     Run run;
     int64_t E;
     size_t act, stream;  // bytes of an element
-    tmk::RowParts parts;
+    tmk::RowParts parts;  // of the backward, by plan_norm_bwd
     size_t part_bytes;
 };
 
@@ -1673,6 +1699,11 @@ tm_status check_norm(const tm_block_norm_desc* d, int32_t n_tok, int64_t first_t
     if ((st = check_modulation(d->batch, d->groups, g->E)) != TM_OK) return st;
     g->act = d->dtype == TM_BF16 ? 2 : 4;
     g->stream = d->stream_dtype == TM_BF16 ? 2 : 4;
+    return TM_OK;
+}
+
+// The backward's parts of rows, and the bytes of their sums.
+void plan_norm_bwd(const tm_block_norm_desc* d, NormGeo* g) {
     // Workgroups for 10 waves a CU (20, which fit, were 3 to 10% slower), for 14 with a stream of half the bytes (10000
     // rows of 4096: 120 us, 155 with 10; 20000 of 2048, fp32: 168 and 159) and 16 of rows up to 1024, whose lanes hold
     // half as much (20000 of 1024, bf16 and fp32: 88 us, 115 with 10). No more than one to 8 rows, since the parts' sums are
@@ -1683,8 +1714,7 @@ tm_status check_norm(const tm_block_norm_desc* d, int32_t n_tok, int64_t first_t
     const int waves = lanes / 64, per_cu = fours == 1 ? 16 : d->stream_dtype == TM_BF16 ? 14 : 10;
     const int64_t fill = tmk::kCUs * std::max(1, (2 * per_cu + waves - 1) / (2 * waves));
     g->parts = row_parts(g->run, std::max<int64_t>(std::min<int64_t>(fill, 2 * tmk::kCUs), std::min(fill, g->run.rows / 8)), 2);
-    g->part_bytes = size_t(g->parts.count()) * tmk::kNormSums * size_t(g->E) * 4;
-    return TM_OK;
+    g->part_bytes = size_t(g->parts.filled()) * tmk::kNormSums * size_t(g->E) * 4;
 }
 
 // Which of a block norm's tensors go together.
@@ -1844,7 +1874,7 @@ LinearBwdPlan plan_linear_bwd(const LinearGeo& g) {
     p.exact = !p.few && rows <= tmk::kExactRows;
     const int64_t blocks = ceil_div(g.N, 256);
     p.parts = row_parts(g.run, std::max<int64_t>(1, 8 * tmk::kCUs / blocks), 32);
-    p.sums_bytes = aligned(size_t(p.parts.count()) * tmk::kLinearSums * size_t(g.N) * 4);
+    p.sums_bytes = aligned(size_t(p.parts.filled()) * tmk::kLinearSums * size_t(g.N) * 4);
     if (p.few) {
         p.R = rows <= 2 ? int32_t(rows) : 4;
         // four workgroups a CU, 16 columns of a wave at least
@@ -1921,7 +1951,9 @@ tm_status tm_block_norm_fwd(const tm_block_norm_desc* desc, int32_t n_tok, int64
 
 size_t tm_block_norm_bwd_workspace(const tm_block_norm_desc* desc, int32_t n_tok, int64_t first_token) {
     NormGeo g;
-    return check_norm(desc, n_tok, first_token, &g) == TM_OK && n_tok > 0 ? g.part_bytes : 0;
+    if (check_norm(desc, n_tok, first_token, &g) != TM_OK || n_tok == 0) return 0;
+    plan_norm_bwd(desc, &g);
+    return g.part_bytes;
 }
 
 tm_status tm_block_norm_bwd(const tm_block_norm_desc* desc, int32_t n_tok, int64_t first_token, const void* r,
@@ -1948,6 +1980,7 @@ tm_status tm_block_norm_bwd(const tm_block_norm_desc* desc, int32_t n_tok, int64
     const size_t elems = size_t(g.run.rows) * size_t(g.E), vec = size_t(g.E) * 4, mod = size_t(g.run.B * g.run.groups) * vec;
     const bool sums = dgate != nullptr || dpost_weight != nullptr || dpre_weight != nullptr || dpre_bias != nullptr ||
                       dscale != nullptr || dshift != nullptr;
+    plan_norm_bwd(desc, &g);
     const size_t need = sums && n_tok > 0 ? g.part_bytes : 0;
     if (need > 0 && (workspace == nullptr || workspace_bytes < need))
         return fail(TM_E_ARG, "workspace of %zu bytes needed", need);

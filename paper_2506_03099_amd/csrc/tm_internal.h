@@ -373,25 +373,35 @@ hipError_t launch_gemm(const GemmArgs& a, int tile, bool a_trans, bool b_trans, 
 
 // Token rows in parts that lie in one group each, for sums over a group's rows: group j of those that the
 // run touches holds tokens [j * len - f0, (j + 1) * len - f0) of each batch element, cut to [0, n), and
-// part p of it the rows_per_part from p * rows_per_part on (none, at the run's ends).
+// part p of it the rows_per_part from p * rows_per_part on. Only parts that have a row are counted and numbered, in the
+// order of their rows: in the run's first and last group its ends leave out some.
 struct RowParts {
     int32_t B, n;
-    int32_t len, f0;        // tokens of a group (n without groups), and of the first one before the run
+    int32_t len, f0;        // tokens of a group (at most what the run has of one), and of the first one before the run
     int32_t touched;        // groups of the run
-    int32_t per_group;      // parts
+    int32_t per_group;      // parts of len tokens
     int32_t rows_per_part;
     int32_t g0, groups;     // the first one's index, of how many
-    __host__ __device__ int32_t count() const { return B * touched * per_group; }
-    // part `i`: its batch element, the modulation's row of its group, its tokens [t0, t1)
-    __device__ __forceinline__ void of(int32_t i, int32_t& b, int64_t& mod, int32_t& t0, int32_t& t1) const {
-        const int32_t p = i % per_group, j = i / per_group % touched;
-        b = i / per_group / touched;
+    int32_t before, empty;  // of a batch element's parts those before its first row, and all without a row
+    __host__ __device__ int32_t count() const { return B * touched * per_group; }  // with those without a row
+    __host__ __device__ int32_t each() const { return touched * per_group - empty; }
+    __host__ __device__ int32_t filled() const { return count() - B * empty; }
+    // part `i` of filled(): its batch element, the modulation's row of its group, its tokens [t0, t1)
+    __host__ __device__ __forceinline__ void of(int32_t i, int32_t& b, int64_t& mod, int32_t& t0, int32_t& t1) const {
+        b = i / each();
+        const int32_t q = i - b * each() + before, j = q / per_group, p = q - j * per_group;
         mod = int64_t(b) * groups + g0 + j;
         const int64_t at = int64_t(j) * len - f0;
         const int64_t lo = at + int64_t(p) * rows_per_part;
         const int64_t hi = lo + rows_per_part < at + len ? lo + rows_per_part : at + len;
-        t0 = static_cast<int32_t>(lo > 0 ? (lo < n ? lo : n) : 0);
-        t1 = static_cast<int32_t>(hi > 0 ? (hi < n ? hi : n) : 0);
+        t0 = static_cast<int32_t>(lo > 0 ? lo : 0);
+        t1 = static_cast<int32_t>(hi < n ? hi : n);
+    }
+    // parts [i0, i1) are those of group j of batch element b
+    __host__ __device__ __forceinline__ void of_group(int32_t b, int32_t j, int32_t& i0, int32_t& i1) const {
+        const int32_t lo = j * per_group - before, hi = lo + per_group;
+        i0 = b * each() + (lo > 0 ? lo : 0);
+        i1 = b * each() + (hi < each() ? hi : each());
     }
 };
 
@@ -417,7 +427,7 @@ struct ColumnSums {
     int32_t n_group, n_total;
     GroupSum group[3];
     TotalSum total[3];
-    FastDiv by_parts, by_touched;  // set by the launcher
+    FastDiv by_parts, by_each;  // of a group, of a batch element; set by the launcher
 };
 hipError_t launch_column_sums(const ColumnSums& a, hipStream_t s);
 

@@ -1,0 +1,97 @@
+// Driver of the plans behind the block norms and linear layers for the sanitizer build, with the functions
+// of tm_internal.h that the kernels themselves call. Exit status 0 and "host block plan driver: all checks passed" when
+// every check holds.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+#include <cstdio>
+#include <vector>
+
+#include "../../paper_2506_03099_amd/csrc/tm_api.cpp"
+
+namespace {
+
+int g_failed = 0;
+int g_checks = 0;
+
+#define EXPECT(cond)                                                            \
+    do {                                                                        \
+        ++g_checks;                                                             \
+        if (!(cond)) {                                                          \
+            ++g_failed;                                                         \
+            std::fprintf(stderr, "FAILED %s:%d: %s\n", __FILE__, __LINE__, #cond); \
+        }                                                                       \
+    } while (0)
+
+// Parts of a run as the kernels number them: none without a row, every token in one part of its group, a group's parts
+// side by side, and as few rows a part as `want` parts allow.
+void parts_checks() {
+    struct Case {
+        int64_t B, groups, group, n, first, want, least;
+    };
+    const Case cases[] = {
+        {1, 21, 1560, 32760, 0, 512, 2},       // whole groups
+        {1, 1, 0, 4680, 0, 256, 2},            // no groups
+        {3, 5, 100, 333, 77, 512, 2},          // groups at both ends cut
+        {1, 7, 1560, 4680, 4000, 256, 2},      // four groups of which two are cut
+        {2, 3, 600, 700, 500, 512, 2},         // three
+        {1, 2, 32760, 4680, 30420, 256, 2},    // over the border of two groups of more tokens than the run
+        {1, 2, 1 << 28, 4680, (1 << 28) - 1, 256, 2},
+        {1, 2, 1 << 28, 4680, (1 << 28) - 4679, 256, 2},
+        {4, 2, 3000, 200, 2900, 512, 2},
+        {1, 3, 1560, 1562, 1559, 512, 2},      // a token of the first, all of the second, a token of the third
+        {2, 9, 7, 50, 11, 4, 2},               // more groups than parts are wanted
+        {1, 40, 1, 40, 0, 512, 2},             // a token a group
+        {1, 2, 1, 2, 0, 512, 2},
+        {1, 1000, 3, 2999, 1, 16, 32},
+        {1, 2, 4, 5, 3, 1, 32},
+        {5, 3, 1000, 1, 999, 512, 2},          // a row
+        {1, 5000, 200000, 1 << 29, 12345, 64, 2},  // offsets far past what a part holds
+    };
+    for (const Case& c : cases) {
+        Run r;
+        EXPECT(check_run(int32_t(c.B), int32_t(c.groups), int32_t(c.group), int32_t(c.n), c.first, &r) == TM_OK);
+        const tmk::RowParts p = row_parts(r, c.want, c.least);
+        EXPECT(p.filled() == p.B * p.each() && p.each() > 0 && p.filled() <= p.count());
+        EXPECT(p.filled() <= std::max(c.want, c.B * r.touched));
+        // a group of so many rows has at most two parts more than rows / rows_per_part, so this many are enough
+        const int64_t spare = c.want - 2 * c.B * r.touched;
+        if (spare > 0) EXPECT(p.rows_per_part <= std::max(ceil_div(c.B * c.n, spare), c.least));
+        std::vector<int32_t> group_end(size_t(c.B) * size_t(r.touched), 0);
+        int64_t at = 0;
+        for (int32_t i = 0; i < p.filled(); ++i) {
+            int32_t b, t0, t1;
+            int64_t mod;
+            p.of(i, b, mod, t0, t1);
+            EXPECT(b == at / c.n && t0 == at % c.n && t1 > t0 && t1 <= c.n);  // in order, and none is left out
+            EXPECT(t1 - t0 <= p.rows_per_part);
+            const int64_t g = c.group ? (c.first + t0) / c.group : 0;
+            EXPECT((c.group ? (c.first + t1 - 1) / c.group : 0) == g && mod == b * c.groups + g);
+            int32_t i0, i1;
+            p.of_group(b, int32_t(g - r.g0), i0, i1);
+            EXPECT(i0 <= i && i < i1);
+            group_end.at(size_t(b * r.touched + g - r.g0)) = i1;
+            at += t1 - t0;
+        }
+        EXPECT(at == c.B * c.n);
+        int32_t end = 0;
+        for (const int32_t e : group_end) {  // each group's parts end where the next one's begin
+            EXPECT(e > end);
+            end = e;
+        }
+        EXPECT(end == p.filled());
+    }
+}
+
+}  // namespace
+
+int main() {
+    parts_checks();
+    if (g_failed) {
+        std::fprintf(stderr, "host block plan driver: %d of %d checks failed\n", g_failed, g_checks);
+        return 1;
+    }
+    std::printf("host block plan driver: all checks passed (%d)\n", g_checks);
+    return 0;
+}

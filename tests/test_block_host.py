@@ -67,3 +67,8 @@ def test_workspace_sizes(tm):
     d = tm.make_linear_desc(1, 5120, 5120, "none", "f32", 21, 1560)
     assert 32760 * 5120 * 2 <= lib.tm_linear_bwd_workspace(d, 32760, 0) < 32760 * 5120 * 2 + (200 << 20)
     assert lib.tm_linear_fwd_workspace(tm.make_linear_desc(1, 64, 64), 1) == 0
+
+
+def test_plans_as_the_kernels_number_them_under_asan_and_ubsan(monkeypatch):
+    monkeypatch.setattr(sanitize, "DRIVER", DRIVER.replace("host_block_driver", "host_block_plan_driver"))
+    sanitize._run()

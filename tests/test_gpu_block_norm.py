@@ -395,3 +395,39 @@ def test_gradient_of_an_output_that_no_norm_takes_does_not_read_it(tm, E, act, p
     assert torch.equal(got.dgate[..., others], want.dgate[..., others])
     assert torch.equal(got.dpost_weight[others], want.dpost_weight[others])
     assert not bool(got.dpost_weight[cols].isfinite().any())
+
+
+# Runs that begin and end inside groups: over the border of two groups of many more tokens than the run, with one
+# token on either side, over several whole groups and parts of two, more groups than parts.
+CUT = [(1, 300, 264, 2, 4000, 3850), (2, 200, 1024, 2, 3000, 2900), (1, 61, 5120, 2, 2 ** 28, 2 ** 28 - 1),
+       (1, 61, 64, 2, 2 ** 28, 2 ** 28 - 60), (2, 700, 1000, 3, 600, 500), (1, 802, 8200, 3, 800, 799),
+       (3, 1000, 136, 4, 400, 250), (2, 1500, 72, 400, 4, 3), (5, 1, 2056, 2, 30, 30)]
+
+
+@pytest.mark.parametrize("B,n,E,groups,group,first", CUT)
+def test_runs_that_cut_their_groups(tm, B, n, E, groups, group, first):
+    test_forward_and_backward(tm, B, n, E, groups, group, first, "rms", "layer", "ygpwbm")
+
+
+def test_infinite_modulations_of_a_cut_group(tm):
+    """Infinities in the gate and the scale of a run's first and last group, of which it has a few tokens, make the
+    weights' gradients infinite in their columns, not NaN, and leave the others' bits alone."""
+    n, E, groups, group, first = 290, 264, 3, 200, 180
+    p = make(1, n, E, "f32", "f32", "ygpwm", groups, 11)
+    d = tm.make_block_norm_desc(1, E, "none", "none", "f32", "f32", EPS, groups, group)
+    p["y"], dr = p["y"].abs() + 0.1, torch.rand((1, n, E), device="cuda") + 0.1
+    want = tm.tm_block_norm_bwd(d, None, None, dr, p["y"], p["gate"], p["post_weight"], first_token=first)
+    gate = p["gate"].clone()
+    gate[0, 0, 5], gate[0, 2, 9] = float("inf"), float("-inf")
+    got = tm.tm_block_norm_bwd(d, None, None, dr, p["y"], gate, p["post_weight"], first_token=first)
+    assert float(got.dpost_weight[5]) == float("inf") and float(got.dpost_weight[9]) == float("-inf")
+    others = [c for c in range(E) if c not in (5, 9)]
+    assert torch.equal(got.dpost_weight[others], want.dpost_weight[others]) and torch.equal(got.dgate, want.dgate)
+    d = tm.make_block_norm_desc(1, E, "layer", "none", "f32", "f32", EPS, groups, group)
+    scale = p["scale"].clone()
+    scale[0, 0, 5], scale[0, 2, 9] = float("inf"), float("inf")
+    dh = dr  # (the sums are of dh, and of dh * n, without the scale)
+    bias = torch.zeros((E,), device="cuda")
+    got = tm.tm_block_norm_bwd(d, p["x"], dh, dr, pre_bias=bias, scale=scale, shift=p["shift"], first_token=first)
+    assert bool((got.dpre_bias[[5, 9]] == float("inf")).all())
+    assert bool(got.dpre_bias[others].isfinite().all()) and bool(got.dscale.isfinite().all())

@@ -384,3 +384,12 @@ def test_offsets_past_32_bits(tm):
     oc = o[0][:, cols].double()
     held(got.dweight[cols], oc.t() @ x[0].double(), 2 * (n + 8) * U * (oc.abs().t() @ x[0].double().abs()), "dweight")
     held(got.dbias[cols], oc.sum(0), (n + 8) * U * oc.abs().sum(0), "dbias")
+
+
+# Runs that begin and end inside groups: over the border of two groups of many more tokens than the run, over
+# whole groups and parts of two, few rows on both sides of a border.
+@pytest.mark.parametrize("B,n,K,N,groups,group,first", [(1, 300, 64, 520, 2, 4000, 3850), (1, 61, 136, 72, 2, 2 ** 28, 2 ** 28 - 1),
+                                                        (2, 700, 72, 264, 3, 600, 500), (1, 12, 72, 1032, 2, 100, 97),
+                                                        (1, 3, 72, 136, 2, 100, 98), (3, 1000, 64, 64, 4, 400, 250)])
+def test_runs_that_cut_their_groups(tm, B, n, K, N, groups, group, first):
+    test_forward_and_backward(tm, B, n, K, N, "silu", "f32", "bgrz", groups, group, first)
