@@ -1764,8 +1764,8 @@ struct GemmPlan {
 
 // What a round of `wgs` workgroups of `stages` stages each takes, in us. A stage of a 256 tile takes 0.94 us with few
 // workgroups at work and 1.36 with one on each CU; one of a 128 tile 0.34 and 0.44, 0.72 once some CUs have two, and
-// 0.94 when all have; one of a 64 tile 0.45, 0.51 with two on each CU and 0.81 with four. Rows that do not begin on
-// cache lines cost the smaller tiles up to 45% more when many workgroups read them.
+// 0.94 when all have; one of a 64 tile 0.45, 0.51 with two on each CU and 0.81 with four. Where k lies side by side in
+// memory, rows that do not begin on cache lines cost the smaller tiles up to 45% more when many workgroups read them.
 double round_us(int tile, double wgs, double stages, bool on_lines) {
     const double f = wgs / tmk::kCUs;
     if (tile == 256) return stages * (0.94 + 0.42 * f) + 11;
@@ -1777,7 +1777,7 @@ double round_us(int tile, double wgs, double stages, bool on_lines) {
     return stages * (f <= 2 ? 0.45 + 0.03 * f : 0.51 + 0.15 * (f - 2)) + 2.8;
 }
 
-GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool may_split) {
+GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool may_split, bool on_lines) {
     GemmPlan best{};
     double best_us = 0;
     for (const int tile : {256, 128, 64}) {
@@ -1789,7 +1789,7 @@ GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool may_split) {
         const int64_t tiles = p.tiles_m * p.tiles_n;
         const int64_t at_once = tmk::kCUs * tmk::gemm_per_cu(tile);
         const int64_t rest = tiles % at_once;
-        auto round = [&](int64_t wgs, int64_t stages) { return round_us(tile, double(wgs), double(stages), K % 64 == 0); };
+        auto round = [&](int64_t wgs, int64_t stages) { return round_us(tile, double(wgs), double(stages), on_lines); };
         const double whole_us = double(tiles / at_once) * round(at_once, p.stages);
         auto take = [&](double us) {
             if (best.tile != 0 && us >= best_us) return;
@@ -1816,6 +1816,9 @@ GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool may_split) {
     }
     return best;
 }
+
+// Rows of K side by side in memory, of both operands or of the first (x W^T, dz W).
+GemmPlan plan_gemm(int64_t M, int64_t N, int64_t K, bool may_split) { return plan_gemm(M, N, K, may_split, K % 64 == 0); }
 
 // Whether a forward call of few rows goes by tiles all the same, if it has the workspace: each workgroup of the
 // few rows' form reads all of x, which costs more than tiles' padding from some 45 MB on with 9 to 16 rows
@@ -1890,7 +1893,7 @@ LinearBwdPlan plan_linear_bwd(const LinearGeo& g) {
         p.dx2_bytes = aligned(size_t(both) * size_t(g.K) * 4);
     }
     p.dx = plan_gemm(both, g.K, g.N, true);
-    p.dw = plan_gemm(g.N, g.K, both, true);
+    p.dw = plan_gemm(g.N, g.K, both, true, true);  // (k are the rows of dz and x, none of which lie side by side)
     p.gemm_bytes = aligned(std::max(p.dx.part_bytes(), p.dw.part_bytes()));
     return p;
 }

@@ -84,10 +84,34 @@ void parts_checks() {
     }
 }
 
+LinearBwdPlan backward_plan(int64_t rows, int64_t K, int64_t N) {
+    tm_linear_desc d{1, int32_t(K), int32_t(N), TM_ACT_NONE, TM_BF16, 1, 0};
+    LinearGeo g;
+    EXPECT(check_linear(&d, int32_t(rows), 0, &g) == TM_OK);
+    return plan_linear_bwd(g);
+}
+
+// dW sums over token rows, which lie side by side nowhere: its plan follows from the number of stages, not from
+// whether the last one is whole.
+void stage_checks() {
+    const int64_t widths[][2] = {{1536, 2048}, {2048, 1536}, {1024, 4096}, {4096, 1024}, {1000, 1352}, {4096, 1000}, {5120, 5120}};
+    for (const auto& w : widths)
+        for (const int64_t stages : {5, 25, 74, 110, 512}) {
+            const GemmPlan whole = backward_plan(64 * stages, w[0], w[1]).dw;
+            EXPECT(whole.stages == stages);
+            for (const int64_t rows : {64 * stages - 63, 64 * stages - 56, 64 * stages - 1}) {
+                const GemmPlan p = backward_plan(rows, w[0], w[1]).dw;
+                EXPECT(p.tile == whole.tile && p.stages == stages && p.whole == whole.whole);
+                EXPECT(p.groups == whole.groups && p.shares == whole.shares);
+            }
+        }
+}
+
 }  // namespace
 
 int main() {
     parts_checks();
+    stage_checks();
     if (g_failed) {
         std::fprintf(stderr, "host block plan driver: %d of %d checks failed\n", g_failed, g_checks);
         return 1;
