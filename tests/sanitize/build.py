@@ -20,6 +20,7 @@ KV8_DRIVER = os.path.join(HERE, "host_kv8_driver")
 KV8_LAYOUT_DRIVER = os.path.join(HERE, "host_kv8_layout_driver")
 BLOCK_DRIVER = os.path.join(HERE, "host_block_driver")
 BLOCK_PLAN_DRIVER = os.path.join(HERE, "host_block_plan_driver")
+BLOCK_REFUSAL_DRIVER = os.path.join(HERE, "host_block_refusal_driver")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 
 SAN = ["-fsanitize=address,undefined", "-fno-sanitize-recover=undefined", "-fno-omit-frame-pointer"]
@@ -30,7 +31,8 @@ CXXFLAGS = ["-std=c++17", "-O1", "-g", "-D__HIP_PLATFORM_AMD__", "-I", os.path.j
 def build(verbose: bool = False) -> str:
     if not os.path.exists(os.path.join(PKG, "libtm.so")):
         raise RuntimeError("libtm.so must be built first")
-    for driver in (DRIVER, KV8_DRIVER, KV8_LAYOUT_DRIVER, BLOCK_DRIVER, BLOCK_PLAN_DRIVER):
+    for driver in (DRIVER, KV8_DRIVER, KV8_LAYOUT_DRIVER, BLOCK_DRIVER, BLOCK_PLAN_DRIVER,
+                   BLOCK_REFUSAL_DRIVER):
         obj = driver + ".o"
         cmd = ["g++", *CXXFLAGS, *SAN, "-c", driver + ".cpp", "-o", obj]
         if verbose:

@@ -72,3 +72,8 @@ def test_workspace_sizes(tm):
 def test_plans_as_the_kernels_number_them_under_asan_and_ubsan(monkeypatch):
     monkeypatch.setattr(sanitize, "DRIVER", DRIVER.replace("host_block_driver", "host_block_plan_driver"))
     sanitize._run()
+
+
+def test_refusals_by_their_messages_under_asan_and_ubsan(monkeypatch):
+    monkeypatch.setattr(sanitize, "DRIVER", DRIVER.replace("host_block_driver", "host_block_refusal_driver"))
+    sanitize._run()
