@@ -195,23 +195,6 @@ struct Tile {
     }
 };
 
-// First of the stages of a group's tiles, in a row, that share c takes. Shares c of all groups go through the same k
-// at the same time, and neighbouring tiles lie in neighbouring groups: so their workgroups, which run on one
-// XCD, bring the same rows and columns to its L2 (dealt out without groups, each brought its own:
-// 42% of the reads missed).
-__device__ __forceinline__ int share_begin(const GemmArgs& a, int c) {
-    const int per_group = (a.tiles_m * a.tiles_n - a.whole) / a.groups;
-    return static_cast<int>(static_cast<int64_t>(per_group) * a.stages * c / a.shares);
-}
-
-// The share that takes stage u of a group.
-__device__ __forceinline__ int share_of(const GemmArgs& a, int u) {
-    const int per_group = (a.tiles_m * a.tiles_n - a.whole) / a.groups;
-    int c = static_cast<int>(static_cast<int64_t>(u) * a.shares / (per_group * a.stages));
-    while (share_begin(a, c + 1) <= u) ++c;
-    return c;
-}
-
 template <int N>
 __device__ __forceinline__ void wait_and_meet() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
@@ -264,8 +247,8 @@ __global__ __launch_bounds__(256, gemm_per_cu(BT, AHEAD)) void gemm_kernel(const
         const int l = xcd_logical_id(blockIdx.x, a.groups * a.shares), c = l / a.groups;
         group = l % a.groups;
         slot2 = 2 * l;
-        u = share_begin(a, c);
-        u_end = share_begin(a, c + 1);
+        u = a.share_begin(c);
+        u_end = a.share_begin(c + 1);
     }
     auto next_work = [&](Work& w) __attribute__((always_inline)) {
         int t;
@@ -276,7 +259,7 @@ __global__ __launch_bounds__(256, gemm_per_cu(BT, AHEAD)) void gemm_kernel(const
             w.s1 = a.stages;
             w.part = nullptr;
         } else if (u < u_end) {
-            t = a.whole + u / a.stages * a.groups + group;
+            t = a.split_tile(u / a.stages, group);
             w.s0 = u % a.stages;
             w.s1 = min(a.stages, w.s0 + (u_end - u));
             w.part = a.part + static_cast<int64_t>(slot2 + seg) * (BT * BT);
@@ -560,12 +543,12 @@ __global__ __launch_bounds__(256) void gemm_merge_kernel(const GemmArgs a) {
     // so that this one is its second.
     const int group = t % a.groups;
     const int u0 = t / a.groups * a.stages, u1 = u0 + a.stages;
-    const int w0 = share_of(a, u0), w1 = share_of(a, u1 - 1);
+    const int w0 = a.share_of(u0), w1 = a.share_of(u1 - 1);
     const float* part = a.part + static_cast<int64_t>(w0 * a.groups + group) * 2 * (BT * BT) + r * BT + c;
     const int64_t step = static_cast<int64_t>(a.groups) * 2 * (BT * BT);
     float z[8] = {}, sum[8];
     if (a.ep.bias != nullptr) load8(a.ep.bias + col, z);
-    load8(part + (share_begin(a, w0) < u0 ? BT * BT : 0), sum);
+    load8(part + (a.share_begin(w0) < u0 ? BT * BT : 0), sum);
 #pragma unroll 4
     for (int w = w0 + 1; w <= w1; ++w) {
         float x[8];

@@ -53,6 +53,7 @@ void parts_checks() {
         Run r;
         EXPECT(check_run(int32_t(c.B), int32_t(c.groups), int32_t(c.group), int32_t(c.n), c.first, &r) == TM_OK);
         const tmk::RowParts p = row_parts(r, c.want, c.least);
+        const tmk::TokenGroups tg = token_groups(r);
         EXPECT(p.filled() == p.B * p.each() && p.each() > 0 && p.filled() <= p.count());
         EXPECT(p.filled() <= std::max(c.want, c.B * r.touched));
         // a group of so many rows has at most two parts more than rows / rows_per_part, so this many are enough
@@ -68,6 +69,7 @@ void parts_checks() {
             EXPECT(t1 - t0 <= p.rows_per_part);
             const int64_t g = c.group ? (c.first + t0) / c.group : 0;
             EXPECT((c.group ? (c.first + t1 - 1) / c.group : 0) == g && mod == b * c.groups + g);
+            EXPECT(tg.row(int32_t(at)) == mod && tg.row(int32_t(at + t1 - t0 - 1)) == mod);
             int32_t i0, i1;
             p.of_group(b, int32_t(g - r.g0), i0, i1);
             EXPECT(i0 <= i && i < i1);
@@ -107,11 +109,55 @@ void stage_checks() {
         }
 }
 
+// Shares of split tiles: each stage of each of these tiles in one share, which writes it into its first part, or its
+// second where it began in the tile before; and the merge finds them.
+void share_checks() {
+    int split = 0;
+    for (const int64_t M : {17, 130, 333, 600, 4680, 5376, 32760})
+        for (const int64_t N : {64, 1032, 5120, 20480})
+            for (const int64_t K : {8, 64, 1000, 5120, 20480, 1 << 30}) {
+                const GemmPlan p = plan_gemm(M, N, K, true);
+                const tmk::GemmArgs a = gemm_args(p, nullptr, nullptr, M, N, K, K, K, nullptr);
+                const int tiles = a.tiles_m * a.tiles_n;
+                if (tiles == a.whole) continue;
+                ++split;
+                EXPECT(a.share_begin(0) == 0 && a.share_begin(a.shares) == a.per_group() * a.stages);
+                std::vector<int64_t> done(size_t(tiles), 0);  // stages of a tile that shares have taken so far
+                std::vector<int> first(size_t(tiles), -1), last(size_t(tiles), -1);
+                for (int c = 0; c < a.shares; ++c)
+                    for (int g = 0; g < a.groups; ++g) {
+                        // as a workgroup goes through its share
+                        int seg = 0;
+                        for (int u = a.share_begin(c), end = a.share_begin(c + 1); u < end; ++seg) {
+                            const size_t t = size_t(a.split_tile(u / a.stages, g));
+                            const int s0 = u % a.stages, s1 = std::min(a.stages, s0 + (end - u));
+                            EXPECT(t >= size_t(a.whole) && t < size_t(tiles) && s0 < s1 && seg < 2);
+                            EXPECT(done.at(t) == s0);
+                            EXPECT((a.share_begin(c) < u / a.stages * a.stages ? 1 : 0) == seg);
+                            EXPECT(a.share_of(u) == c && a.share_of(u + (s1 - s0) - 1) == c);
+                            done.at(t) = s1;
+                            if (first.at(t) < 0) first.at(t) = c;
+                            last.at(t) = c;
+                            u += s1 - s0;
+                        }
+                    }
+                for (int t = a.whole; t < tiles; ++t) {
+                    EXPECT(done.at(size_t(t)) == a.stages);
+                    // as the merge looks them up
+                    const int u0 = (t - a.whole) / a.groups * a.stages;
+                    EXPECT(a.split_tile(u0 / a.stages, (t - a.whole) % a.groups) == t);
+                    EXPECT(a.share_of(u0) == first.at(size_t(t)) && a.share_of(u0 + a.stages - 1) == last.at(size_t(t)));
+                }
+            }
+    EXPECT(split > 20);
+}
+
 }  // namespace
 
 int main() {
     parts_checks();
     stage_checks();
+    share_checks();
     if (g_failed) {
         std::fprintf(stderr, "host block plan driver: %d of %d checks failed\n", g_failed, g_checks);
         return 1;
