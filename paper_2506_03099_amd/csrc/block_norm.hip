@@ -579,14 +579,16 @@ hipError_t launch_block_norm_bwd(const BlockNormBwdArgs& a, bool stream_f32, boo
     return hipErrorInvalidValue;
 }
 
-// With so many parts to a sum. Few columns leave CUs idle, and their threads wait for one load after the other (2560 parts of
-// 64 columns: 26 us of 92 for the backward with 32 threads a column and with 16); wide parts are bound by the lines
-// that they read (2000 parts of 5120: 120 us of the backward with 64 threads a column, 111 with 32).
 static hipError_t launch_for(int parts, const ColumnSums& a, hipStream_t s) {
-    if (parts <= 4) return launch_sums<64, 1>(a, s);
-    if (parts <= 64) return launch_sums<64, 4>(a, s);
-    if (parts <= 512) return launch_sums<64, 16>(a, s);
-    return a.E > 2048 ? launch_sums<32, 32>(a, s) : launch_sums<16, 64>(a, s);
+    int columns, threads;
+    column_sums_shape(parts, a.E, &columns, &threads);
+    switch (threads) {
+        case 1: return launch_sums<64, 1>(a, s);
+        case 4: return launch_sums<64, 4>(a, s);
+        case 16: return launch_sums<64, 16>(a, s);
+        case 32: return launch_sums<32, 32>(a, s);
+    }
+    return launch_sums<16, 64>(a, s);
 }
 
 hipError_t launch_column_sums(const ColumnSums& a, hipStream_t s) {

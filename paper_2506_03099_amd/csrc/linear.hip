@@ -15,7 +15,6 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include <algorithm>
 #include <type_traits>
 
 #include "tm_device.h"
@@ -570,10 +569,9 @@ __global__ __launch_bounds__(256) void gemm_merge_kernel(const GemmArgs a) {
 template <int BT, bool AT, bool BTR>
 hipError_t launch_tiles(const GemmArgs& a, hipStream_t s) {
     const int rest = a.tiles_m * a.tiles_n - a.whole;
-    // as many workgroups as the chip holds at a time; each takes one tile after the other
-    const int wgs = std::min(kCUs * gemm_per_cu(BT), std::max(a.whole, a.groups * a.shares));
+    const int wgs = gemm_workgroups(a, BT);
     hipError_t e = hipSuccess;
-    if (BT < 256 && wgs <= kCUs)
+    if (gemm_ahead(a, BT) == 4)
         e = launch_with(gemm_kernel<BT, AT, BTR, !BTR, BT < 256 ? 4 : 2>, dim3(wgs), 256, s, a);
     else
         e = launch_with(gemm_kernel<BT, AT, BTR, !BTR, 2>, dim3(wgs), 256, s, a);
@@ -895,19 +893,16 @@ hipError_t launch_gemm(const GemmArgs& a, int tile, bool a_trans, bool b_trans, 
 }
 
 hipError_t launch_few_rows(const FewRowsArgs& a, hipStream_t s) {
-    // The fewest columns a workgroup (and pieces of K) that leave 1024 workgroups, as far as the rows allow: one row
-    // of 5120 x 5120 14.2 us with 16, 11.1 with 8, 10.0 with 4; 20480 x 5120 51, 42, 37; 5120 x 20480 37, 39, 37;
-    // 2560 x 40960 39, 37, 45. Their four waves are sixteen where workgroups are few.
-    int pieces = 1;
-    while (pieces < 4 && a.rows * pieces * 2 <= 16 && a.N / 16 * pieces < 1024) pieces *= 2;
+    int pieces, waves;
+    few_rows_shape(a.rows, a.N, &pieces, &waves);
     const int columns = 16 / pieces;
     const dim3 grid((a.N + columns - 1) / columns);
-    const bool many = grid.x >= kCUs;
+    const bool four = waves == 4;
     switch (pieces) {
-        case 1: return many ? launch_with(few_rows_kernel<4, 1>, grid, 256, s, a) : launch_with(few_rows_kernel<16, 1>, grid, 1024, s, a);
-        case 2: return many ? launch_with(few_rows_kernel<4, 2>, grid, 256, s, a) : launch_with(few_rows_kernel<16, 2>, grid, 1024, s, a);
+        case 1: return four ? launch_with(few_rows_kernel<4, 1>, grid, 256, s, a) : launch_with(few_rows_kernel<16, 1>, grid, 1024, s, a);
+        case 2: return four ? launch_with(few_rows_kernel<4, 2>, grid, 256, s, a) : launch_with(few_rows_kernel<16, 2>, grid, 1024, s, a);
     }
-    return many ? launch_with(few_rows_kernel<4, 4>, grid, 256, s, a) : launch_with(few_rows_kernel<16, 4>, grid, 1024, s, a);
+    return four ? launch_with(few_rows_kernel<4, 4>, grid, 256, s, a) : launch_with(few_rows_kernel<16, 4>, grid, 1024, s, a);
 }
 
 hipError_t launch_linear_dz(const LinearDzArgs& a, hipStream_t s) {

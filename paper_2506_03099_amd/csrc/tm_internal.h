@@ -385,6 +385,13 @@ struct GemmArgs {
 constexpr int kGemmDepth = 64;
 // Workgroups of a CU at a time: LDS holds 2 * ahead + 1 parts of 128 * tile bytes for each.
 constexpr int gemm_per_cu(int tile, int ahead = 2) { return 160 * 1024 / ((2 * ahead + 1) * 128 * tile); }
+// As many workgroups as the chip holds at a time; each takes one tile after the other.
+inline int gemm_workgroups(const GemmArgs& a, int tile) {
+    const int most = kCUs * gemm_per_cu(tile), wanted = a.whole > a.groups * a.shares ? a.whole : a.groups * a.shares;
+    return wanted < most ? wanted : most;
+}
+// Stages that its loads run ahead of the MFMAs: more where a smaller tile's workgroup has a CU for itself.
+inline int gemm_ahead(const GemmArgs& a, int tile) { return tile < 256 && gemm_workgroups(a, tile) <= kCUs ? 4 : 2; }
 hipError_t launch_gemm(const GemmArgs& a, int tile, bool a_trans, bool b_trans, hipStream_t s);
 
 // Token rows in parts that lie in one group each, for sums over a group's rows: group j of those that the
@@ -445,6 +452,19 @@ struct ColumnSums {
     TotalSum total[3];
     FastDiv by_parts, by_each;  // of a group, of a batch element; set by the launcher
 };
+// Columns of a workgroup and threads of a column, with so many parts to a sum. Few columns leave CUs idle, and their
+// threads wait for one load after the other (2560 parts of 64 columns: 26 us of 92 for the backward with 32 threads a column
+// and with 16); wide parts are bound by the lines that they read (2000 parts of 5120: 120 us of the backward with 64
+// threads a column, 111 with 32).
+inline void column_sums_shape(int parts, int E, int* columns, int* threads) {
+    if (parts <= 512) {
+        *columns = 64;
+        *threads = parts <= 4 ? 1 : parts <= 64 ? 4 : 16;
+    } else {
+        *columns = E > 2048 ? 32 : 16;
+        *threads = 1024 / *columns;
+    }
+}
 hipError_t launch_column_sums(const ColumnSums& a, hipStream_t s);
 
 // Norms around a block (rows of E): z = post(y) * post_weight, r = x + gate * z, m = pre(r) * pre_weight +
@@ -511,6 +531,15 @@ struct FewRowsArgs {
     int32_t rows, K, N;
     LinearEpilogue ep;
 };
+// Pieces of K that a workgroup takes side by side, and its waves: the fewest columns a workgroup that leave 1024
+// workgroups, as far as the rows allow: one row of 5120 x 5120 14.2 us with 16, 11.1 with 8, 10.0 with 4; 20480 x 5120
+// 51, 42, 37; 5120 x 20480 37, 39, 37; 2560 x 40960 39, 37, 45. Their four waves are sixteen where workgroups are few.
+inline void few_rows_shape(int rows, int N, int* pieces, int* waves) {
+    *pieces = 1;
+    while (*pieces < 4 && rows * *pieces * 2 <= 16 && N / 16 * *pieces < 1024) *pieces *= 2;
+    const int columns = 16 / *pieces;
+    *waves = (N + columns - 1) / columns >= kCUs ? 4 : 16;
+}
 hipError_t launch_few_rows(const FewRowsArgs& a, hipStream_t s);
 
 // dz = dout * gate * act'(pre) of a linear layer's rows, in bf16 [rows, N] (dz) or, of at most kFewRowsBwd rows,

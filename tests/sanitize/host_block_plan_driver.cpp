@@ -1,11 +1,16 @@
 // Driver of the plans behind the block norms and linear layers for the sanitizer build, with the functions
-// of tm_internal.h that the kernels themselves call. Exit status 0 and "host block plan driver: all checks passed" when
-// every check holds.
+// of tm_internal.h that the kernels and their launchers themselves call. Arguments "product rows,in,out" and
+// "sums batch,tokens,width,groups,group,first" are sizes of the GPU tests, which have to take every kernel variant
+// between them. Exit status 0 and "host block plan driver: all checks passed" when every check holds.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <cstdint>
 #include <cstdio>
+#include <cstdlib>
+#include <cstring>
+#include <set>
+#include <string>
 #include <vector>
 
 #include "../../paper_2506_03099_amd/csrc/tm_api.cpp"
@@ -152,12 +157,95 @@ void share_checks() {
     EXPECT(split > 20);
 }
 
+// The variants that sizes take.
+class Variants {
+    std::set<std::string> taken_;
+
+    void product(const char* kind, const GemmPlan& p) {
+        const tmk::GemmArgs a = gemm_args(p, nullptr, nullptr, 8, 8, 8, 8, 8, nullptr);
+        const int wgs = tmk::gemm_workgroups(a, p.tile);
+        const std::string form = std::string(kind) + " " + std::to_string(p.tile) + " ahead " + std::to_string(tmk::gemm_ahead(a, p.tile));
+        if (a.whole > 0) taken_.insert(form + (a.whole > wgs ? " several" : " one"));
+        if (p.tiles_m * p.tiles_n > p.whole) taken_.insert(form + " shared");
+    }
+
+public:
+    void product(int64_t rows, int64_t K, int64_t N) {
+        tm_linear_desc d{1, int32_t(K), int32_t(N), TM_ACT_NONE, TM_BF16, 1, 0};
+        LinearGeo g;
+        EXPECT(check_linear(&d, int32_t(rows), 0, &g) == TM_OK);
+        const LinearBwdPlan b = plan_linear_bwd(g);
+        if (rows > tmk::kFewRows) {
+            product("forward", plan_gemm(rows, N, K, true));
+            product("dx", b.dx);
+            product("dW", b.dw);
+            return;
+        }
+        taken_.insert(b.few ? "gradients of " + std::to_string(b.R) : std::string("gradients in 16 digits"));
+        if (tiles_for_few(g)) {
+            taken_.insert(rows <= 8 ? "8 rows by tiles" : "16 rows by tiles");
+            return;
+        }
+        int pieces, waves;
+        tmk::few_rows_shape(int(rows), int(N), &pieces, &waves);
+        if (K / (64 * pieces) > 3 * waves)  // a wave's four runs at once
+            taken_.insert(std::to_string(pieces) + " pieces, " + std::to_string(waves) + " waves");
+    }
+
+    void sums(const int64_t (&v)[6]) {
+        tm_block_norm_desc d{int32_t(v[0]), int32_t(v[2]), TM_NORM_LAYER, TM_NORM_RMS, TM_BF16, TM_F32, int32_t(v[3]), int32_t(v[4]), 1e-6f};
+        NormGeo g;
+        EXPECT(check_norm(&d, int32_t(v[1]), v[5], &g) == TM_OK);
+        plan_norm_bwd(&d, &g);
+        int columns, threads;
+        tmk::column_sums_shape(g.parts.filled(), d.width, &columns, &threads);
+        taken_.insert("sums " + std::to_string(columns) + " x " + std::to_string(threads));
+        if (g.parts.filled() > 512 && g.parts.per_group <= 4) taken_.insert("sums of groups");
+    }
+
+    void check() const {
+        std::vector<std::string> all;
+        for (const char* kind : {"forward ", "dx ", "dW "})
+            for (const char* form : {"256 ahead 2", "128 ahead 2", "128 ahead 4", "64 ahead 2", "64 ahead 4"})
+                for (const char* tiles : {" one", " several", " shared"})
+                    if (std::strstr(form, "ahead 4") == nullptr || std::strcmp(tiles, " several") != 0)
+                        all.push_back(std::string(kind) + form + tiles);
+        for (const char* few : {"1", "2", "4"}) {
+            all.push_back(std::string(few) + " pieces, 4 waves");
+            all.push_back(std::string(few) + " pieces, 16 waves");
+            all.push_back(std::string("gradients of ") + few);
+        }
+        for (const char* one : {"gradients in 16 digits", "8 rows by tiles", "16 rows by tiles", "sums 64 x 1", "sums 64 x 4", "sums 64 x 16",
+                                "sums 32 x 32", "sums 16 x 64", "sums of groups"})
+            all.push_back(one);
+        for (const std::string& v : all) {
+            ++g_checks;
+            if (taken_.count(v)) continue;
+            ++g_failed;
+            std::fprintf(stderr, "FAILED: no size takes %s\n", v.c_str());
+        }
+    }
+};
+
 }  // namespace
 
-int main() {
+int main(int argc, char** argv) {
     parts_checks();
     stage_checks();
     share_checks();
+    if (argc > 1) {
+        Variants variants;
+        for (int i = 1; i + 1 < argc; i += 2) {
+            int64_t v[6] = {};
+            char* at = argv[i + 1];
+            for (int64_t& x : v) x = std::strtoll(at + (*at == ','), &at, 10);
+            if (std::strcmp(argv[i], "product") == 0)
+                variants.product(v[0], v[1], v[2]);
+            else
+                variants.sums(v);
+        }
+        variants.check();
+    }
     if (g_failed) {
         std::fprintf(stderr, "host block plan driver: %d of %d checks failed\n", g_failed, g_checks);
         return 1;

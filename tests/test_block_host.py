@@ -6,6 +6,7 @@ import pytest
 import torch
 
 import test_host_sanitize as sanitize
+from block_sizes import FEW_ROWS, PRODUCTS, SUMS
 
 DRIVER = sanitize.DRIVER.replace("host_abi_driver", "host_block_driver")
 
@@ -70,8 +71,13 @@ def test_workspace_sizes(tm):
 
 
 def test_plans_as_the_kernels_number_them_under_asan_and_ubsan(monkeypatch):
+    """And that the sizes of the GPU tests take every kernel variant between them."""
     monkeypatch.setattr(sanitize, "DRIVER", DRIVER.replace("host_block_driver", "host_block_plan_driver"))
-    sanitize._run()
+    args = []
+    for kind, sizes in (("product", PRODUCTS + FEW_ROWS), ("sums", SUMS)):
+        for size in sizes:
+            args += [kind, ",".join(map(str, size))]
+    sanitize._run(*args)
 
 
 def test_refusals_by_their_messages_under_asan_and_ubsan(monkeypatch):

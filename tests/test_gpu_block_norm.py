@@ -17,6 +17,7 @@ import pytest
 import torch
 
 from block_reference import as64, block_norm, group_rows, normed
+from block_sizes import SUMS
 from gpu_helpers import say
 
 pytestmark = pytest.mark.gpu
@@ -431,3 +432,8 @@ def test_infinite_modulations_of_a_cut_group(tm):
     got = tm.tm_block_norm_bwd(d, p["x"], dh, dr, pre_bias=bias, scale=scale, shift=p["shift"], first_token=first)
     assert bool((got.dpre_bias[[5, 9]] == float("inf")).all())
     assert bool(got.dpre_bias[others].isfinite().all()) and bool(got.dscale.isfinite().all())
+
+
+@pytest.mark.parametrize("B,n,E,groups,group,first", SUMS)
+def test_every_variant_of_the_sums(tm, B, n, E, groups, group, first):
+    test_forward_and_backward(tm, B, n, E, groups, group, first, "layer", "rms", "ygpwbm")

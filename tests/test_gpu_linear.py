@@ -17,6 +17,7 @@ import pytest
 import torch
 
 from block_reference import activate, as64, group_rows, linear
+from block_sizes import FEW_ROWS, PRODUCTS
 from gpu_helpers import say
 
 pytestmark = pytest.mark.gpu
@@ -393,3 +394,19 @@ def test_offsets_past_32_bits(tm):
                                                         (1, 3, 72, 136, 2, 100, 98), (3, 1000, 64, 64, 4, 400, 250)])
 def test_runs_that_cut_their_groups(tm, B, n, K, N, groups, group, first):
     test_forward_and_backward(tm, B, n, K, N, "silu", "f32", "bgrz", groups, group, first)
+
+
+# (every kernel variant, by tests/block_sizes.py and the host's check of its plans)
+KINDS = [("gelu", "bf16", "bz", 1, 0, 5), ("silu", "f32", "bgrz", 9, 900, 40), ("none", "f32", "bgrz", 1, 0, 0)]
+
+
+@pytest.mark.parametrize("n,K,N", PRODUCTS)
+def test_every_variant_of_the_products(tm, n, K, N):
+    for kind in KINDS:
+        test_forward_and_backward(tm, 1, n, K, N, *kind)
+
+
+@pytest.mark.parametrize("n,K,N", FEW_ROWS)
+def test_every_variant_of_few_rows(tm, n, K, N):
+    for kind in KINDS:
+        test_forward_and_backward(tm, 1, n, K, N, *kind)
