@@ -1,7 +1,8 @@
 """ctypes binding of ``libtm.so`` (the C ABI in ``include/tm.h``).
 
 Argument marshalling only: torch tensors supply device pointers, the current
-HIP stream supplies the stream, and every step of the computation runs in the
+HIP stream supplies the stream (or the caller, who orders it behind what makes the inputs and ahead of
+what uses the outputs), and every step of the computation runs in the
 library's HIP kernels. The binding raises if the library has not been built;
 there is no other implementation to fall back to.
 
@@ -259,6 +260,23 @@ def _stream(stream):
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 
 
+def _new(shape, dtype, device, stream):
+    """A tensor that a call on ``stream`` writes. For another stream than the current one it comes from that stream's
+    memory, since the current stream may still use what it has freed, and is kept from that stream's later calls until
+    the current one is done with it."""
+    if stream is None or _stream(stream) == _current_stream():
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream), device)):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream())
+    return t
+
+
+def _like(t, stream):
+    """The same, like ``t``."""
+    return torch.empty_like(t) if stream is None else _new(t.shape, t.dtype, t.device, stream)
+
+
 def tm_kv_cache_tokens(desc: tm_attn_desc) -> int:
     return lib().tm_kv_cache_tokens(ctypes.byref(desc))
 
@@ -333,7 +351,7 @@ def tm_qkv_produce(cache: KVCache, chunk: int, q, k, v, q_gain=None, k_gain=None
     if n_tok is None:
         n_tok = k.shape[1]
     if q_out is None:
-        q_out = torch.empty_like(q)
+        q_out = _like(q, stream)
     _check(lib().tm_qkv_produce(cache.handle, chunk, _ptr(q), _ptr(k), _ptr(v), _ptr(q_gain),
                                 _ptr(k_gain), eps, _ptr(q_out), n_tok, _stream(stream)))
     return q_out
@@ -380,7 +398,7 @@ def tm_sparse_causal_attn_fwd(desc: tm_attn_desc, q, q_chunk: int, cache: KVCach
                               stream=None):
     """Sparse causal attention; returns ``o`` (allocated like q if not given)."""
     if o is None:
-        o = torch.empty_like(q)
+        o = _like(q, stream)
     return _fwd(desc, q, q_chunk, cache, k, v, n_frames, o, 0, lse, stream)
 
 
@@ -390,7 +408,7 @@ def tm_sparse_causal_attn_fwd_f32out(desc: tm_attn_desc, q, q_chunk: int,
     """The same attention with an fp32 output (``o`` allocated as fp32 like q
     if not given); returns ``o``."""
     if o is None:
-        o = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+        o = _new(q.shape, torch.float32, q.device, stream)
     return _fwd(desc, q, q_chunk, cache, k, v, n_frames, o, 1, lse, stream)
 
 
@@ -410,7 +428,7 @@ def tm_audio_cross_attn_fwd(desc: tm_audio_desc, q, first_frame: int, ak, av, fa
     if n_tok is None:
         n_tok = q.shape[1]
     if o is None:
-        o = torch.empty_like(q)
+        o = _like(q, stream)
     _check(lib().tm_audio_cross_attn_fwd(ctypes.byref(desc), _ptr(q), first_frame, n_tok, _ptr(ak),
                                          _ptr(av), _ptr(face), _ptr(o), _stream(stream)))
     return o
@@ -422,7 +440,7 @@ def tm_audio_cross_attn_fwd_f32out(desc: tm_audio_desc, q, first_frame: int, ak,
     if n_tok is None:
         n_tok = q.shape[1]
     if o is None:
-        o = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+        o = _new(q.shape, torch.float32, q.device, stream)
     _check(lib().tm_audio_cross_attn_fwd_f32out(ctypes.byref(desc), _ptr(q), first_frame, n_tok,
                                                 _ptr(ak), _ptr(av), _ptr(face), _ptr(o),
                                                 _stream(stream)))
@@ -438,10 +456,10 @@ def tm_sparse_causal_attn_bwd(desc: tm_attn_desc, n_frames: int, q, k, v, o, lse
     than the current one, with plain addresses) order them otherwise, as
     ``tm_sparse_causal_attn_bwd_noalloc`` does."""
     if delta is None:
-        delta = torch.empty_like(lse)
-    dq = torch.empty_like(q) if dq is None else dq
-    dk = torch.empty_like(k) if dk is None else dk
-    dv = torch.empty_like(v) if dv is None else dv
+        delta = _like(lse, stream)
+    dq = _like(q, stream) if dq is None else dq
+    dk = _like(k, stream) if dk is None else dk
+    dv = _like(v, stream) if dv is None else dv
     d = ctypes.byref(desc)
     ptrs = [_ptr(t) for t in (q, k, v, o, lse, dout, delta, dq, dk, dv)]
     stream = _stream(stream)
@@ -487,7 +505,7 @@ def tm_rope3d_table(desc: tm_rope_desc, table=None, device="cuda", stream=None):
     fp32 tensor of pairs (allocated if not given)."""
     shape = (_rope_table_rows(desc), 2)
     if table is None:
-        table = torch.empty(shape, dtype=torch.float32, device=device)
+        table = _new(shape, torch.float32, device, stream)
     _expect("table", table, shape, torch.float32)
     _check(lib().tm_rope3d_table(ctypes.byref(desc), _ptr(table), _stream(stream)))
     return table
@@ -514,13 +532,13 @@ def _rope(fn, desc, table, q, k, first_token, q_out, k_out, stream):
             _expect("k_out", k_out, kshape, dtype)
         Hk, pk = kshape[2], _ptr(k)
         if k_out is None:
-            k_out = torch.empty_like(k)
+            k_out = _like(k, stream)
             pko = k_out.data_ptr()
         else:
             pko = _ptr(k_out)
     pq = _ptr(q)
     if q_out is None:
-        q_out = torch.empty_like(q)
+        q_out = _like(q, stream)
         pqo = q_out.data_ptr()
     else:
         pqo = _ptr(q_out)
@@ -643,7 +661,7 @@ def tm_qkv8_produce(cache: KV8Cache, chunk: int, q, k, v, q_gain=None, k_gain=No
         _expect("q_out", q_out, q.shape, torch.bfloat16)
     pq = _ptr(q)
     if q_out is None:
-        q_out = torch.empty_like(q)
+        q_out = _like(q, stream)
         pqo = q_out.data_ptr()
     else:
         pqo = _ptr(q_out)
@@ -665,12 +683,13 @@ def tm_kv8_read(cache: KV8Cache, chunk: int, dtype=torch.bfloat16, k_out=None, v
         _expect("v_out", v_out, shape, dt)
     if k_out is None:
         # (with its strides given: 0.3 us less than torch.empty)
-        k_out = torch.empty_strided(shape, (n * Hk * D, Hk * D, D, 1), dtype=dt, device=cache.pool.device)
+        k_out = (torch.empty_strided(shape, (n * Hk * D, Hk * D, D, 1), dtype=dt, device=cache.pool.device)
+                 if stream is None else _new(shape, dt, cache.pool.device, stream))
         pk = k_out.data_ptr()
     else:
         pk = _ptr(k_out)
     if v_out is None:
-        v_out = torch.empty_like(k_out)
+        v_out = _like(k_out, stream)
         pv = v_out.data_ptr()
     else:
         pv = _ptr(v_out)
@@ -688,7 +707,7 @@ def tm_kv8_attn_fwd(cache: KV8Cache, q, q_chunk: int, o=None, o_f32: bool = Fals
     n_q = cache.rows("q", q, cache.heads)
     pq = _ptr(q)
     if o is None:
-        o = torch.empty(q.shape, dtype=torch.float32, device=q.device) if o_f32 else torch.empty_like(q)
+        o = _new(q.shape, torch.float32, q.device, stream) if o_f32 else _like(q, stream)
         po = o.data_ptr()
     else:
         _expect("o", o, q.shape, torch.float32 if o_f32 else torch.bfloat16)
@@ -739,13 +758,13 @@ def _given(name, t, shape, dtype=torch.float32):
     return _ptr(t)
 
 
-def _grad(name, t, of):
+def _grad(name, t, of, stream):
     """The gradient of tensor ``of`` and its address: the caller's tensor, a new one like ``of`` if it is None,
     nothing if it is False or there is no ``of``."""
     if t is None:
         if of is None:
             return None, None
-        t = torch.empty_like(of)
+        t = _like(of, stream)
         return t, t.data_ptr()
     if t is False:
         return None, None
@@ -755,11 +774,11 @@ def _grad(name, t, of):
     return t, _ptr(t)
 
 
-def _formed(name, t, shape, dtype, like):
+def _formed(name, t, shape, dtype, like, stream):
     """A gradient that there always is, and its address: the caller's tensor, a new one if it is None, nothing if it
     is False."""
     if t is None:
-        t = torch.empty(shape, dtype=dtype, device=like.device)
+        t = _new(shape, dtype, like.device, stream)
         return t, t.data_ptr()
     if t is False:
         return None, None
@@ -785,7 +804,7 @@ def tm_block_norm_fwd(desc: tm_block_norm_desc, x, y=None, gate=None, post_weigh
     if y is not None:
         py = _given("y", y, shape, act)
         if r is None:
-            r = torch.empty_like(x)
+            r = torch.empty_like(x) if stream is None else _like(x, stream)
             pr = r.data_ptr()
         else:
             pr = _given("r", r, shape, st)
@@ -793,7 +812,7 @@ def tm_block_norm_fwd(desc: tm_block_norm_desc, x, y=None, gate=None, post_weigh
         raise TMError(TM_E_ARG, "r goes with y")
     if desc.pre != TM_NORM_NONE:
         if h is None:
-            h = torch.empty_like(x) if act == st else torch.empty(shape, dtype=act, device=x.device)
+            h = torch.empty(shape, dtype=act, device=x.device) if stream is None else _new(shape, act, x.device, stream)
             ph = h.data_ptr()
         else:
             ph = _given("h", h, shape, act)
@@ -844,14 +863,14 @@ def tm_block_norm_bwd(desc: tm_block_norm_desc, r, dh=None, dr=None, y=None, gat
     _given("shift", shift, mod)
     if dx is False or dy is False:
         raise TMError(TM_E_ARG, "dx and dy are always formed")
-    dx, pdx = _grad("dx", dx, like)
-    dy, pdy = _grad("dy", dy, y)
-    dgate, pdg = _grad("dgate", dgate, gate)
-    dpost_weight, pdp = _grad("dpost_weight", dpost_weight, post_weight)
-    dpre_weight, pdw = _grad("dpre_weight", dpre_weight, pre_weight)
-    dpre_bias, pdb = _grad("dpre_bias", dpre_bias, pre_bias)
-    dscale, pdc = _grad("dscale", dscale, scale)
-    dshift, pdh = _grad("dshift", dshift, scale)
+    dx, pdx = _grad("dx", dx, like, stream)
+    dy, pdy = _grad("dy", dy, y, stream)
+    dgate, pdg = _grad("dgate", dgate, gate, stream)
+    dpost_weight, pdp = _grad("dpost_weight", dpost_weight, post_weight, stream)
+    dpre_weight, pdw = _grad("dpre_weight", dpre_weight, pre_weight, stream)
+    dpre_bias, pdb = _grad("dpre_bias", dpre_bias, pre_bias, stream)
+    dscale, pdc = _grad("dscale", dscale, scale, stream)
+    dshift, pdh = _grad("dshift", dshift, scale, stream)
     d, stream = ctypes.byref(desc), _stream(stream)
     L = lib()
     nbytes, ws = 0, None
@@ -883,7 +902,7 @@ def tm_linear_fwd(desc: tm_linear_desc, x, weight, bias=None, gate=None, residua
     shape = (B, n, N)
     px, pw = _ptr(x), _given("weight", weight, (N, K), torch.bfloat16)
     if o is None:
-        o = torch.empty(shape, dtype=out, device=x.device)
+        o = torch.empty(shape, dtype=out, device=x.device) if stream is None else _new(shape, out, x.device, stream)
         po = o.data_ptr()
     else:
         po = _given("o", o, shape, out)
@@ -922,10 +941,10 @@ def tm_linear_bwd(desc: tm_linear_desc, x, weight, dout, gate=None, pre=None, fi
     n = _rows("dout", dout, B, N, _TORCH_DTYPE.get(desc.out_dtype))
     px, pw = _given("x", x, (B, n, K), _BF16), _given("weight", weight, (N, K), _BF16)
     pd, pg, pp = _ptr(dout), _given("gate", gate, (B, desc.groups, N)), _given("pre", pre, (B, n, N), _BF16)
-    dx, pdx = _formed("dx", dx, (B, n, K), _BF16, dout)
-    dweight, pdw = _formed("dweight", dweight, (N, K), _BF16, dout)
-    dbias, pdb = _formed("dbias", dbias, (N,), torch.float32, dout)
-    dgate, pdg = _grad("dgate", dgate, gate)
+    dx, pdx = _formed("dx", dx, (B, n, K), _BF16, dout, stream)
+    dweight, pdw = _formed("dweight", dweight, (N, K), _BF16, dout, stream)
+    dbias, pdb = _formed("dbias", dbias, (N,), torch.float32, dout, stream)
+    dgate, pdg = _grad("dgate", dgate, gate, stream)
     d, stream = ctypes.byref(desc), _stream(stream)
     nbytes = lib().tm_linear_bwd_workspace(d, n, first_token)
     ws = _own_workspace(nbytes, workspace, dout, stream)
