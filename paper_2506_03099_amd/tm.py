@@ -845,8 +845,9 @@ def tm_block_norm_bwd(desc: tm_block_norm_desc, r, dh=None, dr=None, y=None, gat
                       dgate=None, dpost_weight=None, dpre_weight=None, dpre_bias=None, dscale=None, dshift=None,
                       workspace=None, stream=None) -> BlockNormGrads:
     """Gradients of the block norm's inputs from dh and dr (None: r goes nowhere else), the forward's ``r`` (x
-    without y) and its inputs. Each gradient is allocated if not given, and left out with False. ``workspace``: a tensor of ``tm_block_norm_bwd_workspace`` bytes (allocated if
-    not given; needed on another stream than the current one)."""
+    without y; not read without a norm before the block) and its inputs. Each gradient is allocated if not given, and
+    left out with False. ``workspace``: a tensor of ``tm_block_norm_bwd_workspace`` bytes (allocated if not given;
+    needed on another stream than the current one)."""
     B, E = desc.batch, desc.width
     act, st = _TORCH_DTYPE.get(desc.dtype), _TORCH_DTYPE.get(desc.stream_dtype)
     has_pre = desc.pre != TM_NORM_NONE
@@ -923,8 +924,8 @@ def tm_linear_fwd(desc: tm_linear_desc, x, weight, bias=None, gate=None, residua
 
 
 class LinearGrads(NamedTuple):
-    """Gradients of ``tm_linear_fwd``'s inputs; None where the forward had no such input or it is not wanted.
-    (The residual's is the output's.)"""
+    """Gradients of ``tm_linear_fwd``'s inputs; None where one is not wanted, and dgate where the forward had no gate.
+    (dbias is formed unless it is False: the backward does not see the bias. The residual's is the output's.)"""
     dx: torch.Tensor | None
     dweight: torch.Tensor | None
     dbias: torch.Tensor | None
@@ -934,7 +935,8 @@ class LinearGrads(NamedTuple):
 def tm_linear_bwd(desc: tm_linear_desc, x, weight, dout, gate=None, pre=None, first_token: int = 0, dx=None,
                   dweight=None, dbias=None, dgate=None, workspace=None, stream=None) -> LinearGrads:
     """Gradients from that of the output, ``dout``. ``pre``: the forward's (not needed without activation and
-    gate; nor ``x`` without dweight and ``weight`` without dx). Each gradient is allocated if not given, and left out with False (the bias' for a layer without).
+    gate; nor ``x`` without dweight and ``weight`` without dx). Each gradient is allocated if not given, and left out
+    with False (the bias' for a layer without).
     ``workspace``: a tensor of ``tm_linear_bwd_workspace`` bytes (allocated if not given; needed on another
     stream than the current one)."""
     B, K, N = desc.batch, desc.in_width, desc.out_width
